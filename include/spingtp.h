@@ -669,6 +669,107 @@ spingtp_status spingtp_plan_kernel_info(spingtp_plan plan, int* info);
  * precontracted kernel: one workgroup per edge, `units` = 1 (edge). */
 spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
 
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Feed-forward operators: what the layers around the tensor product do with a node's or an edge's
+ * invariant (l = 0, s = 0) channels, as rows of a matrix, and the 8-bit form that operands and
+ * activations are kept in.  No plan: each call runs on the current device and the given stream,
+ * allocates nothing and waits for nothing.
+ *
+ * A matrix [R][D] given as (pointer, ld) has rows of D neighbouring elements, `ld` elements apart
+ * (ld >= D).  Sizes are at most 2^31 - 1 (gated block: K, F <= 4194240), matrices 2^46 elements.
+ * Outputs must not overlap inputs or one another.  R = 0 (M = 0) is valid: gradients of weights are
+ * then zero, everything else is empty.  Sums and statistics are fp32, outputs are rounded to nearest
+ * even.
+ *
+ * The 8-bit block format of a matrix [R][D]: e4m3 values [R][Dp] (Dp = D rounded up to 128; 16-byte
+ * aligned; zeros from column D on, also where the caller makes them) and scales [R][Sp], one e8m0 byte
+ * (2^(byte - 127)) for each row and block of 128 columns (Sp = Dp / 128 rounded up to 4; 4-byte
+ * aligned; the bytes past the last block are not used).  Element = value * scale.  The library chooses
+ * the smallest power of two that brings the block's largest finite magnitude to 448 or below (at least
+ * 2^-126; 1 for a block of zeros); a non-finite element becomes NaN in its own place.
+ */
+typedef enum { SPINGTP_SILU = 0, SPINGTP_GELU = 1 } spingtp_activation; /* gelu: x Phi(x), not its tanh form */
+typedef enum { SPINGTP_SAVE_NONE = 0, SPINGTP_SAVE_BF16 = 1, SPINGTP_SAVE_BLOCK8 = 2 } spingtp_save;
+
+/* x [R][D] to 8-bit blocks: along its rows (values, scales), and / or as the transposed matrix [D][R]
+ * (t_values, t_scales), the operand of a product that sums over the rows.  Either pair may be NULL.
+ * With t_values D <= 128 * 65535. */
+spingtp_status spingtp_pack8(spingtp_dtype dtype, const void* x, int64_t ldx, void* values, void* scales,
+                             void* t_values, void* t_scales, int64_t R, int64_t D, void* stream);
+
+/* x [R][D] = values * scales, in fp32 (exact) or rounded to bf16 (exact as well: 4 significant bits,
+ * unless below bf16's subnormals). */
+spingtp_status spingtp_unpack8(const void* values, const void* scales, spingtp_dtype dtype, void* x, int64_t ldx,
+                               int64_t R, int64_t D, void* stream);
+
+/*
+ * Root-mean-square norm with the residual's addition:
+ *   h = x + residual (rounded to dtype; h = x where residual is NULL),
+ *   rstd = (mean_d h^2 + eps)^(-1/2),  y = h rstd gain,
+ * y in dtype (y, ldy) or in 8-bit blocks (values, scales): one of the two, the other NULL.
+ * h is needed with a residual, optional without; rstd [R] is optional (the backward pass reads both).
+ * gain [D] is fp32; eps >= 0.
+ */
+spingtp_status spingtp_rms_norm(spingtp_dtype dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                                const float* gain, float eps, void* h, int64_t ldh, void* y, int64_t ldy, void* values,
+                                void* scales, float* rstd, int64_t R, int64_t D, void* stream);
+
+/*
+ * Its gradients, with t = gain grad_y and xhat = h rstd:
+ *   grad_x = rstd (t - xhat mean_d(t xhat)) + grad_h   (the gradient of x and of the residual alike),
+ *   grad_gain[d] = sum over the rows of grad_y xhat    (fp32; the same order in every call).
+ * grad_h, the gradient that reaches h directly, and grad_gain may be NULL.  An 8-bit y passes its
+ * gradient through the rounding as it is.  workspace: the size below, needed with grad_gain only.
+ */
+spingtp_status spingtp_rms_norm_backward(spingtp_dtype dtype, const void* grad_y, int64_t ldg, const void* h,
+                                         int64_t ldh, const float* rstd, const float* gain, const void* grad_h,
+                                         int64_t ldgh, void* grad_x, int64_t ldx, float* grad_gain, void* workspace,
+                                         size_t workspace_bytes, int64_t R, int64_t D, void* stream);
+spingtp_status spingtp_rms_norm_backward_workspace_size(int64_t R, int64_t D, size_t* size);
+
+/* c [M][N] = a b^T for a [M][K] and b [N][K] in 8-bit blocks, both packed along K.  The gradients of
+ * such a product are two more of them: grad_a = grad_c b sums over N, grad_b = grad_c^T a over M, with
+ * grad_c packed along its rows and along its columns, and b and a along theirs (spingtp_pack8). */
+spingtp_status spingtp_matmul8(const void* a_values, const void* a_scales, const void* b_values, const void* b_scales,
+                               spingtp_dtype dtype, void* c, int64_t ldc, int64_t M, int64_t N, int64_t K,
+                               void* stream);
+
+/*
+ * Gated feed-forward block, bf16: g = x w_gate^T, u = x w_up^T, h = act(g) u, for x [M][K], w_gate and
+ * w_up [F][K] (the same row stride), h [M][F].  x, w_gate, w_up 16-byte aligned.
+ * save: what is kept of g and u for the backward pass, nothing, dense bf16 [M][F] (g, u), or 8-bit
+ * blocks (g, g_scales, u, u_scales).  workspace: the size below, 0 where K, ldx and ldw are multiples
+ * of 8.
+ */
+spingtp_status spingtp_gated_forward(spingtp_activation act, const void* x, int64_t ldx, const void* w_gate,
+                                     const void* w_up, int64_t ldw, void* h, int64_t ldh, spingtp_save save, void* g,
+                                     void* g_scales, void* u, void* u_scales, void* workspace, size_t workspace_bytes,
+                                     int64_t M, int64_t K, int64_t F, void* stream);
+spingtp_status spingtp_gated_forward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw,
+                                                    size_t* size);
+
+/* The same from 8-bit blocks, for inference: h in bf16 (h_scales NULL) or in 8-bit blocks (h, h_scales),
+ * as the next product takes it. */
+spingtp_status spingtp_gated_forward8(spingtp_activation act, const void* x, const void* x_scales, const void* w_gate,
+                                      const void* w_gate_scales, const void* w_up, const void* w_up_scales, void* h,
+                                      int64_t ldh, void* h_scales, int64_t M, int64_t K, int64_t F, void* stream);
+
+/*
+ * Gradients of the gated block, bf16, from what the forward kept (save, g, u: its outputs) and x, bf16 or
+ * its 8-bit checkpoint (x_scales not NULL):
+ *   dg = grad_h u act'(g), du = grad_h act(g) (rounded to bf16, operands of the matrix units),
+ *   grad_x [M][K] = dg w_gate + du w_up,  grad_w [2F][K] = dg^T x, then du^T x.
+ * grad_x or grad_w may be NULL (then the weights, or x, are not read).
+ */
+spingtp_status spingtp_gated_backward(spingtp_activation act, const void* grad_h, int64_t ldgh, spingtp_save save,
+                                      const void* g, const void* g_scales, const void* u, const void* u_scales,
+                                      const void* x, int64_t ldx, const void* x_scales, const void* w_gate,
+                                      const void* w_up, int64_t ldw, void* grad_x, int64_t ldgx, void* grad_w,
+                                      void* workspace, size_t workspace_bytes, int64_t M, int64_t K, int64_t F,
+                                      void* stream);
+spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, size_t* size);
+
 #ifdef __cplusplus
 }
 #endif

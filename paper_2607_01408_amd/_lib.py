@@ -21,7 +21,10 @@ EXPORTED = ("spingtp_plan_create", "spingtp_forward", "spingtp_plan_destroy", "s
             "spingtp_backward_weighted_workspace_size", "spingtp_forward_depthwise", "spingtp_backward_depthwise",
             "spingtp_backward_depthwise_workspace_size", "spingtp_backward_v1_noalloc",
             "spingtp_plan_upload_selftest_host", "spingtp_forward_fully_connected",
-            "spingtp_backward_fully_connected")
+            "spingtp_backward_fully_connected", "spingtp_pack8", "spingtp_unpack8", "spingtp_rms_norm",
+            "spingtp_rms_norm_backward", "spingtp_rms_norm_backward_workspace_size", "spingtp_matmul8",
+            "spingtp_gated_forward", "spingtp_gated_forward_workspace_size", "spingtp_gated_forward8",
+            "spingtp_gated_backward", "spingtp_gated_backward_workspace_size")
 
 _lib = None
 
@@ -130,8 +133,26 @@ def lib() -> ctypes.CDLL:
         L.spingtp_forward_v1.restype = ctypes.c_int
         L.spingtp_plan_kernel_info_v1.argtypes = [ctypes.c_void_p, c_int_p]
         L.spingtp_plan_kernel_info_v1.restype = ctypes.c_int
+        _feedforward_signatures(L)
         _lib = L
     return _lib
+
+
+def _feedforward_signatures(L):
+    """``p`` pointer, ``i`` enum, ``n`` int64, ``z`` size_t, ``f`` float, ``s`` size_t output."""
+    kinds = {"p": ctypes.c_void_p, "i": ctypes.c_int, "n": ctypes.c_int64, "z": ctypes.c_size_t, "f": ctypes.c_float,
+             "s": ctypes.POINTER(ctypes.c_size_t)}
+    for name, args in (("spingtp_pack8", "ipnppppnnp"), ("spingtp_unpack8", "ppipnnnp"),
+                       ("spingtp_rms_norm", "ipnpnpfpnpnpppnnp"), ("spingtp_rms_norm_backward", "ipnpnpppnpnppznnp"),
+                       ("spingtp_rms_norm_backward_workspace_size", "nns"), ("spingtp_matmul8", "ppppipnnnnp"),
+                       ("spingtp_gated_forward", "ipnppnpnipppppznnnp"),
+                       ("spingtp_gated_forward_workspace_size", "nnnnns"),
+                       ("spingtp_gated_forward8", "ipppppppnpnnnp"),
+                       ("spingtp_gated_backward", "ipnipppppnpppnpnppznnnp"),
+                       ("spingtp_gated_backward_workspace_size", "nnns")):
+        fn = getattr(L, name)
+        fn.argtypes = [kinds[a] for a in args]
+        fn.restype = ctypes.c_int
 
 
 def message(status: int) -> str:

@@ -12,7 +12,8 @@ LIB = os.path.join(PKG, "libspingtp.so")
 SOURCES = ["plan.cpp", "api.cpp", "forward.hip", "forward_big_parity.hip", "forward_big_padded.hip",
            "forward_big_parity_padded.hip", "forward_big_parity_padded_minreg.hip", "forward_mfma.hip", "forward_pre.hip",
            "forward_pre_large.hip", "forward_pre_weighted.hip", "forward_direct.hip", "backward.hip", "backward_v1w.hip", "forward_uvw.hip",
-           "uvw_blocks.hip", "channel_blocks.hip", "gram_x2.hip", "direct_unrolled_paper.hip", "direct_unrolled_paired.hip", "direct_unrolled_parity.hip"]
+           "uvw_blocks.hip", "channel_blocks.hip", "gram_x2.hip", "direct_unrolled_paper.hip", "direct_unrolled_paired.hip", "direct_unrolled_parity.hip",
+           "feedforward.cpp", "norm8.hip", "pack8.hip", "matmul8.hip", "gated.hip"]
 # per-source additions
 # the compile-time tensor patterns take more constant-evaluation steps than the default limit
 _CONSTEXPR = ["-fconstexpr-steps=200000000"]
@@ -74,7 +75,7 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
 
 # host code checked by AddressSanitizer and UndefinedBehaviorSanitizer (device code is
 # built as usual: -Xarch_host applies the flags to the host compilation only)
-SANITIZED_SOURCES = ("plan.cpp", "api.cpp")
+SANITIZED_SOURCES = ("plan.cpp", "api.cpp", "feedforward.cpp")
 SANITIZE_FLAGS = ("-Xarch_host -fsanitize=address -Xarch_host -fsanitize=undefined "
                   "-Xarch_host -fno-sanitize-recover=undefined -Xarch_host -fno-omit-frame-pointer "
                   "-Xarch_host -g").split()

@@ -1,0 +1,512 @@
+// The gated feed-forward block:
+//   g = x Wg^T,  u = x Wu^T,  h = act(g) u
+// and its gradients
+//   dg = dh u act'(g),  du = dh act(g),  dx = dg Wg + du Wu,  dWg = dg^T x,  dWu = du^T x.
+//
+// Forward: one kernel.  A workgroup's tile takes the same 128 outputs from both weight matrices, so
+// the lane that holds an output's g holds its u, and h leaves from registers; g and u are written
+// only where the backward pass is to have them, in bf16 or as 8-bit blocks (a tile's 128 columns are
+// one block of each of its rows).
+//
+// Backward: dg and du are computed once and written side by side, [M][g | u], and transposed; then
+// dx is one product over g | u against the weights side by side, and both weight gradients are one
+// product over M.  All products run along both operands' rows (gemm_nt.h), so x and the weights are
+// transposed first, x straight from its 8-bit checkpoint where that is what was kept.  dg and du are
+// rounded to bf16, as operands of the matrix units; sums are fp32.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "feedforward.h"
+#include "gemm_nt.h"
+#include "internal.h"
+#include "lds_common.h"
+
+namespace spingtp {
+namespace {
+
+// act(g) and its derivative.  exp and the reciprocal are the hardware's (relative error near 2^-22,
+// against the 2^-9 of the outputs).
+template <int ACT>
+__device__ __forceinline__ float act(float g) {
+    if constexpr (ACT == kSilu) return g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
+    return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+}
+template <int ACT>
+__device__ __forceinline__ void act_grad(float g, float& a, float& d) {
+    if constexpr (ACT == kSilu) {
+        const float t = __builtin_amdgcn_rcpf(1.f + __expf(-g));
+        a = g * t;
+        d = t * (1.f + g * (1.f - t));
+    } else {
+        const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        a = g * p;
+        d = p + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+    }
+}
+
+struct GatedOut {
+    void* h;
+    int64_t ldh;
+    uint8_t* h_scales;
+    void* g;
+    void* u;
+    uint8_t* g_scales;
+    uint8_t* u_scales;
+    int64_t pitch, spitch;  // of the 8-bit rows
+};
+
+// A tile's rows of 128 columns as 8-bit blocks: `value(i, j, r)` is column column(i, r) of row row(j).
+template <class Tile, int HALF, int TM, int WN, class V>
+__device__ __forceinline__ void store_blocks(const Tile& t, const GemmArgs& a, int64_t n0, int64_t m0, float* tops,
+                                             uint8_t* values, uint8_t* scales, int64_t pitch, int64_t spitch,
+                                             const V& value) {
+    __syncthreads();  // earlier reads of the LDS are done
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < HALF; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (n0 + t.column(i, r & ~3) + (r & 3) < a.N) top = fmaxf(top, finite_abs(value(i, j, r)));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        if (t.lane < 32) tops[t.wn * Tile::BM + t.row(j)] = top;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        const int64_t m = m0 + t.row(j);
+        float top = 0.f;
+#pragma unroll
+        for (int w = 0; w < WN; ++w) top = fmaxf(top, tops[w * Tile::BM + t.row(j)]);
+        const int e = block8_scale(top);
+        const float inv = block8_inverse(e);
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int i = 0; i < HALF; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int64_t n = n0 + t.column(i, r);
+                float v[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[q] = n + q < a.N ? value(i, j, r + q) : 0.f;
+                *reinterpret_cast<uint32_t*>(values + m * pitch + n) = block8_word(v[0], v[1], v[2], v[3], inv);
+            }
+        if (t.wn == 0 && t.lane < 32) {
+            uint8_t* s = scales + m * spitch + n0 / kBlock8;
+            s[0] = static_cast<uint8_t>(e);
+            if (n0 + kBlock8 >= a.N)  // the row's scale bytes past its last block
+                for (int64_t b = n0 / kBlock8 + 1; b < spitch; ++b) scales[m * spitch + b] = 127;
+        }
+    }
+}
+
+template <class Tile, int HALF, int TM, class V>
+__device__ __forceinline__ void store_bf16(const Tile& t, const GemmArgs& a, int64_t n0, int64_t m0, void* out,
+                                           int64_t ldo, const V& value) {
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        const int64_t m = m0 + t.row(j);
+        if (m >= a.M) continue;
+        uint16_t* p = static_cast<uint16_t*>(out) + m * ldo;
+#pragma unroll
+        for (int i = 0; i < HALF; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int64_t n = n0 + t.column(i, r);
+                store4(p + n, a.N - n, value(i, j, r), value(i, j, r + 1), value(i, j, r + 2), value(i, j, r + 3));
+            }
+    }
+}
+
+template <class E, int TN, int TM, int WN, int WM, int ACT, int SAVE, bool OUT8>
+__global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOut o) {
+    using Tile = GemmTile<E, TN, TM, WN, WM, true>;
+    static_assert(Tile::kRows == kBlock8, "a tile is one block of its rows");
+    constexpr int HALF = TN / 2;
+    extern __shared__ __align__(16) uint8_t gemm_lds[];
+    float* tops = reinterpret_cast<float*>(gemm_lds);
+    int tm, tn;
+    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    const int64_t n0 = static_cast<int64_t>(tn) * Tile::kRows, m0 = static_cast<int64_t>(tm) * Tile::BM;
+    Tile t;
+    t.run(a, n0, m0, gemm_lds);
+    const auto g = [&](int i, int j, int r) { return t.acc[i][j][r]; };
+    const auto u = [&](int i, int j, int r) { return t.acc[HALF + i][j][r]; };
+    if constexpr (SAVE == kSaveBf16) {
+        store_bf16<Tile, HALF, TM>(t, a, n0, m0, o.g, a.N, g);
+        store_bf16<Tile, HALF, TM>(t, a, n0, m0, o.u, a.N, u);
+    }
+    if constexpr (SAVE == kSave8) {
+        store_blocks<Tile, HALF, TM, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.g), o.g_scales, o.pitch,
+                                         o.spitch, g);
+        store_blocks<Tile, HALF, TM, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.u), o.u_scales, o.pitch,
+                                         o.spitch, u);
+    }
+#pragma unroll
+    for (int i = 0; i < HALF; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) t.acc[i][j][r] = act<ACT>(t.acc[i][j][r]) * t.acc[HALF + i][j][r];
+    if constexpr (OUT8)
+        store_blocks<Tile, HALF, TM, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.h), o.h_scales, o.pitch,
+                                         o.spitch, g);
+    else
+        store_bf16<Tile, HALF, TM>(t, a, n0, m0, o.h, o.ldh, g);
+}
+
+// Rows of K bf16 elements to rows of a multiple of 64, zeros behind: what the products read where the
+// caller's rows do not start and end on 16 bytes.
+__global__ __launch_bounds__(256) void stage_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx,
+                                                         uint16_t* __restrict__ out, int64_t R, int64_t K,
+                                                         int64_t pitch) {
+    const int64_t groups = pitch / 8, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t row = i / groups;
+    if (row >= R) return;
+    const int64_t c = (i - row * groups) * 8, left = K - c;
+    float v[8];
+    load8(x + row * ldx + (left > 0 ? c : 0), left >= 8 ? 8 : static_cast<int>(left), v);
+    store8(out + row * pitch + c, 8, v);
+}
+
+// out[c][at + r] = in[r][c], zeros for r from R to the next multiple of 64; in is bf16 [R] rows of ldi
+// elements, or 8-bit blocks.
+template <bool IN8>
+__global__ __launch_bounds__(256) void transpose_kernel(const void* __restrict__ in, const uint8_t* __restrict__ scales,
+                                                        int64_t ldi, uint16_t* __restrict__ out, int64_t ldo,
+                                                        int64_t at, int64_t R, int64_t C) {
+    constexpr int ST = 66;  // elements of a tile column: an odd number of words
+    __shared__ uint16_t tile[64 * ST];
+    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64, c0 = static_cast<int64_t>(blockIdx.y) * 64;
+    const int l = threadIdx.x & 7, g = threadIdx.x >> 3;
+    const int64_t left = C - c0 - l * 8;
+    const int n = left >= 8 ? 8 : static_cast<int>(left);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = i * 32 + g;
+        const int64_t row = r0 + r;
+        float v[8];
+        if constexpr (IN8) {
+            const int64_t pitch = block8_pitch(C);  // c0 + 64 <= pitch
+            const int64_t rr = row < R ? row : R - 1;
+            const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(in) + rr * pitch + c0 + l * 8);
+            const float s = row < R ? block8_power(scales[rr * block8_scale_pitch(C) + c0 / kBlock8]) : 0.f;
+            float a[4], b[4];
+            block8_values(q.x, a);
+            block8_values(q.y, b);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = row < R ? a[j] * s : 0.f, v[4 + j] = row < R ? b[j] * s : 0.f;
+        } else {
+            load8(static_cast<const uint16_t*>(in) + (row < R ? row : 0) * ldi + (n > 0 ? c0 + l * 8 : 0),
+                  row < R ? n : 0, v);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const uint32_t w = bf16_pair(v[j], v[j + 1]);
+            tile[(l * 8 + j) * ST + r] = static_cast<uint16_t>(w);
+            tile[(l * 8 + j + 1) * ST + r] = static_cast<uint16_t>(w >> 16);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c = i * 32 + g;
+        if (c0 + c >= C) continue;
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const uint32_t*>(&tile[c * ST + l * 8 + 2 * j]);
+        *reinterpret_cast<uint4*>(out + (c0 + c) * ldo + at + r0 + l * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// dg and du of a tile of 64 rows x 64 columns: side by side in both [M][2 Fp] and transposed
+// [2 F][Mp] (Fp, Mp: multiples of 64, zeros behind).
+template <int ACT, bool IN8>
+__global__ __launch_bounds__(256) void gated_grad_kernel(const uint16_t* __restrict__ dh, int64_t lddh,
+                                                         const void* __restrict__ g, const void* __restrict__ u,
+                                                         const uint8_t* __restrict__ gs,
+                                                         const uint8_t* __restrict__ us, uint16_t* __restrict__ both,
+                                                         uint16_t* __restrict__ both_t, int64_t M, int64_t F) {
+    constexpr int ST = 66;
+    __shared__ uint16_t tile[2][64 * ST];
+    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 64, f0 = static_cast<int64_t>(blockIdx.y) * 64;
+    const int64_t fp = (F + 63) / 64 * 64, mp = (M + 63) / 64 * 64;
+    const int l = threadIdx.x & 7, k = threadIdx.x >> 3;
+    const int64_t left = F - f0 - l * 8;
+    const int n = left >= 8 ? 8 : static_cast<int>(left);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int r = i * 32 + k;
+        const int64_t m = m0 + r;
+        const bool in = m < M;
+        const int64_t mm = in ? m : M - 1;
+        const int nn = in ? n : 0;
+        const int64_t c = n > 0 ? f0 + l * 8 : 0;
+        float d[8], a[8], b[8];
+        load8(dh + mm * lddh + c, nn, d);
+        if constexpr (IN8) {
+            const int64_t pitch = block8_pitch(F), spitch = block8_scale_pitch(F);  // f0 + 64 <= pitch
+            const int64_t p = mm * pitch + f0 + l * 8, q = mm * spitch + f0 / kBlock8;
+            const uint2 wa = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(g) + p);
+            const uint2 wb = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(u) + p);
+            const float sa = block8_power(gs[q]), sb = block8_power(us[q]);
+            float lo[4], hi[4];
+            block8_values(wa.x, lo);
+            block8_values(wa.y, hi);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[j] = lo[j] * sa, a[4 + j] = hi[j] * sa;
+            block8_values(wb.x, lo);
+            block8_values(wb.y, hi);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = lo[j] * sb, b[4 + j] = hi[j] * sb;
+        } else {
+            load8(static_cast<const uint16_t*>(g) + mm * F + c, nn, a);
+            load8(static_cast<const uint16_t*>(u) + mm * F + c, nn, b);
+        }
+        float dg[8], du[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float y, dy;
+            act_grad<ACT>(a[j], y, dy);
+            dg[j] = j < nn ? d[j] * b[j] * dy : 0.f;
+            du[j] = j < nn ? d[j] * y : 0.f;
+        }
+        const uint4 wg = make_uint4(bf16_pair(dg[0], dg[1]), bf16_pair(dg[2], dg[3]), bf16_pair(dg[4], dg[5]),
+                                    bf16_pair(dg[6], dg[7]));
+        const uint4 wu = make_uint4(bf16_pair(du[0], du[1]), bf16_pair(du[2], du[3]), bf16_pair(du[4], du[5]),
+                                    bf16_pair(du[6], du[7]));
+        if (in && both != nullptr) {
+            *reinterpret_cast<uint4*>(both + m * 2 * fp + f0 + l * 8) = wg;
+            *reinterpret_cast<uint4*>(both + m * 2 * fp + fp + f0 + l * 8) = wu;
+        }
+        const uint32_t pg[4] = {wg.x, wg.y, wg.z, wg.w}, pu[4] = {wu.x, wu.y, wu.z, wu.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            tile[0][(l * 8 + 2 * j) * ST + r] = static_cast<uint16_t>(pg[j]);
+            tile[0][(l * 8 + 2 * j + 1) * ST + r] = static_cast<uint16_t>(pg[j] >> 16);
+            tile[1][(l * 8 + 2 * j) * ST + r] = static_cast<uint16_t>(pu[j]);
+            tile[1][(l * 8 + 2 * j + 1) * ST + r] = static_cast<uint16_t>(pu[j] >> 16);
+        }
+    }
+    if (both_t == nullptr) return;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = i * 32 + k;
+            if (f0 + c >= F) continue;
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const uint32_t*>(&tile[q][c * ST + l * 8 + 2 * j]);
+            *reinterpret_cast<uint4*>(both_t + (q * F + f0 + c) * mp + m0 + l * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (i < n) p[i] = 0;
+}
+
+bool grid_ok(int64_t x, int64_t y = 1) { return x <= (int64_t{1} << 24) - 1 && y <= 65535; }  // below 2^32 threads
+
+template <class E, int TN, int TM, int WN, int WM, int ACT, int SAVE, bool OUT8>
+hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
+    using Tile = GemmTile<E, TN, TM, WN, WM, true>;
+    const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::kRows - 1) / Tile::kRows;
+    if (tm * tn > kMostTiles) return hipErrorInvalidValue;
+    g.tiles_m = static_cast<int>(tm);
+    g.tiles_n = static_cast<int>(tn);
+    constexpr auto kernel = gated_kernel<E, TN, TM, WN, WM, ACT, SAVE, OUT8>;
+    const hipError_t e = raise_lds_limit<kernel>();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g, o);
+    return hipGetLastError();
+}
+
+template <class E, int ACT, int SAVE, bool OUT8>
+hipError_t gated_tiles(const GemmArgs& g, const GatedOut& o, hipStream_t stream) {
+    const auto tiles = [&](int64_t bm) { return ((g.M + bm - 1) / bm) * ((g.N + 127) / 128); };
+    if (tiles(256) >= 192) return gated_launch<E, 4, 2, 2, 4, ACT, SAVE, OUT8>(g, o, stream);
+    if (tiles(128) >= 192) return gated_launch<E, 4, 2, 2, 2, ACT, SAVE, OUT8>(g, o, stream);
+    return gated_launch<E, 2, 2, 4, 1, ACT, SAVE, OUT8>(g, o, stream);
+}
+
+template <class E, int SAVE, bool OUT8>
+hipError_t gated_act(int act, const GemmArgs& g, const GatedOut& o, hipStream_t stream) {
+    return act == kSilu ? gated_tiles<E, kSilu, SAVE, OUT8>(g, o, stream)
+                        : gated_tiles<E, kGelu, SAVE, OUT8>(g, o, stream);
+}
+
+// whether the products can read these rows as they are
+bool rows_fit(int64_t K, int64_t ld) { return K % 8 == 0 && ld % 8 == 0; }
+int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
+
+hipError_t stage(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K, hipStream_t stream) {
+    const int64_t pitch = up64(K), blocks = (R * (pitch / 8) + 255) / 256;
+    if (!grid_ok(blocks)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(stage_rows_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                       static_cast<const uint16_t*>(x), ldx, out, R, K, pitch);
+    return hipGetLastError();
+}
+
+// c [M][N] (bf16) = x [M] rows against w [N] rows, both of K bf16 elements (a multiple of 64)
+template <int TN, int TM, int WN, int WM>
+hipError_t product_launch(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) {
+    using Tile = GemmTile<Bf16, TN, TM, WN, WM, false>;
+    const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
+    if (tm * tn > kMostTiles) return hipErrorInvalidValue;
+    g.tiles_m = static_cast<int>(tm);
+    g.tiles_n = static_cast<int>(tn);
+    constexpr auto kernel = gemm_nt_kernel<Bf16, TN, TM, WN, WM, uint16_t>;
+    const hipError_t e = raise_lds_limit<kernel>();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g,
+                       static_cast<uint16_t*>(c), ldc);
+    return hipGetLastError();
+}
+hipError_t product(const uint16_t* x, const uint16_t* w, void* c, int64_t ldc, int64_t M, int64_t N, int64_t K,
+                   hipStream_t stream) {
+    GemmArgs g{};
+    g.w = reinterpret_cast<const uint8_t*>(w);
+    g.x = reinterpret_cast<const uint8_t*>(x);
+    g.ldw = g.ldx = 2 * K;
+    g.M = M;
+    g.N = N;
+    g.steps = static_cast<int>(K / 64);
+    g.tail = kStepBytes;
+    const auto tiles = [&](int64_t n) { return ((M + n - 1) / n) * ((N + n - 1) / n); };
+    if (tiles(256) >= 192) return product_launch<4, 2, 2, 4>(g, c, ldc, stream);
+    if (tiles(128) >= 192) return product_launch<2, 2, 2, 2>(g, c, ldc, stream);
+    return product_launch<1, 1, 2, 2>(g, c, ldc, stream);
+}
+
+hipError_t transpose(const void* in, const uint8_t* scales, int64_t ldi, uint16_t* out, int64_t ldo, int64_t at,
+                     int64_t R, int64_t C, hipStream_t stream) {
+    const int64_t br = (R + 63) / 64, bc = (C + 63) / 64;
+    if (!grid_ok(br, bc)) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(br), static_cast<unsigned>(bc));
+    if (scales != nullptr)
+        hipLaunchKernelGGL((transpose_kernel<true>), grid, dim3(256), 0, stream, in, scales, ldi, out, ldo, at, R, C);
+    else
+        hipLaunchKernelGGL((transpose_kernel<false>), grid, dim3(256), 0, stream, in, scales, ldi, out, ldo, at, R, C);
+    return hipGetLastError();
+}
+
+template <int ACT>
+hipError_t gated_grad(const GatedBwdArgs& a, uint16_t* both, uint16_t* both_t, hipStream_t stream) {
+    const int64_t bm = (a.M + 63) / 64, bf = (a.F + 63) / 64;
+    if (!grid_ok(bm, bf)) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(bm), static_cast<unsigned>(bf));
+    const uint16_t* dh = static_cast<const uint16_t*>(a.dh);
+    if (a.save == kSave8)
+        hipLaunchKernelGGL((gated_grad_kernel<ACT, true>), grid, dim3(256), 0, stream, dh, a.lddh, a.g, a.u, a.g_scales,
+                           a.u_scales, both, both_t, a.M, a.F);
+    else
+        hipLaunchKernelGGL((gated_grad_kernel<ACT, false>), grid, dim3(256), 0, stream, dh, a.lddh, a.g, a.u,
+                           a.g_scales, a.u_scales, both, both_t, a.M, a.F);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t gated_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw) {
+    const int64_t pitch = up64(K) * 2;
+    return static_cast<size_t>((rows_fit(K, ldx) ? 0 : M * pitch) + (rows_fit(K, ldw) ? 0 : 2 * F * pitch));
+}
+
+hipError_t launch_gated(const GatedArgs& a, hipStream_t stream) {
+    const int64_t pitch = up64(a.K);
+    uint16_t* ws = static_cast<uint16_t*>(a.workspace);
+    GemmArgs g{};
+    g.M = a.M;
+    g.N = a.F;
+    g.x = static_cast<const uint8_t*>(a.x);
+    g.w = static_cast<const uint8_t*>(a.wg);
+    g.w2 = static_cast<const uint8_t*>(a.wu);
+    g.ldx = 2 * a.ldx;
+    g.ldw = 2 * a.ldw;
+    hipError_t e = hipSuccess;
+    if (!rows_fit(a.K, a.ldx)) {
+        e = stage(a.x, a.ldx, ws, a.M, a.K, stream);
+        g.x = reinterpret_cast<const uint8_t*>(ws);
+        g.ldx = 2 * pitch;
+        ws += a.M * pitch;
+    }
+    if (e == hipSuccess && !rows_fit(a.K, a.ldw)) {
+        e = stage(a.wg, a.ldw, ws, a.F, a.K, stream);
+        if (e == hipSuccess) e = stage(a.wu, a.ldw, ws + a.F * pitch, a.F, a.K, stream);
+        g.w = reinterpret_cast<const uint8_t*>(ws);
+        g.w2 = reinterpret_cast<const uint8_t*>(ws + a.F * pitch);
+        g.ldw = 2 * pitch;
+    }
+    if (e != hipSuccess) return e;
+    // a staged row next to one that is not has zeros where the other has none: K up to 8 elements
+    g.steps = static_cast<int>(pitch / 64);
+    const int64_t held = (a.K + 7) / 8 * 16 - (g.steps - 1) * static_cast<int64_t>(kStepBytes);
+    g.tail = static_cast<int>(held);
+    const GatedOut o{a.h, a.ldh, nullptr, a.g, a.u, a.g_scales, a.u_scales, block8_pitch(a.F), block8_scale_pitch(a.F)};
+    switch (a.save) {
+        case kSaveNone: return gated_act<Bf16, kSaveNone, false>(a.act, g, o, stream);
+        case kSaveBf16: return gated_act<Bf16, kSaveBf16, false>(a.act, g, o, stream);
+        default: return gated_act<Bf16, kSave8, false>(a.act, g, o, stream);
+    }
+}
+
+hipError_t launch_gated8(const GatedArgs& a, hipStream_t stream) {
+    GemmArgs g{};
+    g.M = a.M;
+    g.N = a.F;
+    g.x = static_cast<const uint8_t*>(a.x);
+    g.w = static_cast<const uint8_t*>(a.wg);
+    g.w2 = static_cast<const uint8_t*>(a.wu);
+    g.ldx = g.ldw = block8_pitch(a.K);
+    g.xs = a.x_scales;
+    g.ws = a.wg_scales;
+    g.ws2 = a.wu_scales;
+    g.lds = block8_scale_pitch(a.K);
+    g.steps = static_cast<int>(g.ldx / kStepBytes);
+    g.tail = kStepBytes;
+    const GatedOut o{a.h,     a.ldh,   a.h_scales, nullptr, nullptr, nullptr, nullptr, block8_pitch(a.F),
+                     block8_scale_pitch(a.F)};
+    return a.h_scales != nullptr ? gated_act<Fp8, kSaveNone, true>(a.act, g, o, stream)
+                                 : gated_act<Fp8, kSaveNone, false>(a.act, g, o, stream);
+}
+
+size_t gated_backward_workspace(int64_t M, int64_t K, int64_t F) {
+    const int64_t fp = up64(F), mp = up64(M);
+    return static_cast<size_t>(2 * (M * 2 * fp + 2 * F * mp + K * 2 * fp + K * mp));
+}
+
+hipError_t launch_gated_backward(const GatedBwdArgs& a, hipStream_t stream) {
+    if (a.M == 0) {
+        if (a.dw == nullptr) return hipSuccess;
+        const int64_t n = 2 * a.F * a.K, blocks = (n + 255) / 256;
+        if (!grid_ok(blocks)) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(zero_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+                           static_cast<uint16_t*>(a.dw), n);
+        return hipGetLastError();
+    }
+    const int64_t fp = up64(a.F), mp = up64(a.M);
+    uint16_t* both = static_cast<uint16_t*>(a.workspace);
+    uint16_t* both_t = both + a.M * 2 * fp;
+    uint16_t* w_t = both_t + 2 * a.F * mp;
+    uint16_t* x_t = w_t + a.K * 2 * fp;
+    uint16_t* d = a.dx != nullptr ? both : nullptr;
+    uint16_t* d_t = a.dw != nullptr ? both_t : nullptr;
+    hipError_t e = a.act == kSilu ? gated_grad<kSilu>(a, d, d_t, stream) : gated_grad<kGelu>(a, d, d_t, stream);
+    if (e == hipSuccess && a.dx != nullptr) {
+        e = transpose(a.wg, nullptr, a.ldw, w_t, 2 * fp, 0, a.F, a.K, stream);
+        if (e == hipSuccess) e = transpose(a.wu, nullptr, a.ldw, w_t, 2 * fp, fp, a.F, a.K, stream);
+        if (e == hipSuccess) e = product(both, w_t, a.dx, a.lddx, a.M, a.K, 2 * fp, stream);
+    }
+    if (e == hipSuccess && a.dw != nullptr) {
+        e = transpose(a.x, a.x_scales, a.ldx, x_t, mp, 0, a.M, a.K, stream);
+        if (e == hipSuccess) e = product(both_t, x_t, a.dw, a.K, 2 * a.F, a.K, mp, stream);
+    }
+    return e;
+}
+
+}  // namespace spingtp

@@ -1,0 +1,296 @@
+// Matrix product of two matrices whose rows run along the summed axis:
+//   c[m][n] = sum_k x[m][k] w[n][k],
+// bf16 or 8-bit block format (block8.h) operands, bf16 matrix units, fp32 accumulators, one workgroup per tile of BN
+// rows of w and BM rows of x.  The epilogue gets the accumulators.  In the gated form half of the
+// tile's w rows come from a second matrix, so a lane holds both products of an output.
+//
+// A step takes 128 bytes of every row (64 bf16, or 128 8-bit elements: one scale block).  The tiles
+// of two steps lie in LDS: the loads of one go straight from memory to LDS while the other is
+// multiplied.  A row's eight 16-byte chunks are stored rotated by an exclusive or with the row, which
+// the loading lanes bring about by which chunk each of them fetches; so the lanes of a fragment read,
+// which hold one chunk of 32 rows, spread over all banks.
+//
+// v_mfma 32x32: w rows are the matrix unit's rows, x rows its columns, so that a lane's accumulators
+// are one x row (lane mod 32) and runs of four neighbouring w rows: four neighbouring outputs.  The
+// order of k inside a step is the same for both operands and otherwise free.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "block8.h"
+
+namespace spingtp {
+
+struct GemmArgs {
+    const uint8_t* w;   // [N] rows of ldw bytes
+    const uint8_t* w2;  // the second matrix of the gated form
+    const uint8_t* x;   // [M] rows of ldx bytes
+    int64_t ldw, ldx;
+    const uint8_t* ws;  // scales of the 8-bit format
+    const uint8_t* ws2;
+    const uint8_t* xs;
+    int64_t lds;        // bytes of a row of scales (both operands: the same K)
+    int64_t M, N;
+    int steps;          // of 128 bytes
+    int tail;           // bf16: bytes of the last step that exist, a multiple of 16 (128: all)
+    int tiles_m, tiles_n;
+};
+
+namespace {
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+
+constexpr int kStepBytes = 128;
+constexpr int64_t kMostTiles = int64_t{1} << 22;  // of a launch: below 2^32 threads
+
+// An operand's 16 bytes of a row as operands of v_mfma_f32_32x32x16_bf16.
+struct Bf16 {
+    static constexpr bool kScaled = false;
+    static constexpr int kParts = 1;
+    static __device__ __forceinline__ void expand(v4i raw, float, v8bf (&p)[1]) { p[0] = __builtin_bit_cast(v8bf, raw); }
+};
+// e4m3 values times their block's power of two are bf16 numbers exactly, and v_cvt_scalef32 makes them
+// in one instruction for two, so the products are exact in fp32 and only their sum rounds.  (The
+// matrix units' own 8-bit products, at twice the rate, are not taken: they add products cut to about
+// 12 bits below the largest of a group, 1.5e-5 of a result of normal values against 6e-8.)
+struct Fp8 {
+    static constexpr bool kScaled = true;
+    static constexpr int kParts = 2;
+    static __device__ __forceinline__ void expand(v4i raw, float scale, v8bf (&p)[2]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t lo = static_cast<uint32_t>(raw[2 * i]), hi = static_cast<uint32_t>(raw[2 * i + 1]);
+            const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
+            const v2bf b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+            const v2bf c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
+            const v2bf d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+            p[i] = v8bf{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+        }
+    }
+};
+
+__device__ const uint4 kZeroChunk = {0, 0, 0, 0};
+
+// 16 bytes per lane from memory to LDS at `to` + 16 lane
+__device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// The tile of this workgroup.  Neighbouring workgroups go to the 8 chiplets in turn: each chiplet
+// takes a run of tiles, 8 tiles of x by as many of w, so that its L2 serves both operands.
+__device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& tn) {
+    const int total = tiles_m * tiles_n, q = total >> 3, rest = total & 7;
+    const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const int i = xcd * q + (xcd < rest ? xcd : rest) + at;
+    const int group = i / (8 * tiles_n), in = i - group * 8 * tiles_n;
+    const int rows = tiles_m - 8 * group < 8 ? tiles_m - 8 * group : 8;
+    tn = in / rows;
+    tm = 8 * group + in - tn * rows;
+}
+
+// TN x TM accumulators of 32 x 32 per wave, WN x WM waves.
+template <class E, int TN, int TM, int WN, int WM, bool GATED>
+struct GemmTile {
+    static constexpr int kWaves = WN * WM, kThreads = 64 * kWaves;
+    static constexpr int BN = 32 * TN * WN, BM = 32 * TM * WM;
+    static constexpr int kStage = (BN + BM) * kStepBytes, kLds = 2 * kStage;
+    static constexpr int LW = BN / 8 / kWaves, LX = BM / 8 / kWaves;  // 8-row loads per wave and step
+    static_assert(LW * 8 * kWaves == BN && LX * 8 * kWaves == BM && kWaves % 2 == 0, "whole loads");
+    static_assert(!GATED || TN % 2 == 0, "both halves in a wave");
+    // rows of one matrix in the tile, and their count in outputs
+    static constexpr int kRows = GATED ? BN / 2 : BN;
+
+    v16f acc[TN][TM];
+    int lane, wave, wn, wm;
+
+    // first w row (of its matrix) of accumulator i, and of the tile in LDS
+    static __device__ __forceinline__ int row_in(int i, int wn) {
+        if constexpr (GATED) return (i % (TN / 2)) * 32 + wn * (TN / 2) * 32;
+        return (wn * TN + i) * 32;
+    }
+    static __device__ __forceinline__ int lds_row(int i, int wn) {
+        return (GATED && i >= TN / 2 ? kRows : 0) + row_in(i, wn);
+    }
+
+    __device__ __forceinline__ void run(const GemmArgs& a, int64_t n0, int64_t m0, uint8_t* lds) {
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wn = wave % WN;
+        wm = wave / WN;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int j = 0; j < TM; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+
+        // where the lane's chunk of each load lies: row lane / 8 of the load's eight
+        const int key = (4 * (wave & 1) + (lane >> 4)) & 7;  // (row >> 1) & 7
+        const int chunk = ((lane & 7) ^ key) * 16;
+        const uint8_t* pw[LW];
+        const uint8_t* px[LX];
+#pragma unroll
+        for (int t = 0; t < LW; ++t) {
+            int r = 8 * (wave + kWaves * t) + (lane >> 3);
+            const uint8_t* base = a.w;
+            if (GATED && r >= kRows) base = a.w2, r -= kRows;
+            const int64_t n = n0 + r < a.N ? n0 + r : a.N - 1;  // rows past the end are not stored
+            pw[t] = base + n * a.ldw + chunk;
+        }
+#pragma unroll
+        for (int t = 0; t < LX; ++t) {
+            const int r = 8 * (wave + kWaves * t) + (lane >> 3);
+            const int64_t m = m0 + r < a.M ? m0 + r : a.M - 1;
+            px[t] = a.x + m * a.ldx + chunk;
+        }
+        auto load = [&](int k, uint8_t* to) {
+            const int64_t off = static_cast<int64_t>(k) * kStepBytes;
+            if (!E::kScaled && a.tail < kStepBytes && k == a.steps - 1) {  // zeros past the end of the rows
+                const uint8_t* zero = reinterpret_cast<const uint8_t*>(&kZeroChunk);
+                const bool cut = chunk >= a.tail;
+#pragma unroll
+                for (int t = 0; t < LW; ++t) to_lds(cut ? zero : pw[t] + off, to + (wave + kWaves * t) * 1024);
+#pragma unroll
+                for (int t = 0; t < LX; ++t)
+                    to_lds(cut ? zero : px[t] + off, to + (BN / 8 + wave + kWaves * t) * 1024);
+                return;
+            }
+#pragma unroll
+            for (int t = 0; t < LW; ++t) to_lds(pw[t] + off, to + (wave + kWaves * t) * 1024);
+#pragma unroll
+            for (int t = 0; t < LX; ++t) to_lds(px[t] + off, to + (BN / 8 + wave + kWaves * t) * 1024);
+        };
+
+        // scales: a lane's rows, four steps' bytes in a word
+        const uint32_t* sw[TN];
+        const uint32_t* sx[TM];
+        uint32_t cw[TN], cx[TM], nw[TN], nx[TM];
+        if constexpr (E::kScaled) {
+#pragma unroll
+            for (int i = 0; i < TN; ++i) {
+                const int64_t r = n0 + row_in(i, wn) + (lane & 31), n = r < a.N ? r : a.N - 1;
+                sw[i] = reinterpret_cast<const uint32_t*>((GATED && i >= TN / 2 ? a.ws2 : a.ws) + n * a.lds);
+                nw[i] = *sw[i];
+            }
+#pragma unroll
+            for (int j = 0; j < TM; ++j) {
+                const int64_t r = m0 + (wm * TM + j) * 32 + (lane & 31), m = r < a.M ? r : a.M - 1;
+                sx[j] = reinterpret_cast<const uint32_t*>(a.xs + m * a.lds);
+                nx[j] = *sx[j];
+            }
+        }
+
+        const int fkey = (lane >> 1) & 7, half = lane >> 5;
+        int at[4];  // the lane's chunk of quarter step q
+#pragma unroll
+        for (int q = 0; q < 4; ++q) at[q] = (lane & 31) * 128 + (((2 * q + half) ^ fkey) << 4);
+
+        load(0, lds);
+        for (int k = 0; k < a.steps; ++k) {
+            uint8_t* here = lds + (k & 1) * kStage;
+            __syncthreads();  // step k has arrived, and the other stage has been read by all
+            if constexpr (E::kScaled) {
+                if ((k & 3) == 0) {
+                    const int ahead = k + 4 < a.steps ? (k >> 2) + 1 : 0;
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) cw[i] = nw[i], nw[i] = sw[i][ahead];
+#pragma unroll
+                    for (int j = 0; j < TM; ++j) cx[j] = nx[j], nx[j] = sx[j][ahead];
+                }
+            }
+            if (k + 1 < a.steps) load(k + 1, lds + ((k + 1) & 1) * kStage);
+            float fsw[TN], fsx[TM];
+            if constexpr (E::kScaled) {
+#pragma unroll
+                for (int i = 0; i < TN; ++i) fsw[i] = __uint_as_float((cw[i] & 255u) << 23);
+#pragma unroll
+                for (int j = 0; j < TM; ++j) fsx[j] = __uint_as_float((cx[j] & 255u) << 23);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                v8bf fw[TN][E::kParts], fx[TM][E::kParts];
+#pragma unroll
+                for (int j = 0; j < TM; ++j)
+                    E::expand(*reinterpret_cast<const v4i*>(here + BN * 128 + (wm * TM + j) * 4096 + at[q]), fsx[j],
+                              fx[j]);
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+                    E::expand(*reinterpret_cast<const v4i*>(here + lds_row(i, wn) * 128 + at[q]), fsw[i], fw[i]);
+#pragma unroll
+                for (int p = 0; p < E::kParts; ++p)
+#pragma unroll
+                    for (int i = 0; i < TN; ++i)
+#pragma unroll
+                        for (int j = 0; j < TM; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[i][p], fx[j][p], acc[i][j], 0, 0, 0);
+            }
+            if constexpr (E::kScaled) {
+#pragma unroll
+                for (int i = 0; i < TN; ++i) cw[i] >>= 8;
+#pragma unroll
+                for (int j = 0; j < TM; ++j) cx[j] >>= 8;
+            }
+        }
+    }
+
+    // output column (w row) of accumulator register r (a multiple of 4: four neighbours) of tile i, and
+    // output row of tile j
+    __device__ __forceinline__ int column(int i, int r) const { return row_in(i, wn) + 2 * r + 4 * (lane >> 5); }
+    __device__ __forceinline__ int row(int j) const { return (wm * TM + j) * 32 + (lane & 31); }
+};
+
+// Four neighbouring outputs of a row, those before column N.
+__device__ __forceinline__ void store4(float* p, int64_t left, float a, float b, float c, float d) {
+    if (left >= 4) {
+        *reinterpret_cast<u4f*>(p) = u4f{a, b, c, d};
+    } else {
+        if (left > 0) p[0] = a;
+        if (left > 1) p[1] = b;
+        if (left > 2) p[2] = c;
+    }
+}
+typedef uint32_t u2u __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void store4(uint16_t* p, int64_t left, float a, float b, float c, float d) {
+    const uint32_t lo = bf16_pair(a, b), hi = bf16_pair(c, d);
+    if (left >= 4) {
+        *reinterpret_cast<u2u*>(p) = u2u{lo, hi};
+    } else {
+        if (left > 0) p[0] = static_cast<uint16_t>(lo);
+        if (left > 1) p[1] = static_cast<uint16_t>(lo >> 16);
+        if (left > 2) p[2] = static_cast<uint16_t>(hi);
+    }
+}
+
+// The product itself, to out [M] rows of ldo elements.
+template <class E, int TN, int TM, int WN, int WM, typename TO>
+__global__ __launch_bounds__(64 * WN * WM) void gemm_nt_kernel(GemmArgs a, TO* __restrict__ out, int64_t ldo) {
+    using Tile = GemmTile<E, TN, TM, WN, WM, false>;
+    extern __shared__ __align__(16) uint8_t gemm_lds[];
+    int tm, tn;
+    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    const int64_t n0 = static_cast<int64_t>(tn) * Tile::BN, m0 = static_cast<int64_t>(tm) * Tile::BM;
+    Tile t;
+    t.run(a, n0, m0, gemm_lds);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+        const int64_t m = m0 + t.row(j);
+        if (m >= a.M) continue;
+        TO* p = out + m * ldo;
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4) {
+                const int64_t n = n0 + t.column(i, r);
+                const v16f& c = t.acc[i][j];
+                store4(p + n, a.N - n, c[r], c[r + 1], c[r + 2], c[r + 3]);
+            }
+    }
+}
+
+}  // namespace
+}  // namespace spingtp

@@ -1,0 +1,56 @@
+// Product of two matrices in the 8-bit block format: c[m][n] = sum_k a[m][k] b[n][k], both packed
+// along k, fp32 accumulators, c in fp32 or bf16.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "feedforward.h"
+#include "gemm_nt.h"
+#include "internal.h"
+#include "lds_common.h"
+
+namespace spingtp {
+namespace {
+
+template <int TN, int TM, int WN, int WM, typename TO>
+hipError_t launch(GemmArgs g, void* out, int64_t ldo, hipStream_t stream) {
+    using Tile = GemmTile<Fp8, TN, TM, WN, WM, false>;
+    const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
+    if (tm * tn > kMostTiles) return hipErrorInvalidValue;
+    g.tiles_m = static_cast<int>(tm);
+    g.tiles_n = static_cast<int>(tn);
+    constexpr auto kernel = gemm_nt_kernel<Fp8, TN, TM, WN, WM, TO>;
+    const hipError_t e = raise_lds_limit<kernel>();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g,
+                       static_cast<TO*>(out), ldo);
+    return hipGetLastError();
+}
+
+template <typename TO>
+hipError_t dispatch(const GemmArgs& g, void* out, int64_t ldo, hipStream_t stream) {
+    const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
+    // the largest tile that still gives most of the 256 CUs one
+    if (tiles(256) >= 192) return launch<4, 2, 2, 4, TO>(g, out, ldo, stream);
+    if (tiles(128) >= 192) return launch<2, 2, 2, 2, TO>(g, out, ldo, stream);
+    return launch<1, 1, 2, 2, TO>(g, out, ldo, stream);
+}
+
+}  // namespace
+
+hipError_t launch_matmul8(int dtype, const Matmul8Args& a, hipStream_t stream) {
+    GemmArgs g{};
+    g.w = a.b_values;
+    g.x = a.a_values;
+    g.ldw = g.ldx = block8_pitch(a.K);
+    g.ws = a.b_scales;
+    g.xs = a.a_scales;
+    g.lds = block8_scale_pitch(a.K);
+    g.M = a.M;
+    g.N = a.N;
+    g.steps = static_cast<int>(g.ldx / kStepBytes);
+    g.tail = kStepBytes;
+    return dtype == SPINGTP_FP32 ? dispatch<float>(g, a.c, a.ldc, stream) : dispatch<uint16_t>(g, a.c, a.ldc, stream);
+}
+
+}  // namespace spingtp
