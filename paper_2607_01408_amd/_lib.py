@@ -24,7 +24,7 @@ EXPORTED = ("spingtp_plan_create", "spingtp_forward", "spingtp_plan_destroy", "s
             "spingtp_backward_fully_connected", "spingtp_pack8", "spingtp_unpack8", "spingtp_rms_norm",
             "spingtp_rms_norm_backward", "spingtp_rms_norm_backward_workspace_size", "spingtp_matmul8",
             "spingtp_gated_forward", "spingtp_gated_forward_workspace_size", "spingtp_gated_forward8",
-            "spingtp_gated_backward", "spingtp_gated_backward_workspace_size")
+            "spingtp_gated_forward8_workspace_size", "spingtp_gated_backward", "spingtp_gated_backward_workspace_size")
 
 _lib = None
 
@@ -146,8 +146,9 @@ def _feedforward_signatures(L):
                        ("spingtp_rms_norm", "ipnpnpfpnpnpppnnp"), ("spingtp_rms_norm_backward", "ipnpnpppnpnppznnp"),
                        ("spingtp_rms_norm_backward_workspace_size", "nns"), ("spingtp_matmul8", "ppppipnnnnp"),
                        ("spingtp_gated_forward", "ipnppnpnipppppznnnp"),
-                       ("spingtp_gated_forward_workspace_size", "nnnnns"),
-                       ("spingtp_gated_forward8", "ipppppppnpnnnp"),
+                       ("spingtp_gated_forward_workspace_size", "nnnnnis"),
+                       ("spingtp_gated_forward8", "ipppppppnppznnnp"),
+                       ("spingtp_gated_forward8_workspace_size", "nnnis"),
                        ("spingtp_gated_backward", "ipnipppppnpppnpnppznnnp"),
                        ("spingtp_gated_backward_workspace_size", "nnns")):
         fn = getattr(L, name)

@@ -119,13 +119,15 @@ bool gated_sizes_ok(int act, int64_t M, int64_t K, int64_t F) {
            K <= int64_t{65535} * 64 && F <= int64_t{65535} * 64 && matrix_ok(M, K + 511) && matrix_ok(M, 2 * (F + 511)) &&
            matrix_ok(F, 2 * (K + 511));
 }
+bool save_ok(int s) { return s == SPINGTP_SAVE_NONE || s == SPINGTP_SAVE_BF16 || s == SPINGTP_SAVE_BLOCK8; }
 
 }  // namespace
 
 extern "C" spingtp_status spingtp_gated_forward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw,
-                                                               size_t* size) {
-    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || ldx < K || ldw < K) return SPINGTP_ERR_INVALID_ARG;
-    *size = spingtp::gated_workspace(M, K, F, ldx, ldw);
+                                                               spingtp_save save, size_t* size) {
+    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || ldx < K || ldw < K || !save_ok(save))
+        return SPINGTP_ERR_INVALID_ARG;
+    *size = spingtp::gated_workspace(M, K, F, ldx, ldw, save);
     return SPINGTP_OK;
 }
 
@@ -135,9 +137,7 @@ extern "C" spingtp_status spingtp_gated_forward(spingtp_activation act, const vo
                                                 size_t workspace_bytes, int64_t M, int64_t K, int64_t F, void* stream) {
     size_t need = 0;
     if (!gated_sizes_ok(act, M, K, F) || ldh < F || !matrix_ok(M, ldx) || !matrix_ok(F, ldw) || !matrix_ok(M, ldh) ||
-        spingtp_gated_forward_workspace_size(M, K, F, ldx, ldw, &need) != SPINGTP_OK)
-        return SPINGTP_ERR_INVALID_ARG;
-    if (save != SPINGTP_SAVE_NONE && save != SPINGTP_SAVE_BF16 && save != SPINGTP_SAVE_BLOCK8)
+        spingtp_gated_forward_workspace_size(M, K, F, ldx, ldw, save, &need) != SPINGTP_OK)
         return SPINGTP_ERR_INVALID_ARG;
     if (M == 0) return SPINGTP_OK;
     if (bad(x, 16) || bad(w_gate, 16) || bad(w_up, 16) || bad(h, 2)) return SPINGTP_ERR_INVALID_ARG;
@@ -165,16 +165,27 @@ extern "C" spingtp_status spingtp_gated_forward(spingtp_activation act, const vo
     return of(spingtp::launch_gated(a, stream_of(stream)));
 }
 
+extern "C" spingtp_status spingtp_gated_forward8_workspace_size(int64_t M, int64_t K, int64_t F, int out8,
+                                                                size_t* size) {
+    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F)) return SPINGTP_ERR_INVALID_ARG;
+    *size = spingtp::gated8_workspace(M, F, out8 != 0);
+    return SPINGTP_OK;
+}
+
 extern "C" spingtp_status spingtp_gated_forward8(spingtp_activation act, const void* x, const void* x_scales,
                                                  const void* w_gate, const void* w_gate_scales, const void* w_up,
                                                  const void* w_up_scales, void* h, int64_t ldh, void* h_scales,
-                                                 int64_t M, int64_t K, int64_t F, void* stream) {
-    if (!gated_sizes_ok(act, M, K, F) || (h_scales == nullptr && (ldh < F || !matrix_ok(M, ldh))))
+                                                 void* workspace, size_t workspace_bytes, int64_t M, int64_t K,
+                                                 int64_t F, void* stream) {
+    size_t need = 0;
+    if (!gated_sizes_ok(act, M, K, F) ||
+        spingtp_gated_forward8_workspace_size(M, K, F, h_scales != nullptr, &need) != SPINGTP_OK || (h_scales == nullptr && (ldh < F || !matrix_ok(M, ldh))))
         return SPINGTP_ERR_INVALID_ARG;
     if (M == 0) return SPINGTP_OK;
     if (bad(x, 16) || bad(x_scales, 4) || bad(w_gate, 16) || bad(w_gate_scales, 4) || bad(w_up, 16) ||
         bad(w_up_scales, 4) || bad(h, h_scales != nullptr ? 16 : 2) || off(h_scales, 4))
         return SPINGTP_ERR_INVALID_ARG;
+    if (need > 0 && (bad(workspace, 16) || workspace_bytes < need)) return SPINGTP_ERR_INVALID_ARG;
     spingtp::GatedArgs a{};
     a.act = act;
     a.x = x;
@@ -186,6 +197,7 @@ extern "C" spingtp_status spingtp_gated_forward8(spingtp_activation act, const v
     a.h = h;
     a.ldh = ldh;
     a.h_scales = bytes(h_scales);
+    a.workspace = workspace;
     a.M = M;
     a.K = K;
     a.F = F;

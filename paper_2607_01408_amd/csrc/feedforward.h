@@ -96,7 +96,8 @@ struct GatedArgs {
     void* workspace;
     int64_t M, K, F;
 };
-size_t gated_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw);
+size_t gated_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw, int save);
+size_t gated8_workspace(int64_t M, int64_t F, bool out8);
 hipError_t launch_gated(const GatedArgs& a, hipStream_t stream);
 hipError_t launch_gated8(const GatedArgs& a, hipStream_t stream);
 

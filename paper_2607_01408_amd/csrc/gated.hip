@@ -19,29 +19,36 @@
 
 #include "feedforward.h"
 #include "gemm_nt.h"
+#include "gemm_skinny.h"
 #include "internal.h"
 #include "lds_common.h"
 
 namespace spingtp {
 namespace {
 
-// act(g) and its derivative.  exp and the reciprocal are the hardware's (relative error near 2^-22,
-// against the 2^-9 of the outputs).
+// exp(x), off by about 2^-23: the hardware's 2^t of t = x log2 e, and the rounding of t put back.
+__device__ __forceinline__ float exp_of(float x) {
+    const float t = x * 1.44269504088896f;
+    const float rest = fmaf(x, 1.44269504088896f, -t) + x * 1.92596299e-8f;  // log2 e in two parts
+    const float e = __builtin_amdgcn_exp2f(t);
+    return e < __builtin_inff() ? fmaf(e, rest * 0.69314718f, e) : e;
+}
+// act(g) and its derivative; the reciprocal is the hardware's, off by 2^-23
 template <int ACT>
 __device__ __forceinline__ float act(float g) {
-    if constexpr (ACT == kSilu) return g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
+    if constexpr (ACT == kSilu) return g * __builtin_amdgcn_rcpf(1.f + exp_of(-g));
     return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
 }
 template <int ACT>
 __device__ __forceinline__ void act_grad(float g, float& a, float& d) {
     if constexpr (ACT == kSilu) {
-        const float t = __builtin_amdgcn_rcpf(1.f + __expf(-g));
+        const float t = __builtin_amdgcn_rcpf(1.f + exp_of(-g));
         a = g * t;
         d = t * (1.f + g * (1.f - t));
     } else {
         const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
         a = g * p;
-        d = p + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+        d = p + g * 0.39894228040143268f * exp_of(-0.5f * g * g);
     }
 }
 
@@ -155,6 +162,28 @@ __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOu
                                          o.spitch, g);
     else
         store_bf16<Tile, HALF, TM>(t, a, n0, m0, o.h, o.ldh, g);
+}
+
+// At most 32 rows of x.  What is to be 8-bit blocks leaves in fp32 [M][F] and is packed next (a
+// block's 128 columns are eight workgroups'): h with OUT32, g and u with SAVE = kSave8.
+template <class E, int TM, int ACT, int SAVE, bool OUT32>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void gated_skinny_kernel(GemmArgs a, int64_t row_bytes, GatedOut o) {
+    skinny_tile<E, TM, true>(a, row_bytes, static_cast<int64_t>(blockIdx.x) * 16,
+                             [&](int64_t m, int64_t n, float g, float u) {
+                                 if constexpr (SAVE == kSaveBf16) {
+                                     put(static_cast<uint16_t*>(o.g) + m * a.N + n, g);
+                                     put(static_cast<uint16_t*>(o.u) + m * a.N + n, u);
+                                 }
+                                 if constexpr (SAVE == kSave8) {
+                                     put(static_cast<float*>(o.g) + m * a.N + n, g);
+                                     put(static_cast<float*>(o.u) + m * a.N + n, u);
+                                 }
+                                 const float h = act<ACT>(g) * u;
+                                 if constexpr (OUT32)
+                                     put(static_cast<float*>(o.h) + m * a.N + n, h);
+                                 else
+                                     put(static_cast<uint16_t*>(o.h) + m * o.ldh + n, h);
+                             });
 }
 
 // Rows of K bf16 elements to rows of a multiple of 64, zeros behind: what the products read where the
@@ -334,6 +363,24 @@ hipError_t gated_tiles(const GemmArgs& g, const GatedOut& o, hipStream_t stream)
     return gated_launch<E, 2, 2, 4, 1, ACT, SAVE, OUT8>(g, o, stream);
 }
 
+template <class E, int ACT, int SAVE, bool OUT32>
+hipError_t gated_skinny(const GemmArgs& g, int64_t row_bytes, const GatedOut& o, hipStream_t stream) {
+    const int64_t blocks = (g.N + 15) / 16;
+    if (blocks > kMostTiles) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(blocks)), threads(64 * kSkinnyWaves);
+    if (g.M <= 16)
+        hipLaunchKernelGGL((gated_skinny_kernel<E, 1, ACT, SAVE, OUT32>), grid, threads, 0, stream, g, row_bytes, o);
+    else
+        hipLaunchKernelGGL((gated_skinny_kernel<E, 2, ACT, SAVE, OUT32>), grid, threads, 0, stream, g, row_bytes, o);
+    return hipGetLastError();
+}
+
+template <class E, int SAVE, bool OUT32>
+hipError_t gated_skinny_act(int act, const GemmArgs& g, int64_t row_bytes, const GatedOut& o, hipStream_t stream) {
+    return act == kSilu ? gated_skinny<E, kSilu, SAVE, OUT32>(g, row_bytes, o, stream)
+                        : gated_skinny<E, kGelu, SAVE, OUT32>(g, row_bytes, o, stream);
+}
+
 template <class E, int SAVE, bool OUT8>
 hipError_t gated_act(int act, const GemmArgs& g, const GatedOut& o, hipStream_t stream) {
     return act == kSilu ? gated_tiles<E, kSilu, SAVE, OUT8>(g, o, stream)
@@ -412,7 +459,8 @@ hipError_t gated_grad(const GatedBwdArgs& a, uint16_t* both, uint16_t* both_t, h
 
 }  // namespace
 
-size_t gated_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw) {
+size_t gated_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw, int save) {
+    if (M <= kSkinnyRows) return save == kSave8 ? static_cast<size_t>(2 * M * F) * sizeof(float) : 0;
     const int64_t pitch = up64(K) * 2;
     return static_cast<size_t>((rows_fit(K, ldx) ? 0 : M * pitch) + (rows_fit(K, ldw) ? 0 : 2 * F * pitch));
 }
@@ -428,6 +476,23 @@ hipError_t launch_gated(const GatedArgs& a, hipStream_t stream) {
     g.w2 = static_cast<const uint8_t*>(a.wu);
     g.ldx = 2 * a.ldx;
     g.ldw = 2 * a.ldw;
+    const GatedOut o{a.h, a.ldh, nullptr, a.g, a.u, a.g_scales, a.u_scales, block8_pitch(a.F), block8_scale_pitch(a.F)};
+    if (a.M <= kSkinnyRows) {  // rows of any alignment are read as they are
+        g.steps = static_cast<int>(pitch / 64);
+        if (a.save == kSaveNone) return gated_skinny_act<Bf16, kSaveNone, false>(a.act, g, 2 * a.K, o, stream);
+        if (a.save == kSaveBf16) return gated_skinny_act<Bf16, kSaveBf16, false>(a.act, g, 2 * a.K, o, stream);
+        GatedOut to32 = o;
+        to32.g = ws;
+        to32.u = reinterpret_cast<float*>(ws) + a.M * a.F;
+        hipError_t e = gated_skinny_act<Bf16, kSave8, false>(a.act, g, 2 * a.K, to32, stream);
+        if (e == hipSuccess)
+            e = launch_pack8(SPINGTP_FP32, to32.g, a.F, static_cast<uint8_t*>(a.g), a.g_scales, nullptr, nullptr, a.M,
+                             a.F, stream);
+        if (e == hipSuccess)
+            e = launch_pack8(SPINGTP_FP32, to32.u, a.F, static_cast<uint8_t*>(a.u), a.u_scales, nullptr, nullptr, a.M,
+                             a.F, stream);
+        return e;
+    }
     hipError_t e = hipSuccess;
     if (!rows_fit(a.K, a.ldx)) {
         e = stage(a.x, a.ldx, ws, a.M, a.K, stream);
@@ -447,12 +512,15 @@ hipError_t launch_gated(const GatedArgs& a, hipStream_t stream) {
     g.steps = static_cast<int>(pitch / 64);
     const int64_t held = (a.K + 7) / 8 * 16 - (g.steps - 1) * static_cast<int64_t>(kStepBytes);
     g.tail = static_cast<int>(held);
-    const GatedOut o{a.h, a.ldh, nullptr, a.g, a.u, a.g_scales, a.u_scales, block8_pitch(a.F), block8_scale_pitch(a.F)};
     switch (a.save) {
         case kSaveNone: return gated_act<Bf16, kSaveNone, false>(a.act, g, o, stream);
         case kSaveBf16: return gated_act<Bf16, kSaveBf16, false>(a.act, g, o, stream);
         default: return gated_act<Bf16, kSave8, false>(a.act, g, o, stream);
     }
+}
+
+size_t gated8_workspace(int64_t M, int64_t F, bool out8) {
+    return out8 && M <= kSkinnyRows ? static_cast<size_t>(M * F) * sizeof(float) : 0;
 }
 
 hipError_t launch_gated8(const GatedArgs& a, hipStream_t stream) {
@@ -471,6 +539,15 @@ hipError_t launch_gated8(const GatedArgs& a, hipStream_t stream) {
     g.tail = kStepBytes;
     const GatedOut o{a.h,     a.ldh,   a.h_scales, nullptr, nullptr, nullptr, nullptr, block8_pitch(a.F),
                      block8_scale_pitch(a.F)};
+    if (a.M <= kSkinnyRows) {
+        if (a.h_scales == nullptr) return gated_skinny_act<Fp8, kSaveNone, false>(a.act, g, 0, o, stream);
+        GatedOut to32 = o;
+        to32.h = a.workspace;
+        const hipError_t e = gated_skinny_act<Fp8, kSaveNone, true>(a.act, g, 0, to32, stream);
+        if (e != hipSuccess) return e;
+        return launch_pack8(SPINGTP_FP32, a.workspace, a.F, static_cast<uint8_t*>(a.h), a.h_scales, nullptr, nullptr,
+                            a.M, a.F, stream);
+    }
     return a.h_scales != nullptr ? gated_act<Fp8, kSaveNone, true>(a.act, g, o, stream)
                                  : gated_act<Fp8, kSaveNone, false>(a.act, g, o, stream);
 }

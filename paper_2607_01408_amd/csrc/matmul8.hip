@@ -6,6 +6,7 @@
 
 #include "feedforward.h"
 #include "gemm_nt.h"
+#include "gemm_skinny.h"
 #include "internal.h"
 #include "lds_common.h"
 
@@ -27,8 +28,19 @@ hipError_t launch(GemmArgs g, void* out, int64_t ldo, hipStream_t stream) {
     return hipGetLastError();
 }
 
+template <int TM, typename TO>
+hipError_t launch_skinny(const GemmArgs& g, void* out, int64_t ldo, hipStream_t stream) {
+    const int64_t blocks = (g.N + 15) / 16;
+    if (blocks > kMostTiles) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((gemm_skinny_kernel<Fp8, TM, TO>), dim3(static_cast<unsigned>(blocks)), dim3(64 * kSkinnyWaves),
+                       0, stream, g, int64_t{0}, static_cast<TO*>(out), ldo);
+    return hipGetLastError();
+}
+
 template <typename TO>
 hipError_t dispatch(const GemmArgs& g, void* out, int64_t ldo, hipStream_t stream) {
+    if (g.M <= 16) return launch_skinny<1, TO>(g, out, ldo, stream);
+    if (g.M <= kSkinnyRows) return launch_skinny<2, TO>(g, out, ldo, stream);
     const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
     // the largest tile that still gives most of the 256 CUs one
     if (tiles(256) >= 192) return launch<4, 2, 2, 4, TO>(g, out, ldo, stream);

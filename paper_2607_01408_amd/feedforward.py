@@ -280,13 +280,19 @@ def gated(x, w_gate, w_up, act="silu", save=None, out8=False):
         pg, pu = _block(w_gate, "w_gate", (F, K), dev), _block(w_up, "w_up", (F, K), dev)
         if F < 1:
             raise ValueError("the weights have no rows")
+        n, ws = ctypes.c_size_t(0), None
         if out8:
             h = Block8.empty(M, F, dev)
             o = (h.values.data_ptr(), 0, h.scales.data_ptr())
+            _lib.check(_call("spingtp_gated_forward8_workspace_size")(M, K, F, 1, ctypes.byref(n)),
+                       "spingtp_gated_forward8_workspace_size")
+            if n.value:
+                ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
         else:
             h = torch.empty((M, F), dtype=torch.bfloat16, device=dev)
             o = (h.data_ptr(), F, None)
-        _run("spingtp_gated_forward8", dev, _ACTS[act], *px, *pg, *pu, *o, M, K, F)
+        _run("spingtp_gated_forward8", dev, _ACTS[act], *px, *pg, *pu, *o, ws.data_ptr() if ws is not None else None,
+             n.value, M, K, F)
         return h, None
     if out8:
         raise ValueError("out8 needs Block8 operands")
@@ -310,8 +316,8 @@ def gated(x, w_gate, w_up, act="silu", save=None, out8=False):
         saved = GatedSaved(pack8(x), Block8.empty(M, F, dev), Block8.empty(M, F, dev), act, save)
         g = (saved.g.values.data_ptr(), saved.g.scales.data_ptr(), saved.u.values.data_ptr(), saved.u.scales.data_ptr())
     n, ws = ctypes.c_size_t(0), None
-    if K % 8 or ldx % 8 or ldw % 8:  # rows that the products cannot read as they are
-        _lib.check(_call("spingtp_gated_forward_workspace_size")(M, K, F, ldx, ldw, ctypes.byref(n)),
+    if K % 8 or ldx % 8 or ldw % 8 or (M <= 32 and save == "8bit"):  # otherwise none is needed
+        _lib.check(_call("spingtp_gated_forward_workspace_size")(M, K, F, ldx, ldw, _SAVES[save], ctypes.byref(n)),
                    "spingtp_gated_forward_workspace_size")
         ws = torch.empty(n.value, dtype=torch.uint8, device=dev)
     _run("spingtp_gated_forward", dev, _ACTS[act], px, ldx, pg, pu, ldw, h.data_ptr(), F, _SAVES[save], *g,

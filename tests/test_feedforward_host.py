@@ -19,8 +19,8 @@ NORM_BWD = dict(dtype=1, grad_y=P, ldg=8, h=P, ldh=8, rstd=P, gain=P, grad_h=Non
 MATMUL = dict(a_values=P, a_scales=P, b_values=P, b_scales=P, dtype=0, c=P, ldc=4, M=2, N=4, K=8, stream=None)
 GATED = dict(act=0, x=P, ldx=8, w_gate=P, w_up=P, ldw=8, h=P, ldh=4, save=0, g=None, g_scales=None, u=None, u_scales=None,
              workspace=None, workspace_bytes=0, M=2, K=8, F=4, stream=None)
-GATED8 = dict(act=0, x=P, x_scales=P, w_gate=P, w_gate_scales=P, w_up=P, w_up_scales=P, h=P, ldh=4, h_scales=None, M=2,
-              K=8, F=4, stream=None)
+GATED8 = dict(act=0, x=P, x_scales=P, w_gate=P, w_gate_scales=P, w_up=P, w_up_scales=P, h=P, ldh=4, h_scales=None,
+              workspace=P, workspace_bytes=4096, M=2, K=8, F=4, stream=None)
 GATED_BWD = dict(act=0, grad_h=P, ldgh=4, save=1, g=P, g_scales=None, u=P, u_scales=None, x=P, ldx=8, x_scales=None,
                  w_gate=P, w_up=P, ldw=8, grad_x=P, ldgx=8, grad_w=P, workspace=P, workspace_bytes=1 << 30, M=2, K=8, F=4,
                  stream=None)
@@ -44,11 +44,13 @@ REFUSED = [
                                  dict(c=None), dict(c=P + 2)]),
     ("spingtp_gated_forward", GATED, [dict(act=2), dict(K=0), dict(F=0), dict(M=-1), dict(ldx=7), dict(ldw=7), dict(ldh=3),
                                       dict(x=P + 2), dict(w_gate=None), dict(w_up=P + 8), dict(h=None), dict(save=3),
-                                      dict(save=1), dict(save=1, g=P), dict(save=2, g=P, u=P), dict(K=7),
-                                      dict(ldx=9), dict(K=7, workspace=P, workspace_bytes=16), dict(F=64 * 65535 + 1, ldh=BIG)]),
+                                      dict(save=1), dict(save=1, g=P), dict(save=2, g=P, u=P),
+                                      dict(save=2, g=P, u=P, g_scales=P, u_scales=P),
+                                      dict(K=7, M=33), dict(ldx=9, M=33), dict(K=7, M=33, workspace=P, workspace_bytes=16), dict(F=64 * 65535 + 1, ldh=BIG)]),
     ("spingtp_gated_forward8", GATED8, [dict(act=-1), dict(K=0), dict(F=0), dict(ldh=3), dict(x=None), dict(x_scales=None),
                                         dict(w_gate=P + 8), dict(w_gate_scales=None), dict(w_up=None),
-                                        dict(w_up_scales=P + 2), dict(h=None), dict(h=P + 2, h_scales=P)]),
+                                        dict(w_up_scales=P + 2), dict(h=None), dict(h=P + 2, h_scales=P),
+                                        dict(h_scales=P, workspace=None), dict(h_scales=P, workspace_bytes=16)]),
     ("spingtp_gated_backward", GATED_BWD, [dict(act=2), dict(save=0), dict(save=2), dict(ldgh=3), dict(ldx=7), dict(ldw=7),
                                            dict(ldgx=7), dict(g=None), dict(u=P + 8), dict(x=None), dict(w_gate=None),
                                            dict(grad_h=None), dict(workspace=None), dict(workspace_bytes=64),
@@ -77,20 +79,28 @@ def test_nothing_to_do(name, good, none):
 
 
 @pytest.mark.parametrize("name,sizes", [("spingtp_rms_norm_backward_workspace_size", (2, 0)),
-                                        ("spingtp_gated_forward_workspace_size", (2, 8, 4, 7, 8)),
+                                        ("spingtp_gated_forward_workspace_size", (33, 8, 4, 7, 8, 0)),
+                                        ("spingtp_gated_forward8_workspace_size", (0, 0, 4, 1)),
                                         ("spingtp_gated_backward_workspace_size", (2, 8, 0))])
 def test_workspace_sizes(name, sizes):
     n = ctypes.c_size_t(0)
     fn = getattr(_lib.lib(), name)
     assert fn(*sizes, ctypes.byref(n)) == INVALID
-    assert fn(*(abs(s) or 1 for s in sizes[:3]), *((8,) * (len(sizes) - 3)), None) == INVALID
-    good = tuple(s or 5 for s in sizes[:3]) + (9,) * (len(sizes) - 3)
+    good = tuple(max(s, 9) if i < 5 else s for i, s in enumerate(sizes))
+    assert fn(*good, None) == INVALID
     assert fn(*good, ctypes.byref(n)) == OK and n.value > 0
 
 
 def test_workspace_grows_with_the_operands():
     n = ctypes.c_size_t(0)
     fn = _lib.lib().spingtp_gated_forward_workspace_size
-    assert fn(100, 64, 32, 64, 64, ctypes.byref(n)) == OK and n.value == 0  # rows on 16 bytes: read as they are
-    assert fn(100, 63, 32, 63, 63, ctypes.byref(n)) == OK and n.value == 2 * 64 * (100 + 2 * 32)
-    assert fn(100, 64, 32, 65, 64, ctypes.byref(n)) == OK and n.value == 2 * 64 * 100
+    assert fn(100, 64, 32, 64, 64, 0, ctypes.byref(n)) == OK and n.value == 0  # rows on 16 bytes: read as they are
+    assert fn(100, 63, 32, 63, 63, 1, ctypes.byref(n)) == OK and n.value == 2 * 64 * (100 + 2 * 32)
+    assert fn(100, 64, 32, 65, 64, 2, ctypes.byref(n)) == OK and n.value == 2 * 64 * 100
+    assert fn(32, 63, 32, 63, 63, 1, ctypes.byref(n)) == OK and n.value == 0  # few rows: as they are
+    assert fn(32, 63, 32, 63, 63, 2, ctypes.byref(n)) == OK and n.value == 4 * 2 * 32 * 32  # g and u in fp32
+    assert fn(32, 63, 32, 63, 63, 3, ctypes.byref(n)) == INVALID
+    fn = _lib.lib().spingtp_gated_forward8_workspace_size
+    assert fn(32, 64, 100, 1, ctypes.byref(n)) == OK and n.value == 4 * 32 * 100
+    assert fn(33, 64, 100, 1, ctypes.byref(n)) == OK and n.value == 0
+    assert fn(1, 64, 100, 0, ctypes.byref(n)) == OK and n.value == 0
