@@ -677,7 +677,9 @@ spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
  * allocates nothing and waits for nothing.
  *
  * A matrix [R][D] given as (pointer, ld) has rows of D neighbouring elements, `ld` elements apart
- * (ld >= D).  Sizes are at most 2^31 - 1 (gated block: K, F <= 4194240), matrices 2^46 elements.
+ * (ld >= D).  Sizes are at most 2^31 - 1, matrices 2^46 elements; the products' summed axes are
+ * shorter: K <= 8388480 (spingtp_matmul8), K <= 4194240, F <= 2097120 and, for the gradients,
+ * M <= 4194240 (gated block).
  * Outputs must not overlap inputs or one another.  R = 0 (M = 0) is valid: gradients of weights are
  * then zero, everything else is empty.  Sums and statistics are fp32, outputs are rounded to nearest
  * even.

@@ -102,7 +102,7 @@ extern "C" spingtp_status spingtp_rms_norm_backward(spingtp_dtype dtype, const v
 extern "C" spingtp_status spingtp_matmul8(const void* a_values, const void* a_scales, const void* b_values,
                                           const void* b_scales, spingtp_dtype dtype, void* c, int64_t ldc, int64_t M,
                                           int64_t N, int64_t K, void* stream) {
-    if (!dtype_ok(dtype) || !size_ok(M, 0) || !size_ok(N, 0) || !size_ok(K, 1) || ldc < N || ldc < 1 ||
+    if (!dtype_ok(dtype) || !size_ok(M, 0) || !size_ok(N, 0) || !size_ok(K, 1) || K > int64_t{65535} * 128 || ldc < N || ldc < 1 ||
         !matrix_ok(M, ldc) || !matrix_ok(M, K + 511) || !matrix_ok(N, K + 511))
         return SPINGTP_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return SPINGTP_OK;
@@ -116,7 +116,7 @@ namespace {
 
 bool gated_sizes_ok(int act, int64_t M, int64_t K, int64_t F) {
     return (act == spingtp::kSilu || act == spingtp::kGelu) && size_ok(M, 0) && size_ok(K, 1) && size_ok(F, 1) &&
-           K <= int64_t{65535} * 64 && F <= int64_t{65535} * 64 && matrix_ok(M, K + 511) && matrix_ok(M, 2 * (F + 511)) &&
+           K <= int64_t{65535} * 64 && F <= int64_t{65535} * 32 && matrix_ok(M, K + 511) && matrix_ok(M, 2 * (F + 511)) &&
            matrix_ok(F, 2 * (K + 511));
 }
 bool save_ok(int s) { return s == SPINGTP_SAVE_NONE || s == SPINGTP_SAVE_BF16 || s == SPINGTP_SAVE_BLOCK8; }
@@ -205,7 +205,8 @@ extern "C" spingtp_status spingtp_gated_forward8(spingtp_activation act, const v
 }
 
 extern "C" spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, size_t* size) {
-    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F)) return SPINGTP_ERR_INVALID_ARG;
+    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || M > int64_t{65535} * 64)
+        return SPINGTP_ERR_INVALID_ARG;
     *size = spingtp::gated_backward_workspace(M, K, F);
     return SPINGTP_OK;
 }

@@ -388,7 +388,7 @@ hipError_t gated_act(int act, const GemmArgs& g, const GatedOut& o, hipStream_t 
 }
 
 // whether the products can read these rows as they are
-bool rows_fit(int64_t K, int64_t ld) { return K % 8 == 0 && ld % 8 == 0; }
+bool rows_fit(int64_t K, int64_t ld) { return K % 8 == 0 && ld % 8 == 0 && 2 * ld <= kMostRowBytes; }
 int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
 
 hipError_t stage(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K, hipStream_t stream) {

@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "block8.h"
 
@@ -27,7 +28,7 @@ struct GemmArgs {
     const uint8_t* w;   // [N] rows of ldw bytes
     const uint8_t* w2;  // the second matrix of the gated form
     const uint8_t* x;   // [M] rows of ldx bytes
-    int64_t ldw, ldx;
+    int64_t ldw, ldx;   // at most kMostRowBytes
     const uint8_t* ws;  // scales of the 8-bit format
     const uint8_t* ws2;
     const uint8_t* xs;
@@ -73,13 +74,20 @@ struct Fp8 {
     }
 };
 
-__device__ const uint4 kZeroChunk = {0, 0, 0, 0};
-
-// 16 bytes per lane from memory to LDS at `to` + 16 lane
-__device__ __forceinline__ void to_lds(const uint8_t* from, uint8_t* to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                     (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// Rows from `base` on as a buffer of `bytes` bytes: what a load asks for past them is zero.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ __forceinline__ Buffer buffer_of(const uint8_t* base, uint32_t bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, static_cast<int>(bytes), 0x00027000);
 }
+// 16 bytes per lane from the buffer to LDS at `to` + 16 lane.  (As a buffer instruction: the compiler
+// takes a global load to LDS for one that may touch LDS in any order, and lets every later read of
+// LDS wait for all before it.)
+__device__ __forceinline__ void to_lds(Buffer from, uint32_t lane_at, int at, uint8_t* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16,
+                                             static_cast<int>(lane_at), at, 0, 0);
+}
+// Most bytes between the rows of an operand: a tile's 256 rows in a buffer's 32-bit offsets.
+constexpr int64_t kMostRowBytes = (int64_t{1} << 23);
 
 // The tile of this workgroup.  Neighbouring workgroups go to the 8 chiplets in turn: each chiplet
 // takes a run of tiles, 8 tiles of x by as many of w, so that its L2 serves both operands.
@@ -101,7 +109,7 @@ struct GemmTile {
     static constexpr int kStage = (BN + BM) * kStepBytes, kLds = 2 * kStage;
     static constexpr int LW = BN / 8 / kWaves, LX = BM / 8 / kWaves;  // 8-row loads per wave and step
     static_assert(LW * 8 * kWaves == BN && LX * 8 * kWaves == BM && kWaves % 2 == 0, "whole loads");
-    static_assert(!GATED || TN % 2 == 0, "both halves in a wave");
+    static_assert(!GATED || (TN % 2 == 0 && LW % 2 == 0), "both halves in a wave, and in its loads");
     // rows of one matrix in the tile, and their count in outputs
     static constexpr int kRows = GATED ? BN / 2 : BN;
 
@@ -132,38 +140,43 @@ struct GemmTile {
         // where the lane's chunk of each load lies: row lane / 8 of the load's eight
         const int key = (4 * (wave & 1) + (lane >> 4)) & 7;  // (row >> 1) & 7
         const int chunk = ((lane & 7) ^ key) * 16;
-        const uint8_t* pw[LW];
-        const uint8_t* px[LX];
+        const uint32_t ldw = static_cast<uint32_t>(a.ldw), ldx = static_cast<uint32_t>(a.ldx);
+        const int rows_w = a.N - n0 < kRows ? static_cast<int>(a.N - n0) : kRows;
+        const int rows_x = a.M - m0 < BM ? static_cast<int>(a.M - m0) : BM;
+        const uint32_t held = static_cast<uint32_t>(a.steps - 1) * kStepBytes + (E::kScaled ? kStepBytes : a.tail);
+        const uint32_t bytes_w = (rows_w - 1) * ldw + held, bytes_x = (rows_x - 1) * ldx + held;
+        const Buffer bw = buffer_of(a.w + n0 * a.ldw, bytes_w);
+        const Buffer bw2 = buffer_of((GATED ? a.w2 : a.w) + n0 * a.ldw, bytes_w);
+        const Buffer bx = buffer_of(a.x + m0 * a.ldx, bytes_x);
+        uint32_t ow[LW], ox[LX];
 #pragma unroll
         for (int t = 0; t < LW; ++t) {
-            int r = 8 * (wave + kWaves * t) + (lane >> 3);
-            const uint8_t* base = a.w;
-            if (GATED && r >= kRows) base = a.w2, r -= kRows;
-            const int64_t n = n0 + r < a.N ? n0 + r : a.N - 1;  // rows past the end are not stored
-            pw[t] = base + n * a.ldw + chunk;
+            const int r = 8 * (wave + kWaves * t) + (lane >> 3) - (GATED && t >= LW / 2 ? kRows : 0);
+            ow[t] = (r < rows_w ? r : rows_w - 1) * ldw + chunk;  // rows past the end are not stored
         }
 #pragma unroll
         for (int t = 0; t < LX; ++t) {
             const int r = 8 * (wave + kWaves * t) + (lane >> 3);
-            const int64_t m = m0 + r < a.M ? m0 + r : a.M - 1;
-            px[t] = a.x + m * a.ldx + chunk;
+            ox[t] = (r < rows_x ? r : rows_x - 1) * ldx + chunk;
         }
         auto load = [&](int k, uint8_t* to) {
-            const int64_t off = static_cast<int64_t>(k) * kStepBytes;
-            if (!E::kScaled && a.tail < kStepBytes && k == a.steps - 1) {  // zeros past the end of the rows
-                const uint8_t* zero = reinterpret_cast<const uint8_t*>(&kZeroChunk);
+#pragma unroll
+            for (int t = 0; t < LW; ++t)
+                to_lds(GATED && t >= LW / 2 ? bw2 : bw, ow[t], k * kStepBytes, to + (wave + kWaves * t) * 1024);
+#pragma unroll
+            for (int t = 0; t < LX; ++t)
+                to_lds(bx, ox[t], k * kStepBytes, to + (BN / 8 + wave + kWaves * t) * 1024);
+        };
+        // the last step, where its rows end inside: zeros past their end
+        auto load_any = [&](int k, uint8_t* to) {
+            if (!E::kScaled && a.tail < kStepBytes && k == a.steps - 1) {
                 const bool cut = chunk >= a.tail;
 #pragma unroll
-                for (int t = 0; t < LW; ++t) to_lds(cut ? zero : pw[t] + off, to + (wave + kWaves * t) * 1024);
+                for (int t = 0; t < LW; ++t) ow[t] = cut ? 0x80000000u : ow[t];  // past the buffer
 #pragma unroll
-                for (int t = 0; t < LX; ++t)
-                    to_lds(cut ? zero : px[t] + off, to + (BN / 8 + wave + kWaves * t) * 1024);
-                return;
+                for (int t = 0; t < LX; ++t) ox[t] = cut ? 0x80000000u : ox[t];
             }
-#pragma unroll
-            for (int t = 0; t < LW; ++t) to_lds(pw[t] + off, to + (wave + kWaves * t) * 1024);
-#pragma unroll
-            for (int t = 0; t < LX; ++t) to_lds(px[t] + off, to + (BN / 8 + wave + kWaves * t) * 1024);
+            load(k, to);
         };
 
         // scales: a lane's rows, four steps' bytes in a word
@@ -190,10 +203,45 @@ struct GemmTile {
 #pragma unroll
         for (int q = 0; q < 4; ++q) at[q] = (lane & 31) * 128 + (((2 * q + half) ^ fkey) << 4);
 
-        load(0, lds);
-        for (int k = 0; k < a.steps; ++k) {
+        // Fragments are read a quarter step ahead, and the last quarter of a step is multiplied behind the
+        // barrier that ends its reads, so the matrix units have work while the next step's first
+        // fragments come.
+        v4i rw[2][TN], rx[2][TM];
+        auto read = [&](const uint8_t* from, int q, int buffer) {
+#pragma unroll
+            for (int j = 0; j < TM; ++j)
+                rx[buffer][j] = *reinterpret_cast<const v4i*>(from + BN * 128 + (wm * TM + j) * 4096 + at[q]);
+#pragma unroll
+            for (int i = 0; i < TN; ++i)
+                rw[buffer][i] = *reinterpret_cast<const v4i*>(from + lds_row(i, wn) * 128 + at[q]);
+            __builtin_amdgcn_sched_barrier(0);  // before the products that do not need them
+        };
+        float fsw[TN], fsx[TM];
+        auto multiply = [&](int buffer) {
+            v8bf fw[TN][E::kParts], fx[TM][E::kParts];
+#pragma unroll
+            for (int j = 0; j < TM; ++j) E::expand(rx[buffer][j], fsx[j], fx[j]);
+#pragma unroll
+            for (int i = 0; i < TN; ++i) E::expand(rw[buffer][i], fsw[i], fw[i]);
+#pragma unroll
+            for (int p = 0; p < E::kParts; ++p)
+#pragma unroll
+                for (int i = 0; i < TN; ++i)
+#pragma unroll
+                    for (int j = 0; j < TM; ++j)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[i][p], fx[j][p], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+
+        load_any(0, lds);
+        __syncthreads();
+        if (a.steps > 1) load_any(1, lds + kStage);
+        read(lds, 0, 0);
+        // step k: its products, the loads of step k + 2 (MORE = 2: some step before the last, 1: any), the
+        // first fragments of step k + 1
+        auto step = [&](int k, auto more, auto follows) {
             uint8_t* here = lds + (k & 1) * kStage;
-            __syncthreads();  // step k has arrived, and the other stage has been read by all
+            uint8_t* next = lds + ((k + 1) & 1) * kStage;
             if constexpr (E::kScaled) {
                 if ((k & 3) == 0) {
                     const int ahead = k + 4 < a.steps ? (k >> 2) + 1 : 0;
@@ -202,40 +250,28 @@ struct GemmTile {
 #pragma unroll
                     for (int j = 0; j < TM; ++j) cx[j] = nx[j], nx[j] = sx[j][ahead];
                 }
-            }
-            if (k + 1 < a.steps) load(k + 1, lds + ((k + 1) & 1) * kStage);
-            float fsw[TN], fsx[TM];
-            if constexpr (E::kScaled) {
 #pragma unroll
-                for (int i = 0; i < TN; ++i) fsw[i] = __uint_as_float((cw[i] & 255u) << 23);
+                for (int i = 0; i < TN; ++i) fsw[i] = __uint_as_float((cw[i] & 255u) << 23), cw[i] >>= 8;
 #pragma unroll
-                for (int j = 0; j < TM; ++j) fsx[j] = __uint_as_float((cx[j] & 255u) << 23);
+                for (int j = 0; j < TM; ++j) fsx[j] = __uint_as_float((cx[j] & 255u) << 23), cx[j] >>= 8;
             }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                v8bf fw[TN][E::kParts], fx[TM][E::kParts];
-#pragma unroll
-                for (int j = 0; j < TM; ++j)
-                    E::expand(*reinterpret_cast<const v4i*>(here + BN * 128 + (wm * TM + j) * 4096 + at[q]), fsx[j],
-                              fx[j]);
-#pragma unroll
-                for (int i = 0; i < TN; ++i)
-                    E::expand(*reinterpret_cast<const v4i*>(here + lds_row(i, wn) * 128 + at[q]), fsw[i], fw[i]);
-#pragma unroll
-                for (int p = 0; p < E::kParts; ++p)
-#pragma unroll
-                    for (int i = 0; i < TN; ++i)
-#pragma unroll
-                        for (int j = 0; j < TM; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[i][p], fx[j][p], acc[i][j], 0, 0, 0);
+            for (int q = 0; q < 3; ++q) {
+                read(here, q + 1, (q + 1) & 1);
+                multiply(q & 1);
             }
-            if constexpr (E::kScaled) {
-#pragma unroll
-                for (int i = 0; i < TN; ++i) cw[i] >>= 8;
-#pragma unroll
-                for (int j = 0; j < TM; ++j) cx[j] >>= 8;
-            }
-        }
+            __syncthreads();  // step k + 1 has arrived, and step k has been read by all
+            if constexpr (decltype(more)::value == 2) load(k + 2, here);
+            if constexpr (decltype(more)::value == 1) load_any(k + 2, here);
+            if constexpr (decltype(follows)::value) read(next, 0, 0);
+            multiply(1);
+        };
+        using std::integral_constant;
+        int k = 0;
+        for (; k + 3 < a.steps; ++k) step(k, integral_constant<int, 2>{}, std::true_type{});
+        if (k + 2 < a.steps) step(k++, integral_constant<int, 1>{}, std::true_type{});
+        if (k + 1 < a.steps) step(k++, integral_constant<int, 0>{}, std::true_type{});
+        step(k, integral_constant<int, 0>{}, std::false_type{});
     }
 
     // output column (w row) of accumulator register r (a multiple of 4: four neighbours) of tile i, and

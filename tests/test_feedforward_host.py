@@ -41,12 +41,12 @@ REFUSED = [
                                              dict(grad_h=P, ldgh=7), dict(workspace=None), dict(workspace_bytes=8)]),
     ("spingtp_matmul8", MATMUL, [dict(dtype=2), dict(K=0), dict(M=-1), dict(N=BIG), dict(ldc=3), dict(a_values=None),
                                  dict(a_values=P + 8), dict(a_scales=None), dict(b_scales=P + 1), dict(b_values=None),
-                                 dict(c=None), dict(c=P + 2)]),
+                                 dict(c=None), dict(c=P + 2), dict(K=128 * 65535 + 1)]),
     ("spingtp_gated_forward", GATED, [dict(act=2), dict(K=0), dict(F=0), dict(M=-1), dict(ldx=7), dict(ldw=7), dict(ldh=3),
                                       dict(x=P + 2), dict(w_gate=None), dict(w_up=P + 8), dict(h=None), dict(save=3),
                                       dict(save=1), dict(save=1, g=P), dict(save=2, g=P, u=P),
                                       dict(save=2, g=P, u=P, g_scales=P, u_scales=P),
-                                      dict(K=7, M=33), dict(ldx=9, M=33), dict(K=7, M=33, workspace=P, workspace_bytes=16), dict(F=64 * 65535 + 1, ldh=BIG)]),
+                                      dict(K=7, M=33), dict(ldx=9, M=33), dict(K=7, M=33, workspace=P, workspace_bytes=16), dict(F=32 * 65535 + 1, ldh=BIG), dict(K=64 * 65535 + 1, ldx=BIG, ldw=BIG)]),
     ("spingtp_gated_forward8", GATED8, [dict(act=-1), dict(K=0), dict(F=0), dict(ldh=3), dict(x=None), dict(x_scales=None),
                                         dict(w_gate=P + 8), dict(w_gate_scales=None), dict(w_up=None),
                                         dict(w_up_scales=P + 2), dict(h=None), dict(h=P + 2, h_scales=P),
@@ -54,7 +54,7 @@ REFUSED = [
     ("spingtp_gated_backward", GATED_BWD, [dict(act=2), dict(save=0), dict(save=2), dict(ldgh=3), dict(ldx=7), dict(ldw=7),
                                            dict(ldgx=7), dict(g=None), dict(u=P + 8), dict(x=None), dict(w_gate=None),
                                            dict(grad_h=None), dict(workspace=None), dict(workspace_bytes=64),
-                                           dict(x_scales=P + 1)]),
+                                           dict(x_scales=P + 1), dict(M=64 * 65535 + 1)]),
 ]
 
 
