@@ -86,6 +86,12 @@ __device__ __forceinline__ void to_lds(Buffer from, uint32_t lane_at, int at, ui
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16,
                                              static_cast<int>(lane_at), at, 0, 0);
 }
+// Waits for all of the wave's loads and LDS reads, then for all waves of the workgroup.  Written out: what
+// __syncthreads waits for is the compiler's account, which has lost loads to LDS here where register
+// loads of one branch came between.
+__device__ __forceinline__ void arrived_and_read() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 // Most bytes between the rows of an operand: a tile's 256 rows in a buffer's 32-bit offsets.
 constexpr int64_t kMostRowBytes = (int64_t{1} << 23);
 
@@ -159,13 +165,18 @@ struct GemmTile {
             const int r = 8 * (wave + kWaves * t) + (lane >> 3);
             ox[t] = (r < rows_x ? r : rows_x - 1) * ldx + chunk;
         }
+        // load t of the wave's LW + LX of step k
+        auto load_part = [&](int t, int k, uint8_t* to) {
+            if (t < LW)
+                to_lds(GATED && t >= LW / 2 ? bw2 : bw, ow[t < LW ? t : 0], k * kStepBytes,
+                       to + (wave + kWaves * t) * 1024);
+            else
+                to_lds(bx, ox[t < LW ? 0 : t - LW], k * kStepBytes,
+                       to + (BN / 8 + wave + kWaves * (t - LW)) * 1024);
+        };
         auto load = [&](int k, uint8_t* to) {
 #pragma unroll
-            for (int t = 0; t < LW; ++t)
-                to_lds(GATED && t >= LW / 2 ? bw2 : bw, ow[t], k * kStepBytes, to + (wave + kWaves * t) * 1024);
-#pragma unroll
-            for (int t = 0; t < LX; ++t)
-                to_lds(bx, ox[t], k * kStepBytes, to + (BN / 8 + wave + kWaves * t) * 1024);
+            for (int t = 0; t < LW + LX; ++t) load_part(t, k, to);
         };
         // the last step, where its rows end inside: zeros past their end
         auto load_any = [&](int k, uint8_t* to) {
@@ -217,24 +228,29 @@ struct GemmTile {
             __builtin_amdgcn_sched_barrier(0);  // before the products that do not need them
         };
         float fsw[TN], fsx[TM];
-        auto multiply = [&](int buffer) {
+        // `between(n)` comes behind the n-th product
+        auto multiply = [&](int buffer, auto between) {
             v8bf fw[TN][E::kParts], fx[TM][E::kParts];
 #pragma unroll
             for (int j = 0; j < TM; ++j) E::expand(rx[buffer][j], fsx[j], fx[j]);
 #pragma unroll
             for (int i = 0; i < TN; ++i) E::expand(rw[buffer][i], fsw[i], fw[i]);
+            int n = 0;
 #pragma unroll
             for (int p = 0; p < E::kParts; ++p)
 #pragma unroll
                 for (int i = 0; i < TN; ++i)
 #pragma unroll
-                    for (int j = 0; j < TM; ++j)
+                    for (int j = 0; j < TM; ++j) {
                         acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[i][p], fx[j][p], acc[i][j], 0, 0, 0);
+                        between(n++);
+                    }
             __builtin_amdgcn_sched_barrier(0);
         };
+        const auto nothing = [](int) {};
 
         load_any(0, lds);
-        __syncthreads();
+        arrived_and_read();
         if (a.steps > 1) load_any(1, lds + kStage);
         read(lds, 0, 0);
         // step k: its products, the loads of step k + 2 (MORE = 2: some step before the last, 1: any), the
@@ -258,13 +274,22 @@ struct GemmTile {
 #pragma unroll
             for (int q = 0; q < 3; ++q) {
                 read(here, q + 1, (q + 1) & 1);
-                multiply(q & 1);
+                multiply(q & 1, nothing);
             }
-            __syncthreads();  // step k + 1 has arrived, and step k has been read by all
-            if constexpr (decltype(more)::value == 2) load(k + 2, here);
-            if constexpr (decltype(more)::value == 1) load_any(k + 2, here);
+            arrived_and_read();  // step k + 1 has arrived, and step k has been read by all
             if constexpr (decltype(follows)::value) read(next, 0, 0);
-            multiply(1);
+            if constexpr (decltype(more)::value == 1) load_any(k + 2, here);
+            if constexpr (decltype(more)::value == 2) {
+                // spread over the products: a burst of loads would hold the wave up at their issue
+                constexpr int products = TN * TM * E::kParts, loads = LW + LX;
+                multiply(1, [&](int n) {
+#pragma unroll
+                    for (int t = n * loads / products; t < (n + 1) * loads / products; ++t) load_part(t, k + 2, here);
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            } else {
+                multiply(1, nothing);
+            }
         };
         using std::integral_constant;
         int k = 0;
