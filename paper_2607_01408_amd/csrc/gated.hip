@@ -63,11 +63,12 @@ struct GatedOut {
     int64_t pitch, spitch;  // of the 8-bit rows
 };
 
-// A tile's rows of 128 columns as 8-bit blocks: `value(i, j, r)` is column column(i, r) of row row(j).
-template <class Tile, int HALF, int TM, int WN, class V>
+// A tile's rows of 128 columns as 8-bit blocks: `value(i, j, r)` is column column(i, r / 4) + r % 4 of row row(j).
+template <class Tile, int WN, class V>
 __device__ __forceinline__ void store_blocks(const Tile& t, const GemmArgs& a, int64_t n0, int64_t m0, float* tops,
                                              uint8_t* values, uint8_t* scales, int64_t pitch, int64_t spitch,
                                              const V& value) {
+    constexpr int HALF = Tile::TN / 2, TM = Tile::TM, Q = Tile::kQuads;
     __syncthreads();  // earlier reads of the LDS are done
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
@@ -75,10 +76,11 @@ __device__ __forceinline__ void store_blocks(const Tile& t, const GemmArgs& a, i
 #pragma unroll
         for (int i = 0; i < HALF; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (n0 + t.column(i, r & ~3) + (r & 3) < a.N) top = fmaxf(top, finite_abs(value(i, j, r)));
+            for (int r = 0; r < 4 * Q; ++r)
+                if (n0 + t.column(i, r / 4) + r % 4 < a.N) top = fmaxf(top, finite_abs(value(i, j, r)));
+        if constexpr (Tile::kTile == 16) top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        if (t.lane < 32) tops[t.wn * Tile::BM + t.row(j)] = top;
+        if (t.lane < Tile::kTile) tops[t.wn * Tile::BM + t.row(j)] = top;
     }
     __syncthreads();
 #pragma unroll
@@ -93,14 +95,14 @@ __device__ __forceinline__ void store_blocks(const Tile& t, const GemmArgs& a, i
 #pragma unroll
         for (int i = 0; i < HALF; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
+            for (int r = 0; r < Q; ++r) {
                 const int64_t n = n0 + t.column(i, r);
                 float v[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = n + q < a.N ? value(i, j, r + q) : 0.f;
+                for (int q = 0; q < 4; ++q) v[q] = n + q < a.N ? value(i, j, 4 * r + q) : 0.f;
                 *reinterpret_cast<uint32_t*>(values + m * pitch + n) = block8_word(v[0], v[1], v[2], v[3], inv);
             }
-        if (t.wn == 0 && t.lane < 32) {
+        if (t.wn == 0 && t.lane < Tile::kTile) {
             uint8_t* s = scales + m * spitch + n0 / kBlock8;
             s[0] = static_cast<uint8_t>(e);
             if (n0 + kBlock8 >= a.N)  // the row's scale bytes past its last block
@@ -109,29 +111,30 @@ __device__ __forceinline__ void store_blocks(const Tile& t, const GemmArgs& a, i
     }
 }
 
-template <class Tile, int HALF, int TM, class V>
+template <class Tile, class V>
 __device__ __forceinline__ void store_bf16(const Tile& t, const GemmArgs& a, int64_t n0, int64_t m0, void* out,
                                            int64_t ldo, const V& value) {
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
+    for (int j = 0; j < Tile::TM; ++j) {
         const int64_t m = m0 + t.row(j);
         if (m >= a.M) continue;
         uint16_t* p = static_cast<uint16_t*>(out) + m * ldo;
 #pragma unroll
-        for (int i = 0; i < HALF; ++i)
+        for (int i = 0; i < Tile::TN / 2; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
+            for (int r = 0; r < Tile::kQuads; ++r) {
                 const int64_t n = n0 + t.column(i, r);
-                store4(p + n, a.N - n, value(i, j, r), value(i, j, r + 1), value(i, j, r + 2), value(i, j, r + 3));
+                store4(p + n, a.N - n, value(i, j, 4 * r), value(i, j, 4 * r + 1), value(i, j, 4 * r + 2),
+                       value(i, j, 4 * r + 3));
             }
     }
 }
 
-template <class E, int TN, int TM, int WN, int WM, int ACT, int SAVE, bool OUT8>
+template <class E, int PN, int PM, int WN, int WM, int ACT, int SAVE, bool OUT8>
 __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOut o) {
-    using Tile = GemmTile<E, TN, TM, WN, WM, true>;
+    using Tile = GemmTile<E, PN, PM, WN, WM, true>;
     static_assert(Tile::kRows == kBlock8, "a tile is one block of its rows");
-    constexpr int HALF = TN / 2;
+    constexpr int HALF = Tile::TN / 2;
     extern __shared__ __align__(16) uint8_t gemm_lds[];
     float* tops = reinterpret_cast<float*>(gemm_lds);
     int tm, tn;
@@ -142,26 +145,26 @@ __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOu
     const auto g = [&](int i, int j, int r) { return t.acc[i][j][r]; };
     const auto u = [&](int i, int j, int r) { return t.acc[HALF + i][j][r]; };
     if constexpr (SAVE == kSaveBf16) {
-        store_bf16<Tile, HALF, TM>(t, a, n0, m0, o.g, a.N, g);
-        store_bf16<Tile, HALF, TM>(t, a, n0, m0, o.u, a.N, u);
+        store_bf16<Tile>(t, a, n0, m0, o.g, a.N, g);
+        store_bf16<Tile>(t, a, n0, m0, o.u, a.N, u);
     }
     if constexpr (SAVE == kSave8) {
-        store_blocks<Tile, HALF, TM, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.g), o.g_scales, o.pitch,
+        store_blocks<Tile, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.g), o.g_scales, o.pitch,
                                          o.spitch, g);
-        store_blocks<Tile, HALF, TM, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.u), o.u_scales, o.pitch,
+        store_blocks<Tile, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.u), o.u_scales, o.pitch,
                                          o.spitch, u);
     }
 #pragma unroll
     for (int i = 0; i < HALF; ++i)
 #pragma unroll
-        for (int j = 0; j < TM; ++j)
+        for (int j = 0; j < Tile::TM; ++j)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) t.acc[i][j][r] = act<ACT>(t.acc[i][j][r]) * t.acc[HALF + i][j][r];
+            for (int r = 0; r < 4 * Tile::kQuads; ++r) t.acc[i][j][r] = act<ACT>(t.acc[i][j][r]) * t.acc[HALF + i][j][r];
     if constexpr (OUT8)
-        store_blocks<Tile, HALF, TM, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.h), o.h_scales, o.pitch,
+        store_blocks<Tile, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.h), o.h_scales, o.pitch,
                                          o.spitch, g);
     else
-        store_bf16<Tile, HALF, TM>(t, a, n0, m0, o.h, o.ldh, g);
+        store_bf16<Tile>(t, a, n0, m0, o.h, o.ldh, g);
 }
 
 // At most 32 rows of x.  What is to be 8-bit blocks leaves in fp32 [M][F] and is packed next (a
@@ -341,14 +344,14 @@ __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
 
 bool grid_ok(int64_t x, int64_t y = 1) { return x <= (int64_t{1} << 24) - 1 && y <= 65535; }  // below 2^32 threads
 
-template <class E, int TN, int TM, int WN, int WM, int ACT, int SAVE, bool OUT8>
+template <class E, int PN, int PM, int WN, int WM, int ACT, int SAVE, bool OUT8>
 hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
-    using Tile = GemmTile<E, TN, TM, WN, WM, true>;
+    using Tile = GemmTile<E, PN, PM, WN, WM, true>;
     const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::kRows - 1) / Tile::kRows;
     if (tm * tn > kMostTiles) return hipErrorInvalidValue;
     g.tiles_m = static_cast<int>(tm);
     g.tiles_n = static_cast<int>(tn);
-    constexpr auto kernel = gated_kernel<E, TN, TM, WN, WM, ACT, SAVE, OUT8>;
+    constexpr auto kernel = gated_kernel<E, PN, PM, WN, WM, ACT, SAVE, OUT8>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g, o);
@@ -358,9 +361,9 @@ hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
 template <class E, int ACT, int SAVE, bool OUT8>
 hipError_t gated_tiles(const GemmArgs& g, const GatedOut& o, hipStream_t stream) {
     const auto tiles = [&](int64_t bm) { return ((g.M + bm - 1) / bm) * ((g.N + 127) / 128); };
-    if (tiles(256) >= 192) return gated_launch<E, 4, 2, 2, 4, ACT, SAVE, OUT8>(g, o, stream);
-    if (tiles(128) >= 192) return gated_launch<E, 4, 2, 2, 2, ACT, SAVE, OUT8>(g, o, stream);
-    return gated_launch<E, 2, 2, 4, 1, ACT, SAVE, OUT8>(g, o, stream);
+    if (tiles(256) >= 192) return gated_launch<E, 128, 64, 2, 4, ACT, SAVE, OUT8>(g, o, stream);
+    if (tiles(128) >= 192) return gated_launch<E, 128, 64, 2, 2, ACT, SAVE, OUT8>(g, o, stream);
+    return gated_launch<E, 64, 64, 4, 1, ACT, SAVE, OUT8>(g, o, stream);
 }
 
 template <class E, int ACT, int SAVE, bool OUT32>
@@ -400,14 +403,14 @@ hipError_t stage(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K
 }
 
 // c [M][N] (bf16) = x [M] rows against w [N] rows, both of K bf16 elements (a multiple of 64)
-template <int TN, int TM, int WN, int WM>
+template <int PN, int PM, int WN, int WM>
 hipError_t product_launch(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) {
-    using Tile = GemmTile<Bf16, TN, TM, WN, WM, false>;
+    using Tile = GemmTile<Bf16, PN, PM, WN, WM, false>;
     const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
     if (tm * tn > kMostTiles) return hipErrorInvalidValue;
     g.tiles_m = static_cast<int>(tm);
     g.tiles_n = static_cast<int>(tn);
-    constexpr auto kernel = gemm_nt_kernel<Bf16, TN, TM, WN, WM, uint16_t>;
+    constexpr auto kernel = gemm_nt_kernel<Bf16, PN, PM, WN, WM, uint16_t>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g,
@@ -425,9 +428,9 @@ hipError_t product(const uint16_t* x, const uint16_t* w, void* c, int64_t ldc, i
     g.steps = static_cast<int>(K / 64);
     g.tail = kStepBytes;
     const auto tiles = [&](int64_t n) { return ((M + n - 1) / n) * ((N + n - 1) / n); };
-    if (tiles(256) >= 192) return product_launch<4, 2, 2, 4>(g, c, ldc, stream);
-    if (tiles(128) >= 192) return product_launch<2, 2, 2, 2>(g, c, ldc, stream);
-    return product_launch<1, 1, 2, 2>(g, c, ldc, stream);
+    if (tiles(256) >= 192) return product_launch<128, 64, 2, 4>(g, c, ldc, stream);
+    if (tiles(128) >= 192) return product_launch<64, 64, 2, 2>(g, c, ldc, stream);
+    return product_launch<32, 32, 2, 2>(g, c, ldc, stream);
 }
 
 hipError_t transpose(const void* in, const uint8_t* scales, int64_t ldi, uint16_t* out, int64_t ldo, int64_t at,

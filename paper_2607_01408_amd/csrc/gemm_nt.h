@@ -8,11 +8,11 @@
 // of two steps lie in LDS: the loads of one go straight from memory to LDS while the other is
 // multiplied.  A row's eight 16-byte chunks are stored rotated by an exclusive or with the row, which
 // the loading lanes bring about by which chunk each of them fetches; so the lanes of a fragment read,
-// which hold one chunk of 32 rows, spread over all banks.
+// which hold one chunk of 16 rows, spread over all banks.
 //
-// v_mfma 32x32: w rows are the matrix unit's rows, x rows its columns, so that a lane's accumulators
-// are one x row (lane mod 32) and runs of four neighbouring w rows: four neighbouring outputs.  The
-// order of k inside a step is the same for both operands and otherwise free.
+// w rows are the matrix unit's rows, x rows its columns, so that a lane's accumulators are one x row and
+// runs of four neighbouring w rows: four neighbouring outputs.  The order of k inside a step is the same
+// for both operands and otherwise free.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -48,11 +48,17 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 constexpr int kStepBytes = 128;
 constexpr int64_t kMostTiles = int64_t{1} << 22;  // of a launch: below 2^32 threads
 
-// An operand's 16 bytes of a row as operands of v_mfma_f32_32x32x16_bf16.
+// An operand's 16 bytes of a row as bf16 operands of the matrix units, and their shape: bf16 16 x 16 x 32,
+// which takes less power for the same products than 32 x 32 x 16 (the clock falls with the power: 2,048 x
+// 16,384 outputs of 8,192 terms 438 against 410 us); 8 bits 32 x 32 x 16, for registers.
 struct Bf16 {
     static constexpr bool kScaled = false;
-    static constexpr int kParts = 1;
+    static constexpr int kTile = 16, kParts = 1;
+    typedef v4f Acc;
     static __device__ __forceinline__ void expand(v4i raw, float, v8bf (&p)[1]) { p[0] = __builtin_bit_cast(v8bf, raw); }
+    static __device__ __forceinline__ Acc product(v8bf a, v8bf b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
 };
 // e4m3 values times their block's power of two are bf16 numbers exactly, and v_cvt_scalef32 makes them
 // in one instruction for two, so the products are exact in fp32 and only their sum rounds.  (The
@@ -60,7 +66,8 @@ struct Bf16 {
 // 12 bits below the largest of a group, 1.5e-5 of a result of normal values against 6e-8.)
 struct Fp8 {
     static constexpr bool kScaled = true;
-    static constexpr int kParts = 2;
+    static constexpr int kTile = 32, kParts = 2;
+    typedef v16f Acc;
     static __device__ __forceinline__ void expand(v4i raw, float scale, v8bf (&p)[2]) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -71,6 +78,9 @@ struct Fp8 {
             const v2bf d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
             p[i] = v8bf{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
         }
+    }
+    static __device__ __forceinline__ Acc product(v8bf a, v8bf b, Acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
 };
 
@@ -107,25 +117,30 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& 
     tm = 8 * group + in - tn * rows;
 }
 
-// TN x TM accumulators of 32 x 32 per wave, WN x WM waves.
-template <class E, int TN, int TM, int WN, int WM, bool GATED>
+// A wave's tile is PN rows of w by PM rows of x; WN x WM waves.
+template <class E, int PN, int PM, int WN, int WM, bool GATED>
 struct GemmTile {
+    static constexpr int kTile = E::kTile, TN = PN / kTile, TM = PM / kTile;  // accumulators of kTile x kTile
+    static constexpr int kPhases = kTile == 16 ? 2 : 4;                    // fragment reads of a step
+    static constexpr int kQuads = kTile == 16 ? 1 : 4;                     // runs of four outputs in an accumulator
     static constexpr int kWaves = WN * WM, kThreads = 64 * kWaves;
-    static constexpr int BN = 32 * TN * WN, BM = 32 * TM * WM;
-    static constexpr int kStage = (BN + BM) * kStepBytes, kLds = 2 * kStage;
+    static constexpr int BN = PN * WN, BM = PM * WM;
+    static constexpr int kRows = GATED ? BN / 2 : BN;  // of one matrix
+    static constexpr int kStage = (BN + BM) * kStepBytes;
+    static constexpr int kLds = 2 * kStage + (E::kScaled ? 2 * (BN + BM) * 4 : 0);
+    static constexpr int kScaleLoads = (BN + BM + 64 * kWaves - 1) / (64 * kWaves);  // 64-row loads per wave and group
     static constexpr int LW = BN / 8 / kWaves, LX = BM / 8 / kWaves;  // 8-row loads per wave and step
     static_assert(LW * 8 * kWaves == BN && LX * 8 * kWaves == BM && kWaves % 2 == 0, "whole loads");
+    static_assert(BN % 64 == 0 && (!GATED || kRows % 64 == 0), "a load of scales is one operand's");
     static_assert(!GATED || (TN % 2 == 0 && LW % 2 == 0), "both halves in a wave, and in its loads");
-    // rows of one matrix in the tile, and their count in outputs
-    static constexpr int kRows = GATED ? BN / 2 : BN;
 
-    v16f acc[TN][TM];
+    typename E::Acc acc[TN][TM];
     int lane, wave, wn, wm;
 
     // first w row (of its matrix) of accumulator i, and of the tile in LDS
     static __device__ __forceinline__ int row_in(int i, int wn) {
-        if constexpr (GATED) return (i % (TN / 2)) * 32 + wn * (TN / 2) * 32;
-        return (wn * TN + i) * 32;
+        if constexpr (GATED) return (i % (TN / 2)) * kTile + wn * (PN / 2);
+        return wn * PN + i * kTile;
     }
     static __device__ __forceinline__ int lds_row(int i, int wn) {
         return (GATED && i >= TN / 2 ? kRows : 0) + row_in(i, wn);
@@ -141,7 +156,7 @@ struct GemmTile {
 #pragma unroll
             for (int j = 0; j < TM; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+                for (int r = 0; r < 4 * kQuads; ++r) acc[i][j][r] = 0.f;
 
         // where the lane's chunk of each load lies: row lane / 8 of the load's eight
         const int key = (4 * (wave & 1) + (lane >> 4)) & 7;  // (row >> 1) & 7
@@ -190,38 +205,61 @@ struct GemmTile {
             load(k, to);
         };
 
-        // scales: a lane's rows, four steps' bytes in a word
-        const uint32_t* sw[TN];
-        const uint32_t* sx[TM];
-        uint32_t cw[TN], cx[TM], nw[TN], nx[TM];
+        // Scales (8 bits): four steps' bytes of a row are a word, the words of the tile's rows a group in LDS;
+        // two groups, and in registers the bytes of the lane's rows for a step, read half a step ahead.
+        uint8_t* const groups = lds + 2 * kStage;
+        constexpr int kGroup = E::kScaled ? (BN + BM) * 4 : 0;
+        constexpr int LS = kScaleLoads;
+        const int last_word = (a.steps - 1) >> 2;
+        const uint32_t lds_w = static_cast<uint32_t>(a.lds);
+        Buffer bs[LS];
+        uint32_t os[LS];
         if constexpr (E::kScaled) {
 #pragma unroll
-            for (int i = 0; i < TN; ++i) {
-                const int64_t r = n0 + row_in(i, wn) + (lane & 31), n = r < a.N ? r : a.N - 1;
-                sw[i] = reinterpret_cast<const uint32_t*>((GATED && i >= TN / 2 ? a.ws2 : a.ws) + n * a.lds);
-                nw[i] = *sw[i];
-            }
-#pragma unroll
-            for (int j = 0; j < TM; ++j) {
-                const int64_t r = m0 + (wm * TM + j) * 32 + (lane & 31), m = r < a.M ? r : a.M - 1;
-                sx[j] = reinterpret_cast<const uint32_t*>(a.xs + m * a.lds);
-                nx[j] = *sx[j];
+            for (int t = 0; t < LS; ++t) {
+                const int first = 64 * (wave + kWaves * t);  // 64 rows of one operand
+                const bool in_x = first >= BN, second = GATED && !in_x && first >= kRows;
+                const int rows = in_x ? rows_x : rows_w;
+                const int r = first - (in_x ? BN : (second ? kRows : 0)) + lane;
+                bs[t] = buffer_of(in_x ? a.xs + m0 * a.lds : (second ? a.ws2 : a.ws) + n0 * a.lds,
+                                  (rows - 1) * lds_w + (last_word + 1) * 4);
+                os[t] = (r < rows ? r : rows - 1) * lds_w;
             }
         }
-
-        const int fkey = (lane >> 1) & 7, half = lane >> 5;
-        int at[4];  // the lane's chunk of quarter step q
+        auto load_scales = [&](int g) {
+            if constexpr (E::kScaled) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) at[q] = (lane & 31) * 128 + (((2 * q + half) ^ fkey) << 4);
+                for (int t = 0; t < LS; ++t)
+                    if (kScaleLoads * kWaves * 64 == BN + BM || 64 * (wave + kWaves * t) < BN + BM)
+                        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+                            bs[t],
+                            (__attribute__((address_space(3))) void*)(groups + (g & 1) * kGroup + 256 * (wave + kWaves * t)),
+                            4, static_cast<int>(os[t]), (g < last_word ? g : last_word) * 4, 0, 0);
+            }
+        };
+        uint32_t ew[TN], ex[TM];
+        auto read_scales = [&](int k) {
+            if constexpr (E::kScaled) {
+                const uint8_t* from = groups + ((k >> 2) & 1) * kGroup + (lane & (kTile - 1)) * 4 + (k & 3);
+#pragma unroll
+                for (int i = 0; i < TN; ++i) ew[i] = from[lds_row(i, wn) * 4];
+#pragma unroll
+                for (int j = 0; j < TM; ++j) ex[j] = from[(BN + wm * PM + j * kTile) * 4];
+            }
+        };
 
-        // Fragments are read a quarter step ahead, and the last quarter of a step is multiplied behind the
-        // barrier that ends its reads, so the matrix units have work while the next step's first
-        // fragments come.
+        const int fkey = (lane >> 1) & 7, in = lane & (kTile - 1);
+        int at[kPhases];  // the lane's chunk of phase q
+#pragma unroll
+        for (int q = 0; q < kPhases; ++q) at[q] = in * 128 + (((8 / kPhases * q + lane / kTile) ^ fkey) << 4);
+
+        // Fragments are read a phase ahead, and the last phase of a step is multiplied behind the barrier that
+        // ends its reads, so the matrix units have work while the next step's first fragments come.
         v4i rw[2][TN], rx[2][TM];
         auto read = [&](const uint8_t* from, int q, int buffer) {
 #pragma unroll
             for (int j = 0; j < TM; ++j)
-                rx[buffer][j] = *reinterpret_cast<const v4i*>(from + BN * 128 + (wm * TM + j) * 4096 + at[q]);
+                rx[buffer][j] = *reinterpret_cast<const v4i*>(from + (BN + wm * PM + j * kTile) * 128 + at[q]);
 #pragma unroll
             for (int i = 0; i < TN; ++i)
                 rw[buffer][i] = *reinterpret_cast<const v4i*>(from + lds_row(i, wn) * 128 + at[q]);
@@ -242,7 +280,7 @@ struct GemmTile {
                 for (int i = 0; i < TN; ++i)
 #pragma unroll
                     for (int j = 0; j < TM; ++j) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fw[i][p], fx[j][p], acc[i][j], 0, 0, 0);
+                        acc[i][j] = E::product(fw[i][p], fx[j][p], acc[i][j]);
                         between(n++);
                     }
             __builtin_amdgcn_sched_barrier(0);
@@ -250,46 +288,45 @@ struct GemmTile {
         const auto nothing = [](int) {};
 
         load_any(0, lds);
+        load_scales(0);
+        load_scales(1);
         arrived_and_read();
         if (a.steps > 1) load_any(1, lds + kStage);
         read(lds, 0, 0);
+        read_scales(0);
         // step k: its products, the loads of step k + 2 (MORE = 2: some step before the last, 1: any), the
         // first fragments of step k + 1
         auto step = [&](int k, auto more, auto follows) {
             uint8_t* here = lds + (k & 1) * kStage;
             uint8_t* next = lds + ((k + 1) & 1) * kStage;
             if constexpr (E::kScaled) {
-                if ((k & 3) == 0) {
-                    const int ahead = k + 4 < a.steps ? (k >> 2) + 1 : 0;
 #pragma unroll
-                    for (int i = 0; i < TN; ++i) cw[i] = nw[i], nw[i] = sw[i][ahead];
+                for (int i = 0; i < TN; ++i) fsw[i] = __uint_as_float(ew[i] << 23);
 #pragma unroll
-                    for (int j = 0; j < TM; ++j) cx[j] = nx[j], nx[j] = sx[j][ahead];
-                }
-#pragma unroll
-                for (int i = 0; i < TN; ++i) fsw[i] = __uint_as_float((cw[i] & 255u) << 23), cw[i] >>= 8;
-#pragma unroll
-                for (int j = 0; j < TM; ++j) fsx[j] = __uint_as_float((cx[j] & 255u) << 23), cx[j] >>= 8;
+                for (int j = 0; j < TM; ++j) fsx[j] = __uint_as_float(ex[j] << 23);
             }
 #pragma unroll
-            for (int q = 0; q < 3; ++q) {
+            for (int q = 0; q < kPhases - 1; ++q) {
                 read(here, q + 1, (q + 1) & 1);
                 multiply(q & 1, nothing);
             }
             arrived_and_read();  // step k + 1 has arrived, and step k has been read by all
-            if constexpr (decltype(follows)::value) read(next, 0, 0);
-            if constexpr (decltype(more)::value == 1) load_any(k + 2, here);
-            if constexpr (decltype(more)::value == 2) {
-                // spread over the products: a burst of loads would hold the wave up at their issue
-                constexpr int products = TN * TM * E::kParts, loads = LW + LX;
-                multiply(1, [&](int n) {
-#pragma unroll
-                    for (int t = n * loads / products; t < (n + 1) * loads / products; ++t) load_part(t, k + 2, here);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-            } else {
-                multiply(1, nothing);
+            if constexpr (decltype(follows)::value) {
+                read_scales(k + 1);
+                read(next, 0, 0);
             }
+            if constexpr (decltype(more)::value == 1) load_any(k + 2, here);
+            // the group of this step's scales has been read by all
+            if (E::kScaled && decltype(more)::value > 0 && (k & 3) == 3) load_scales((k >> 2) + 2);
+            // loads spread over the products: a burst of them would hold the wave up at their issue
+            multiply(1, [&](int n) {
+                constexpr int products = TN * TM * E::kParts, all = LW + LX;
+                if (decltype(more)::value == 2 && (n + 1) * all / products > n * all / products) {
+#pragma unroll
+                    for (int t = n * all / products; t < (n + 1) * all / products; ++t) load_part(t, k + 2, here);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            });
         };
         using std::integral_constant;
         int k = 0;
@@ -299,10 +336,9 @@ struct GemmTile {
         step(k, integral_constant<int, 0>{}, std::false_type{});
     }
 
-    // output column (w row) of accumulator register r (a multiple of 4: four neighbours) of tile i, and
-    // output row of tile j
-    __device__ __forceinline__ int column(int i, int r) const { return row_in(i, wn) + 2 * r + 4 * (lane >> 5); }
-    __device__ __forceinline__ int row(int j) const { return (wm * TM + j) * 32 + (lane & 31); }
+    // the output column (w row) of the first of run r of tile i's accumulators, and the output row of tile j
+    __device__ __forceinline__ int column(int i, int r) const { return row_in(i, wn) + 8 * r + 4 * (lane / kTile); }
+    __device__ __forceinline__ int row(int j) const { return wm * PM + j * kTile + (lane & (kTile - 1)); }
 };
 
 // Four neighbouring outputs of a row, those before column N.
@@ -328,9 +364,9 @@ __device__ __forceinline__ void store4(uint16_t* p, int64_t left, float a, float
 }
 
 // The product itself, to out [M] rows of ldo elements.
-template <class E, int TN, int TM, int WN, int WM, typename TO>
+template <class E, int PN, int PM, int WN, int WM, typename TO>
 __global__ __launch_bounds__(64 * WN * WM) void gemm_nt_kernel(GemmArgs a, TO* __restrict__ out, int64_t ldo) {
-    using Tile = GemmTile<E, TN, TM, WN, WM, false>;
+    using Tile = GemmTile<E, PN, PM, WN, WM, false>;
     extern __shared__ __align__(16) uint8_t gemm_lds[];
     int tm, tn;
     tile_of(a.tiles_m, a.tiles_n, tm, tn);
@@ -338,17 +374,17 @@ __global__ __launch_bounds__(64 * WN * WM) void gemm_nt_kernel(GemmArgs a, TO* _
     Tile t;
     t.run(a, n0, m0, gemm_lds);
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
+    for (int j = 0; j < Tile::TM; ++j) {
         const int64_t m = m0 + t.row(j);
         if (m >= a.M) continue;
         TO* p = out + m * ldo;
 #pragma unroll
-        for (int i = 0; i < TN; ++i)
+        for (int i = 0; i < Tile::TN; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4) {
+            for (int r = 0; r < Tile::kQuads; ++r) {
                 const int64_t n = n0 + t.column(i, r);
-                const v16f& c = t.acc[i][j];
-                store4(p + n, a.N - n, c[r], c[r + 1], c[r + 2], c[r + 3]);
+                const auto& c = t.acc[i][j];
+                store4(p + n, a.N - n, c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]);
             }
     }
 }
