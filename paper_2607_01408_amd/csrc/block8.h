@@ -38,13 +38,11 @@ __device__ __forceinline__ float block8_power(uint32_t scale) {
     return scale == 0 ? __uint_as_float(0x400000u) : __uint_as_float(scale << 23);
 }
 
-// v / scale to e4m3 (nearest, ties to even; |v| / scale <= 448 for finite v), four to a word.
-__device__ __forceinline__ float block8_operand(float v, float inv) {
-    return fabsf(v) < __builtin_inff() ? v * inv : __builtin_nanf("");
-}
+// v / scale to e4m3 (nearest, ties to even; |v| / scale <= 448 for finite v, NaN for others), four to
+// a word.
 __device__ __forceinline__ uint32_t block8_word(float a, float b, float c, float d, float inv) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(block8_operand(a, inv), block8_operand(b, inv), 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(block8_operand(c, inv), block8_operand(d, inv), w, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
     return static_cast<uint32_t>(w);
 }
 typedef float v2f __attribute__((ext_vector_type(2)));
@@ -59,6 +57,21 @@ __device__ __forceinline__ float max16(float v) {
 #pragma unroll
     for (int d = 1; d < 16; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
     return v;
+}
+
+// Largest finite magnitude of a block held by 16 lanes, N values each.  Infinities are rare: only a block
+// whose plain maximum is one looks at its values again.
+template <int N>
+__device__ __forceinline__ float block8_top(const float (&v)[N]) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, fabsf(v[j]));  // a NaN loses
+    top = max16(top);
+    if (top < __builtin_inff()) return top;
+    top = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) top = fmaxf(top, finite_abs(v[j]));
+    return max16(top);
 }
 
 // Eight neighbouring elements of a row at any element address (global memory takes unaligned wide

@@ -63,46 +63,89 @@ struct GatedOut {
     int64_t pitch, spitch;  // of the 8-bit rows
 };
 
-// A tile's rows of 128 columns as 8-bit blocks: `value(i, j, r)` is column column(i, r / 4) + r % 4 of row row(j).
-template <class Tile, int WN, class V>
-__device__ __forceinline__ void store_blocks(const Tile& t, const GemmArgs& a, int64_t n0, int64_t m0, float* tops,
-                                             uint8_t* values, uint8_t* scales, int64_t pitch, int64_t spitch,
-                                             const V& value) {
-    constexpr int HALF = Tile::TN / 2, TM = Tile::TM, Q = Tile::kQuads;
-    __syncthreads();  // earlier reads of the LDS are done
+// A tile's outputs go through LDS, so that a row's 128 columns leave as whole lines, 16 bytes a lane.
+// `value(i, j, r)` is column column(i, r / 4) + r % 4 of row row(j).
+constexpr int kPad = 16;  // bytes of an LDS row past its columns: rows start in different banks
+
+template <class Tile, class V>
+__device__ __forceinline__ void stage_bf16(const Tile& t, uint8_t* lds, const V& value) {
+    constexpr int PITCH = 2 * kBlock8 + kPad;
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
+    for (int j = 0; j < Tile::TM; ++j)
+#pragma unroll
+        for (int i = 0; i < Tile::TN / 2; ++i)
+#pragma unroll
+            for (int r = 0; r < Tile::kQuads; ++r)
+                *reinterpret_cast<uint2*>(lds + t.row(j) * PITCH + 2 * t.column(i, r)) =
+                    make_uint2(bf16_pair(value(i, j, 4 * r), value(i, j, 4 * r + 1)),
+                               bf16_pair(value(i, j, 4 * r + 2), value(i, j, 4 * r + 3)));
+}
+template <class Tile>
+__device__ __forceinline__ void send_bf16(const uint8_t* lds, const GemmArgs& a, int64_t n0, int64_t m0, void* out,
+                                          int64_t ldo) {
+    constexpr int PITCH = 2 * kBlock8 + kPad;
+    const int l = threadIdx.x & 15;
+    const int64_t left = a.N - n0 - 8 * l;
+    const int rows = a.M - m0 < Tile::BM ? static_cast<int>(a.M - m0) : Tile::BM;
+    uint16_t* p = static_cast<uint16_t*>(out) + m0 * ldo + n0 + 8 * l;
+    for (int r = threadIdx.x >> 4; r < rows; r += Tile::kThreads / 16) {
+        const uint4 v = *reinterpret_cast<const uint4*>(lds + r * PITCH + 16 * l);
+        uint16_t* to = p + r * ldo;
+        if (left >= 8) {
+            *reinterpret_cast<u4u*>(to) = u4u{v.x, v.y, v.z, v.w};
+        } else {
+            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (q < left) to[q] = static_cast<uint16_t>(w[q / 2] >> (16 * (q & 1)));
+        }
+    }
+}
+
+// The rows as 8-bit blocks: first each wave's largest magnitudes (tops [WN][BM]), then, when all are there,
+// the values.
+template <class Tile, class V>
+__device__ __forceinline__ void block_tops(const Tile& t, float* tops, const V& value) {
+#pragma unroll
+    for (int j = 0; j < Tile::TM; ++j) {
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < HALF; ++i)
+        for (int i = 0; i < Tile::TN / 2; ++i)
 #pragma unroll
-            for (int r = 0; r < 4 * Q; ++r)
-                if (n0 + t.column(i, r / 4) + r % 4 < a.N) top = fmaxf(top, finite_abs(value(i, j, r)));
+            for (int r = 0; r < 4 * Tile::kQuads; ++r) top = fmaxf(top, fabsf(value(i, j, r)));
+        if (!(top < __builtin_inff())) {
+            top = 0.f;
+#pragma unroll
+            for (int i = 0; i < Tile::TN / 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 4 * Tile::kQuads; ++r) top = fmaxf(top, finite_abs(value(i, j, r)));
+        }
         if constexpr (Tile::kTile == 16) top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
         if (t.lane < Tile::kTile) tops[t.wn * Tile::BM + t.row(j)] = top;
     }
-    __syncthreads();
+}
+template <class Tile, int WN, class V>
+__device__ __forceinline__ void stage_blocks(const Tile& t, const GemmArgs& a, int64_t n0, int64_t m0,
+                                             const float* tops, uint8_t* lds, uint8_t* scales, int64_t spitch,
+                                             const V& value) {
+    constexpr int PITCH = kBlock8 + kPad;
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-        const int64_t m = m0 + t.row(j);
+    for (int j = 0; j < Tile::TM; ++j) {
         float top = 0.f;
 #pragma unroll
         for (int w = 0; w < WN; ++w) top = fmaxf(top, tops[w * Tile::BM + t.row(j)]);
         const int e = block8_scale(top);
         const float inv = block8_inverse(e);
-        if (m >= a.M) continue;
 #pragma unroll
-        for (int i = 0; i < HALF; ++i)
+        for (int i = 0; i < Tile::TN / 2; ++i)
 #pragma unroll
-            for (int r = 0; r < Q; ++r) {
-                const int64_t n = n0 + t.column(i, r);
-                float v[4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) v[q] = n + q < a.N ? value(i, j, 4 * r + q) : 0.f;
-                *reinterpret_cast<uint32_t*>(values + m * pitch + n) = block8_word(v[0], v[1], v[2], v[3], inv);
-            }
-        if (t.wn == 0 && t.lane < Tile::kTile) {
+            for (int r = 0; r < Tile::kQuads; ++r)
+                *reinterpret_cast<uint32_t*>(lds + t.row(j) * PITCH + t.column(i, r)) =
+                    block8_word(value(i, j, 4 * r), value(i, j, 4 * r + 1), value(i, j, 4 * r + 2),
+                                value(i, j, 4 * r + 3), inv);
+        const int64_t m = m0 + t.row(j);
+        if (t.wn == 0 && t.lane < Tile::kTile && m < a.M) {
             uint8_t* s = scales + m * spitch + n0 / kBlock8;
             s[0] = static_cast<uint8_t>(e);
             if (n0 + kBlock8 >= a.N)  // the row's scale bytes past its last block
@@ -110,61 +153,82 @@ __device__ __forceinline__ void store_blocks(const Tile& t, const GemmArgs& a, i
         }
     }
 }
-
-template <class Tile, class V>
-__device__ __forceinline__ void store_bf16(const Tile& t, const GemmArgs& a, int64_t n0, int64_t m0, void* out,
-                                           int64_t ldo, const V& value) {
-#pragma unroll
-    for (int j = 0; j < Tile::TM; ++j) {
-        const int64_t m = m0 + t.row(j);
-        if (m >= a.M) continue;
-        uint16_t* p = static_cast<uint16_t*>(out) + m * ldo;
-#pragma unroll
-        for (int i = 0; i < Tile::TN / 2; ++i)
-#pragma unroll
-            for (int r = 0; r < Tile::kQuads; ++r) {
-                const int64_t n = n0 + t.column(i, r);
-                store4(p + n, a.N - n, value(i, j, 4 * r), value(i, j, 4 * r + 1), value(i, j, 4 * r + 2),
-                       value(i, j, 4 * r + 3));
-            }
-    }
+template <class Tile>
+__device__ __forceinline__ void send_blocks(const uint8_t* lds, const GemmArgs& a, int64_t n0, int64_t m0, void* out,
+                                            int64_t pitch) {
+    constexpr int PITCH = kBlock8 + kPad;
+    const int l = threadIdx.x & 7;
+    const int rows = a.M - m0 < Tile::BM ? static_cast<int>(a.M - m0) : Tile::BM;
+    uint8_t* p = static_cast<uint8_t*>(out) + m0 * pitch + n0 + 16 * l;  // a block lies in the pitch as a whole
+    for (int r = threadIdx.x >> 3; r < rows; r += Tile::kThreads / 8)
+        *reinterpret_cast<uint4*>(p + r * pitch) = *reinterpret_cast<const uint4*>(lds + r * PITCH + 16 * l);
 }
 
 template <class E, int PN, int PM, int WN, int WM, int ACT, int SAVE, bool OUT8>
 __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOut o) {
     using Tile = GemmTile<E, PN, PM, WN, WM, true>;
     static_assert(Tile::kRows == kBlock8, "a tile is one block of its rows");
-    constexpr int HALF = Tile::TN / 2;
+    constexpr int HALF = Tile::TN / 2, BM = Tile::BM;
+    // two places for outputs in turn: one is written while the other leaves
+    constexpr int kPlace = BM * (2 * kBlock8 + kPad), kTops = 2 * WN * BM * 4;
+    static_assert(2 * kPlace + kTops <= 160 * 1024, "in LDS");
     extern __shared__ __align__(16) uint8_t gemm_lds[];
-    float* tops = reinterpret_cast<float*>(gemm_lds);
+    uint8_t* const place[2] = {gemm_lds, gemm_lds + kPlace};
+    float* const tops = reinterpret_cast<float*>(gemm_lds + 2 * kPlace);
+    float* const tops2 = tops + WN * BM;
     int tm, tn;
     tile_of(a.tiles_m, a.tiles_n, tm, tn);
-    const int64_t n0 = static_cast<int64_t>(tn) * Tile::kRows, m0 = static_cast<int64_t>(tm) * Tile::BM;
+    const int64_t n0 = static_cast<int64_t>(tn) * Tile::kRows, m0 = static_cast<int64_t>(tm) * BM;
     Tile t;
-    t.run(a, n0, m0, gemm_lds);
+    t.run(a, n0, m0, gemm_lds);  // ends with a barrier behind its reads of LDS
     const auto g = [&](int i, int j, int r) { return t.acc[i][j][r]; };
     const auto u = [&](int i, int j, int r) { return t.acc[HALF + i][j][r]; };
+    if ((SAVE == kSave8 || OUT8) && n0 + kBlock8 > a.N) {  // 8-bit rows end in zeros
+#pragma unroll
+        for (int i = 0; i < HALF; ++i)
+#pragma unroll
+            for (int r = 0; r < 4 * Tile::kQuads; ++r)
+                if (n0 + t.column(i, r / 4) + r % 4 >= a.N) {
+#pragma unroll
+                    for (int j = 0; j < Tile::TM; ++j) t.acc[i][j][r] = t.acc[HALF + i][j][r] = 0.f;
+                }
+    }
     if constexpr (SAVE == kSaveBf16) {
-        store_bf16<Tile>(t, a, n0, m0, o.g, a.N, g);
-        store_bf16<Tile>(t, a, n0, m0, o.u, a.N, u);
+        stage_bf16(t, place[0], g);
+        stage_bf16(t, place[1], u);
+        __syncthreads();
+        send_bf16<Tile>(place[0], a, n0, m0, o.g, a.N);
+        send_bf16<Tile>(place[1], a, n0, m0, o.u, a.N);
     }
     if constexpr (SAVE == kSave8) {
-        store_blocks<Tile, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.g), o.g_scales, o.pitch,
-                                         o.spitch, g);
-        store_blocks<Tile, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.u), o.u_scales, o.pitch,
-                                         o.spitch, u);
+        block_tops(t, tops, g);
+        block_tops(t, tops2, u);
+        __syncthreads();
+        stage_blocks<Tile, WN>(t, a, n0, m0, tops, place[0], o.g_scales, o.spitch, g);
+        stage_blocks<Tile, WN>(t, a, n0, m0, tops2, place[1], o.u_scales, o.spitch, u);
+        __syncthreads();
+        send_blocks<Tile>(place[0], a, n0, m0, o.g, o.pitch);
+        send_blocks<Tile>(place[1], a, n0, m0, o.u, o.pitch);
     }
 #pragma unroll
     for (int i = 0; i < HALF; ++i)
 #pragma unroll
         for (int j = 0; j < Tile::TM; ++j)
 #pragma unroll
-            for (int r = 0; r < 4 * Tile::kQuads; ++r) t.acc[i][j][r] = act<ACT>(t.acc[i][j][r]) * t.acc[HALF + i][j][r];
-    if constexpr (OUT8)
-        store_blocks<Tile, WN>(t, a, n0, m0, tops, static_cast<uint8_t*>(o.h), o.h_scales, o.pitch,
-                                         o.spitch, g);
-    else
-        store_bf16<Tile>(t, a, n0, m0, o.h, o.ldh, g);
+            for (int r = 0; r < 4 * Tile::kQuads; ++r)
+                t.acc[i][j][r] = act<ACT>(t.acc[i][j][r]) * t.acc[HALF + i][j][r];
+    if constexpr (SAVE != kSaveNone) __syncthreads();  // g and u have left their places
+    if constexpr (OUT8) {
+        block_tops(t, tops, g);
+        __syncthreads();
+        stage_blocks<Tile, WN>(t, a, n0, m0, tops, place[0], o.h_scales, o.spitch, g);
+        __syncthreads();
+        send_blocks<Tile>(place[0], a, n0, m0, o.h, o.pitch);
+    } else {
+        stage_bf16(t, place[0], g);
+        __syncthreads();
+        send_bf16<Tile>(place[0], a, n0, m0, o.h, o.ldh);
+    }
 }
 
 // At most 32 rows of x.  What is to be 8-bit blocks leaves in fp32 [M][F] and is packed next (a
@@ -344,6 +408,13 @@ __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
 
 bool grid_ok(int64_t x, int64_t y = 1) { return x <= (int64_t{1} << 24) - 1 && y <= 65535; }  // below 2^32 threads
 
+// LDS of a workgroup: the operands' tiles, then the outputs'
+template <class Tile, int WN>
+constexpr int gated_lds() {
+    constexpr int out = 2 * Tile::BM * (2 * kBlock8 + kPad) + 2 * WN * Tile::BM * 4;
+    return out > Tile::kLds ? out : Tile::kLds;
+}
+
 template <class E, int PN, int PM, int WN, int WM, int ACT, int SAVE, bool OUT8>
 hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
     using Tile = GemmTile<E, PN, PM, WN, WM, true>;
@@ -354,7 +425,8 @@ hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
     constexpr auto kernel = gated_kernel<E, PN, PM, WN, WM, ACT, SAVE, OUT8>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g, o);
+    constexpr int lds = gated_lds<Tile, WN>();
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), lds, stream, g, o);
     return hipGetLastError();
 }
 

@@ -65,18 +65,18 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(
             if (pr != nullptr) {
                 float q[8];
                 load8(pr + (n > 0 ? c : 0), n, q);
-    #pragma unroll
+#pragma unroll
                 for (int j = 0; j < 8; ++j) w[j] = as_type(w[j] + q[j], px);
             }
         };
         if constexpr (V > 0) {
-    #pragma unroll
+#pragma unroll
             for (int i = 0; i < V; ++i) take(i, v[i]);
-    #pragma unroll
+#pragma unroll
             for (int i = 0; i < V; ++i) {
                 const int64_t c = (static_cast<int64_t>(i) * TPR + t) * 8;
                 if (ph != nullptr && c < D) store8(ph + c, left(c), v[i]);
-    #pragma unroll
+#pragma unroll
                 for (int j = 0; j < 8; ++j) s = fmaf(v[i][j], v[i][j], s);
             }
         } else {
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(
                 take(i, v[0]);
                 const int64_t c = (i * TPR + t) * 8;
                 if (ph != nullptr && c < D) store8(ph + c, left(c), v[0]);
-    #pragma unroll
+#pragma unroll
                 for (int j = 0; j < 8; ++j) s = fmaf(v[0][j], v[0][j], s);
             }
         }
@@ -98,14 +98,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(
             const int n = left(c);
             float gn[8];
             load8(gain + (n > 0 ? c : 0), n, gn);
-    #pragma unroll
+#pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = w[j] * rstd * gn[j];
             if constexpr (OUT8) {
-                float top = 0.f;
-    #pragma unroll
-                for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(w[j]));
-                top = max16(top);
-                const int e = block8_scale(top);
+                const int e = block8_scale(block8_top(w));
                 const float inv = block8_inverse(e);
                 *reinterpret_cast<uint2*>(values + row * pitch + c) =
                     make_uint2(block8_word(w[0], w[1], w[2], w[3], inv), block8_word(w[4], w[5], w[6], w[7], inv));
@@ -115,7 +111,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(
             }
         };
         if constexpr (V > 0) {
-    #pragma unroll
+#pragma unroll
             for (int i = 0; i < V; ++i) give(i, v[i]);
         } else {
             for (int64_t i = 0; i < steps; ++i) {

@@ -38,10 +38,7 @@ __global__ __launch_bounds__(256) void pack8_rows_kernel(const T* __restrict__ x
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t c = c0 + i * kBlock8;
-            float top = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[i][j]));
-            const int e = block8_scale(max16(top));  // 127 past the last block
+            const int e = block8_scale(block8_top(v[i]));  // 127 past the last block
             const float inv = block8_inverse(e);
             word |= static_cast<uint32_t>(e) << (8 * i);
             if (c < pitch)
@@ -75,10 +72,7 @@ __global__ __launch_bounds__(256) void pack8_both_kernel(const T* __restrict__ x
         *reinterpret_cast<float4*>(&tile[r * ST + l * 8]) = make_float4(v[0], v[1], v[2], v[3]);
         *reinterpret_cast<float4*>(&tile[r * ST + l * 8 + 4]) = make_float4(v[4], v[5], v[6], v[7]);
         if constexpr (ROWS) {
-            float top = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, finite_abs(v[j]));
-            const int e = block8_scale(max16(top));
+            const int e = block8_scale(block8_top(v));
             const float inv = block8_inverse(e);
             if (row < R) {
                 *reinterpret_cast<uint2*>(values + row * pitch + c0 + l * 8) =
@@ -97,13 +91,10 @@ __global__ __launch_bounds__(256) void pack8_both_kernel(const T* __restrict__ x
     for (int i = 0; i < 8; ++i) {
         const int c = i * 16 + g;
         const int64_t column = c0 + c;
-        float v[8], top = 0.f;
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = tile[(l * 8 + j) * ST + c];
-            top = fmaxf(top, finite_abs(v[j]));
-        }
-        const int e = block8_scale(max16(top));
+        for (int j = 0; j < 8; ++j) v[j] = tile[(l * 8 + j) * ST + c];
+        const int e = block8_scale(block8_top(v));
         const float inv = block8_inverse(e);
         if (column < D) {
             *reinterpret_cast<uint2*>(t_values + column * tpitch + r0 + l * 8) =
