@@ -22,6 +22,9 @@ _MINREG = ["-mllvm", "-amdgpu-sched-strategy=iterative-minreg"]
 EXTRA_FLAGS = {"forward_big_parity_padded_minreg.hip": _MINREG, "direct_unrolled_paper.hip": _CONSTEXPR, "direct_unrolled_paired.hip": _CONSTEXPR,
                "direct_unrolled_parity.hip": _CONSTEXPR}
 
+# the Python functions of the feed-forward operators on torch tensors (host code only)
+BINDING = os.path.join(PKG, "_binding.so")
+
 # -packed-fp32-ops: no v_pk_{add,mul,fma}_f32 in generated code.
 HIP_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -37,8 +40,29 @@ def hipcc() -> str:
     return path
 
 
+def binding_command(out: str) -> list:
+    """The compiler's command for csrc/binding.cpp, a Python extension module on torch's headers."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if cxx is None:
+        raise RuntimeError("no host C++ compiler found")
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-I", sysconfig.get_paths()["include"]]
+    for path in cpp_extension.include_paths():
+        cmd += ["-isystem", path]
+    cmd += [os.path.join(CSRC, "binding.cpp"), "-o", out]
+    for path in cpp_extension.library_paths():
+        cmd += ["-L", path]
+    return cmd + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+
+
 def build(verbose: bool = False, jobs: int = 8) -> str:
-    """Compile every source to an object (in parallel), then link the shared library."""
+    """Compile every source to an object (in parallel), then link the shared library; and the binding."""
     objdir = os.path.join(ROOT, "_build")
     os.makedirs(objdir, exist_ok=True)
     procs, objs = [], []
@@ -53,6 +77,10 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
+    cmd = binding_command(BINDING + ".tmp")
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    procs.append(("binding.cpp", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
     failed = []
     for src, p in procs:
         out, _ = p.communicate()
@@ -63,7 +91,8 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
             print(text)
     if failed:
         msg = "\n".join(f"--- {s} ---\n{t}" for s, t in failed)
-        raise RuntimeError("hipcc failed:\n" + msg)
+        raise RuntimeError("compilation failed:\n" + msg)
+    os.replace(BINDING + ".tmp", BINDING)
     tmp = LIB + ".tmp"
     cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs
     if verbose:
