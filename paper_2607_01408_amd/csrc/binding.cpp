@@ -53,6 +53,8 @@ std::string shape_text(int64_t rows, int64_t columns) {
     return "[" + std::to_string(rows) + ", " + std::to_string(columns) + "]";
 }
 
+typedef PyObject* const* Args;
+
 // ---------------------------------------------------------------- arguments
 
 const at::Tensor& tensor(PyObject* o, const char* name) {
@@ -133,6 +135,22 @@ Block block(PyObject* values, PyObject* scales) {
     return b;
 }
 
+// values, scales, R, D: refuses what is no Block8 of that shape
+PyObject* check_block(Args a) {
+    const at::Tensor& v = tensor(a[0], "values");
+    const at::Tensor& s = tensor(a[1], "scales");
+    const int64_t R = integer(a[2]), D = integer(a[3]);
+    if (R < 0 || D < 1) throw Refused("no matrix has the shape " + shape_text(R, D));
+    const int64_t pitch = up(D, 128), spitch = up(D, 512) / 128;
+    if (v.scalar_type() != at::kFloat8_e4m3fn || v.dim() != 2 || v.size(0) != R || v.size(1) != pitch ||
+        !v.is_contiguous() || !v.is_cuda())
+        throw Refused("values must be a contiguous float8_e4m3fn " + shape_text(R, pitch) + " device tensor");
+    if (s.scalar_type() != at::kFloat8_e8m0fnu || s.dim() != 2 || s.size(0) != R || s.size(1) != spitch ||
+        !s.is_contiguous() || s.device() != v.device())
+        throw Refused("scales must be a contiguous float8_e8m0fnu " + shape_text(R, spitch) + " tensor beside the values");
+    Py_RETURN_NONE;
+}
+
 // ---------------------------------------------------------------- results
 
 at::Tensor empty(at::IntArrayRef shape, at::ScalarType type, const at::Tensor& beside) {
@@ -180,8 +198,6 @@ void done(spingtp_status s, const char* where) {
 }
 void* stream_of(PyObject* o) { return reinterpret_cast<void*>(static_cast<intptr_t>(integer(o))); }
 spingtp_dtype dtype_of(at::ScalarType t) { return t == at::kFloat ? SPINGTP_FP32 : SPINGTP_BF16; }
-
-typedef PyObject* const* Args;
 
 // ---------------------------------------------------------------- operators
 
@@ -442,6 +458,7 @@ PyObject* bind(Args a) {
 #define OP(NAME, N) \
     { #NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<&NAME, N>)), METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {OP(bind, 2),
+                         OP(check_block, 4),
                          OP(pack8, 3),
                          OP(unpack8, 7),
                          OP(rms_norm, 6),

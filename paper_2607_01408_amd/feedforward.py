@@ -86,15 +86,7 @@ class Block8:
 
     def __init__(self, values, scales, shape):
         R, D = shape
-        if R < 0 or D < 1:
-            raise ValueError(f"no matrix has the shape {(R, D)}")
-        pitch, spitch = -(-D // 128) * 128, -(-D // 512) * 4
-        if (values.dtype != torch.float8_e4m3fn or values.shape != (R, pitch) or not values.is_contiguous()
-                or not values.is_cuda):
-            raise ValueError(f"values must be a contiguous float8_e4m3fn [{R}, {pitch}] device tensor")
-        if (scales.dtype != torch.float8_e8m0fnu or scales.shape != (R, spitch) or not scales.is_contiguous()
-                or scales.device != values.device):
-            raise ValueError(f"scales must be a contiguous float8_e8m0fnu [{R}, {spitch}] tensor beside the values")
+        _ops.check_block(values, scales, R, D)
         self.values, self.scales, self.shape = values, scales, (R, D)
 
     @property
