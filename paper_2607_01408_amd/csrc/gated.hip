@@ -164,9 +164,9 @@ __device__ __forceinline__ void send_blocks(const uint8_t* lds, const GemmArgs& 
         *reinterpret_cast<uint4*>(p + r * pitch) = *reinterpret_cast<const uint4*>(lds + r * PITCH + 16 * l);
 }
 
-template <class E, int PN, int PM, int WN, int WM, int ACT, int SAVE, bool OUT8>
+template <class E, int PN, int PM, int WN, int WM, int NS, int ACT, int SAVE, bool OUT8>
 __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOut o) {
-    using Tile = GemmTile<E, PN, PM, WN, WM, true>;
+    using Tile = GemmTile<E, PN, PM, WN, WM, NS, true>;
     static_assert(Tile::kRows == kBlock8, "a tile is one block of its rows");
     constexpr int HALF = Tile::TN / 2, BM = Tile::BM;
     // two places for outputs in turn: one is written while the other leaves
@@ -415,14 +415,14 @@ constexpr int gated_lds() {
     return out > Tile::kLds ? out : Tile::kLds;
 }
 
-template <class E, int PN, int PM, int WN, int WM, int ACT, int SAVE, bool OUT8>
+template <class E, int PN, int PM, int WN, int WM, int NS, int ACT, int SAVE, bool OUT8>
 hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
-    using Tile = GemmTile<E, PN, PM, WN, WM, true>;
+    using Tile = GemmTile<E, PN, PM, WN, WM, NS, true>;
     const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::kRows - 1) / Tile::kRows;
     if (tm * tn > kMostTiles) return hipErrorInvalidValue;
     g.tiles_m = static_cast<int>(tm);
     g.tiles_n = static_cast<int>(tn);
-    constexpr auto kernel = gated_kernel<E, PN, PM, WN, WM, ACT, SAVE, OUT8>;
+    constexpr auto kernel = gated_kernel<E, PN, PM, WN, WM, NS, ACT, SAVE, OUT8>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
     constexpr int lds = gated_lds<Tile, WN>();
@@ -433,9 +433,9 @@ hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
 template <class E, int ACT, int SAVE, bool OUT8>
 hipError_t gated_tiles(const GemmArgs& g, const GatedOut& o, hipStream_t stream) {
     const auto tiles = [&](int64_t bm) { return ((g.M + bm - 1) / bm) * ((g.N + 127) / 128); };
-    if (tiles(256) >= 192) return gated_launch<E, 128, 64, 2, 4, ACT, SAVE, OUT8>(g, o, stream);
-    if (tiles(128) >= 192) return gated_launch<E, 128, 64, 2, 2, ACT, SAVE, OUT8>(g, o, stream);
-    return gated_launch<E, 64, 64, 4, 1, ACT, SAVE, OUT8>(g, o, stream);
+    if (tiles(256) >= 192) return gated_launch<E, 128, 64, 2, 4, 2, ACT, SAVE, OUT8>(g, o, stream);
+    if (tiles(128) >= 192) return gated_launch<E, 128, 64, 2, 2, 3, ACT, SAVE, OUT8>(g, o, stream);
+    return gated_launch<E, 64, 64, 4, 1, 2, ACT, SAVE, OUT8>(g, o, stream);
 }
 
 template <class E, int ACT, int SAVE, bool OUT32>
@@ -475,14 +475,14 @@ hipError_t stage(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K
 }
 
 // c [M][N] (bf16) = x [M] rows against w [N] rows, both of K bf16 elements (a multiple of 64)
-template <int PN, int PM, int WN, int WM>
+template <int PN, int PM, int WN, int WM, int NS>
 hipError_t product_launch(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) {
-    using Tile = GemmTile<Bf16, PN, PM, WN, WM, false>;
+    using Tile = GemmTile<Bf16, PN, PM, WN, WM, NS, false>;
     const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
     if (tm * tn > kMostTiles) return hipErrorInvalidValue;
     g.tiles_m = static_cast<int>(tm);
     g.tiles_n = static_cast<int>(tn);
-    constexpr auto kernel = gemm_nt_kernel<Bf16, PN, PM, WN, WM, uint16_t>;
+    constexpr auto kernel = gemm_nt_kernel<Bf16, PN, PM, WN, WM, NS, uint16_t>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g,
@@ -500,9 +500,9 @@ hipError_t product(const uint16_t* x, const uint16_t* w, void* c, int64_t ldc, i
     g.steps = static_cast<int>(K / 64);
     g.tail = kStepBytes;
     const auto tiles = [&](int64_t n) { return ((M + n - 1) / n) * ((N + n - 1) / n); };
-    if (tiles(256) >= 192) return product_launch<128, 64, 2, 4>(g, c, ldc, stream);
-    if (tiles(128) >= 192) return product_launch<64, 64, 2, 2>(g, c, ldc, stream);
-    return product_launch<32, 32, 2, 2>(g, c, ldc, stream);
+    if (tiles(256) >= 192) return product_launch<128, 64, 2, 4, 2>(g, c, ldc, stream);
+    if (tiles(128) >= 192) return product_launch<64, 64, 2, 2, 2>(g, c, ldc, stream);
+    return product_launch<32, 32, 2, 2, 4>(g, c, ldc, stream);
 }
 
 hipError_t transpose(const void* in, const uint8_t* scales, int64_t ldi, uint16_t* out, int64_t ldo, int64_t at,

@@ -96,11 +96,13 @@ __device__ __forceinline__ void to_lds(Buffer from, uint32_t lane_at, int at, ui
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16,
                                              static_cast<int>(lane_at), at, 0, 0);
 }
-// Waits for all of the wave's loads and LDS reads, then for all waves of the workgroup.  Written out: what
-// __syncthreads waits for is the compiler's account, which has lost loads to LDS here where register
-// loads of one branch came between.
+// Waits until at most LEFT of the wave's loads are in flight (they return in order) and its LDS reads are
+// done, then for all waves of the workgroup.  Written out: what __syncthreads waits for is the compiler's
+// account, which has lost loads to LDS here where register loads of one branch came between.
+template <int LEFT>
 __device__ __forceinline__ void arrived_and_read() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    static_assert(LEFT < 64, "the counter's range");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
 }
 // Most bytes between the rows of an operand: a tile's 256 rows in a buffer's 32-bit offsets.
 constexpr int64_t kMostRowBytes = (int64_t{1} << 23);
@@ -117,8 +119,8 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& 
     tm = 8 * group + in - tn * rows;
 }
 
-// A wave's tile is PN rows of w by PM rows of x; WN x WM waves.
-template <class E, int PN, int PM, int WN, int WM, bool GATED>
+// A wave's tile is PN rows of w by PM rows of x; WN x WM waves; NS steps in LDS.
+template <class E, int PN, int PM, int WN, int WM, int NS, bool GATED>
 struct GemmTile {
     static constexpr int kTile = E::kTile, TN = PN / kTile, TM = PM / kTile;  // accumulators of kTile x kTile
     static constexpr int kPhases = kTile == 16 ? 2 : 4;                    // fragment reads of a step
@@ -127,7 +129,7 @@ struct GemmTile {
     static constexpr int BN = PN * WN, BM = PM * WM;
     static constexpr int kRows = GATED ? BN / 2 : BN;  // of one matrix
     static constexpr int kStage = (BN + BM) * kStepBytes;
-    static constexpr int kLds = 2 * kStage + (E::kScaled ? 2 * (BN + BM) * 4 : 0);
+    static constexpr int kLds = NS * kStage + (E::kScaled ? 2 * (BN + BM) * 4 : 0);
     static constexpr int kScaleLoads = (BN + BM + 64 * kWaves - 1) / (64 * kWaves);  // 64-row loads per wave and group
     static constexpr int LW = BN / 8 / kWaves, LX = BM / 8 / kWaves;  // 8-row loads per wave and step
     static_assert(LW * 8 * kWaves == BN && LX * 8 * kWaves == BM && kWaves % 2 == 0, "whole loads");
@@ -207,7 +209,7 @@ struct GemmTile {
 
         // Scales (8 bits): four steps' bytes of a row are a word, the words of the tile's rows a group in LDS;
         // two groups, and in registers the bytes of the lane's rows for a step, read half a step ahead.
-        uint8_t* const groups = lds + 2 * kStage;
+        uint8_t* const groups = lds + NS * kStage;
         constexpr int kGroup = E::kScaled ? (BN + BM) * 4 : 0;
         constexpr int LS = kScaleLoads;
         const int last_word = (a.steps - 1) >> 2;
@@ -287,18 +289,24 @@ struct GemmTile {
         };
         const auto nothing = [](int) {};
 
-        load_any(0, lds);
         load_scales(0);
         load_scales(1);
-        arrived_and_read();
-        if (a.steps > 1) load_any(1, lds + kStage);
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+            if (k < a.steps) load_any(k, lds + k * kStage);
+        if (a.steps >= NS)
+            arrived_and_read<(NS - 1) * (LW + LX)>();
+        else
+            arrived_and_read<0>();
         read(lds, 0, 0);
         read_scales(0);
-        // step k: its products, the loads of step k + 2 (MORE = 2: some step before the last, 1: any), the
-        // first fragments of step k + 1
+        int at_step = 0;  // where the step lies
+        // step k: its products, the loads of step k + NS into its place (MORE = 2: some step before the last, 1:
+        // any), the first fragments of step k + 1
         auto step = [&](int k, auto more, auto follows) {
-            uint8_t* here = lds + (k & 1) * kStage;
-            uint8_t* next = lds + ((k + 1) & 1) * kStage;
+            uint8_t* here = lds + at_step;
+            at_step = at_step + kStage < NS * kStage ? at_step + kStage : 0;
+            uint8_t* next = lds + at_step;
             if constexpr (E::kScaled) {
 #pragma unroll
                 for (int i = 0; i < TN; ++i) fsw[i] = __uint_as_float(ew[i] << 23);
@@ -310,29 +318,32 @@ struct GemmTile {
                 read(here, q + 1, (q + 1) & 1);
                 multiply(q & 1, nothing);
             }
-            arrived_and_read();  // step k + 1 has arrived, and step k has been read by all
+            // Step k has been read by all, and step k + 1 has arrived: of the loads in flight, in order, only those
+            // of the NS - 2 steps behind it may be left.  (Scales between them make the wait longer, not
+            // shorter; a group's are waited for two steps after their issue and read four steps after it.)
+            arrived_and_read<decltype(more)::value == 2 ? (NS - 2) * (LW + LX) : 0>();
             if constexpr (decltype(follows)::value) {
                 read_scales(k + 1);
                 read(next, 0, 0);
             }
-            if constexpr (decltype(more)::value == 1) load_any(k + 2, here);
+            if constexpr (decltype(more)::value == 1) load_any(k + NS, here);
             // the group of this step's scales has been read by all
-            if (E::kScaled && decltype(more)::value > 0 && (k & 3) == 3) load_scales((k >> 2) + 2);
+            if (E::kScaled && (k & 3) == 3 && (k >> 2) + 2 <= last_word) load_scales((k >> 2) + 2);
             // loads spread over the products: a burst of them would hold the wave up at their issue
             multiply(1, [&](int n) {
                 constexpr int products = TN * TM * E::kParts, all = LW + LX;
                 if (decltype(more)::value == 2 && (n + 1) * all / products > n * all / products) {
 #pragma unroll
-                    for (int t = n * all / products; t < (n + 1) * all / products; ++t) load_part(t, k + 2, here);
+                    for (int t = n * all / products; t < (n + 1) * all / products; ++t) load_part(t, k + NS, here);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             });
         };
         using std::integral_constant;
         int k = 0;
-        for (; k + 3 < a.steps; ++k) step(k, integral_constant<int, 2>{}, std::true_type{});
-        if (k + 2 < a.steps) step(k++, integral_constant<int, 1>{}, std::true_type{});
-        if (k + 1 < a.steps) step(k++, integral_constant<int, 0>{}, std::true_type{});
+        for (; k + NS + 1 < a.steps; ++k) step(k, integral_constant<int, 2>{}, std::true_type{});
+        if (k + NS < a.steps) step(k++, integral_constant<int, 1>{}, std::true_type{});
+        for (; k + 1 < a.steps; ++k) step(k, integral_constant<int, 0>{}, std::true_type{});
         step(k, integral_constant<int, 0>{}, std::false_type{});
     }
 
@@ -364,9 +375,9 @@ __device__ __forceinline__ void store4(uint16_t* p, int64_t left, float a, float
 }
 
 // The product itself, to out [M] rows of ldo elements.
-template <class E, int PN, int PM, int WN, int WM, typename TO>
+template <class E, int PN, int PM, int WN, int WM, int NS, typename TO>
 __global__ __launch_bounds__(64 * WN * WM) void gemm_nt_kernel(GemmArgs a, TO* __restrict__ out, int64_t ldo) {
-    using Tile = GemmTile<E, PN, PM, WN, WM, false>;
+    using Tile = GemmTile<E, PN, PM, WN, WM, NS, false>;
     extern __shared__ __align__(16) uint8_t gemm_lds[];
     int tm, tn;
     tile_of(a.tiles_m, a.tiles_n, tm, tn);

@@ -13,14 +13,14 @@
 namespace spingtp {
 namespace {
 
-template <int PN, int PM, int WN, int WM, typename TO>
+template <int PN, int PM, int WN, int WM, int NS, typename TO>
 hipError_t launch(GemmArgs g, void* out, int64_t ldo, hipStream_t stream) {
-    using Tile = GemmTile<Fp8, PN, PM, WN, WM, false>;
+    using Tile = GemmTile<Fp8, PN, PM, WN, WM, NS, false>;
     const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
     if (tm * tn > kMostTiles) return hipErrorInvalidValue;
     g.tiles_m = static_cast<int>(tm);
     g.tiles_n = static_cast<int>(tn);
-    constexpr auto kernel = gemm_nt_kernel<Fp8, PN, PM, WN, WM, TO>;
+    constexpr auto kernel = gemm_nt_kernel<Fp8, PN, PM, WN, WM, NS, TO>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g,
@@ -43,9 +43,9 @@ hipError_t dispatch(const GemmArgs& g, void* out, int64_t ldo, hipStream_t strea
     if (g.M <= kSkinnyRows) return launch_skinny<2, TO>(g, out, ldo, stream);
     const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
     // the largest tile that still gives most of the 256 CUs one
-    if (tiles(256) >= 192) return launch<128, 64, 2, 4, TO>(g, out, ldo, stream);
-    if (tiles(128) >= 192) return launch<64, 64, 2, 2, TO>(g, out, ldo, stream);
-    return launch<32, 32, 2, 2, TO>(g, out, ldo, stream);
+    if (tiles(256) >= 192) return launch<128, 64, 2, 4, 2, TO>(g, out, ldo, stream);
+    if (tiles(128) >= 192) return launch<64, 64, 2, 2, 2, TO>(g, out, ldo, stream);
+    return launch<32, 32, 2, 2, 4, TO>(g, out, ldo, stream);
 }
 
 }  // namespace

@@ -243,21 +243,29 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_bwd_kernel(
     }
 }
 
-// dgain[d] = sum of the partial rows: 64 columns x 16 row strides per workgroup
+// dgain[d] = sum of the partial rows, in a fixed order: 32 columns a workgroup, 32 row strides with eight
+// rows in flight each
 __global__ __launch_bounds__(1024) void norm_gain_kernel(const float* __restrict__ partial, float* __restrict__ dgain,
                                                          int n, int64_t D) {
-    __shared__ float part[16][64];
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + (threadIdx.x & 63);
-    const int w = threadIdx.x >> 6;
+    __shared__ float part[32][33];
+    const int l = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + l;
     float s = 0.f;
-    if (c < D)
-        for (int i = w; i < n; i += 16) s += partial[i * D + c];
-    part[w][threadIdx.x & 63] = s;
+    if (c < D) {
+        for (int i = w; i < n; i += 256) {
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = i + 32 * j < n ? partial[(i + 32 * j) * D + c] : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += v[j];
+        }
+    }
+    part[w][l] = s;
     __syncthreads();
     if (w == 0 && c < D) {
         s = 0.f;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s += part[i][threadIdx.x & 63];
+        for (int i = 0; i < 32; ++i) s += part[i][l];
         dgain[c] = s;
     }
 }
@@ -312,7 +320,7 @@ hipError_t norm_bwd_launch(const NormBwdArgs& a, hipStream_t stream) {
                        static_cast<const T*>(a.gh), a.ldgh, static_cast<T*>(a.dx), a.lddx,
                        a.dgain != nullptr ? a.partial : nullptr, a.R, a.D);
     if (a.dgain != nullptr)
-        hipLaunchKernelGGL(norm_gain_kernel, dim3(static_cast<unsigned>((a.D + 63) / 64)), dim3(1024), 0, stream,
+        hipLaunchKernelGGL(norm_gain_kernel, dim3(static_cast<unsigned>((a.D + 31) / 32)), dim3(1024), 0, stream,
                            a.partial, a.dgain, static_cast<int>(grid), a.D);
     return hipGetLastError();
 }

@@ -50,33 +50,57 @@ __global__ __launch_bounds__(256) void pack8_rows_kernel(const T* __restrict__ x
     }
 }
 
-// Tile blockIdx.x (rows) x blockIdx.y (columns) of 128 x 128.
+// Two neighbouring columns of a row of the LDS tile.
+__device__ __forceinline__ void two(const float* p, float& a, float& b) {
+    const float2 v = *reinterpret_cast<const float2*>(p);
+    a = v.x, b = v.y;
+}
+__device__ __forceinline__ void two(const uint16_t* p, float& a, float& b) {
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+    a = __uint_as_float(v << 16), b = __uint_as_float(v & 0xffff0000u);
+}
+__device__ __forceinline__ void keep8(float* p, const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(p + 2 * i) = make_float2(v[2 * i], v[2 * i + 1]);
+}
+__device__ __forceinline__ void keep8(uint16_t* p, const float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(p + 2 * i) = bf16_pair(v[2 * i], v[2 * i + 1]);
+}
+
+// Tile blockIdx.x (rows) x blockIdx.y (columns) of 128 x 128.  It lies in LDS in its own type.  Along the
+// columns a lane takes two neighbouring ones and a wave a quarter of their rows, so its reads of LDS run
+// along the rows, without conflicts, and 32 bytes of each column leave in two stores.
 template <typename T, bool ROWS>
 __global__ __launch_bounds__(256) void pack8_both_kernel(const T* __restrict__ x, int64_t ldx,
                                                          uint8_t* __restrict__ values, uint8_t* __restrict__ scales,
                                                          uint8_t* __restrict__ t_values,
                                                          uint8_t* __restrict__ t_scales, int64_t R, int64_t D) {
-    constexpr int ST = 132;  // floats of a tile row
-    __shared__ float tile[128 * ST];
+    constexpr int ST = 130;  // elements of a tile row
+    __shared__ __align__(16) T tile[128 * ST];
+    __shared__ float tops[4][128];
     const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 128, c0 = static_cast<int64_t>(blockIdx.y) * 128;
     const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t pitch = block8_pitch(D), spitch = block8_scale_pitch(D);
     const int64_t left = D - c0 - l * 8;
     const int n = left >= 8 ? 8 : static_cast<int>(left);
+    float v[8][8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int r = i * 16 + g;
-        const int64_t row = r0 + r;
-        float v[8];
-        load8(x + (row < R ? row : 0) * ldx + (n > 0 ? c0 + l * 8 : 0), row < R ? n : 0, v);
-        *reinterpret_cast<float4*>(&tile[r * ST + l * 8]) = make_float4(v[0], v[1], v[2], v[3]);
-        *reinterpret_cast<float4*>(&tile[r * ST + l * 8 + 4]) = make_float4(v[4], v[5], v[6], v[7]);
+        const int64_t row = r0 + i * 16 + g;
+        load8(x + (row < R ? row : 0) * ldx + (n > 0 ? c0 + l * 8 : 0), row < R ? n : 0, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t row = r0 + i * 16 + g;
+        keep8(&tile[(i * 16 + g) * ST + l * 8], v[i]);
         if constexpr (ROWS) {
-            const int e = block8_scale(block8_top(v));
+            const int e = block8_scale(block8_top(v[i]));
             const float inv = block8_inverse(e);
             if (row < R) {
                 *reinterpret_cast<uint2*>(values + row * pitch + c0 + l * 8) =
-                    make_uint2(block8_word(v[0], v[1], v[2], v[3], inv), block8_word(v[4], v[5], v[6], v[7], inv));
+                    make_uint2(block8_word(v[i][0], v[i][1], v[i][2], v[i][3], inv),
+                               block8_word(v[i][4], v[i][5], v[i][6], v[i][7], inv));
                 if (l == 0) scales[row * spitch + blockIdx.y] = static_cast<uint8_t>(e);
                 // the row's scale bytes past its last block
                 if (blockIdx.y == gridDim.y - 1 && l >= 1 && blockIdx.y + l < spitch)
@@ -85,24 +109,43 @@ __global__ __launch_bounds__(256) void pack8_both_kernel(const T* __restrict__ x
         }
     }
     __syncthreads();
-    // columns: 16 lanes take the column's 128 rows, 8 neighbouring rows each
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float a[32], b[32], ta = 0.f, tb = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        two(&tile[(32 * wave + i) * ST + 2 * lane], a[i], b[i]);
+        ta = fmaxf(ta, fabsf(a[i]));
+        tb = fmaxf(tb, fabsf(b[i]));
+    }
+    if (!(fmaxf(ta, tb) < __builtin_inff())) {  // an infinity: the largest finite ones
+        ta = tb = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) ta = fmaxf(ta, finite_abs(a[i])), tb = fmaxf(tb, finite_abs(b[i]));
+    }
+    *reinterpret_cast<float2*>(&tops[wave][2 * lane]) = make_float2(ta, tb);
+    __syncthreads();
     const int64_t tpitch = block8_pitch(R), tspitch = block8_scale_pitch(R);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = i * 16 + g;
+    for (int h = 0; h < 2; ++h) {
+        const int c = 2 * lane + h;
         const int64_t column = c0 + c;
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = tile[(l * 8 + j) * ST + c];
-        const int e = block8_scale(block8_top(v));
+        if (column >= D) continue;
+        const float top = fmaxf(fmaxf(tops[0][c], tops[1][c]), fmaxf(tops[2][c], tops[3][c]));
+        const int e = block8_scale(top);
         const float inv = block8_inverse(e);
-        if (column < D) {
-            *reinterpret_cast<uint2*>(t_values + column * tpitch + r0 + l * 8) =
-                make_uint2(block8_word(v[0], v[1], v[2], v[3], inv), block8_word(v[4], v[5], v[6], v[7], inv));
-            if (l == 0) t_scales[column * tspitch + blockIdx.x] = static_cast<uint8_t>(e);
-            if (blockIdx.x == gridDim.x - 1 && l >= 1 && blockIdx.x + l < tspitch)
-                t_scales[column * tspitch + blockIdx.x + l] = 127;
-        }
+        const float(&w)[32] = h == 0 ? a : b;
+        uint8_t* to = t_values + column * tpitch + r0 + 32 * wave;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            *reinterpret_cast<uint4*>(to + 16 * i) =
+                make_uint4(block8_word(w[16 * i], w[16 * i + 1], w[16 * i + 2], w[16 * i + 3], inv),
+                           block8_word(w[16 * i + 4], w[16 * i + 5], w[16 * i + 6], w[16 * i + 7], inv),
+                           block8_word(w[16 * i + 8], w[16 * i + 9], w[16 * i + 10], w[16 * i + 11], inv),
+                           block8_word(w[16 * i + 12], w[16 * i + 13], w[16 * i + 14], w[16 * i + 15], inv));
+        // the scale, and behind the column's last block the bytes up to the word's end
+        if (wave == 0) t_scales[column * tspitch + blockIdx.x] = static_cast<uint8_t>(e);
+        if (wave > 0 && blockIdx.x == gridDim.x - 1 && blockIdx.x + wave < tspitch)
+            t_scales[column * tspitch + blockIdx.x + wave] = 127;
     }
 }
 
