@@ -433,9 +433,11 @@ hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
 template <class E, int ACT, int SAVE, bool OUT8>
 hipError_t gated_tiles(const GemmArgs& g, const GatedOut& o, hipStream_t stream) {
     const auto tiles = [&](int64_t bm) { return ((g.M + bm - 1) / bm) * ((g.N + 127) / 128); };
-    if (tiles(256) >= 192) return gated_launch<E, 128, 64, 2, 4, 2, ACT, SAVE, OUT8>(g, o, stream);
-    if (tiles(128) >= 192) return gated_launch<E, 128, 64, 2, 2, 3, ACT, SAVE, OUT8>(g, o, stream);
-    return gated_launch<E, 64, 64, 4, 1, 2, ACT, SAVE, OUT8>(g, o, stream);
+    switch (pick_tile(kGated, tiles(64), tiles(128), tiles(256))) {
+        case 256: return gated_launch<E, 128, 64, 2, 4, 2, ACT, SAVE, OUT8>(g, o, stream);
+        case 128: return gated_launch<E, 128, 32, 2, 4, 3, ACT, SAVE, OUT8>(g, o, stream);
+        default: return gated_launch<E, 64, 32, 4, 2, 2, ACT, SAVE, OUT8>(g, o, stream);
+    }
 }
 
 template <class E, int ACT, int SAVE, bool OUT32>
@@ -500,9 +502,11 @@ hipError_t product(const uint16_t* x, const uint16_t* w, void* c, int64_t ldc, i
     g.steps = static_cast<int>(K / 64);
     g.tail = kStepBytes;
     const auto tiles = [&](int64_t n) { return ((M + n - 1) / n) * ((N + n - 1) / n); };
-    if (tiles(256) >= 192) return product_launch<128, 64, 2, 4, 2>(g, c, ldc, stream);
-    if (tiles(128) >= 192) return product_launch<64, 64, 2, 2, 2>(g, c, ldc, stream);
-    return product_launch<32, 32, 2, 2, 4>(g, c, ldc, stream);
+    switch (pick_tile(kPlain16, tiles(64), tiles(128), tiles(256))) {
+        case 256: return product_launch<128, 64, 2, 4, 2>(g, c, ldc, stream);
+        case 128: return product_launch<64, 32, 2, 4, 2>(g, c, ldc, stream);
+        default: return product_launch<32, 32, 2, 2, 4>(g, c, ldc, stream);
+    }
 }
 
 hipError_t transpose(const void* in, const uint8_t* scales, int64_t ldi, uint16_t* out, int64_t ldo, int64_t at,

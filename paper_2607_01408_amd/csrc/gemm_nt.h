@@ -107,6 +107,35 @@ __device__ __forceinline__ void arrived_and_read() {
 // Most bytes between the rows of an operand: a tile's 256 rows in a buffer's 32-bit offsets.
 constexpr int64_t kMostRowBytes = (int64_t{1} << 23);
 
+// Which tile a product takes (64, 128 or 256 rows of x, and as many of w or their like): the one of least
+// estimated time.  A tile's time is a part for the first 256 tiles (one for each CU), its share of CUs
+// included, and a part for each 256 more; smaller tiles lie several to a CU and overlap, so theirs is nearly
+// proportional to their number, but they read more for each product.  Units: about a microsecond for 2,048
+// terms.  Measured (us, 64 / 128 / 256):
+//   8 bits, 1,024^2 11 / 20 / 45, 2,048^2 27 / 23 / 46, 2,048 x 4,096 51 / 38 / 50, 4,096^2 97 / 71 / 78,
+//     4,096 x 8,192 187 / 130 / 121;
+//   bf16 (with what else the gradient does), 1,024^2 27 / 38 / 61, 2,048^2 46 / 41 / 62, 4,096 x 2,048
+//     77 / 52 / 66, 4,096^2 126 / 85 / 80;
+//   gated (rows of x x outputs), 512 x 1,024 17 / 26 / 42, 2,048 x 1,024 28 / 28 / 43, 2,048^2 38 / 33 / 45,
+//     4,096 x 1,280 56 / 55 / 45, 4,096 x 2,560 93 / 91 / 94, 4,096^2 134 / 126 / 109.
+struct TileCost {
+    double first, share, more;  // first 256 tiles: first + share (their number / 256); each 256 more: more
+};
+struct TileCosts {
+    TileCost of64, of128, of256;
+};
+inline double tile_time(const TileCost& c, int64_t tiles) {
+    const int64_t full = (tiles - 1) / 256;
+    return c.more * static_cast<double>(full) + c.first + c.share * static_cast<double>(tiles - 256 * full) / 256;
+}
+inline int pick_tile(const TileCosts& c, int64_t t64, int64_t t128, int64_t t256) {
+    const double a = tile_time(c.of64, t64), b = tile_time(c.of128, t128), d = tile_time(c.of256, t256);
+    return a <= b && a <= d ? 64 : (b <= d ? 128 : 256);
+}
+constexpr TileCosts kPlain8 = {{10, 1, 6}, {18, 5, 15}, {33, 44, 44}};
+constexpr TileCosts kPlain16 = {{10, 1, 6}, {20, 3, 13}, {40, 15, 55}};
+constexpr TileCosts kGated = {{16, 11, 17}, {25, 8, 33}, {40, 15, 55}};
+
 // The tile of this workgroup.  Neighbouring workgroups go to the 8 chiplets in turn: each chiplet
 // takes a run of tiles, 8 tiles of x by as many of w, so that its L2 serves both operands.
 __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& tn) {

@@ -42,10 +42,11 @@ hipError_t dispatch(const GemmArgs& g, void* out, int64_t ldo, hipStream_t strea
     if (g.M <= 16) return launch_skinny<1, TO>(g, out, ldo, stream);
     if (g.M <= kSkinnyRows) return launch_skinny<2, TO>(g, out, ldo, stream);
     const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
-    // the largest tile that still gives most of the 256 CUs one
-    if (tiles(256) >= 192) return launch<128, 64, 2, 4, 2, TO>(g, out, ldo, stream);
-    if (tiles(128) >= 192) return launch<64, 64, 2, 2, 2, TO>(g, out, ldo, stream);
-    return launch<32, 32, 2, 2, 4, TO>(g, out, ldo, stream);
+    switch (pick_tile(kPlain8, tiles(64), tiles(128), tiles(256))) {
+        case 256: return launch<128, 64, 2, 4, 2, TO>(g, out, ldo, stream);
+        case 128: return launch<64, 64, 2, 2, 2, TO>(g, out, ldo, stream);
+        default: return launch<32, 32, 2, 2, 4, TO>(g, out, ldo, stream);
+    }
 }
 
 }  // namespace
