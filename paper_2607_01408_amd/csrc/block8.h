@@ -101,6 +101,29 @@ __device__ __forceinline__ void load8(const uint16_t* p, int n, float (&v)[8]) {
         for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_to_f32(p[i]) : 0.f;
     }
 }
+// load8 of a matrix that is not read again soon: around the caches.
+__device__ __forceinline__ void pass8(const float* p, int n, float (&v)[8]) {
+    if (n >= 8) {
+        const u4f a = __builtin_nontemporal_load(reinterpret_cast<const u4f*>(p));
+        const u4f b = __builtin_nontemporal_load(reinterpret_cast<const u4f*>(p + 4));
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    } else {
+        load8(p, n, v);
+    }
+}
+__device__ __forceinline__ void pass8(const uint16_t* p, int n, float (&v)[8]) {
+    if (n >= 8) {
+        const u4u a = __builtin_nontemporal_load(reinterpret_cast<const u4u*>(p));
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    } else {
+        load8(p, n, v);
+    }
+}
 // two floats to bf16, nearest with ties to even (one instruction)
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {

@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const uint16_t* __restr
         const int nn = in ? n : 0;
         const int64_t c = n > 0 ? f0 + l * 8 : 0;
         float d[8], a[8], b[8];
-        load8(dh + mm * lddh + c, nn, d);
+        pass8(dh + mm * lddh + c, nn, d);
         if constexpr (IN8) {
             const int64_t pitch = block8_pitch(F), spitch = block8_scale_pitch(F);  // f0 + 64 <= pitch
             const int64_t p = mm * pitch + f0 + l * 8, q = mm * spitch + f0 / kBlock8;
@@ -358,8 +358,8 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const uint16_t* __restr
 #pragma unroll
             for (int j = 0; j < 4; ++j) b[j] = lo[j] * sb, b[4 + j] = hi[j] * sb;
         } else {
-            load8(static_cast<const uint16_t*>(g) + mm * F + c, nn, a);
-            load8(static_cast<const uint16_t*>(u) + mm * F + c, nn, b);
+            pass8(static_cast<const uint16_t*>(g) + mm * F + c, nn, a);
+            pass8(static_cast<const uint16_t*>(u) + mm * F + c, nn, b);
         }
         float dg[8], du[8];
 #pragma unroll

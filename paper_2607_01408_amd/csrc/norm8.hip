@@ -163,8 +163,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_bwd_kernel(
             const int k = V > 0 ? static_cast<int>(i) : 0;
             const int64_t c = (i * TPR + t) * 8;
             const int n = left(c);
-            load8(pd + (n > 0 ? c : 0), n, d[k]);
-            load8(ph + (n > 0 ? c : 0), n, w[k]);
+            if (V > 0) {  // read once: around the caches (16,384 x 4,096 bf16: 111 -> 107 us)
+                pass8(pd + (n > 0 ? c : 0), n, d[k]);
+                pass8(ph + (n > 0 ? c : 0), n, w[k]);
+            } else {
+                load8(pd + (n > 0 ? c : 0), n, d[k]);
+                load8(ph + (n > 0 ? c : 0), n, w[k]);
+            }
             if (V == 0) load8(gain + (n > 0 ? c : 0), n, gn[0]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -192,7 +197,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_bwd_kernel(
                 if (V > 0) sum[k][j] = fmaf(d[k][j], w[k][j], sum[k][j]);
             }
             if (gh != nullptr) {
-                load8(gh + row * ldgh + c, n, e);
+                pass8(gh + row * ldgh + c, n, e);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[j] += e[j];
             }
