@@ -742,7 +742,7 @@ spingtp_status spingtp_matmul8(const void* a_values, const void* a_scales, const
  * w_up [F][K] (the same row stride), h [M][F].  x, w_gate, w_up 16-byte aligned.
  * save: what is kept of g and u for the backward pass, nothing, dense bf16 [M][F] (g, u), or 8-bit
  * blocks (g, g_scales, u, u_scales).  workspace: the size below, 0 where K, ldx and ldw are multiples
- * of 8 (M <= 32: where nothing is kept in 8 bits).
+ * of 8 (M <= 64: where nothing is kept in 8 bits).
  */
 spingtp_status spingtp_gated_forward(spingtp_activation act, const void* x, int64_t ldx, const void* w_gate,
                                      const void* w_up, int64_t ldw, void* h, int64_t ldh, spingtp_save save, void* g,
@@ -753,7 +753,7 @@ spingtp_status spingtp_gated_forward_workspace_size(int64_t M, int64_t K, int64_
 
 /* The same from 8-bit blocks, for inference: h in bf16 (h_scales NULL) or in 8-bit blocks (h, h_scales),
  * as the next product takes it.  workspace: the size below (out8: whether h_scales is given), 0 for M
- * above 32 or a bf16 h. */
+ * above 64 or a bf16 h. */
 spingtp_status spingtp_gated_forward8(spingtp_activation act, const void* x, const void* x_scales, const void* w_gate,
                                       const void* w_gate_scales, const void* w_up, const void* w_up_scales, void* h,
                                       int64_t ldh, void* h_scales, void* workspace, size_t workspace_bytes, int64_t M,

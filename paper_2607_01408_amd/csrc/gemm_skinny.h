@@ -1,4 +1,4 @@
-// The products of gemm_nt.h for at most 32 rows of x (single tokens, small batches): bound by the
+// The products of gemm_nt.h for at most 64 rows of x (single tokens, small batches): bound by the
 // reading of w, once.
 //
 // A workgroup takes 16 rows of w (of both matrices in the gated form); its eight waves share the
@@ -17,7 +17,7 @@
 namespace spingtp {
 namespace {
 
-constexpr int kSkinnyRows = 32;   // of x
+constexpr int kSkinnyRows = 64;   // of x
 constexpr int kSkinnyWaves = 8;
 
 // Sixteen bytes of a row from byte `at` on, zeros behind its end (bf16).
@@ -41,7 +41,7 @@ __device__ __forceinline__ v4i row_chunk(const uint8_t* row, int64_t at, int64_t
 // `row_bytes`: of a bf16 row.
 template <class E, int TM, bool GATED, class Done>
 __device__ __forceinline__ void skinny_tile(const GemmArgs& a, int64_t row_bytes, int64_t n0, const Done& done) {
-    constexpr int S = GATED ? 2 : 1, U = TM * S > 2 ? 2 : 4;  // matrices; steps in flight
+    constexpr int S = GATED ? 2 : 1, U = TM * S > 4 ? 1 : (TM * S > 2 ? 2 : 4);  // matrices; steps in flight
     __shared__ float part[kSkinnyWaves][S * TM][16][17];
     const int lane = threadIdx.x & 63, row = lane & 15, group = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -114,14 +114,18 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& a, int64_t row_bytes
 #pragma unroll
             for (int r = 0; r < 4; ++r) part[wave][i * TM + j][4 * group + r][row] = acc[i][j][r];
     __syncthreads();
-    const int at = threadIdx.x & 15, m = threadIdx.x >> 4;  // 32 rows of 16 columns
-    if (m < 16 * TM && m < a.M && n0 + at < a.N) {
-        float s[2] = {0.f, 0.f};
+    const int at = threadIdx.x & 15;
 #pragma unroll
-        for (int i = 0; i < S; ++i)
+    for (int first = 0; first < 16 * TM; first += 32) {  // 32 rows of 16 columns at a time
+        const int m = first + (threadIdx.x >> 4);
+        if (m < 16 * TM && m < a.M && n0 + at < a.N) {
+            float s[2] = {0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kSkinnyWaves; ++w) s[i] += part[w][i * TM + m / 16][at][m & 15];
-        done(m, n0 + at, s[0], s[1]);
+            for (int i = 0; i < S; ++i)
+#pragma unroll
+                for (int w = 0; w < kSkinnyWaves; ++w) s[i] += part[w][i * TM + m / 16][at][m & 15];
+            done(m, n0 + at, s[0], s[1]);
+        }
     }
 }
 

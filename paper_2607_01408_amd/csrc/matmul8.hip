@@ -38,9 +38,13 @@ hipError_t launch_skinny(const GemmArgs& g, void* out, int64_t ldo, hipStream_t 
 }
 
 template <typename TO>
-hipError_t dispatch(const GemmArgs& g, void* out, int64_t ldo, hipStream_t stream) {
+hipError_t dispatch(const GemmArgs& g, int64_t k, void* out, int64_t ldo, hipStream_t stream) {
+    // Few rows: the kernel for them, us against the smallest tile's: one row, 1,024^2 2.6 / 5.9, 4,096^2 5.4 / 16.6,
+    // 8,192 x 2,048 4.7 / 9.5; 32 rows 3.6 / 5.9, 10.2 / 16.7, 8.7 / 9.6; 64 rows 4.7 / 6.2, 15.7 / 16.9, but
+    // 13.3 / 10.2, where there are enough tiles for the sums of 2,048 terms.
     if (g.M <= 16) return launch_skinny<1, TO>(g, out, ldo, stream);
-    if (g.M <= kSkinnyRows) return launch_skinny<2, TO>(g, out, ldo, stream);
+    if (g.M <= 32) return launch_skinny<2, TO>(g, out, ldo, stream);
+    if (g.M <= kSkinnyRows && g.N <= 2 * k) return launch_skinny<4, TO>(g, out, ldo, stream);
     const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
     switch (pick_tile(kPlain8, tiles(64), tiles(128), tiles(256))) {
         case 256: return launch<128, 64, 2, 4, 2, TO>(g, out, ldo, stream);
@@ -63,7 +67,8 @@ hipError_t launch_matmul8(int dtype, const Matmul8Args& a, hipStream_t stream) {
     g.N = a.N;
     g.steps = static_cast<int>(g.ldx / kStepBytes);
     g.tail = kStepBytes;
-    return dtype == SPINGTP_FP32 ? dispatch<float>(g, a.c, a.ldc, stream) : dispatch<uint16_t>(g, a.c, a.ldc, stream);
+    return dtype == SPINGTP_FP32 ? dispatch<float>(g, a.K, a.c, a.ldc, stream)
+                                 : dispatch<uint16_t>(g, a.K, a.c, a.ldc, stream);
 }
 
 }  // namespace spingtp

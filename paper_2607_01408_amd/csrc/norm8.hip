@@ -286,8 +286,9 @@ struct NormShape {
 constexpr int kForwardGroups = 4;   // a row in 32 registers
 constexpr int kBackwardGroups = 2;  // two rows, the gain and its gradient: 64 registers
 
-// Threads per row and column groups per thread.  Many rows: as few threads as hold the row in
-// `groups_most` groups each; few rows: a group per thread, for latency.
+// Threads per row and column groups per thread.  Many rows: as few threads as hold the row in `groups_most`
+// groups each (4,096 x 4,096 bf16 23 us, with one group a thread 33; 16,384 x 1,024 23 / 30).  Few rows: a group
+// per thread, for latency (1 x 2,048 3.2 us, with four groups 5.9; 1,000 x 2,048 5.3 / 7.6).
 NormShape norm_shape(int64_t R, int64_t D, int groups_most) {
     const int64_t groups = (D + 7) / 8;
     for (int tpr : {16, 64, 256, 1024}) {

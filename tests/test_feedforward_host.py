@@ -46,7 +46,7 @@ REFUSED = [
                                       dict(x=P + 2), dict(w_gate=None), dict(w_up=P + 8), dict(h=None), dict(save=3),
                                       dict(save=1), dict(save=1, g=P), dict(save=2, g=P, u=P),
                                       dict(save=2, g=P, u=P, g_scales=P, u_scales=P),
-                                      dict(K=7, M=33), dict(ldx=9, M=33), dict(K=7, M=33, workspace=P, workspace_bytes=16), dict(F=32 * 65535 + 1, ldh=BIG), dict(K=64 * 65535 + 1, ldx=BIG, ldw=BIG)]),
+                                      dict(K=7, M=65), dict(ldx=9, M=65), dict(K=7, M=65, workspace=P, workspace_bytes=16), dict(F=32 * 65535 + 1, ldh=BIG), dict(K=64 * 65535 + 1, ldx=BIG, ldw=BIG)]),
     ("spingtp_gated_forward8", GATED8, [dict(act=-1), dict(K=0), dict(F=0), dict(ldh=3), dict(x=None), dict(x_scales=None),
                                         dict(w_gate=P + 8), dict(w_gate_scales=None), dict(w_up=None),
                                         dict(w_up_scales=P + 2), dict(h=None), dict(h=P + 2, h_scales=P),
@@ -79,7 +79,7 @@ def test_nothing_to_do(name, good, none):
 
 
 @pytest.mark.parametrize("name,sizes", [("spingtp_rms_norm_backward_workspace_size", (2, 0)),
-                                        ("spingtp_gated_forward_workspace_size", (33, 8, 4, 7, 8, 0)),
+                                        ("spingtp_gated_forward_workspace_size", (65, 8, 4, 7, 8, 0)),
                                         ("spingtp_gated_forward8_workspace_size", (0, 0, 4, 1)),
                                         ("spingtp_gated_backward_workspace_size", (2, 8, 0))])
 def test_workspace_sizes(name, sizes):
@@ -102,5 +102,5 @@ def test_workspace_grows_with_the_operands():
     assert fn(32, 63, 32, 63, 63, 3, ctypes.byref(n)) == INVALID
     fn = _lib.lib().spingtp_gated_forward8_workspace_size
     assert fn(32, 64, 100, 1, ctypes.byref(n)) == OK and n.value == 4 * 32 * 100
-    assert fn(33, 64, 100, 1, ctypes.byref(n)) == OK and n.value == 0
+    assert fn(65, 64, 100, 1, ctypes.byref(n)) == OK and n.value == 0
     assert fn(1, 64, 100, 0, ctypes.byref(n)) == OK and n.value == 0

@@ -273,7 +273,7 @@ def check_product(c, a, b, K):
 
 
 MATMULS = [(1, 1, 1), (1, 64, 128), (1, 4096, 512), (2, 17, 130), (5, 300, 1000), (16, 256, 640), (17, 33, 257),
-           (31, 1024, 2048), (33, 65, 129), (64, 64, 512), (100, 700, 900), (257, 129, 1030), (777, 1000, 300),
+           (31, 1024, 2048), (33, 65, 129), (50, 700, 300), (64, 64, 512), (100, 700, 900), (257, 129, 1030), (777, 1000, 300),
            (1600, 1700, 384), (4100, 3900, 256), (300, 9, 5000), (9, 9, 9000)]
 
 
@@ -351,7 +351,7 @@ def gated_bound(x, wg, wu, name, K):
     return g, u, eg, eu, a * u, bound
 
 
-GATED = [(1, 1, 1), (1, 64, 128), (1, 2048, 300), (3, 130, 70), (16, 640, 200), (17, 96, 129), (33, 100, 130),
+GATED = [(1, 1, 1), (1, 64, 128), (1, 2048, 300), (3, 130, 70), (16, 640, 200), (17, 96, 129), (33, 100, 130), (64, 72, 300),
          (65, 257, 64), (300, 72, 500), (999, 200, 273), (513, 1000, 1100), (2050, 64, 3000)]
 
 
