@@ -678,8 +678,7 @@ spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
  *
  * A matrix [R][D] given as (pointer, ld) has rows of D neighbouring elements, `ld` elements apart
  * (ld >= D).  Sizes are at most 2^31 - 1, matrices 2^46 elements; the products' summed axes are
- * shorter: K <= 8388480 (spingtp_matmul8), K <= 4194240, F <= 2097120 and, for the gradients,
- * M <= 4194240 (gated block).
+ * shorter: K <= 8388480 (spingtp_matmul8), K <= 4194240 and F <= 2097120 (gated block).
  * Outputs must not overlap inputs or one another.  R = 0 (M = 0) is valid: gradients of weights are
  * then zero, everything else is empty.  Sums and statistics are fp32, outputs are rounded to nearest
  * even.
@@ -765,7 +764,9 @@ spingtp_status spingtp_gated_forward8_workspace_size(int64_t M, int64_t K, int64
  * its 8-bit checkpoint (x_scales not NULL):
  *   dg = grad_h u act'(g), du = grad_h act(g) (rounded to bf16, operands of the matrix units),
  *   grad_x [M][K] = dg w_gate + du w_up,  grad_w [2F][K] = dg^T x, then du^T x.
- * grad_x or grad_w may be NULL (then the weights, or x, are not read).
+ * grad_x or grad_w may be NULL (then the weights, or x, are not read).  x, w_gate, w_up 16-byte aligned.
+ * workspace: the size below (x8: whether x is 8-bit; ldx is then not used): 4 bytes for each element of g, and
+ * copies of x and the weights only where x is 8-bit or their rows do not start and end on 16 bytes.
  */
 spingtp_status spingtp_gated_backward(spingtp_activation act, const void* grad_h, int64_t ldgh, spingtp_save save,
                                       const void* g, const void* g_scales, const void* u, const void* u_scales,
@@ -773,7 +774,8 @@ spingtp_status spingtp_gated_backward(spingtp_activation act, const void* grad_h
                                       const void* w_up, int64_t ldw, void* grad_x, int64_t ldgx, void* grad_w,
                                       void* workspace, size_t workspace_bytes, int64_t M, int64_t K, int64_t F,
                                       void* stream);
-spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, size_t* size);
+spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw,
+                                                     int x8, size_t* size);
 
 #ifdef __cplusplus
 }

@@ -150,7 +150,7 @@ def _feedforward_signatures(L):
                        ("spingtp_gated_forward8", "ipppppppnppznnnp"),
                        ("spingtp_gated_forward8_workspace_size", "nnnis"),
                        ("spingtp_gated_backward", "ipnipppppnpppnpnppznnnp"),
-                       ("spingtp_gated_backward_workspace_size", "nnns")):
+                       ("spingtp_gated_backward_workspace_size", "nnnnnis")):
         fn = getattr(L, name)
         fn.argtypes = [kinds[a] for a in args]
         fn.restype = ctypes.c_int

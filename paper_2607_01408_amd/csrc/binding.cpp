@@ -410,7 +410,8 @@ PyObject* gated_backward(Args a) {
     if (truth(a[8])) dx = empty({M, K}, at::kBFloat16, *dh.t);
     if (truth(a[9])) dw = empty({2 * F, K}, at::kBFloat16, *dh.t);
     size_t bytes = 0;
-    done(lib.gated_backward_workspace_size(M, K, F, &bytes), "spingtp_gated_backward_workspace_size");
+    done(lib.gated_backward_workspace_size(M, K, F, kept[0].ld, w.first.ld, save == SPINGTP_SAVE_BLOCK8, &bytes),
+         "spingtp_gated_backward_workspace_size");
     const at::Tensor ws = workspace(bytes, *dh.t);
     done(lib.gated_backward(static_cast<spingtp_activation>(integer(a[7])), dh.p, dh.ld, save, kept[1].p, kept8[1].scales,
                             kept[2].p, kept8[2].scales, kept[0].p, kept[0].ld, kept8[0].scales, w.first.p, w.second.p,

@@ -204,10 +204,11 @@ extern "C" spingtp_status spingtp_gated_forward8(spingtp_activation act, const v
     return of(spingtp::launch_gated8(a, stream_of(stream)));
 }
 
-extern "C" spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, size_t* size) {
-    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || M > int64_t{65535} * 64)
+extern "C" spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx,
+                                                                int64_t ldw, int x8, size_t* size) {
+    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || (x8 == 0 && ldx < K) || ldw < K)
         return SPINGTP_ERR_INVALID_ARG;
-    *size = spingtp::gated_backward_workspace(M, K, F);
+    *size = spingtp::gated_backward_workspace(M, K, F, ldx, ldw, x8 != 0);
     return SPINGTP_OK;
 }
 
@@ -218,19 +219,20 @@ extern "C" spingtp_status spingtp_gated_backward(spingtp_activation act, const v
                                                  int64_t ldgx, void* grad_w, void* workspace, size_t workspace_bytes,
                                                  int64_t M, int64_t K, int64_t F, void* stream) {
     size_t need = 0;
-    if (!gated_sizes_ok(act, M, K, F) || spingtp_gated_backward_workspace_size(M, K, F, &need) != SPINGTP_OK)
+    if (!gated_sizes_ok(act, M, K, F) ||
+        spingtp_gated_backward_workspace_size(M, K, F, ldx, ldw, x_scales != nullptr, &need) != SPINGTP_OK)
         return SPINGTP_ERR_INVALID_ARG;
     if (ldgh < F || !matrix_ok(M, ldgh) || (save != SPINGTP_SAVE_BF16 && save != SPINGTP_SAVE_BLOCK8))
         return SPINGTP_ERR_INVALID_ARG;
-    if (grad_x != nullptr && (ldgx < K || !matrix_ok(M, ldgx) || ldw < K || !matrix_ok(F, ldw) || off(grad_x, 2)))
+    if (grad_x != nullptr && (ldgx < K || !matrix_ok(M, ldgx) || !matrix_ok(F, ldw) || off(grad_x, 2)))
         return SPINGTP_ERR_INVALID_ARG;
-    if (grad_w != nullptr && ((x_scales == nullptr && (ldx < K || !matrix_ok(M, ldx))) || off(grad_w, 2)))
+    if (grad_w != nullptr && ((x_scales == nullptr && !matrix_ok(M, ldx)) || off(grad_w, 2)))
         return SPINGTP_ERR_INVALID_ARG;
     if (M > 0) {
         if (bad(grad_h, 2) || bad(g, 16) || bad(u, 16)) return SPINGTP_ERR_INVALID_ARG;
         if (save == SPINGTP_SAVE_BLOCK8 && (bad(g_scales, 4) || bad(u_scales, 4))) return SPINGTP_ERR_INVALID_ARG;
-        if (grad_x != nullptr && (bad(w_gate, 2) || bad(w_up, 2))) return SPINGTP_ERR_INVALID_ARG;
-        if (grad_w != nullptr && (bad(x, x_scales != nullptr ? 16 : 2) || off(x_scales, 4)))
+        if (grad_x != nullptr && (bad(w_gate, 16) || bad(w_up, 16))) return SPINGTP_ERR_INVALID_ARG;
+        if (grad_w != nullptr && (bad(x, 16) || off(x_scales, 4)))
             return SPINGTP_ERR_INVALID_ARG;
         if (bad(workspace, 16) || workspace_bytes < need) return SPINGTP_ERR_INVALID_ARG;
     }

@@ -122,7 +122,7 @@ struct GatedBwdArgs {
     void* workspace;
     int64_t M, K, F;
 };
-size_t gated_backward_workspace(int64_t M, int64_t K, int64_t F);
+size_t gated_backward_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw, bool x8);
 hipError_t launch_gated_backward(const GatedBwdArgs& a, hipStream_t stream);
 
 }  // namespace spingtp

@@ -8,11 +8,11 @@
 // only where the backward pass is to have them, in bf16 or as 8-bit blocks (a tile's 128 columns are
 // one block of each of its rows).
 //
-// Backward: dg and du are computed once and written side by side, [M][g | u], and transposed; then
-// dx is one product over g | u against the weights side by side, and both weight gradients are one
-// product over M.  All products run along both operands' rows (gemm_nt.h), so x and the weights are
-// transposed first, x straight from its 8-bit checkpoint where that is what was kept.  dg and du are
-// rounded to bf16, as operands of the matrix units; sums are fp32.
+// Backward: dg and du are computed once and written side by side, [M][g | u]; then dx is one product of them
+// with the weights, and both weight gradients are one product over M.  The weights' rows and, for the
+// weight gradients, both operands' run across the summed axis: the products read them as they are.  An
+// 8-bit checkpoint of x is unpacked first.  dg and du are rounded to bf16, as operands of the matrix
+// units; sums are fp32.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -267,84 +267,24 @@ __global__ __launch_bounds__(256) void stage_rows_kernel(const uint16_t* __restr
     store8(out + row * pitch + c, 8, v);
 }
 
-// out[c][at + r] = in[r][c], zeros for r from R to the next multiple of 64; in is bf16 [R] rows of ldi
-// elements, or 8-bit blocks.
-template <bool IN8>
-__global__ __launch_bounds__(256) void transpose_kernel(const void* __restrict__ in, const uint8_t* __restrict__ scales,
-                                                        int64_t ldi, uint16_t* __restrict__ out, int64_t ldo,
-                                                        int64_t at, int64_t R, int64_t C) {
-    constexpr int ST = 66;  // elements of a tile column: an odd number of words
-    __shared__ uint16_t tile[64 * ST];
-    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 64, c0 = static_cast<int64_t>(blockIdx.y) * 64;
-    const int l = threadIdx.x & 7, g = threadIdx.x >> 3;
-    const int64_t left = C - c0 - l * 8;
-    const int n = left >= 8 ? 8 : static_cast<int>(left);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = i * 32 + g;
-        const int64_t row = r0 + r;
-        float v[8];
-        if constexpr (IN8) {
-            const int64_t pitch = block8_pitch(C);  // c0 + 64 <= pitch
-            const int64_t rr = row < R ? row : R - 1;
-            const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(in) + rr * pitch + c0 + l * 8);
-            const float s = row < R ? block8_power(scales[rr * block8_scale_pitch(C) + c0 / kBlock8]) : 0.f;
-            float a[4], b[4];
-            block8_values(q.x, a);
-            block8_values(q.y, b);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = row < R ? a[j] * s : 0.f, v[4 + j] = row < R ? b[j] * s : 0.f;
-        } else {
-            load8(static_cast<const uint16_t*>(in) + (row < R ? row : 0) * ldi + (n > 0 ? c0 + l * 8 : 0),
-                  row < R ? n : 0, v);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            const uint32_t w = bf16_pair(v[j], v[j + 1]);
-            tile[(l * 8 + j) * ST + r] = static_cast<uint16_t>(w);
-            tile[(l * 8 + j + 1) * ST + r] = static_cast<uint16_t>(w >> 16);
-        }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int c = i * 32 + g;
-        if (c0 + c >= C) continue;
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const uint32_t*>(&tile[c * ST + l * 8 + 2 * j]);
-        *reinterpret_cast<uint4*>(out + (c0 + c) * ldo + at + r0 + l * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-}
-
-// dg and du of a tile of 64 rows x 64 columns: side by side in both [M][2 Fp] and transposed
-// [2 F][Mp] (Fp, Mp: multiples of 64, zeros behind).
+// dg and du side by side, [M][2 Fp] (Fp: F up to a multiple of 64, zeros behind): 8 neighbouring columns of both
+// per thread.  Everything passes through once, g, u and dh around the caches.
 template <int ACT, bool IN8>
 __global__ __launch_bounds__(256) void gated_grad_kernel(const uint16_t* __restrict__ dh, int64_t lddh,
                                                          const void* __restrict__ g, const void* __restrict__ u,
                                                          const uint8_t* __restrict__ gs,
                                                          const uint8_t* __restrict__ us, uint16_t* __restrict__ both,
-                                                         uint16_t* __restrict__ both_t, int64_t M, int64_t F) {
-    constexpr int ST = 66;
-    __shared__ uint16_t tile[2][64 * ST];
-    const int64_t m0 = static_cast<int64_t>(blockIdx.x) * 64, f0 = static_cast<int64_t>(blockIdx.y) * 64;
-    const int64_t fp = (F + 63) / 64 * 64, mp = (M + 63) / 64 * 64;
-    const int l = threadIdx.x & 7, k = threadIdx.x >> 3;
-    const int64_t left = F - f0 - l * 8;
-    const int n = left >= 8 ? 8 : static_cast<int>(left);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int r = i * 32 + k;
-        const int64_t m = m0 + r;
-        const bool in = m < M;
-        const int64_t mm = in ? m : M - 1;
-        const int nn = in ? n : 0;
-        const int64_t c = n > 0 ? f0 + l * 8 : 0;
+                                                         int64_t M, int64_t F) {
+    const int64_t fp = (F + 63) / 64 * 64, stride = static_cast<int64_t>(gridDim.x) * 256;
+    const uint32_t groups = static_cast<uint32_t>(fp / 8);
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < M * groups; at += stride) {
+        const int64_t m = at / groups, f = (at - m * groups) * 8, left = F - f;
+        const int n = left >= 8 ? 8 : static_cast<int>(left);
+        const int64_t c = n > 0 ? f : 0;
         float d[8], a[8], b[8];
-        pass8(dh + mm * lddh + c, nn, d);
+        pass8(dh + m * lddh + c, n, d);
         if constexpr (IN8) {
-            const int64_t pitch = block8_pitch(F), spitch = block8_scale_pitch(F);  // f0 + 64 <= pitch
-            const int64_t p = mm * pitch + f0 + l * 8, q = mm * spitch + f0 / kBlock8;
+            const int64_t p = m * block8_pitch(F) + f, q = m * block8_scale_pitch(F) + f / kBlock8;  // f < the pitch
             const uint2 wa = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(g) + p);
             const uint2 wb = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(u) + p);
             const float sa = block8_power(gs[q]), sb = block8_power(us[q]);
@@ -358,47 +298,20 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const uint16_t* __restr
 #pragma unroll
             for (int j = 0; j < 4; ++j) b[j] = lo[j] * sb, b[4 + j] = hi[j] * sb;
         } else {
-            pass8(static_cast<const uint16_t*>(g) + mm * F + c, nn, a);
-            pass8(static_cast<const uint16_t*>(u) + mm * F + c, nn, b);
+            pass8(static_cast<const uint16_t*>(g) + m * F + c, n, a);
+            pass8(static_cast<const uint16_t*>(u) + m * F + c, n, b);
         }
         float dg[8], du[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float y, dy;
             act_grad<ACT>(a[j], y, dy);
-            dg[j] = j < nn ? d[j] * b[j] * dy : 0.f;
-            du[j] = j < nn ? d[j] * y : 0.f;
+            dg[j] = j < n ? d[j] * b[j] * dy : 0.f;
+            du[j] = j < n ? d[j] * y : 0.f;
         }
-        const uint4 wg = make_uint4(bf16_pair(dg[0], dg[1]), bf16_pair(dg[2], dg[3]), bf16_pair(dg[4], dg[5]),
-                                    bf16_pair(dg[6], dg[7]));
-        const uint4 wu = make_uint4(bf16_pair(du[0], du[1]), bf16_pair(du[2], du[3]), bf16_pair(du[4], du[5]),
-                                    bf16_pair(du[6], du[7]));
-        if (in && both != nullptr) {
-            *reinterpret_cast<uint4*>(both + m * 2 * fp + f0 + l * 8) = wg;
-            *reinterpret_cast<uint4*>(both + m * 2 * fp + fp + f0 + l * 8) = wu;
-        }
-        const uint32_t pg[4] = {wg.x, wg.y, wg.z, wg.w}, pu[4] = {wu.x, wu.y, wu.z, wu.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            tile[0][(l * 8 + 2 * j) * ST + r] = static_cast<uint16_t>(pg[j]);
-            tile[0][(l * 8 + 2 * j + 1) * ST + r] = static_cast<uint16_t>(pg[j] >> 16);
-            tile[1][(l * 8 + 2 * j) * ST + r] = static_cast<uint16_t>(pu[j]);
-            tile[1][(l * 8 + 2 * j + 1) * ST + r] = static_cast<uint16_t>(pu[j] >> 16);
-        }
+        store8(both + m * 2 * fp + f, 8, dg);
+        store8(both + m * 2 * fp + fp + f, 8, du);
     }
-    if (both_t == nullptr) return;
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int c = i * 32 + k;
-            if (f0 + c >= F) continue;
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const uint32_t*>(&tile[q][c * ST + l * 8 + 2 * j]);
-            *reinterpret_cast<uint4*>(both_t + (q * F + f0 + c) * mp + m0 + l * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
@@ -406,7 +319,7 @@ __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
     if (i < n) p[i] = 0;
 }
 
-bool grid_ok(int64_t x, int64_t y = 1) { return x <= (int64_t{1} << 24) - 1 && y <= 65535; }  // below 2^32 threads
+bool grid_ok(int64_t x) { return x <= (int64_t{1} << 24) - 1; }  // below 2^32 threads
 
 // LDS of a workgroup: the operands' tiles, then the outputs'
 template <class Tile, int WN>
@@ -480,63 +393,43 @@ hipError_t stage(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K
     return hipGetLastError();
 }
 
-// c [M][N] (bf16) = x [M] rows against w [N] rows, both of K bf16 elements (a multiple of 64)
-template <int PN, int PM, int WN, int WM, int NS>
+// The gradients' products: w's columns run along the summed axis, x's with KX.
+template <int PN, int PM, int WN, int WM, int NS, bool KX>
 hipError_t product_launch(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) {
-    using Tile = GemmTile<Bf16, PN, PM, WN, WM, NS, false>;
+    using Tile = GemmTile<Bf16, PN, PM, WN, WM, NS, false, true, KX>;
     const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
     if (tm * tn > kMostTiles) return hipErrorInvalidValue;
     g.tiles_m = static_cast<int>(tm);
     g.tiles_n = static_cast<int>(tn);
-    constexpr auto kernel = gemm_nt_kernel<Bf16, PN, PM, WN, WM, NS, uint16_t>;
+    constexpr auto kernel = gemm_nt_kernel<Bf16, PN, PM, WN, WM, NS, uint16_t, true, KX>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn)), dim3(Tile::kThreads), Tile::kLds, stream, g,
                        static_cast<uint16_t*>(c), ldc);
     return hipGetLastError();
 }
-hipError_t product(const uint16_t* x, const uint16_t* w, void* c, int64_t ldc, int64_t M, int64_t N, int64_t K,
-                   hipStream_t stream) {
-    GemmArgs g{};
-    g.w = reinterpret_cast<const uint8_t*>(w);
-    g.x = reinterpret_cast<const uint8_t*>(x);
-    g.ldw = g.ldx = 2 * K;
-    g.M = M;
-    g.N = N;
-    g.steps = static_cast<int>(K / 64);
+template <bool KX>
+hipError_t product(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) {
     g.tail = kStepBytes;
-    const auto tiles = [&](int64_t n) { return ((M + n - 1) / n) * ((N + n - 1) / n); };
+    const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
     switch (pick_tile(kPlain16, tiles(64), tiles(128), tiles(256))) {
-        case 256: return product_launch<128, 64, 2, 4, 2>(g, c, ldc, stream);
-        case 128: return product_launch<64, 32, 2, 4, 2>(g, c, ldc, stream);
-        default: return product_launch<32, 32, 2, 2, 4>(g, c, ldc, stream);
+        case 256: return product_launch<128, 64, 2, 4, 2, KX>(g, c, ldc, stream);
+        case 128: return product_launch<64, 32, 2, 4, 2, KX>(g, c, ldc, stream);
+        default: return product_launch<32, 32, 2, 2, 4, KX>(g, c, ldc, stream);
     }
 }
 
-hipError_t transpose(const void* in, const uint8_t* scales, int64_t ldi, uint16_t* out, int64_t ldo, int64_t at,
-                     int64_t R, int64_t C, hipStream_t stream) {
-    const int64_t br = (R + 63) / 64, bc = (C + 63) / 64;
-    if (!grid_ok(br, bc)) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(br), static_cast<unsigned>(bc));
-    if (scales != nullptr)
-        hipLaunchKernelGGL((transpose_kernel<true>), grid, dim3(256), 0, stream, in, scales, ldi, out, ldo, at, R, C);
-    else
-        hipLaunchKernelGGL((transpose_kernel<false>), grid, dim3(256), 0, stream, in, scales, ldi, out, ldo, at, R, C);
-    return hipGetLastError();
-}
-
 template <int ACT>
-hipError_t gated_grad(const GatedBwdArgs& a, uint16_t* both, uint16_t* both_t, hipStream_t stream) {
-    const int64_t bm = (a.M + 63) / 64, bf = (a.F + 63) / 64;
-    if (!grid_ok(bm, bf)) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(bm), static_cast<unsigned>(bf));
+hipError_t gated_grad(const GatedBwdArgs& a, uint16_t* both, hipStream_t stream) {
+    const int64_t blocks = (a.M * (up64(a.F) / 8) + 255) / 256;
+    const dim3 grid(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks));
     const uint16_t* dh = static_cast<const uint16_t*>(a.dh);
     if (a.save == kSave8)
         hipLaunchKernelGGL((gated_grad_kernel<ACT, true>), grid, dim3(256), 0, stream, dh, a.lddh, a.g, a.u, a.g_scales,
-                           a.u_scales, both, both_t, a.M, a.F);
+                           a.u_scales, both, a.M, a.F);
     else
         hipLaunchKernelGGL((gated_grad_kernel<ACT, false>), grid, dim3(256), 0, stream, dh, a.lddh, a.g, a.u,
-                           a.g_scales, a.u_scales, both, both_t, a.M, a.F);
+                           a.g_scales, a.u_scales, both, a.M, a.F);
     return hipGetLastError();
 }
 
@@ -635,9 +528,9 @@ hipError_t launch_gated8(const GatedArgs& a, hipStream_t stream) {
                                  : gated_act<Fp8, kSaveNone, false>(a.act, g, o, stream);
 }
 
-size_t gated_backward_workspace(int64_t M, int64_t K, int64_t F) {
-    const int64_t fp = up64(F), mp = up64(M);
-    return static_cast<size_t>(2 * (M * 2 * fp + 2 * F * mp + K * 2 * fp + K * mp));
+size_t gated_backward_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw, bool x8) {
+    const int64_t x = x8 || !rows_fit(K, ldx) ? M * up64(K) : 0, w = rows_fit(K, ldw) ? 0 : 2 * F * up64(K);
+    return static_cast<size_t>(2 * (M * 2 * up64(F) + x + w));
 }
 
 hipError_t launch_gated_backward(const GatedBwdArgs& a, hipStream_t stream) {
@@ -649,22 +542,56 @@ hipError_t launch_gated_backward(const GatedBwdArgs& a, hipStream_t stream) {
                            static_cast<uint16_t*>(a.dw), n);
         return hipGetLastError();
     }
-    const int64_t fp = up64(a.F), mp = up64(a.M);
+    const int64_t fp = up64(a.F), kp = up64(a.K);
     uint16_t* both = static_cast<uint16_t*>(a.workspace);
-    uint16_t* both_t = both + a.M * 2 * fp;
-    uint16_t* w_t = both_t + 2 * a.F * mp;
-    uint16_t* x_t = w_t + a.K * 2 * fp;
-    uint16_t* d = a.dx != nullptr ? both : nullptr;
-    uint16_t* d_t = a.dw != nullptr ? both_t : nullptr;
-    hipError_t e = a.act == kSilu ? gated_grad<kSilu>(a, d, d_t, stream) : gated_grad<kGelu>(a, d, d_t, stream);
+    uint16_t* free_at = both + a.M * 2 * fp;
+    hipError_t e = a.act == kSilu ? gated_grad<kSilu>(a, both, stream) : gated_grad<kGelu>(a, both, stream);
     if (e == hipSuccess && a.dx != nullptr) {
-        e = transpose(a.wg, nullptr, a.ldw, w_t, 2 * fp, 0, a.F, a.K, stream);
-        if (e == hipSuccess) e = transpose(a.wu, nullptr, a.ldw, w_t, 2 * fp, fp, a.F, a.K, stream);
-        if (e == hipSuccess) e = product(both, w_t, a.dx, a.lddx, a.M, a.K, 2 * fp, stream);
+        GemmArgs g{};
+        g.x = reinterpret_cast<const uint8_t*>(both);
+        g.ldx = 4 * fp;
+        g.w = static_cast<const uint8_t*>(a.wg);
+        g.w2 = static_cast<const uint8_t*>(a.wu);
+        g.ldw = 2 * a.ldw;
+        if (!rows_fit(a.K, a.ldw)) {
+            e = stage(a.wg, a.ldw, free_at, a.F, a.K, stream);
+            if (e == hipSuccess) e = stage(a.wu, a.ldw, free_at + a.F * kp, a.F, a.K, stream);
+            g.w = reinterpret_cast<const uint8_t*>(free_at);
+            g.w2 = reinterpret_cast<const uint8_t*>(free_at + a.F * kp);
+            g.ldw = 2 * kp;
+            free_at += 2 * a.F * kp;
+        }
+        g.M = a.M;
+        g.N = a.K;
+        g.steps = static_cast<int>(2 * fp / 64);
+        g.w_rows = a.F;
+        g.w_split = static_cast<int>(fp / 64);
+        if (e == hipSuccess) e = product<false>(g, a.dx, a.lddx, stream);
     }
     if (e == hipSuccess && a.dw != nullptr) {
-        e = transpose(a.x, a.x_scales, a.ldx, x_t, mp, 0, a.M, a.K, stream);
-        if (e == hipSuccess) e = product(both_t, x_t, a.dw, a.K, 2 * a.F, a.K, mp, stream);
+        GemmArgs g{};
+        g.w = static_cast<const uint8_t*>(a.x);
+        g.ldw = 2 * a.ldx;
+        if (a.x_scales != nullptr) {
+            e = launch_unpack8(SPINGTP_BF16, static_cast<const uint8_t*>(a.x), a.x_scales, free_at, kp, a.M, a.K, stream);
+        } else if (!rows_fit(a.K, a.ldx)) {
+            e = stage(a.x, a.ldx, free_at, a.M, a.K, stream);
+        }
+        if (a.x_scales != nullptr || !rows_fit(a.K, a.ldx)) {
+            g.w = reinterpret_cast<const uint8_t*>(free_at);
+            g.ldw = 2 * kp;
+        }
+        g.w2 = g.w;
+        g.x = reinterpret_cast<const uint8_t*>(both);
+        g.ldx = 4 * fp;
+        g.M = fp + a.F;
+        g.N = a.K;
+        g.steps = static_cast<int>((a.M + 63) / 64);
+        g.w_rows = g.x_rows = a.M;
+        g.w_split = g.steps;
+        g.gap_at = a.F;
+        g.gap = fp - a.F;
+        if (e == hipSuccess) e = product<true>(g, a.dw, a.K, stream);
     }
     return e;
 }

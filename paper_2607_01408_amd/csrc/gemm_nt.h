@@ -1,4 +1,4 @@
-// Matrix product of two matrices whose rows run along the summed axis:
+// Matrix product of two matrices, here with rows that run along the summed axis:
 //   c[m][n] = sum_k x[m][k] w[n][k],
 // bf16 or 8-bit block format (block8.h) operands, bf16 matrix units, fp32 accumulators, one workgroup per tile of BN
 // rows of w and BM rows of x.  The epilogue gets the accumulators.  In the gated form half of the
@@ -9,6 +9,12 @@
 // multiplied.  A row's eight 16-byte chunks are stored rotated by an exclusive or with the row, which
 // the loading lanes bring about by which chunk each of them fetches; so the lanes of a fragment read,
 // which hold one chunk of 16 rows, spread over all banks.
+//
+// Either operand may instead have columns that run along the summed axis (bf16: w[k][n], x[k][m]; the
+// gradients' products).  A step is then 64 of its rows, the tile's columns of each; they lie in LDS as
+// they come, and the fragment reads transpose (ds_read_b64_tr_b16: 16 lanes read 4 rows of 16 columns and
+// each gets a column's four).  The order of k is the same as of the other form, so the two can meet.  Here
+// 32-byte pairs of chunks are rotated by the row, so that the 16 rows of a read spread over all banks.
 //
 // w rows are the matrix unit's rows, x rows its columns, so that a lane's accumulators are one x row and
 // runs of four neighbouring w rows: four neighbouring outputs.  The order of k inside a step is the same
@@ -37,6 +43,11 @@ struct GemmArgs {
     int steps;          // of 128 bytes
     int tail;           // bf16: bytes of the last step that exist, a multiple of 16 (128: all)
     int tiles_m, tiles_n;
+    // columns along k: rows of w (of each matrix) and x, the step from which on w2 is read, and output rows left
+    // out: [gap_at, gap_at + gap), those behind move up
+    int64_t w_rows, x_rows;
+    int w_split;
+    int64_t gap_at, gap;
 };
 
 namespace {
@@ -149,7 +160,8 @@ __device__ __forceinline__ void tile_of(int tiles_m, int tiles_n, int& tm, int& 
 }
 
 // A wave's tile is PN rows of w by PM rows of x; WN x WM waves; NS steps in LDS.
-template <class E, int PN, int PM, int WN, int WM, int NS, bool GATED>
+// KW, KX: the columns of w, x run along the summed axis.
+template <class E, int PN, int PM, int WN, int WM, int NS, bool GATED, bool KW = false, bool KX = false>
 struct GemmTile {
     static constexpr int kTile = E::kTile, TN = PN / kTile, TM = PM / kTile;  // accumulators of kTile x kTile
     static constexpr int kPhases = kTile == 16 ? 2 : 4;                    // fragment reads of a step
@@ -163,6 +175,8 @@ struct GemmTile {
     static constexpr int LW = BN / 8 / kWaves, LX = BM / 8 / kWaves;  // 8-row loads per wave and step
     static_assert(LW * 8 * kWaves == BN && LX * 8 * kWaves == BM && kWaves % 2 == 0, "whole loads");
     static_assert(BN % 64 == 0 && (!GATED || kRows % 64 == 0), "a load of scales is one operand's");
+    static_assert(!KX || KW);
+    static_assert(!KW || (E::kTile == 16 && !E::kScaled && !GATED), "bf16");
     static_assert(!GATED || (TN % 2 == 0 && LW % 2 == 0), "both halves in a wave, and in its loads");
 
     typename E::Acc acc[TN][TM];
@@ -175,6 +189,22 @@ struct GemmTile {
     }
     static __device__ __forceinline__ int lds_row(int i, int wn) {
         return (GATED && i >= TN / 2 ? kRows : 0) + row_in(i, wn);
+    }
+
+    // columns along k: what the chunk's number in row r of `cpr` chunks is turned by
+    static __device__ __forceinline__ int turn(int cpr, int r) {
+        return cpr >= 16 ? 2 * ((r & 3) | ((r >> 3) & 1) << 2) : 2 * (((r >> 1) & 1) | ((r >> 3) & 1) << 1);
+    }
+    // Eight rows of the lane's column: four at `from`'s row and four `four` bytes on.  (__restrict__: what is known
+    // of a pointer keeps the compiler from waiting here for every load to LDS in flight, as with the plain
+    // reads' types; dx of 8,192 x 2,048 x 8,192 565 us without it.)
+    static __device__ __forceinline__ v4i turned(const uint8_t* __restrict__ from, int four) {
+        typedef short v4s __attribute__((ext_vector_type(4)));
+        typedef int v2i __attribute__((ext_vector_type(2)));
+        typedef __attribute__((address_space(3))) v4s* P;
+        const v2i lo = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(from)));
+        const v2i hi = __builtin_bit_cast(v2i, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(from + four)));
+        return v4i{lo.x, lo.y, hi.x, hi.y};
     }
 
     __device__ __forceinline__ void run(const GemmArgs& a, int64_t n0, int64_t m0, uint8_t* lds) {
@@ -200,25 +230,59 @@ struct GemmTile {
         const Buffer bw = buffer_of(a.w + n0 * a.ldw, bytes_w);
         const Buffer bw2 = buffer_of((GATED ? a.w2 : a.w) + n0 * a.ldw, bytes_w);
         const Buffer bx = buffer_of(a.x + m0 * a.ldx, bytes_x);
+        // Columns along k: the next step's rows of an operand as a buffer from the tile's first column on, and the
+        // lane's place in load t, `cpr` chunks a row; zeros past the matrix's last row and column.
+        const uint8_t* aw = a.w + 2 * n0;
+        const uint8_t* ax = a.x + 2 * m0;
+        const uint32_t all_w = 64 * ldw - 2 * n0, all_x = 64 * ldx - 2 * m0;
+        const uint32_t last_w = KW ? (a.w_rows - 64 * (a.w_split - 1)) * ldw - 2 * n0 : 0;
+        const uint32_t last_x = KX ? (a.x_rows - 64 * (a.steps - 1)) * ldx - 2 * m0 : 0;
+        const auto size_w = [&](int k) { return k + 1 == a.w_split || k + 1 == a.steps ? last_w : all_w; };
+        const auto size_x = [&](int k) { return k + 1 == a.steps ? last_x : all_x; };
+        uint32_t sw = size_w(0), sx = size_x(0);
+        const auto place = [&](int t, int cpr, uint32_t ld, int64_t column, int64_t columns) {
+            const int r = (wave + kWaves * t) * (64 / cpr) + lane / cpr, c = (lane % cpr) ^ turn(cpr, r);
+            return column + 8 * c < columns ? r * ld + 16 * c : 0x80000000u;
+        };
         uint32_t ow[LW], ox[LX];
 #pragma unroll
         for (int t = 0; t < LW; ++t) {
+            if constexpr (KW) {
+                ow[t] = place(t, BN / 8, ldw, n0, a.N);
+                continue;
+            }
             const int r = 8 * (wave + kWaves * t) + (lane >> 3) - (GATED && t >= LW / 2 ? kRows : 0);
             ow[t] = (r < rows_w ? r : rows_w - 1) * ldw + chunk;  // rows past the end are not stored
         }
 #pragma unroll
         for (int t = 0; t < LX; ++t) {
+            if constexpr (KX) {
+                ox[t] = place(t, BM / 8, ldx, m0, a.M);
+                continue;
+            }
             const int r = 8 * (wave + kWaves * t) + (lane >> 3);
             ox[t] = (r < rows_x ? r : rows_x - 1) * ldx + chunk;
         }
-        // load t of the wave's LW + LX of step k
+        // load t of the wave's LW + LX of step k; steps and loads in order
         auto load_part = [&](int t, int k, uint8_t* to) {
-            if (t < LW)
-                to_lds(GATED && t >= LW / 2 ? bw2 : bw, ow[t < LW ? t : 0], k * kStepBytes,
-                       to + (wave + kWaves * t) * 1024);
-            else
-                to_lds(bx, ox[t < LW ? 0 : t - LW], k * kStepBytes,
-                       to + (BN / 8 + wave + kWaves * (t - LW)) * 1024);
+            if (t < LW) {
+                uint8_t* const at = to + (wave + kWaves * t) * 1024;
+                if constexpr (KW) {
+                    to_lds(buffer_of(aw, sw), ow[t < LW ? t : 0], 0, at);
+                    if (t == LW - 1) {  // here, among the products, not ahead of them
+                        aw = k + 1 == a.w_split ? a.w2 + 2 * n0 : aw + 64 * a.ldw;
+                        sw = size_w(k + 1);
+                    }
+                } else
+                    to_lds(GATED && t >= LW / 2 ? bw2 : bw, ow[t < LW ? t : 0], k * kStepBytes, at);
+            } else {
+                uint8_t* const at = to + (BN / 8 + wave + kWaves * (t - LW)) * 1024;
+                if constexpr (KX) {
+                    to_lds(buffer_of(ax, sx), ox[t < LW ? 0 : t - LW], 0, at);
+                    if (t == LW + LX - 1) ax += 64 * a.ldx, sx = size_x(k + 1);
+                } else
+                    to_lds(bx, ox[t < LW ? 0 : t - LW], k * kStepBytes, at);
+            }
         };
         auto load = [&](int k, uint8_t* to) {
 #pragma unroll
@@ -226,7 +290,7 @@ struct GemmTile {
         };
         // the last step, where its rows end inside: zeros past their end
         auto load_any = [&](int k, uint8_t* to) {
-            if (!E::kScaled && a.tail < kStepBytes && k == a.steps - 1) {
+            if (!E::kScaled && !KW && a.tail < kStepBytes && k == a.steps - 1) {
                 const bool cut = chunk >= a.tail;
 #pragma unroll
                 for (int t = 0; t < LW; ++t) ow[t] = cut ? 0x80000000u : ow[t];  // past the buffer
@@ -284,16 +348,26 @@ struct GemmTile {
 #pragma unroll
         for (int q = 0; q < kPhases; ++q) at[q] = in * 128 + (((8 / kPhases * q + lane / kTile) ^ fkey) << 4);
 
+        // The lane's place in the tile's columns along k: row lane / 16 * 8 + lane % 16 / 4, four columns of the
+        // wave's first 16; those of fragment i lie 2 i chunks on, bits 5 to 7 of the address, which rows leave free.
+        const auto corner = [&](int column, int cpr) {
+            const int r = 8 * (lane >> 4) + ((lane & 15) >> 2), c = (column >> 3) + ((lane & 3) >> 1);
+            return r * 16 * cpr + ((c ^ turn(cpr, r)) << 4) + ((lane & 1) << 3);
+        };
+        const int tw = KW ? corner(wn * PN, BN / 8) : 0, tx = KX ? corner(wm * PM, BM / 8) : 0;
+
         // Fragments are read a phase ahead, and the last phase of a step is multiplied behind the barrier that
         // ends its reads, so the matrix units have work while the next step's first fragments come.
         v4i rw[2][TN], rx[2][TM];
         auto read = [&](const uint8_t* from, int q, int buffer) {
 #pragma unroll
             for (int j = 0; j < TM; ++j)
-                rx[buffer][j] = *reinterpret_cast<const v4i*>(from + (BN + wm * PM + j * kTile) * 128 + at[q]);
+                rx[buffer][j] = KX ? turned(from + BN * 128 + (tx ^ j << 5) + q * 64 * BM, 8 * BM)
+                                   : *reinterpret_cast<const v4i*>(from + (BN + wm * PM + j * kTile) * 128 + at[q]);
 #pragma unroll
             for (int i = 0; i < TN; ++i)
-                rw[buffer][i] = *reinterpret_cast<const v4i*>(from + lds_row(i, wn) * 128 + at[q]);
+                rw[buffer][i] = KW ? turned(from + (tw ^ i << 5) + q * 64 * BN, 8 * BN)
+                                   : *reinterpret_cast<const v4i*>(from + lds_row(i, wn) * 128 + at[q]);
             __builtin_amdgcn_sched_barrier(0);  // before the products that do not need them
         };
         float fsw[TN], fsx[TM];
@@ -404,9 +478,9 @@ __device__ __forceinline__ void store4(uint16_t* p, int64_t left, float a, float
 }
 
 // The product itself, to out [M] rows of ldo elements.
-template <class E, int PN, int PM, int WN, int WM, int NS, typename TO>
+template <class E, int PN, int PM, int WN, int WM, int NS, typename TO, bool KW = false, bool KX = false>
 __global__ __launch_bounds__(64 * WN * WM) void gemm_nt_kernel(GemmArgs a, TO* __restrict__ out, int64_t ldo) {
-    using Tile = GemmTile<E, PN, PM, WN, WM, NS, false>;
+    using Tile = GemmTile<E, PN, PM, WN, WM, NS, false, KW, KX>;
     extern __shared__ __align__(16) uint8_t gemm_lds[];
     int tm, tn;
     tile_of(a.tiles_m, a.tiles_n, tm, tn);
@@ -415,8 +489,12 @@ __global__ __launch_bounds__(64 * WN * WM) void gemm_nt_kernel(GemmArgs a, TO* _
     t.run(a, n0, m0, gemm_lds);
 #pragma unroll
     for (int j = 0; j < Tile::TM; ++j) {
-        const int64_t m = m0 + t.row(j);
+        int64_t m = m0 + t.row(j);
         if (m >= a.M) continue;
+        if (KX && m >= a.gap_at) {
+            m -= a.gap;
+            if (m < a.gap_at) continue;
+        }
         TO* p = out + m * ldo;
 #pragma unroll
         for (int i = 0; i < Tile::TN; ++i)

@@ -54,7 +54,7 @@ REFUSED = [
     ("spingtp_gated_backward", GATED_BWD, [dict(act=2), dict(save=0), dict(save=2), dict(ldgh=3), dict(ldx=7), dict(ldw=7),
                                            dict(ldgx=7), dict(g=None), dict(u=P + 8), dict(x=None), dict(w_gate=None),
                                            dict(grad_h=None), dict(workspace=None), dict(workspace_bytes=64),
-                                           dict(x_scales=P + 1), dict(M=64 * 65535 + 1)]),
+                                           dict(x_scales=P + 1), dict(w_gate=P + 2), dict(x=P + 2)]),
 ]
 
 
@@ -81,7 +81,7 @@ def test_nothing_to_do(name, good, none):
 @pytest.mark.parametrize("name,sizes", [("spingtp_rms_norm_backward_workspace_size", (2, 0)),
                                         ("spingtp_gated_forward_workspace_size", (65, 8, 4, 7, 8, 0)),
                                         ("spingtp_gated_forward8_workspace_size", (0, 0, 4, 1)),
-                                        ("spingtp_gated_backward_workspace_size", (2, 8, 0))])
+                                        ("spingtp_gated_backward_workspace_size", (2, 8, 0, 8, 8, 0))])
 def test_workspace_sizes(name, sizes):
     n = ctypes.c_size_t(0)
     fn = getattr(_lib.lib(), name)
@@ -104,3 +104,9 @@ def test_workspace_grows_with_the_operands():
     assert fn(32, 64, 100, 1, ctypes.byref(n)) == OK and n.value == 4 * 32 * 100
     assert fn(65, 64, 100, 1, ctypes.byref(n)) == OK and n.value == 0
     assert fn(1, 64, 100, 0, ctypes.byref(n)) == OK and n.value == 0
+    fn = _lib.lib().spingtp_gated_backward_workspace_size
+    assert fn(100, 64, 100, 64, 72, 0, ctypes.byref(n)) == OK and n.value == 2 * 100 * 256  # g and u alone
+    assert fn(100, 64, 100, 65, 72, 0, ctypes.byref(n)) == OK and n.value == 2 * 100 * (256 + 64)
+    assert fn(100, 64, 100, 0, 72, 1, ctypes.byref(n)) == OK and n.value == 2 * 100 * (256 + 64)
+    assert fn(100, 63, 100, 63, 63, 0, ctypes.byref(n)) == OK and n.value == 2 * (100 * (256 + 64) + 2 * 100 * 64)
+    assert fn(100, 64, 100, 63, 64, 0, ctypes.byref(n)) == INVALID

@@ -480,6 +480,21 @@ def test_gated_backward_against_differences(act):
         assert abs(float(terms.sum()) - along) <= 4 * 2.0**-9 * float(terms.abs().sum())
 
 
+@pytest.mark.parametrize("M, K, F", [(70, 72, 100), (65, 24, 65), (257, 264, 200), (1, 8, 1), (129, 65, 64)])
+def test_gated_backward_reads_nothing_beside_its_rows(M, K, F):
+    def amid(t):  # the same numbers with NaN behind every row and below the last
+        wide = torch.full((t.shape[0] + 70, (t.shape[1] + 23) // 8 * 8), NAN, dtype=BF16, device="cuda")
+        wide[: t.shape[0], : t.shape[1]] = t
+        return wide[: t.shape[0], : t.shape[1]]
+
+    x, wg, wu = rand((M, K), BF16, 1), rand((F, K), BF16, 2, K**-0.5), rand((F, K), BF16, 3, K**-0.5)
+    dh = rand((M, F), BF16, 4)
+    want = sg.gated_backward(dh, sg.gated(x, wg, wu, save="same")[1], wg, wu)
+    far = [amid(t) for t in (x, wg, wu)]
+    got = sg.gated_backward(amid(dh), sg.gated(*far, save="same")[1], far[1], far[2])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_gated_of_no_rows():
     wg, wu = rand((30, 20), BF16, 1), rand((30, 20), BF16, 2)
     for save in ("same", "8bit"):
