@@ -692,16 +692,17 @@ spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
  */
 typedef enum { SPINGTP_SILU = 0, SPINGTP_GELU = 1 } spingtp_activation; /* gelu: x Phi(x), not its tanh form */
 typedef enum { SPINGTP_SAVE_NONE = 0, SPINGTP_SAVE_BF16 = 1, SPINGTP_SAVE_BLOCK8 = 2 } spingtp_save;
+/* These and spingtp_dtype are passed as int below, so that a value that is none of theirs can be refused. */
 
 /* x [R][D] to 8-bit blocks: along its rows (values, scales), and / or as the transposed matrix [D][R]
  * (t_values, t_scales), the operand of a product that sums over the rows.  Either pair may be NULL.
  * With t_values D <= 128 * 65535. */
-spingtp_status spingtp_pack8(spingtp_dtype dtype, const void* x, int64_t ldx, void* values, void* scales,
+spingtp_status spingtp_pack8(int dtype, const void* x, int64_t ldx, void* values, void* scales,
                              void* t_values, void* t_scales, int64_t R, int64_t D, void* stream);
 
 /* x [R][D] = values * scales, in fp32 (exact) or rounded to bf16 (exact as well: 4 significant bits,
  * unless below bf16's subnormals). */
-spingtp_status spingtp_unpack8(const void* values, const void* scales, spingtp_dtype dtype, void* x, int64_t ldx,
+spingtp_status spingtp_unpack8(const void* values, const void* scales, int dtype, void* x, int64_t ldx,
                                int64_t R, int64_t D, void* stream);
 
 /*
@@ -712,7 +713,7 @@ spingtp_status spingtp_unpack8(const void* values, const void* scales, spingtp_d
  * h is needed with a residual, optional without; rstd [R] is optional (the backward pass reads both).
  * gain [D] is fp32; eps >= 0.
  */
-spingtp_status spingtp_rms_norm(spingtp_dtype dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+spingtp_status spingtp_rms_norm(int dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr,
                                 const float* gain, float eps, void* h, int64_t ldh, void* y, int64_t ldy, void* values,
                                 void* scales, float* rstd, int64_t R, int64_t D, void* stream);
 
@@ -723,7 +724,7 @@ spingtp_status spingtp_rms_norm(spingtp_dtype dtype, const void* x, int64_t ldx,
  * grad_h, the gradient that reaches h directly, and grad_gain may be NULL.  An 8-bit y passes its
  * gradient through the rounding as it is.  workspace: the size below, needed with grad_gain only.
  */
-spingtp_status spingtp_rms_norm_backward(spingtp_dtype dtype, const void* grad_y, int64_t ldg, const void* h,
+spingtp_status spingtp_rms_norm_backward(int dtype, const void* grad_y, int64_t ldg, const void* h,
                                          int64_t ldh, const float* rstd, const float* gain, const void* grad_h,
                                          int64_t ldgh, void* grad_x, int64_t ldx, float* grad_gain, void* workspace,
                                          size_t workspace_bytes, int64_t R, int64_t D, void* stream);
@@ -733,7 +734,7 @@ spingtp_status spingtp_rms_norm_backward_workspace_size(int64_t R, int64_t D, si
  * such a product are two more of them: grad_a = grad_c b sums over N, grad_b = grad_c^T a over M, with
  * grad_c packed along its rows and along its columns, and b and a along theirs (spingtp_pack8). */
 spingtp_status spingtp_matmul8(const void* a_values, const void* a_scales, const void* b_values, const void* b_scales,
-                               spingtp_dtype dtype, void* c, int64_t ldc, int64_t M, int64_t N, int64_t K,
+                               int dtype, void* c, int64_t ldc, int64_t M, int64_t N, int64_t K,
                                void* stream);
 
 /*
@@ -743,17 +744,17 @@ spingtp_status spingtp_matmul8(const void* a_values, const void* a_scales, const
  * blocks (g, g_scales, u, u_scales).  workspace: the size below, 0 where K, ldx and ldw are multiples
  * of 8 (M <= 64: where nothing is kept in 8 bits).
  */
-spingtp_status spingtp_gated_forward(spingtp_activation act, const void* x, int64_t ldx, const void* w_gate,
-                                     const void* w_up, int64_t ldw, void* h, int64_t ldh, spingtp_save save, void* g,
+spingtp_status spingtp_gated_forward(int act, const void* x, int64_t ldx, const void* w_gate,
+                                     const void* w_up, int64_t ldw, void* h, int64_t ldh, int save, void* g,
                                      void* g_scales, void* u, void* u_scales, void* workspace, size_t workspace_bytes,
                                      int64_t M, int64_t K, int64_t F, void* stream);
 spingtp_status spingtp_gated_forward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw,
-                                                    spingtp_save save, size_t* size);
+                                                    int save, size_t* size);
 
 /* The same from 8-bit blocks, for inference: h in bf16 (h_scales NULL) or in 8-bit blocks (h, h_scales),
  * as the next product takes it.  workspace: the size below (out8: whether h_scales is given), 0 for M
  * above 64 or a bf16 h. */
-spingtp_status spingtp_gated_forward8(spingtp_activation act, const void* x, const void* x_scales, const void* w_gate,
+spingtp_status spingtp_gated_forward8(int act, const void* x, const void* x_scales, const void* w_gate,
                                       const void* w_gate_scales, const void* w_up, const void* w_up_scales, void* h,
                                       int64_t ldh, void* h_scales, void* workspace, size_t workspace_bytes, int64_t M,
                                       int64_t K, int64_t F, void* stream);
@@ -768,7 +769,7 @@ spingtp_status spingtp_gated_forward8_workspace_size(int64_t M, int64_t K, int64
  * workspace: the size below (x8: whether x is 8-bit; ldx is then not used): 4 bytes for each element of g, and
  * copies of x and the weights only where x is 8-bit or their rows do not start and end on 16 bytes.
  */
-spingtp_status spingtp_gated_backward(spingtp_activation act, const void* grad_h, int64_t ldgh, spingtp_save save,
+spingtp_status spingtp_gated_backward(int act, const void* grad_h, int64_t ldgh, int save,
                                       const void* g, const void* g_scales, const void* u, const void* u_scales,
                                       const void* x, int64_t ldx, const void* x_scales, const void* w_gate,
                                       const void* w_up, int64_t ldw, void* grad_x, int64_t ldgx, void* grad_w,

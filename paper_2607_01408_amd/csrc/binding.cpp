@@ -327,8 +327,8 @@ PyObject* gated(Args a) {
     const int64_t M = x.rows, K = x.columns;
     const auto w = weights(a[1], a[2], x, -1, K);
     const int64_t F = w.first.rows;
-    const auto act = static_cast<spingtp_activation>(integer(a[3]));
-    const auto save = static_cast<spingtp_save>(integer(a[4]));
+    const auto act = integer(a[3]);
+    const auto save = integer(a[4]);
     void* stream = stream_of(a[5]);
     const at::Tensor h = empty({M, F}, at::kBFloat16, *x.t);
     at::Tensor g, u;
@@ -361,7 +361,7 @@ PyObject* gated8(Args a) {
     if (x.t->device() != g.t->device() || x.t->device() != u.t->device())
         throw Refused("x and the weights must be on one device");
     const int64_t M = integer(a[6]), K = integer(a[7]), F = integer(a[8]);
-    const auto act = static_cast<spingtp_activation>(integer(a[9]));
+    const auto act = integer(a[9]);
     const bool out8 = truth(a[10]);
     at::Tensor h, ws;
     NewBlock h8;
@@ -385,7 +385,7 @@ PyObject* gated_backward(Args a) {
     const Matrix dh = matrix(a[0], "grad_h");
     need_bf16(dh, "grad_h");
     const int64_t M = dh.rows, F = dh.columns;
-    const auto save = static_cast<spingtp_save>(integer(a[1]));
+    const auto save = integer(a[1]);
     const auto w = weights(a[5], a[6], dh, F, -1);
     const int64_t K = w.first.columns;
     Matrix kept[3];
@@ -413,7 +413,7 @@ PyObject* gated_backward(Args a) {
     done(lib.gated_backward_workspace_size(M, K, F, kept[0].ld, w.first.ld, save == SPINGTP_SAVE_BLOCK8, &bytes),
          "spingtp_gated_backward_workspace_size");
     const at::Tensor ws = workspace(bytes, *dh.t);
-    done(lib.gated_backward(static_cast<spingtp_activation>(integer(a[7])), dh.p, dh.ld, save, kept[1].p, kept8[1].scales,
+    done(lib.gated_backward(integer(a[7]), dh.p, dh.ld, save, kept[1].p, kept8[1].scales,
                             kept[2].p, kept8[2].scales, kept[0].p, kept[0].ld, kept8[0].scales, w.first.p, w.second.p,
                             w.first.ld, address(dx), K, address(dw), address(ws), bytes, M, K, F, stream_of(a[10])),
          "spingtp_gated_backward");

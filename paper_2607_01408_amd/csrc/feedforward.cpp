@@ -26,7 +26,7 @@ const uint8_t* bytes(const void* p) { return static_cast<const uint8_t*>(p); }
 
 }  // namespace
 
-extern "C" spingtp_status spingtp_pack8(spingtp_dtype dtype, const void* x, int64_t ldx, void* values, void* scales,
+extern "C" spingtp_status spingtp_pack8(int dtype, const void* x, int64_t ldx, void* values, void* scales,
                                         void* t_values, void* t_scales, int64_t R, int64_t D, void* stream) {
     if (!dtype_ok(dtype) || !size_ok(R, 0) || !size_ok(D, 1) || ldx < D || !matrix_ok(R, ldx) || !matrix_ok(R, D + 511))
         return SPINGTP_ERR_INVALID_ARG;
@@ -41,7 +41,7 @@ extern "C" spingtp_status spingtp_pack8(spingtp_dtype dtype, const void* x, int6
                                     stream_of(stream)));
 }
 
-extern "C" spingtp_status spingtp_unpack8(const void* values, const void* scales, spingtp_dtype dtype, void* x,
+extern "C" spingtp_status spingtp_unpack8(const void* values, const void* scales, int dtype, void* x,
                                           int64_t ldx, int64_t R, int64_t D, void* stream) {
     if (!dtype_ok(dtype) || !size_ok(R, 0) || !size_ok(D, 1) || ldx < D || !matrix_ok(R, ldx) || !matrix_ok(R, D + 511))
         return SPINGTP_ERR_INVALID_ARG;
@@ -50,7 +50,7 @@ extern "C" spingtp_status spingtp_unpack8(const void* values, const void* scales
     return of(spingtp::launch_unpack8(dtype, bytes(values), bytes(scales), x, ldx, R, D, stream_of(stream)));
 }
 
-extern "C" spingtp_status spingtp_rms_norm(spingtp_dtype dtype, const void* x, int64_t ldx, const void* residual,
+extern "C" spingtp_status spingtp_rms_norm(int dtype, const void* x, int64_t ldx, const void* residual,
                                            int64_t ldr, const float* gain, float eps, void* h, int64_t ldh, void* y,
                                            int64_t ldy, void* values, void* scales, float* rstd, int64_t R, int64_t D,
                                            void* stream) {
@@ -78,7 +78,7 @@ extern "C" spingtp_status spingtp_rms_norm_backward_workspace_size(int64_t R, in
     return SPINGTP_OK;
 }
 
-extern "C" spingtp_status spingtp_rms_norm_backward(spingtp_dtype dtype, const void* grad_y, int64_t ldg, const void* h,
+extern "C" spingtp_status spingtp_rms_norm_backward(int dtype, const void* grad_y, int64_t ldg, const void* h,
                                                     int64_t ldh, const float* rstd, const float* gain,
                                                     const void* grad_h, int64_t ldgh, void* grad_x, int64_t ldx,
                                                     float* grad_gain, void* workspace, size_t workspace_bytes,
@@ -100,7 +100,7 @@ extern "C" spingtp_status spingtp_rms_norm_backward(spingtp_dtype dtype, const v
 }
 
 extern "C" spingtp_status spingtp_matmul8(const void* a_values, const void* a_scales, const void* b_values,
-                                          const void* b_scales, spingtp_dtype dtype, void* c, int64_t ldc, int64_t M,
+                                          const void* b_scales, int dtype, void* c, int64_t ldc, int64_t M,
                                           int64_t N, int64_t K, void* stream) {
     if (!dtype_ok(dtype) || !size_ok(M, 0) || !size_ok(N, 0) || !size_ok(K, 1) || K > int64_t{65535} * 128 || ldc < N || ldc < 1 ||
         !matrix_ok(M, ldc) || !matrix_ok(M, K + 511) || !matrix_ok(N, K + 511))
@@ -124,15 +124,15 @@ bool save_ok(int s) { return s == SPINGTP_SAVE_NONE || s == SPINGTP_SAVE_BF16 ||
 }  // namespace
 
 extern "C" spingtp_status spingtp_gated_forward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw,
-                                                               spingtp_save save, size_t* size) {
+                                                               int save, size_t* size) {
     if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || ldx < K || ldw < K || !save_ok(save))
         return SPINGTP_ERR_INVALID_ARG;
     *size = spingtp::gated_workspace(M, K, F, ldx, ldw, save);
     return SPINGTP_OK;
 }
 
-extern "C" spingtp_status spingtp_gated_forward(spingtp_activation act, const void* x, int64_t ldx, const void* w_gate,
-                                                const void* w_up, int64_t ldw, void* h, int64_t ldh, spingtp_save save,
+extern "C" spingtp_status spingtp_gated_forward(int act, const void* x, int64_t ldx, const void* w_gate,
+                                                const void* w_up, int64_t ldw, void* h, int64_t ldh, int save,
                                                 void* g, void* g_scales, void* u, void* u_scales, void* workspace,
                                                 size_t workspace_bytes, int64_t M, int64_t K, int64_t F, void* stream) {
     size_t need = 0;
@@ -172,7 +172,7 @@ extern "C" spingtp_status spingtp_gated_forward8_workspace_size(int64_t M, int64
     return SPINGTP_OK;
 }
 
-extern "C" spingtp_status spingtp_gated_forward8(spingtp_activation act, const void* x, const void* x_scales,
+extern "C" spingtp_status spingtp_gated_forward8(int act, const void* x, const void* x_scales,
                                                  const void* w_gate, const void* w_gate_scales, const void* w_up,
                                                  const void* w_up_scales, void* h, int64_t ldh, void* h_scales,
                                                  void* workspace, size_t workspace_bytes, int64_t M, int64_t K,
@@ -212,8 +212,8 @@ extern "C" spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64
     return SPINGTP_OK;
 }
 
-extern "C" spingtp_status spingtp_gated_backward(spingtp_activation act, const void* grad_h, int64_t ldgh,
-                                                 spingtp_save save, const void* g, const void* g_scales, const void* u,
+extern "C" spingtp_status spingtp_gated_backward(int act, const void* grad_h, int64_t ldgh,
+                                                 int save, const void* g, const void* g_scales, const void* u,
                                                  const void* u_scales, const void* x, int64_t ldx, const void* x_scales,
                                                  const void* w_gate, const void* w_up, int64_t ldw, void* grad_x,
                                                  int64_t ldgx, void* grad_w, void* workspace, size_t workspace_bytes,
