@@ -119,33 +119,33 @@ __device__ __forceinline__ void arrived_and_read() {
 constexpr int64_t kMostRowBytes = (int64_t{1} << 23);
 
 // Which tile a product takes (64, 128 or 256 rows of x, and as many of w or their like): the one of least
-// estimated time.  A tile's time is a part for the first 256 tiles (one for each CU), its share of CUs
-// included, and a part for each 256 more; smaller tiles lie several to a CU and overlap, so theirs is nearly
-// proportional to their number, but they read more for each product.  Units: about a microsecond for 2,048
-// terms.  Measured (us, 64 / 128 / 256):
-//   8 bits, 1,024^2 11 / 20 / 45, 2,048^2 27 / 23 / 46, 2,048 x 4,096 51 / 38 / 50, 4,096^2 97 / 71 / 78,
-//     4,096 x 8,192 187 / 130 / 121;
-//   bf16 (with what else the gradient does), 1,024^2 27 / 38 / 61, 2,048^2 46 / 41 / 62, 4,096 x 2,048
-//     77 / 52 / 66, 4,096^2 126 / 85 / 80;
-//   gated (rows of x x outputs), 512 x 1,024 17 / 26 / 42, 2,048 x 1,024 28 / 28 / 43, 2,048^2 38 / 33 / 45,
-//     4,096 x 1,280 56 / 55 / 45, 4,096 x 2,560 93 / 91 / 94, 4,096^2 134 / 126 / 109.
+// estimated time.  A tile's time is a part for what the CUs take at once, its share of them included, and a part
+// for each further lot; small tiles lie two to a CU, but they read more for each product.  Units: about a
+// microsecond for 2,048 terms.  Measured (us, 64 / 128 / 256):
+//   8 bits, 1,024^2 11 / 20 / 45, 2,048^2 28 / 24 / 48, 2,500^2 45 / 33 / 48, 3,000^2 55 / 47 / 50,
+//     4,096^2 91 / 66 / 75, 6,000^2 190 / 131 / 153, 4,096 x 8,192 187 / 130 / 121;
+//   bf16 (with the gradient's elementwise part), 1,024^2 19 / 32 / 55, 2,048^2 42 / 35 / 58, 4,096 x 2,048
+//     73 / 49 / 62, 3,000^2 81 / 71 / 57, 4,096^2 121 / 83 / 72;
+//   gated (rows of x x outputs), 512 x 1,024 17 / 27 / 42, 2,048 x 1,024 28 / 28 / 43, 2,048^2 37 / 33 / 45,
+//     3,000 x 1,500 57 / 58 / 47, 4,096 x 2,560 91 / 87 / 92, 4,096^2 134 / 126 / 109.
 struct TileCost {
-    double first, share, more;  // first 256 tiles: first + share (their number / 256); each 256 more: more
+    int at_once;               // workgroups, those that share a CU included
+    double first, share, more;  // up to that many tiles: first + share (their part of it); each further lot: more
 };
 struct TileCosts {
     TileCost of64, of128, of256;
 };
 inline double tile_time(const TileCost& c, int64_t tiles) {
-    const int64_t full = (tiles - 1) / 256;
-    return c.more * static_cast<double>(full) + c.first + c.share * static_cast<double>(tiles - 256 * full) / 256;
+    const int64_t full = (tiles - 1) / c.at_once;
+    return c.more * static_cast<double>(full) + c.first + c.share * static_cast<double>(tiles - c.at_once * full) / c.at_once;
 }
 inline int pick_tile(const TileCosts& c, int64_t t64, int64_t t128, int64_t t256) {
     const double a = tile_time(c.of64, t64), b = tile_time(c.of128, t128), d = tile_time(c.of256, t256);
     return a <= b && a <= d ? 64 : (b <= d ? 128 : 256);
 }
-constexpr TileCosts kPlain8 = {{10, 1, 6}, {18, 5, 15}, {33, 44, 44}};
-constexpr TileCosts kPlain16 = {{10, 1, 6}, {20, 3, 13}, {40, 15, 55}};
-constexpr TileCosts kGated = {{16, 11, 17}, {25, 8, 33}, {40, 15, 55}};
+constexpr TileCosts kPlain8 = {{512, 5, 11.5, 11.5}, {512, 12, 24, 28}, {256, 38, 34, 46}};
+constexpr TileCosts kPlain16 = {{512, 6, 14, 14}, {512, 23, 20, 36}, {256, 48, 16, 56}};
+constexpr TileCosts kGated = {{256, 16, 11, 17}, {256, 25, 8, 33}, {256, 40, 15, 55}};
 
 // The tile of this workgroup.  Neighbouring workgroups go to the 8 chiplets in turn: each chiplet
 // takes a run of tiles, 8 tiles of x by as many of w, so that its L2 serves both operands.
