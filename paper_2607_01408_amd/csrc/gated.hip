@@ -67,44 +67,55 @@ struct GatedOut {
     int64_t pitch, spitch;  // of the 8-bit rows
 };
 
-// A tile's outputs go through LDS, so that a row's 128 columns leave as whole lines, 16 bytes a lane.
+// A tile's outputs go through LDS, so that a row's columns leave as whole lines, 16 bytes a lane.
 // `value(i, j, r)` is column column(i, r / 4) + r % 4 of row row(j).
 constexpr int kPad = 16;  // bytes of an LDS row past its columns: rows start in different banks
 
-template <class Tile, class V>
-__device__ __forceinline__ void stage_bf16(const Tile& t, uint8_t* lds, const V& value) {
-    constexpr int PITCH = 2 * kBlock8 + kPad;
-#pragma unroll
-    for (int j = 0; j < Tile::TM; ++j)
-#pragma unroll
-        for (int i = 0; i < Tile::TN / 2; ++i)
-#pragma unroll
-            for (int r = 0; r < Tile::kQuads; ++r)
-                *reinterpret_cast<uint2*>(lds + t.row(j) * PITCH + 2 * t.column(i, r)) =
-                    make_uint2(bf16_pair(value(i, j, 4 * r), value(i, j, 4 * r + 1)),
-                               bf16_pair(value(i, j, 4 * r + 2), value(i, j, 4 * r + 3)));
-}
+// bf16: each wave's own PM rows of PN / 2 columns, in its own place, without barriers.
 template <class Tile>
-__device__ __forceinline__ void send_bf16(const uint8_t* lds, const GemmArgs& a, int64_t n0, int64_t m0, void* out,
-                                          int64_t ldo) {
-    constexpr int PITCH = 2 * kBlock8 + kPad;
-    const int l = threadIdx.x & 15;
-    const int64_t left = a.N - n0 - 8 * l;
-    const int rows = a.M - m0 < Tile::BM ? static_cast<int>(a.M - m0) : Tile::BM;
-    uint16_t* p = static_cast<uint16_t*>(out) + m0 * ldo + n0 + 8 * l;
-    for (int r = threadIdx.x >> 4; r < rows; r += Tile::kThreads / 16) {
-        const uint4 v = *reinterpret_cast<const uint4*>(lds + r * PITCH + 16 * l);
-        uint16_t* to = p + r * ldo;
-        if (left >= 8) {
-            *reinterpret_cast<u4u*>(to) = u4u{v.x, v.y, v.z, v.w};
-        } else {
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+struct WaveOut {
+    static constexpr int kColumns = Tile::kRows / Tile::kWavesN, kRows = Tile::TM * Tile::kTile;
+    static constexpr int kPitch = 2 * kColumns + kPad, kBytes = kRows * kPitch;
+    static constexpr int kLanes = kColumns / 8;  // of a row
+
+    template <class V>
+    static __device__ __forceinline__ void stage(const Tile& t, uint8_t* mine, const V& value) {
+        const int row = t.wm * kRows, column = t.wn * kColumns;
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                if (q < left) to[q] = static_cast<uint16_t>(w[q / 2] >> (16 * (q & 1)));
+        for (int j = 0; j < Tile::TM; ++j)
+#pragma unroll
+            for (int i = 0; i < Tile::TN / 2; ++i)
+#pragma unroll
+                for (int r = 0; r < Tile::kQuads; ++r)
+                    *reinterpret_cast<uint2*>(mine + (t.row(j) - row) * kPitch + 2 * (t.column(i, r) - column)) =
+                        make_uint2(bf16_pair(value(i, j, 4 * r), value(i, j, 4 * r + 1)),
+                                   bf16_pair(value(i, j, 4 * r + 2), value(i, j, 4 * r + 3)));
+    }
+    static __device__ __forceinline__ void send(const Tile& t, const uint8_t* mine, const GemmArgs& a, int64_t n0,
+                                                int64_t m0, void* out, int64_t ldo) {
+        constexpr int kAtOnce = 64 / kLanes;
+        const int l = t.lane % kLanes, r0 = t.lane / kLanes;
+        const int64_t left = a.N - n0 - t.wn * kColumns - 8 * l, m = m0 + t.wm * kRows + r0, rows = a.M - m;
+        uint16_t* p = static_cast<uint16_t*>(out) + m * ldo + n0 + t.wn * kColumns + 8 * l;
+        uint4 v[kRows / kAtOnce];
+#pragma unroll
+        for (int q = 0; q < kRows / kAtOnce; ++q)
+            v[q] = *reinterpret_cast<const uint4*>(mine + (r0 + q * kAtOnce) * kPitch + 16 * l);
+#pragma unroll
+        for (int q = 0; q < kRows / kAtOnce; ++q) {
+            uint16_t* to = p + q * kAtOnce * ldo;
+            if (q * kAtOnce >= rows) continue;
+            if (left >= 8) {
+                *reinterpret_cast<u4u*>(to) = u4u{v[q].x, v[q].y, v[q].z, v[q].w};
+            } else {
+                const uint32_t w[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+#pragma unroll
+                for (int b = 0; b < 8; ++b)
+                    if (b < left) to[b] = static_cast<uint16_t>(w[b / 2] >> (16 * (b & 1)));
+            }
         }
     }
-}
+};
 
 // The rows as 8-bit blocks: first each wave's largest magnitudes (tops [WN][BM]), then, when all are there,
 // the values.
@@ -164,8 +175,15 @@ __device__ __forceinline__ void send_blocks(const uint8_t* lds, const GemmArgs& 
     const int l = threadIdx.x & 7;
     const int rows = a.M - m0 < Tile::BM ? static_cast<int>(a.M - m0) : Tile::BM;
     uint8_t* p = static_cast<uint8_t*>(out) + m0 * pitch + n0 + 16 * l;  // a block lies in the pitch as a whole
-    for (int r = threadIdx.x >> 3; r < rows; r += Tile::kThreads / 8)
-        *reinterpret_cast<uint4*>(p + r * pitch) = *reinterpret_cast<const uint4*>(lds + r * PITCH + 16 * l);
+    constexpr int kAtOnce = Tile::kThreads / 8;
+    const int r0 = threadIdx.x >> 3;
+    uint4 v[Tile::BM / kAtOnce];
+#pragma unroll
+    for (int q = 0; q < Tile::BM / kAtOnce; ++q)
+        v[q] = *reinterpret_cast<const uint4*>(lds + (r0 + q * kAtOnce) * PITCH + 16 * l);
+#pragma unroll
+    for (int q = 0; q < Tile::BM / kAtOnce; ++q)
+        if (r0 + q * kAtOnce < rows) *reinterpret_cast<uint4*>(p + (r0 + q * kAtOnce) * pitch) = v[q];
 }
 
 template <class E, int PN, int PM, int WN, int WM, int NS, int ACT, int SAVE, bool OUT8>
@@ -173,11 +191,11 @@ __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOu
     using Tile = GemmTile<E, PN, PM, WN, WM, NS, true>;
     static_assert(Tile::kRows == kBlock8, "a tile is one block of its rows");
     constexpr int HALF = Tile::TN / 2, BM = Tile::BM;
-    // two places for outputs in turn: one is written while the other leaves
-    constexpr int kPlace = BM * (2 * kBlock8 + kPad), kTops = 2 * WN * BM * 4;
-    static_assert(2 * kPlace + kTops <= 160 * 1024, "in LDS");
+    using Out = WaveOut<Tile>;
+    constexpr int kPlace = BM * (kBlock8 + kPad);  // of 8-bit rows
     extern __shared__ __align__(16) uint8_t gemm_lds[];
     uint8_t* const place[2] = {gemm_lds, gemm_lds + kPlace};
+    uint8_t* const mine[2] = {gemm_lds + (threadIdx.x >> 6) * 2 * Out::kBytes, gemm_lds + ((threadIdx.x >> 6) * 2 + 1) * Out::kBytes};
     float* const tops = reinterpret_cast<float*>(gemm_lds + 2 * kPlace);
     float* const tops2 = tops + WN * BM;
     int tm, tn;
@@ -198,11 +216,8 @@ __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOu
                 }
     }
     if constexpr (SAVE == kSaveBf16) {
-        stage_bf16(t, place[0], g);
-        stage_bf16(t, place[1], u);
-        __syncthreads();
-        send_bf16<Tile>(place[0], a, n0, m0, o.g, a.N);
-        send_bf16<Tile>(place[1], a, n0, m0, o.u, a.N);
+        Out::stage(t, mine[0], g);
+        Out::stage(t, mine[1], u);
     }
     if constexpr (SAVE == kSave8) {
         block_tops(t, tops, g);
@@ -214,14 +229,26 @@ __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOu
         send_blocks<Tile>(place[0], a, n0, m0, o.g, o.pitch);
         send_blocks<Tile>(place[1], a, n0, m0, o.u, o.pitch);
     }
+    __builtin_amdgcn_sched_barrier(0);  // here and below: for registers
 #pragma unroll
     for (int i = 0; i < HALF; ++i)
 #pragma unroll
-        for (int j = 0; j < Tile::TM; ++j)
+        for (int j = 0; j < Tile::TM; ++j) {
 #pragma unroll
-            for (int r = 0; r < 4 * Tile::kQuads; ++r)
-                t.acc[i][j][r] = act<ACT>(t.acc[i][j][r]) * t.acc[HALF + i][j][r];
-    if constexpr (SAVE != kSaveNone) __syncthreads();  // g and u have left their places
+            for (int r = 0; r < 4 * Tile::kQuads; ++r) {
+                float h = act<ACT>(t.acc[i][j][r]) * t.acc[HALF + i][j][r];
+                asm volatile("" : "+v"(h));  // computed here, not half of it where it is used
+                t.acc[i][j][r] = h;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    if constexpr (SAVE == kSaveBf16) {
+        wave_lds_order();
+        Out::send(t, mine[0], a, n0, m0, o.g, a.N);
+        __builtin_amdgcn_sched_barrier(0);
+        Out::send(t, mine[1], a, n0, m0, o.u, a.N);
+    }
+    if constexpr (SAVE == kSave8 || (OUT8 && SAVE != kSaveNone)) __syncthreads();  // g and u have left their places
     if constexpr (OUT8) {
         block_tops(t, tops, g);
         __syncthreads();
@@ -229,9 +256,10 @@ __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOu
         __syncthreads();
         send_blocks<Tile>(place[0], a, n0, m0, o.h, o.pitch);
     } else {
-        stage_bf16(t, place[0], g);
-        __syncthreads();
-        send_bf16<Tile>(place[0], a, n0, m0, o.h, o.ldh);
+        wave_lds_order();
+        Out::stage(t, mine[0], g);
+        wave_lds_order();
+        Out::send(t, mine[0], a, n0, m0, o.h, o.ldh);
     }
 }
 
@@ -328,7 +356,9 @@ bool grid_ok(int64_t x) { return x <= (int64_t{1} << 24) - 1; }  // below 2^32 t
 // LDS of a workgroup: the operands' tiles, then the outputs'
 template <class Tile, int WN>
 constexpr int gated_lds() {
-    constexpr int out = 2 * Tile::BM * (2 * kBlock8 + kPad) + 2 * WN * Tile::BM * 4;
+    constexpr int blocks = 2 * Tile::BM * (kBlock8 + kPad) + 2 * WN * Tile::BM * 4;
+    constexpr int rows = 2 * Tile::kWaves * WaveOut<Tile>::kBytes, out = blocks > rows ? blocks : rows;
+    static_assert(out <= 160 * 1024, "in LDS");
     return out > Tile::kLds ? out : Tile::kLds;
 }
 
@@ -352,7 +382,7 @@ hipError_t gated_tiles(const GemmArgs& g, const GatedOut& o, hipStream_t stream)
     const auto tiles = [&](int64_t bm) { return ((g.M + bm - 1) / bm) * ((g.N + 127) / 128); };
     switch (pick_tile(kGated, tiles(64), tiles(128), tiles(256))) {
         case 256: return gated_launch<E, 128, 64, 2, 4, 2, ACT, SAVE, OUT8>(g, o, stream);
-        case 128: return gated_launch<E, 128, 32, 2, 4, 3, ACT, SAVE, OUT8>(g, o, stream);
+        case 128: return gated_launch<E, 64, 64, 4, 2, 3, ACT, SAVE, OUT8>(g, o, stream);
         default: return gated_launch<E, 64, 32, 4, 2, 2, ACT, SAVE, OUT8>(g, o, stream);
     }
 }

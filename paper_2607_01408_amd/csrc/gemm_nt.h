@@ -168,7 +168,7 @@ struct GemmTile {
     static constexpr int kTile = E::kTile, TN = PN / kTile, TM = PM / kTile;  // accumulators of kTile x kTile
     static constexpr int kPhases = kTile == 16 ? 2 : 4;                    // fragment reads of a step
     static constexpr int kQuads = kTile == 16 ? 1 : 4;                     // runs of four outputs in an accumulator
-    static constexpr int kWaves = WN * WM, kThreads = 64 * kWaves;
+    static constexpr int kWavesN = WN, kWaves = WN * WM, kThreads = 64 * kWaves;
     static constexpr int BN = PN * WN, BM = PM * WM;
     static constexpr int kRows = GATED ? BN / 2 : BN;  // of one matrix
     static constexpr int kStage = (BN + BM) * kStepBytes;
