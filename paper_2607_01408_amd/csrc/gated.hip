@@ -15,7 +15,7 @@
 // units; sums are fp32.
 //
 // Bound by power and by what leaves between rounds of tiles.  Measured at 8,192 x 2,048 x 8,192 (550 GFLOP a
-// product): forward 404-415 us, 475-500 with g and u kept in bf16, 490 in 8 bits; dg and du 110 us, 6.1 TB/s;
+// product): forward 404-418 us, 475-480 with g and u kept in bf16, 498 in 8 bits; dg and du 110 us, 6.1 TB/s;
 // dx 420-470 us, dW 440-460 us, 1.2-1.3 PFLOP/s.
 #include <hip/hip_runtime.h>
 
