@@ -102,8 +102,8 @@ extern "C" spingtp_status spingtp_rms_norm_backward(int dtype, const void* grad_
 extern "C" spingtp_status spingtp_matmul8(const void* a_values, const void* a_scales, const void* b_values,
                                           const void* b_scales, int dtype, void* c, int64_t ldc, int64_t M,
                                           int64_t N, int64_t K, void* stream) {
-    if (!dtype_ok(dtype) || !size_ok(M, 0) || !size_ok(N, 0) || !size_ok(K, 1) || K > int64_t{65535} * 128 || ldc < N || ldc < 1 ||
-        !matrix_ok(M, ldc) || !matrix_ok(M, K + 511) || !matrix_ok(N, K + 511))
+    if (!dtype_ok(dtype) || !size_ok(M, 0) || !size_ok(N, 0) || !size_ok(K, 1) || K > int64_t{65535} * 128 ||
+        ldc < N || ldc < 1 || !matrix_ok(M, ldc) || !matrix_ok(M, K + 511) || !matrix_ok(N, K + 511))
         return SPINGTP_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return SPINGTP_OK;
     if (bad(a_values, 16) || bad(a_scales, 4) || bad(b_values, 16) || bad(b_scales, 4) || bad(c, width(dtype)))

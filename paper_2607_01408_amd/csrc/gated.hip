@@ -195,7 +195,8 @@ __global__ __launch_bounds__(64 * WN * WM) void gated_kernel(GemmArgs a, GatedOu
     constexpr int kPlace = BM * (kBlock8 + kPad);  // of 8-bit rows
     extern __shared__ __align__(16) uint8_t gemm_lds[];
     uint8_t* const place[2] = {gemm_lds, gemm_lds + kPlace};
-    uint8_t* const mine[2] = {gemm_lds + (threadIdx.x >> 6) * 2 * Out::kBytes, gemm_lds + ((threadIdx.x >> 6) * 2 + 1) * Out::kBytes};
+    uint8_t* const own = gemm_lds + (threadIdx.x >> 6) * 2 * Out::kBytes;
+    uint8_t* const mine[2] = {own, own + Out::kBytes};
     float* const tops = reinterpret_cast<float*>(gemm_lds + 2 * kPlace);
     float* const tops2 = tops + WN * BM;
     int tm, tn;
