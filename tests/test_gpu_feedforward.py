@@ -495,6 +495,28 @@ def test_gated_backward_reads_nothing_beside_its_rows(M, K, F):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_gated_backward_past_two_to_the_31_elements():
+    M, K, F, n = 70_001, 64, 16_384, 100  # dg and du together 2.3 10^9 elements; only the last rows have a gradient
+    x, wg, wu = rand((M, K), BF16, 1), rand((F, K), BF16, 2, K**-0.5), rand((F, K), BF16, 3, K**-0.5)
+    g, u = torch.ones((M, F), dtype=BF16, device="cuda"), torch.ones((M, F), dtype=BF16, device="cuda")
+    dh = torch.zeros((M, F), dtype=BF16, device="cuda")
+    g[-n:], u[-n:], dh[-n:] = rand((n, F), BF16, 4), rand((n, F), BF16, 5), rand((n, F), BF16, 6)
+    dx, dwg, dwu = sg.gated_backward(dh, sg.GatedSaved(x, g, u, "silu", "same"), wg, wu)
+    assert bool((dx[:-n] == 0).all())
+    a, da = act64(g[-n:].double(), "silu")
+    d, u64, xs = dh[-n:].double(), u[-n:].double(), x[-n:].double()
+    dg, du = d * u64 * da, d * a
+    # as in test_gated_backward: dg and du rounded to bf16, sums in fp32, the result rounded
+    eg = dg.abs() * 2.0**-8 + (d * u64).abs() * 2.0**-20 * (1 + g[-n:].double().abs())
+    eu = du.abs() * 2.0**-8 + d.abs() * 2.0**-20 * g[-n:].double().abs()
+    for y, ref, size, err, terms in (
+            (dx[-n:], dg @ wg.double() + du @ wu.double(), dg.abs() @ wg.double().abs() + du.abs() @ wu.double().abs(),
+             eg @ wg.double().abs() + eu @ wu.double().abs(), 2 * F),
+            (dwg, dg.t() @ xs, dg.abs().t() @ xs.abs(), eg.t() @ xs.abs(), M),
+            (dwu, du.t() @ xs, du.abs().t() @ xs.abs(), eu.t() @ xs.abs(), M)):
+        within(y, ref, 2.0**-8 * ref.abs() + (terms + 128) * 2.0**-24 * size + err + 1e-38)
+
+
 def test_gated_of_no_rows():
     wg, wu = rand((30, 20), BF16, 1), rand((30, 20), BF16, 2)
     for save in ("same", "8bit"):
