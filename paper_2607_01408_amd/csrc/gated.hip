@@ -30,12 +30,14 @@
 namespace spingtp {
 namespace {
 
-// exp(x), off by about 2^-23: the hardware's 2^t of t = x log2 e, and the rounding of t put back.
+// exp(x), off by about 2^-23: the hardware's 2^t of t = x log2 e, and the rounding of t put back.  Where t is
+// infinite that rounding is no number, nor is its sum with an infinite 2^t: 2^t stands as it is.
 __device__ __forceinline__ float exp_of(float x) {
     const float t = x * 1.44269504088896f;
     const float rest = fmaf(x, 1.44269504088896f, -t) + x * 1.92596299e-8f;  // log2 e in two parts
     const float e = __builtin_amdgcn_exp2f(t);
-    return e < __builtin_inff() ? fmaf(e, rest * 0.69314718f, e) : e;
+    const float near = fmaf(e, rest * 0.69314718f, e);
+    return near == near ? near : e;
 }
 // act(g) and its derivative; the reciprocal is the hardware's, off by 2^-23
 template <int ACT>

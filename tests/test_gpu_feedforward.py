@@ -423,6 +423,42 @@ def test_gated_saturates_and_keeps_nan_in_its_row():
     assert bool(torch.isnan(g[3]).all()) and int(torch.isnan(g).sum()) == F
 
 
+def one_column(values, M):
+    """x [M, 8] and weights [2, 8] whose g is `values` in turn and whose u is 1."""
+    x = torch.zeros((M, 8), dtype=BF16, device="cuda")
+    x[:, 0] = torch.tensor(values, device="cuda").repeat(-(-M // len(values)))[:M].to(BF16)
+    x[:, 1] = 1
+    wg, wu = (torch.zeros((2, 8), dtype=BF16, device="cuda") for _ in range(2))
+    wg[:, 0] = 1
+    wu[:, 1] = 1
+    return x, wg, wu
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M", [30, 90])
+def test_gated_at_the_ends_of_the_range(M, act):
+    values = [s * v for v in (1e4, 1e15, 2e19, 1e20, 1e30, 2e38, 3.3e38) for s in (1, -1)]
+    x, wg, wu = one_column(values, M)
+    g = x[:, :1].double()
+    # far from zero: act is g or 0, its derivative 1 or 0, and every step of that is exact
+    a, da = g.clamp(min=0), (g > 0).double()
+    h, saved = sg.gated(x, wg, wu, act=act, save="same")
+    assert torch.equal(h.double(), a.expand(M, 2))
+    dh = torch.zeros((M, 2), dtype=BF16, device="cuda")
+    dh[:, 0] = 1
+    dx = sg.gated_backward(dh, saved, wg, wu)[0]
+    assert torch.equal(dx[:, 0].double(), da[:, 0]) and torch.equal(dx[:, 1].double(), a[:, 0])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M", [30, 90])
+def test_gated_keeps_an_infinity(M, act):
+    x, w, _ = one_column([INF, 2.0, 3e38], M)
+    x[:, 1] = 0
+    assert bool((sg.gated(2 * x, w, w, act=act)[0][::3] == INF).all())  # act(inf) inf
+    assert bool((sg.gated(2 * x, w, w, act=act)[0][2::3] == INF).all())
+
+
 def kept64(saved):
     if saved.save == "8bit":
         return as64(saved.x), as64(saved.g), as64(saved.u)
