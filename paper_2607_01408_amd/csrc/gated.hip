@@ -39,11 +39,31 @@ __device__ __forceinline__ float exp_of(float x) {
     const float near = fmaf(e, rest * 0.69314718f, e);
     return near == near ? near : e;
 }
-// act(g) and its derivative; the reciprocal is the hardware's, off by 2^-23
+// The normal distribution's Phi(g), and `bell` e^(-g^2 / 2): e^(a^2 / 2) Phi(-a), a = |g|, is a polynomial in
+// t = 1 / (1 + 0.35 a) times t, fitted for the least largest relative error over a up to 14.5 (beyond that Phi(-a) is
+// below fp32's range); off by 6 2^-24 and g^2 / 2 of them by the exponent's rounding.  (1 + erf cancels below zero:
+// x Phi(x) was off by 4 % at -5 and zero at -6.  The library's erfc took 10 % longer for the forward of 20,000 x 128 x
+// 512.)
+__device__ __forceinline__ float normal(float g, float& bell) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, fabsf(g), 1.f));
+    bell = exp_of(-0.5f * g * g);
+    float p = fmaf(-0.0291580297f, t, 0.144031614f);
+    p = fmaf(p, t, -0.255840391f);
+    p = fmaf(p, t, 0.159321249f);
+    p = fmaf(p, t, -0.023213394f);
+    p = fmaf(p, t, 0.105552927f);
+    p = fmaf(p, t, 0.119821183f);
+    p = fmaf(p, t, 0.139863536f);
+    p = fmaf(p, t, 0.139621302f);
+    const float below = p * t * bell;
+    return g > 0.f ? 1.f - below : below;
+}
+// act(g) and its derivative; the reciprocals are the hardware's, off by 2^-23
 template <int ACT>
 __device__ __forceinline__ float act(float g) {
     if constexpr (ACT == kSilu) return g * __builtin_amdgcn_rcpf(1.f + exp_of(-g));
-    return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+    float bell;
+    return g * normal(g, bell);
 }
 template <int ACT>
 __device__ __forceinline__ void act_grad(float g, float& a, float& d) {
@@ -52,9 +72,10 @@ __device__ __forceinline__ void act_grad(float g, float& a, float& d) {
         a = g * t;
         d = t * (1.f + g * (1.f - t));
     } else {
-        const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+        float bell;
+        const float p = normal(g, bell);
         a = g * p;
-        d = p + g * 0.39894228040143268f * exp_of(-0.5f * g * g);
+        d = p + g * 0.39894228040143268f * bell;
     }
 }
 

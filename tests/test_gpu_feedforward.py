@@ -459,6 +459,24 @@ def test_gated_keeps_an_infinity(M, act):
     assert bool((sg.gated(2 * x, w, w, act=act)[0][2::3] == INF).all())
 
 
+@pytest.mark.parametrize("M", [30, 90])
+def test_gelu_far_below_zero(M):
+    values = [-8 + i / 5 for i in range(26)]  # from -8 to -3, where 1 + erf cancels
+    x, wg, wu = one_column(values, M)
+    g = x[:, 0].double()
+    p = 0.5 * torch.special.erfc(-g / math.sqrt(2))
+    d = g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    h, saved = sg.gated(x, wg, wu, act="gelu", save="same")
+    # the argument z = -g / sqrt 2 is off by 2^-24 z, so erfc by 2 z^2 2^-24 < 2^-18 of itself, and the exponential
+    # likewise; 2^-16 with the functions' own few units
+    within(h[:, 0], g * p, (2.0**-8 + 2.0**-16) * (g * p).abs())
+    dh = torch.zeros((M, 2), dtype=BF16, device="cuda")
+    dh[:, 0] = 1
+    dx = sg.gated_backward(dh, saved, wg, wu)[0]
+    within(dx[:, 0], p + d, 2 * 2.0**-8 * (p + d).abs() + 2.0**-16 * (p + d.abs()))
+    within(dx[:, 1], g * p, (2 * 2.0**-8 + 2.0**-16) * (g * p).abs())
+
+
 def kept64(saved):
     if saved.save == "8bit":
         return as64(saved.x), as64(saved.g), as64(saved.u)
