@@ -104,6 +104,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_kernel(
 #pragma unroll
             for (int j = 0; j < 8; ++j) w[j] = w[j] * rstd * gn[j];
             if constexpr (OUT8) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) w[j] = j < n ? w[j] : 0.f;  // behind the row, whatever rstd is
                 const int e = block8_scale(block8_top(w));
                 const float inv = block8_inverse(e);
                 *reinterpret_cast<uint2*>(values + row * pitch + c) =

@@ -197,6 +197,16 @@ def test_norm_of_zeros_and_non_finite_rows(out8):
     within(y[3:], ref, ref.abs() * (2.0**-4 if out8 else 1e-5) + (0.01 if out8 else 0))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("D", [7, 100, 300, 1001, 2050, 33000])
+def test_norm_pads_with_zeros_whatever_the_row_holds(D, dtype):
+    x = rand((6, D), dtype, D)
+    x[1, D // 2], x[2, 0], x[3] = NAN, INF, 0
+    for eps in (0.0, 1e-6):
+        y, _, _ = sg.rms_norm(x, torch.ones(D, device="cuda"), eps=eps, out8=True)
+        assert bool((y.values.float()[:, D:] == 0).all())
+
+
 def test_norm_takes_strided_rows():
     big = rand((50, 700), BF16, 2)
     x, r = big[1:30, 3:404], big[20:49, 101:502]
