@@ -685,7 +685,7 @@ spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
  *
  * The 8-bit block format of a matrix [R][D]: e4m3 values [R][Dp] (Dp = D rounded up to 128; 16-byte
  * aligned; zeros from column D on, also where the caller makes them) and scales [R][Sp], one e8m0 byte
- * (2^(byte - 127)) for each row and block of 128 columns (Sp = Dp / 128 rounded up to 4; 4-byte
+ * (2^(byte - 127); 255: NaN) for each row and block of 128 columns (Sp = Dp / 128 rounded up to 4; 4-byte
  * aligned; the bytes past the last block are not used).  Element = value * scale.  The library chooses
  * the smallest power of two that brings the block's largest finite magnitude to 448 or below (at least
  * 2^-126; 1 for a block of zeros); a non-finite element becomes NaN in its own place.

@@ -34,8 +34,10 @@ __device__ __forceinline__ int block8_scale(float top) {
 }
 // 1 / scale, a power of two as well
 __device__ __forceinline__ float block8_inverse(int scale) { return __uint_as_float(static_cast<uint32_t>(254 - scale) << 23); }
+// of any e8m0 byte: 0 is 2^-127, 255 is NaN (as the products' conversion takes them)
 __device__ __forceinline__ float block8_power(uint32_t scale) {
-    return scale == 0 ? __uint_as_float(0x400000u) : __uint_as_float(scale << 23);
+    const float power = scale == 0 ? __uint_as_float(0x400000u) : __uint_as_float(scale << 23);
+    return scale == 255 ? __builtin_nanf("") : power;
 }
 
 // v / scale to e4m3 (nearest, ties to even; |v| / scale <= 448 for finite v, NaN for others), four to

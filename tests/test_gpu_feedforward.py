@@ -141,6 +141,30 @@ def test_past_two_to_the_31_elements():
     assert abs(float(rstd[R // 2]) - 2) < 1e-4
 
 
+@pytest.mark.parametrize("M", [1, 40, 100, 300])  # few rows, and the tiles
+def test_a_scale_that_is_nan(M):
+    K, N = 300, 50
+    a, b = sg.pack8(rand((M, K), F32, 1)), sg.pack8(rand((N, K), F32, 2))
+    a.scales.view(torch.uint8)[0, 0] = 255
+    for dtype in (F32, BF16):
+        y = sg.unpack8(a, dtype=dtype)
+        assert bool(torch.isnan(y[0, :128]).all()) and int(torch.isnan(y).sum()) == 128
+        assert bool(torch.isfinite(y[0, 128:]).all()) and bool(torch.isfinite(y[1:]).all())
+        c = sg.matmul8(a, b, dtype=dtype)
+        assert bool(torch.isnan(c[0]).all()) and bool(torch.isfinite(c[1:]).all())
+    x, w, dh = rand((M, K), BF16, 1), rand((N, K), BF16, 2), rand((M, N), BF16, 3)
+    _, saved = sg.gated(x, w, w, save="8bit")
+    saved.u.scales.view(torch.uint8)[0, 0] = 255
+    dx = sg.gated_backward(dh, saved, w, w)[0]
+    assert bool(torch.isnan(dx[0]).all()) and bool(torch.isfinite(dx[1:]).all())
+
+
+def test_the_smallest_scale():
+    a = sg.pack8(rand((5, 300), F32, 1))
+    a.scales.view(torch.uint8)[:] = 0
+    assert torch.equal(sg.unpack8(a, dtype=F32).double(), a.values.double()[:, :300] * 2.0**-127)
+
+
 # ------------------------------------------------------------------ norm
 
 def ref_norm(x, r, gain, eps):
