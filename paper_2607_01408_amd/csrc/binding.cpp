@@ -379,7 +379,7 @@ PyObject* gated8(Args a) {
     return out8 ? wrap(h8) : wrap(h);
 }
 
-// grad_h, save, x | (values, scales), g, u likewise, w_gate, w_up, act, need_x, need_w, stream
+// grad_h, save, x | (values, scales, columns), g, u likewise, w_gate, w_up, act, need_x, need_w, stream
 // -> (grad_x | None, grad_w [2F, K] | None)
 PyObject* gated_backward(Args a) {
     const Matrix dh = matrix(a[0], "grad_h");
@@ -394,9 +394,9 @@ PyObject* gated_backward(Args a) {
     for (int i = 0; i < 3; ++i) {
         const int64_t columns = i == 0 ? K : F;
         if (save == SPINGTP_SAVE_BLOCK8) {
-            if (!PyTuple_Check(a[2 + i]) || PyTuple_GET_SIZE(a[2 + i]) != 2) throw Refused(std::string(names[i]) + " must be a Block8");
+            if (!PyTuple_Check(a[2 + i]) || PyTuple_GET_SIZE(a[2 + i]) != 3) throw Refused(std::string(names[i]) + " must be a Block8");
             kept8[i] = block(PyTuple_GET_ITEM(a[2 + i], 0), PyTuple_GET_ITEM(a[2 + i], 1));
-            if (kept8[i].t->size(0) != M || kept8[i].t->size(1) != up(columns, 128) ||
+            if (kept8[i].t->size(0) != M || integer(PyTuple_GET_ITEM(a[2 + i], 2)) != columns ||
                 kept8[i].t->device() != dh.t->device())
                 throw Refused(std::string(names[i]) + " must be " + shape_text(M, columns) + " beside grad_h");
             kept[i].p = kept8[i].values;

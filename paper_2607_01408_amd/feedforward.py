@@ -226,7 +226,8 @@ def gated_backward(grad_h, saved, w_gate, w_up, need_x=True, need_w=True):
     keep = _choice(_SAVES, saved.save, "saved.save")
     kept = saved.x, saved.g, saved.u
     if keep == 2:
-        kept = tuple(_block(b, n) for b, n in zip(kept, ("saved.x", "saved.g", "saved.u")))
+        # with their widths: blocks of another width may have the same padded one
+        kept = tuple((*_block(b, n), b.shape[1]) for b, n in zip(kept, ("saved.x", "saved.g", "saved.u")))
     grad_x, grad_w = _run(_ops.gated_backward, grad_h, grad_h, keep, *kept, w_gate, w_up,
                           _choice(_ACTS, saved.act, "saved.act"), need_x, need_w)
     if grad_w is None:

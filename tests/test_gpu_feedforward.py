@@ -692,3 +692,14 @@ def test_refusals():
             pytest.fail(f"call {i} was not refused")
     with pytest.raises(sg.SpinGTPError):  # rows that start at an odd address
         sg.gated(rand((8, 66), BF16, 1)[:, 1:65], w, w)
+
+
+def test_saved_blocks_of_another_width_are_refused():
+    x, w, dh = rand((70, 100), BF16, 1), rand((40, 100), BF16, 2), rand((70, 40), BF16, 3)
+    _, saved = sg.gated(x, w, w, save="8bit")
+    wide = rand((40, 120), BF16, 4)  # the same padded width
+    with pytest.raises(ValueError):
+        sg.gated_backward(dh, saved, wide, wide)
+    w50, dh50 = rand((50, 100), BF16, 2), rand((70, 50), BF16, 3)
+    with pytest.raises(ValueError):
+        sg.gated_backward(dh50, saved, w50, w50)
