@@ -48,14 +48,17 @@ _current_device = torch.cuda.current_device
 def _on_stream(op):
     """``stream=``: the call and what it allocates are that stream's, as under ``torch.cuda.stream(stream)``."""
 
+    name = op.__code__.co_varnames[0]  # the first operand's, whose device the stream must be of
+
     @functools.wraps(op)
-    def call(first, *args, stream=None, **kwargs):
+    def call(*args, stream=None, **kwargs):
         if stream is None:
-            return op(first, *args, **kwargs)
+            return op(*args, **kwargs)
+        first = args[0] if args else kwargs.get(name)
         if stream.device != getattr(first, "device", stream.device):
             raise ValueError(f"the stream is of {stream.device}, the tensors are on {first.device}")
         with torch.cuda.stream(stream):
-            return op(first, *args, **kwargs)
+            return op(*args, **kwargs)
 
     return call
 

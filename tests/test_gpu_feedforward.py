@@ -644,6 +644,31 @@ def test_a_captured_chain_replays(M):
         assert torch.equal(c, want) and torch.equal(h, wh)
 
 
+def test_arguments_by_their_names():
+    x, w, gain = rand((8, 64), BF16, 1), rand((16, 64), BF16, 2), torch.ones(64, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def step(**on):
+        b = sg.pack8(x=x, transpose=False, **on)
+        y, h, rstd = sg.rms_norm(x=x, gain=gain, residual=x, eps=1e-6, out8=False, **on)
+        c = sg.matmul8(a=b, b=b, dtype=F32, out=None, **on)
+        a, saved = sg.gated(x=x, w_gate=w, w_up=w, act="gelu", save="same", out8=False, **on)
+        return (sg.unpack8(b=b, dtype=F32, out=None, **on), y, c, a,
+                *sg.rms_norm_backward(grad_y=y, h=h, rstd=rstd, gain=gain, grad_h=y, need_gain=True, **on),
+                *sg.matmul8_backward(grad_out=c, a_t=sg.pack8(x=x, transpose=True, **on),
+                                     b_t=sg.pack8(x=x, transpose=True, **on), **on),
+                *sg.gated_backward(grad_h=a, saved=saved, w_gate=w, w_up=w, need_x=True, need_w=True, **on))
+
+    here, there = step(), step(stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(here, there))
+    with pytest.raises(TypeError):
+        sg.pack8()
+    with pytest.raises(TypeError):
+        sg.gated(w_gate=w, w_up=w, stream=side)
+
+
 def test_another_stream():
     x, wg, wu = rand((300, 200), BF16, 1), rand((260, 200), BF16, 2, 0.1), rand((260, 200), BF16, 3, 0.1)
     dh, gain = rand((300, 260), BF16, 4), torch.ones(200, device="cuda")
