@@ -140,7 +140,7 @@ PyObject* check_block(Args a) {
     const at::Tensor& v = tensor(a[0], "values");
     const at::Tensor& s = tensor(a[1], "scales");
     const int64_t R = integer(a[2]), D = integer(a[3]);
-    if (R < 0 || D < 1) throw Refused("no matrix has the shape " + shape_text(R, D));
+    if (R < 0 || D < 0) throw Refused("no matrix has the shape " + shape_text(R, D));
     const int64_t pitch = up(D, 128), spitch = up(D, 512) / 128;
     if (v.scalar_type() != at::kFloat8_e4m3fn || v.dim() != 2 || v.size(0) != R || v.size(1) != pitch ||
         !v.is_contiguous() || !v.is_cuda())
@@ -205,8 +205,7 @@ spingtp_dtype dtype_of(at::ScalarType t) { return t == at::kFloat ? SPINGTP_FP32
 PyObject* pack8(Args a) {
     const Matrix x = matrix(a[0], "x");
     const int64_t how = integer(a[1]);
-    if (x.columns < 1 || (how != 0 && x.rows < 1))
-        throw Refused("no blocks in a matrix of shape " + shape_text(x.rows, x.columns));
+    if (x.columns < 1) throw Refused("no blocks in a matrix of shape " + shape_text(x.rows, x.columns));
     NewBlock rows, columns;
     if (how != 1) rows = NewBlock(x.rows, x.columns, *x.t);
     if (how != 0) columns = NewBlock(x.columns, x.rows, *x.t);
@@ -234,7 +233,8 @@ PyObject* unpack8(Args a) {
         out.p = made.data_ptr();
         out.ld = D;
     }
-    done(lib.unpack8(b.values, b.scales, dtype_of(type), out.p, out.ld, R, D, stream_of(a[6])), "spingtp_unpack8");
+    if (D > 0)  // else a transposed matrix of no rows
+        done(lib.unpack8(b.values, b.scales, dtype_of(type), out.p, out.ld, R, D, stream_of(a[6])), "spingtp_unpack8");
     return made.defined() ? wrap(made) : Py_NewRef(a[5]);
 }
 
@@ -306,8 +306,12 @@ PyObject* matmul8(Args a) {
         out.p = made.data_ptr();
         out.ld = N > 0 ? N : 1;
     }
-    done(lib.matmul8(x.values, x.scales, w.values, w.scales, dtype_of(type), out.p, out.ld, M, N, K, stream_of(a[9])),
-         "spingtp_matmul8");
+    if (K == 0)  // sums of no terms: a gradient over an empty batch
+        (made.defined() ? made : *out.t).zero_();
+    else
+        done(lib.matmul8(x.values, x.scales, w.values, w.scales, dtype_of(type), out.p, out.ld, M, N, K,
+                         stream_of(a[9])),
+             "spingtp_matmul8");
     return made.defined() ? wrap(made) : Py_NewRef(a[8]);
 }
 

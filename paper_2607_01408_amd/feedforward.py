@@ -83,7 +83,8 @@ def _choice(table, value, name):
 
 class Block8:
     """A matrix in the 8-bit block format (``spingtp.h``): ``values`` [R, Dp] float8_e4m3fn, ``scales``
-    [R, Sp] float8_e8m0fnu, ``shape`` (R, D).  Columns of ``values`` from D on must be zero."""
+    [R, Sp] float8_e8m0fnu, ``shape`` (R, D).  Columns of ``values`` from D on must be zero.  D = 0 is the transpose of a
+    matrix of no rows."""
 
     __slots__ = ("values", "scales", "shape")
 
@@ -205,7 +206,7 @@ def gated(x, w_gate, w_up, act="silu", save=None, out8=False):
         pg = _block(w_gate, "w_gate", None, K)
         F = w_gate.shape[0]
         pu = _block(w_up, "w_up", F, K)
-        if F < 1:
+        if F < 1 or K < 1:
             raise ValueError("the weights are empty")
         h = _run(_ops.gated8, x, x.values, x.scales, *pg, *pu, M, K, F, code, out8)
         return _made(h, M, F) if out8 else h, None

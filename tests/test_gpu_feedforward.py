@@ -365,6 +365,23 @@ def test_matmul8_of_nothing():
     assert tuple(sg.matmul8(none, b).shape) == (0, 5) and tuple(sg.matmul8(b, none).shape) == (5, 0)
 
 
+def test_matmul8_backward_of_no_rows():
+    x, w = torch.empty((0, 20), dtype=BF16, device="cuda"), rand((30, 20), BF16, 2)
+    a_t, b_t = sg.pack8(x, transpose=True), sg.pack8(w, transpose=True)
+    assert a_t.shape == (20, 0) and tuple(sg.unpack8(a_t).shape) == (20, 0)
+    for dtype in (F32, BF16):
+        da, db = sg.matmul8_backward(torch.empty((0, 30), dtype=dtype, device="cuda"), a_t, b_t)
+        assert tuple(da.shape) == (0, 20) and da.dtype == dtype
+        assert tuple(db.shape) == (30, 20) and db.dtype == dtype and bool((db == 0).all())
+    out = torch.full((30, 25), 7.0, device="cuda")
+    rows, cols = sg.pack8(torch.empty((0, 30), device="cuda"), transpose="both")
+    assert rows.shape == (0, 30) and cols.shape == (30, 0)
+    sg.matmul8(cols, a_t, dtype=F32, out=out[:, 2:22])
+    assert bool((out[:, 2:22] == 0).all()) and bool((out[:, :2] == 7).all()) and bool((out[:, 22:] == 7).all())
+    with pytest.raises(ValueError):
+        sg.gated(sg.pack8(x, transpose=True), a_t, a_t)
+
+
 # ------------------------------------------------------------------ gated block
 
 def act64(g, name):
