@@ -678,7 +678,9 @@ spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
  *
  * A matrix [R][D] given as (pointer, ld) has rows of D neighbouring elements, `ld` elements apart
  * (ld >= D).  Sizes are at most 2^31 - 1, matrices 2^46 elements; the products' summed axes are
- * shorter: K <= 8388480 (spingtp_matmul8), K <= 4194240 and F <= 2097120 (gated block).
+ * shorter: K <= 8388480 (spingtp_matmul8), K <= 4194240 and F <= 2097120 (gated block), and a product of
+ * [M][N] has ceil(M / 256) ceil(N / 256) <= 2^22 (gated block: [M][F] ceil(M / 256) ceil(F / 128) <= 2^22,
+ * and for the gradients [M][K] and [2F + 63][K] as a product).
  * Outputs must not overlap inputs or one another.  R = 0 (M = 0) is valid: gradients of weights are
  * then zero, everything else is empty.  Sums and statistics are fp32, outputs are rounded to nearest
  * even.

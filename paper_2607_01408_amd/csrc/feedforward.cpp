@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "internal.h"
+#include "tile_rule.h"
 
 namespace {
 
@@ -103,7 +104,8 @@ extern "C" spingtp_status spingtp_matmul8(const void* a_values, const void* a_sc
                                           const void* b_scales, int dtype, void* c, int64_t ldc, int64_t M,
                                           int64_t N, int64_t K, void* stream) {
     if (!dtype_ok(dtype) || !size_ok(M, 0) || !size_ok(N, 0) || !size_ok(K, 1) || K > int64_t{65535} * 128 ||
-        ldc < N || ldc < 1 || !matrix_ok(M, ldc) || !matrix_ok(M, K + 511) || !matrix_ok(N, K + 511))
+        ldc < N || ldc < 1 || !matrix_ok(M, ldc) || !matrix_ok(M, K + 511) || !matrix_ok(N, K + 511) ||
+        !spingtp::product_fits(M, N))
         return SPINGTP_ERR_INVALID_ARG;
     if (M == 0 || N == 0) return SPINGTP_OK;
     if (bad(a_values, 16) || bad(a_scales, 4) || bad(b_values, 16) || bad(b_scales, 4) || bad(c, width(dtype)))
@@ -117,7 +119,7 @@ namespace {
 bool gated_sizes_ok(int act, int64_t M, int64_t K, int64_t F) {
     return (act == spingtp::kSilu || act == spingtp::kGelu) && size_ok(M, 0) && size_ok(K, 1) && size_ok(F, 1) &&
            K <= int64_t{65535} * 64 && F <= int64_t{65535} * 32 && matrix_ok(M, K + 511) && matrix_ok(M, 2 * (F + 511)) &&
-           matrix_ok(F, 2 * (K + 511));
+           matrix_ok(F, 2 * (K + 511)) && spingtp::gated_fits(M, F);
 }
 bool save_ok(int s) { return s == SPINGTP_SAVE_NONE || s == SPINGTP_SAVE_BF16 || s == SPINGTP_SAVE_BLOCK8; }
 
@@ -231,6 +233,9 @@ extern "C" spingtp_status spingtp_gated_backward(int act, const void* grad_h, in
     if (M > 0) {
         if (bad(grad_h, 2) || bad(g, 16) || bad(u, 16)) return SPINGTP_ERR_INVALID_ARG;
         if (save == SPINGTP_SAVE_BLOCK8 && (bad(g_scales, 4) || bad(u_scales, 4))) return SPINGTP_ERR_INVALID_ARG;
+        if ((grad_x != nullptr && !spingtp::product_fits(M, K)) ||
+            (grad_w != nullptr && !spingtp::product_fits(2 * F + 63, K)))
+            return SPINGTP_ERR_INVALID_ARG;
         if (grad_x != nullptr && (bad(w_gate, 16) || bad(w_up, 16))) return SPINGTP_ERR_INVALID_ARG;
         if (grad_w != nullptr && (bad(x, 16) || off(x_scales, 4)))
             return SPINGTP_ERR_INVALID_ARG;

@@ -403,8 +403,7 @@ hipError_t gated_launch(GemmArgs g, const GatedOut& o, hipStream_t stream) {
 
 template <class E, int ACT, int SAVE, bool OUT8>
 hipError_t gated_tiles(const GemmArgs& g, const GatedOut& o, hipStream_t stream) {
-    const auto tiles = [&](int64_t bm) { return ((g.M + bm - 1) / bm) * ((g.N + 127) / 128); };
-    switch (pick_tile(kGated, tiles(64), tiles(128), tiles(256))) {
+    switch (gated_tile(g.M, g.N)) {
         case 256: return gated_launch<E, 128, 64, 2, 4, 2, ACT, SAVE, OUT8>(g, o, stream);
         case 128: return gated_launch<E, 64, 64, 4, 2, 3, ACT, SAVE, OUT8>(g, o, stream);
         default: return gated_launch<E, 64, 32, 4, 2, 2, ACT, SAVE, OUT8>(g, o, stream);
@@ -469,8 +468,7 @@ hipError_t product_launch(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) 
 template <bool KX>
 hipError_t product(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) {
     g.tail = kStepBytes;
-    const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
-    switch (pick_tile(kPlain16, tiles(64), tiles(128), tiles(256))) {
+    switch (product_tile(kPlain16, g.M, g.N)) {
         case 256: return product_launch<128, 64, 2, 4, 2, KX>(g, c, ldc, stream);
         case 128: return product_launch<64, 32, 2, 4, 2, KX>(g, c, ldc, stream);
         default: return product_launch<32, 32, 2, 2, 4, KX>(g, c, ldc, stream);

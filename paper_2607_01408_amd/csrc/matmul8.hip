@@ -49,8 +49,7 @@ hipError_t dispatch(const GemmArgs& g, int64_t k, void* out, int64_t ldo, hipStr
     if (g.M <= 16) return launch_skinny<1, TO>(g, out, ldo, stream);
     if (g.M <= 32) return launch_skinny<2, TO>(g, out, ldo, stream);
     if (g.M <= kSkinnyRows && g.N <= 2 * k) return launch_skinny<4, TO>(g, out, ldo, stream);
-    const auto tiles = [&](int64_t n) { return ((g.M + n - 1) / n) * ((g.N + n - 1) / n); };
-    switch (pick_tile(kPlain8, tiles(64), tiles(128), tiles(256))) {
+    switch (product_tile(kPlain8, g.M, g.N)) {
         case 256: return launch<128, 64, 2, 4, 2, TO>(g, out, ldo, stream);
         case 128: return launch<64, 64, 2, 2, 2, TO>(g, out, ldo, stream);
         default: return launch<32, 32, 2, 2, 4, TO>(g, out, ldo, stream);

@@ -110,3 +110,13 @@ def test_workspace_grows_with_the_operands():
     assert fn(100, 64, 100, 0, 72, 1, ctypes.byref(n)) == OK and n.value == 2 * 100 * (256 + 64)
     assert fn(100, 63, 100, 63, 63, 0, ctypes.byref(n)) == OK and n.value == 2 * (100 * (256 + 64) + 2 * 100 * 64)
     assert fn(100, 64, 100, 63, 64, 0, ctypes.byref(n)) == INVALID
+
+
+@pytest.mark.parametrize("name,good,change", [
+    ("spingtp_matmul8", MATMUL, dict(M=(1 << 30) + 1, N=4)), ("spingtp_matmul8", MATMUL, dict(M=2, N=(1 << 30) + 1, ldc=BIG)),
+    ("spingtp_gated_forward", GATED, dict(M=(1 << 30) + 1)), ("spingtp_gated_forward8", GATED8, dict(M=(1 << 30) + 1)),
+    ("spingtp_gated_backward", GATED_BWD, dict(M=(1 << 30) + 1, workspace_bytes=1 << 60)),
+    ("spingtp_gated_backward", GATED_BWD, dict(M=(1 << 23), K=1 << 18, ldx=1 << 18, ldw=1 << 18, ldgx=1 << 18, workspace_bytes=1 << 60)),
+])
+def test_more_tiles_than_a_launch_holds_are_refused(name, good, change):
+    assert call(name, {**good, **change}) == INVALID
