@@ -70,18 +70,19 @@ __device__ __forceinline__ void keep8(uint16_t* p, const float (&v)[8]) {
     for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(p + 2 * i) = bf16_pair(v[2 * i], v[2 * i + 1]);
 }
 
-// Tile blockIdx.x (rows) x blockIdx.y (columns) of 128 x 128.  It lies in LDS in its own type.  Along the
+// Tile first + blockIdx.x (rows; `last` is the matrix's last) x blockIdx.y (columns) of 128 x 128.  It lies in LDS in its own type.  Along the
 // columns a lane takes two neighbouring ones and a wave a quarter of their rows, so its reads of LDS run
 // along the rows, without conflicts, and 32 bytes of each column leave in two stores.
 template <typename T, bool ROWS>
 __global__ __launch_bounds__(256) void pack8_both_kernel(const T* __restrict__ x, int64_t ldx,
                                                          uint8_t* __restrict__ values, uint8_t* __restrict__ scales,
                                                          uint8_t* __restrict__ t_values,
-                                                         uint8_t* __restrict__ t_scales, int64_t R, int64_t D) {
+                                                         uint8_t* __restrict__ t_scales, int64_t R, int64_t D,
+                                                         int64_t first, int64_t last) {
     constexpr int ST = 130;  // elements of a tile row
     __shared__ __align__(16) T tile[128 * ST];
     __shared__ float tops[4][128];
-    const int64_t r0 = static_cast<int64_t>(blockIdx.x) * 128, c0 = static_cast<int64_t>(blockIdx.y) * 128;
+    const int64_t rows = first + blockIdx.x, r0 = rows * 128, c0 = static_cast<int64_t>(blockIdx.y) * 128;
     const int l = threadIdx.x & 15, g = threadIdx.x >> 4;
     const int64_t pitch = block8_pitch(D), spitch = block8_scale_pitch(D);
     const int64_t left = D - c0 - l * 8;
@@ -145,9 +146,8 @@ __global__ __launch_bounds__(256) void pack8_both_kernel(const T* __restrict__ x
                            block8_word(w[16 * i + 8], w[16 * i + 9], w[16 * i + 10], w[16 * i + 11], inv),
                            block8_word(w[16 * i + 12], w[16 * i + 13], w[16 * i + 14], w[16 * i + 15], inv));
         // the scale, and behind the column's last block the bytes up to the word's end
-        if (wave == 0) t_scales[column * tspitch + blockIdx.x] = static_cast<uint8_t>(e);
-        if (wave > 0 && blockIdx.x == gridDim.x - 1 && blockIdx.x + wave < tspitch)
-            t_scales[column * tspitch + blockIdx.x + wave] = 127;
+        if (wave == 0) t_scales[column * tspitch + rows] = static_cast<uint8_t>(e);
+        if (wave > 0 && rows == last && rows + wave < tspitch) t_scales[column * tspitch + rows + wave] = 127;
     }
 }
 
@@ -194,15 +194,20 @@ hipError_t pack(const T* x, int64_t ldx, uint8_t* values, uint8_t* scales, uint8
         return hipGetLastError();
     }
     const int64_t br = (R + 127) / 128, bc = (D + 127) / 128;
-    if (br > kMostBlocks || bc > 65535) return hipErrorInvalidValue;
-    const dim3 grid(static_cast<unsigned>(br), static_cast<unsigned>(bc));
-    if (values != nullptr)
-        hipLaunchKernelGGL((pack8_both_kernel<T, true>), grid, dim3(256), 0, stream, x, ldx, values, scales, t_values,
-                           t_scales, R, D);
-    else
-        hipLaunchKernelGGL((pack8_both_kernel<T, false>), grid, dim3(256), 0, stream, x, ldx, values, scales,
-                           t_values, t_scales, R, D);
-    return hipGetLastError();
+    if (bc > 65535) return hipErrorInvalidValue;
+    for (int64_t first = 0; first < br; first += kMostBlocks) {  // as many rows as one launch holds
+        const dim3 grid(static_cast<unsigned>(br - first < kMostBlocks ? br - first : kMostBlocks),
+                        static_cast<unsigned>(bc));
+        if (values != nullptr)
+            hipLaunchKernelGGL((pack8_both_kernel<T, true>), grid, dim3(256), 0, stream, x, ldx, values, scales,
+                               t_values, t_scales, R, D, first, br - 1);
+        else
+            hipLaunchKernelGGL((pack8_both_kernel<T, false>), grid, dim3(256), 0, stream, x, ldx, values, scales,
+                               t_values, t_scales, R, D, first, br - 1);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

@@ -165,6 +165,15 @@ def test_the_smallest_scale():
     assert torch.equal(sg.unpack8(a, dtype=F32).double(), a.values.double()[:, :300] * 2.0**-127)
 
 
+def test_transposed_packing_of_more_rows_than_one_launch():
+    R, D = (1 << 27) + 900, 2
+    x = rand((R, D), BF16, 1)
+    x[-3:] = NAN
+    t, want = sg.pack8(x, transpose=True), sg.pack8(x.t().contiguous())
+    assert torch.equal(t.values.view(torch.uint8), want.values.view(torch.uint8))
+    assert torch.equal(t.scales.view(torch.uint8), want.scales.view(torch.uint8))
+
+
 # ------------------------------------------------------------------ norm
 
 def ref_norm(x, r, gain, eps):
