@@ -34,11 +34,18 @@ hipError_t launch(GemmArgs g, void* out, int64_t ldo, hipStream_t stream) {
 
 template <int TM, typename TO>
 hipError_t launch_skinny(const GemmArgs& g, void* out, int64_t ldo, hipStream_t stream) {
-    const int64_t blocks = (g.N + 15) / 16;
-    if (blocks > kMostTiles) return hipErrorInvalidValue;
-    hipLaunchKernelGGL((gemm_skinny_kernel<Fp8, TM, TO>), dim3(static_cast<unsigned>(blocks)), dim3(64 * kSkinnyWaves),
-                       0, stream, g, int64_t{0}, static_cast<TO*>(out), ldo);
-    return hipGetLastError();
+    // as many rows of w as one launch holds workgroups for
+    for (int64_t n = 0; n < g.N; n += 16 * kMostTiles) {
+        GemmArgs part = g;
+        part.w += n * g.ldw;
+        part.ws += n * g.lds;
+        part.N = g.N - n < 16 * kMostTiles ? g.N - n : 16 * kMostTiles;
+        hipLaunchKernelGGL((gemm_skinny_kernel<Fp8, TM, TO>), dim3(static_cast<unsigned>((part.N + 15) / 16)),
+                           dim3(64 * kSkinnyWaves), 0, stream, part, int64_t{0}, static_cast<TO*>(out) + n, ldo);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <typename TO>

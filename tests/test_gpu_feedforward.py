@@ -355,6 +355,15 @@ def test_matmul8_result_past_two_to_the_31_elements():
         check_product(c[r, s], as64(a)[r], as64(b)[s], K)
 
 
+def test_matmul8_of_few_rows_and_more_columns_than_one_launch():
+    M, N, K, cut = 3, (1 << 26) + 1000, 5, 1 << 26
+    a, b = sg.pack8(rand((M, K), BF16, 1)), sg.pack8(rand((N, K), BF16, 2))
+    c = sg.matmul8(a, b)
+    for at in (slice(0, 100), slice(cut - 100, cut + 100), slice(N - 100, N)):
+        rows = sg.Block8(b.values[at].contiguous(), b.scales[at].contiguous(), (at.stop - at.start, K))
+        check_product(c[:, at], as64(a), as64(rows), K)
+
+
 @pytest.mark.parametrize("M,N,K", [(3, 50, 70), (200, 130, 300), (1000, 520, 390)])
 def test_matmul8_backward(M, N, K):
     x, w, dc = rand((M, K), BF16, 1), rand((N, K), BF16, 2, 0.1), rand((M, N), BF16, 3)
