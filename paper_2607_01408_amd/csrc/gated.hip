@@ -314,13 +314,13 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void gated_skinny_kernel(GemmArg
 __global__ __launch_bounds__(256) void stage_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx,
                                                          uint16_t* __restrict__ out, int64_t R, int64_t K,
                                                          int64_t pitch) {
-    const int64_t groups = pitch / 8, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = i / groups;
-    if (row >= R) return;
-    const int64_t c = (i - row * groups) * 8, left = K - c;
-    float v[8];
-    load8(x + row * ldx + (left > 0 ? c : 0), left >= 8 ? 8 : static_cast<int>(left), v);
-    store8(out + row * pitch + c, 8, v);
+    const int64_t groups = pitch / 8, stride = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < R * groups; i += stride) {
+        const int64_t row = i / groups, c = (i - row * groups) * 8, left = K - c;
+        float v[8];
+        load8(x + row * ldx + (left > 0 ? c : 0), left >= 8 ? 8 : static_cast<int>(left), v);
+        store8(out + row * pitch + c, 8, v);
+    }
 }
 
 // dg and du side by side, [M][2 Fp] (Fp: F up to a multiple of 64, zeros behind): 8 neighbouring columns of both
@@ -371,11 +371,15 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const uint16_t* __restr
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(uint16_t* p, int64_t n) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (i < n) p[i] = 0;
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += stride) p[i] = 0;
 }
 
-bool grid_ok(int64_t x) { return x <= (int64_t{1} << 24) - 1; }  // below 2^32 threads
+// of 256 threads, for kernels that walk what is left
+dim3 walking_grid(int64_t threads) {
+    const int64_t blocks = (threads + 255) / 256;
+    return dim3(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks));
+}
 
 // LDS of a workgroup: the operands' tiles, then the outputs'
 template <class Tile, int WN>
@@ -443,9 +447,8 @@ bool rows_fit(int64_t K, int64_t ld) { return K % 8 == 0 && ld % 8 == 0 && 2 * l
 int64_t up64(int64_t n) { return (n + 63) / 64 * 64; }
 
 hipError_t stage(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K, hipStream_t stream) {
-    const int64_t pitch = up64(K), blocks = (R * (pitch / 8) + 255) / 256;
-    if (!grid_ok(blocks)) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(stage_rows_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
+    const int64_t pitch = up64(K);
+    hipLaunchKernelGGL(stage_rows_kernel, walking_grid(R * (pitch / 8)), dim3(256), 0, stream,
                        static_cast<const uint16_t*>(x), ldx, out, R, K, pitch);
     return hipGetLastError();
 }
@@ -477,8 +480,7 @@ hipError_t product(GemmArgs g, void* c, int64_t ldc, hipStream_t stream) {
 
 template <int ACT>
 hipError_t gated_grad(const GatedBwdArgs& a, uint16_t* both, hipStream_t stream) {
-    const int64_t blocks = (a.M * (up64(a.F) / 8) + 255) / 256;
-    const dim3 grid(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks));
+    const dim3 grid = walking_grid(a.M * (up64(a.F) / 8));
     const uint16_t* dh = static_cast<const uint16_t*>(a.dh);
     if (a.save == kSave8)
         hipLaunchKernelGGL((gated_grad_kernel<ACT, true>), grid, dim3(256), 0, stream, dh, a.lddh, a.g, a.u, a.g_scales,
@@ -592,10 +594,8 @@ size_t gated_backward_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, in
 hipError_t launch_gated_backward(const GatedBwdArgs& a, hipStream_t stream) {
     if (a.M == 0) {
         if (a.dw == nullptr) return hipSuccess;
-        const int64_t n = 2 * a.F * a.K, blocks = (n + 255) / 256;
-        if (!grid_ok(blocks)) return hipErrorInvalidValue;
-        hipLaunchKernelGGL(zero_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream,
-                           static_cast<uint16_t*>(a.dw), n);
+        const int64_t n = 2 * a.F * a.K;
+        hipLaunchKernelGGL(zero_kernel, walking_grid(n), dim3(256), 0, stream, static_cast<uint16_t*>(a.dw), n);
         return hipGetLastError();
     }
     const int64_t fp = up64(a.F), kp = up64(a.K);

@@ -649,6 +649,30 @@ def test_gated_of_no_rows():
         assert tuple(dwg.shape) == (30, 20) and bool((dwg == 0).all()) and bool((dwu == 0).all())
 
 
+def test_gated_of_no_rows_and_more_weights_than_one_launch_has_threads():
+    F, K = 70_001, 32_768
+    w = torch.empty((F, K), dtype=BF16, device="cuda")
+    junk = torch.ones((2 * F, K), dtype=BF16, device="cuda")  # the gradients' memory, most likely
+    del junk
+    g = torch.empty((0, F), dtype=BF16, device="cuda")
+    saved = sg.GatedSaved(torch.empty((0, K), dtype=BF16, device="cuda"), g, g, "silu", "same")
+    _, dwg, dwu = sg.gated_backward(g, saved, w, w)
+    assert not bool(dwg.any()) and not bool(dwu.any())
+
+
+def test_gated_copies_more_rows_than_one_launch_has_threads():
+    M, K, F = (1 << 29) + 1001, 3, 2  # rows of six bytes: copied into rows of 128, 69 GB
+    torch.cuda.empty_cache()
+    x, wg, wu = torch.zeros((M, K), dtype=BF16, device="cuda"), rand((F, K), BF16, 2), rand((F, K), BF16, 3)
+    x[:500], x[-500:] = rand((500, K), BF16, 4), rand((500, K), BF16, 5)
+    h = sg.gated(x, wg, wu)[0]
+    for at in (slice(0, 600), slice(M - 600, M)):
+        _, _, _, _, ref, bound = gated_bound(x[at].double(), wg.double(), wu.double(), "silu", K)
+        within(h[at], ref, 2.0**-8 * ref.abs() + bound + 1e-38)
+    del x, h
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------ as programs call them
 
 def serve(x, residual, gain, w):
