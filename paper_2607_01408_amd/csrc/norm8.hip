@@ -253,13 +253,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void rms_norm_bwd_kernel(
     }
 }
 
-// dgain[d] = sum of the partial rows, in a fixed order: 32 columns a workgroup, 32 row strides with eight
-// rows in flight each
+// dgain[d] = sum of the partial rows, in a fixed order, from column `first` on: 32 columns a workgroup, 32 row
+// strides with eight rows in flight each
 __global__ __launch_bounds__(1024) void norm_gain_kernel(const float* __restrict__ partial, float* __restrict__ dgain,
-                                                         int n, int64_t D) {
+                                                         int n, int64_t D, int64_t first) {
     __shared__ float part[32][33];
     const int l = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + l;
+    const int64_t c = first + static_cast<int64_t>(blockIdx.x) * 32 + l;
     float s = 0.f;
     if (c < D) {
         for (int i = w; i < n; i += 256) {
@@ -330,10 +330,15 @@ hipError_t norm_bwd_launch(const NormBwdArgs& a, hipStream_t stream) {
                        static_cast<const T*>(a.dy), a.lddy, static_cast<const T*>(a.h), a.ldh, a.rstd, a.gain,
                        static_cast<const T*>(a.gh), a.ldgh, static_cast<T*>(a.dx), a.lddx,
                        a.dgain != nullptr ? a.partial : nullptr, a.R, a.D);
-    if (a.dgain != nullptr)
-        hipLaunchKernelGGL(norm_gain_kernel, dim3(static_cast<unsigned>((a.D + 31) / 32)), dim3(1024), 0, stream,
-                           a.partial, a.dgain, static_cast<int>(grid), a.D);
-    return hipGetLastError();
+    hipError_t e = hipGetLastError();
+    constexpr int64_t kColumns = 32 * kMostBlocks;  // of a launch
+    for (int64_t first = 0; a.dgain != nullptr && e == hipSuccess && first < a.D; first += kColumns) {
+        const int64_t columns = a.D - first < kColumns ? a.D - first : kColumns;
+        hipLaunchKernelGGL(norm_gain_kernel, dim3(static_cast<unsigned>((columns + 31) / 32)), dim3(1024), 0, stream,
+                           a.partial, a.dgain, static_cast<int>(grid), a.D, first);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 #define NORM_SHAPES(CALL, MORE)                                               \

@@ -275,6 +275,16 @@ def test_norm_backward(R, D, dtype):
     assert torch.equal(again[0], dx) and torch.equal(again[1], dgain)
 
 
+def test_norm_backward_of_more_columns_than_one_launch_has_threads():
+    R, D = 2, (1 << 27) + 100
+    h, dy, gain = rand((R, D), BF16, 1), rand((R, D), BF16, 2), torch.ones(D, device="cuda")
+    rstd = torch.tensor([0.5, 2.0], device="cuda")
+    dx, dgain = sg.rms_norm_backward(dy, h, rstd, gain)
+    for at in (slice(0, 300), slice((1 << 25) - 100, (1 << 25) + 100), slice(D - 300, D)):
+        terms = dy[:, at].double() * h[:, at].double() * rstd.double()[:, None]
+        within(dgain[at], terms.sum(0), 4 * 2.0**-24 * terms.abs().sum(0) + 1e-38)
+
+
 def test_norm_backward_against_differences():
     R, D = 6, 200
     x, dy, v = (rand((R, D), F32, s) for s in (1, 2, 3))
