@@ -127,7 +127,8 @@ bool save_ok(int s) { return s == SPINGTP_SAVE_NONE || s == SPINGTP_SAVE_BF16 ||
 
 extern "C" spingtp_status spingtp_gated_forward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw,
                                                                int save, size_t* size) {
-    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || ldx < K || ldw < K || !save_ok(save))
+    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || ldx < K || ldw < K || !matrix_ok(M, ldx) ||
+        !matrix_ok(F, ldw) || !save_ok(save))
         return SPINGTP_ERR_INVALID_ARG;
     *size = spingtp::gated_workspace(M, K, F, ldx, ldw, save);
     return SPINGTP_OK;
@@ -138,7 +139,7 @@ extern "C" spingtp_status spingtp_gated_forward(int act, const void* x, int64_t 
                                                 void* g, void* g_scales, void* u, void* u_scales, void* workspace,
                                                 size_t workspace_bytes, int64_t M, int64_t K, int64_t F, void* stream) {
     size_t need = 0;
-    if (!gated_sizes_ok(act, M, K, F) || ldh < F || !matrix_ok(M, ldx) || !matrix_ok(F, ldw) || !matrix_ok(M, ldh) ||
+    if (!gated_sizes_ok(act, M, K, F) || ldh < F || !matrix_ok(M, ldh) ||
         spingtp_gated_forward_workspace_size(M, K, F, ldx, ldw, save, &need) != SPINGTP_OK)
         return SPINGTP_ERR_INVALID_ARG;
     if (M == 0) return SPINGTP_OK;
@@ -208,7 +209,8 @@ extern "C" spingtp_status spingtp_gated_forward8(int act, const void* x, const v
 
 extern "C" spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx,
                                                                 int64_t ldw, int x8, size_t* size) {
-    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || (x8 == 0 && ldx < K) || ldw < K)
+    if (size == nullptr || !gated_sizes_ok(spingtp::kSilu, M, K, F) || (x8 == 0 && (ldx < K || !matrix_ok(M, ldx))) ||
+        ldw < K || !matrix_ok(F, ldw))
         return SPINGTP_ERR_INVALID_ARG;
     *size = spingtp::gated_backward_workspace(M, K, F, ldx, ldw, x8 != 0);
     return SPINGTP_OK;
@@ -226,9 +228,7 @@ extern "C" spingtp_status spingtp_gated_backward(int act, const void* grad_h, in
         return SPINGTP_ERR_INVALID_ARG;
     if (ldgh < F || !matrix_ok(M, ldgh) || (save != SPINGTP_SAVE_BF16 && save != SPINGTP_SAVE_BLOCK8))
         return SPINGTP_ERR_INVALID_ARG;
-    if (grad_x != nullptr && (ldgx < K || !matrix_ok(M, ldgx) || !matrix_ok(F, ldw) || off(grad_x, 2)))
-        return SPINGTP_ERR_INVALID_ARG;
-    if (grad_w != nullptr && ((x_scales == nullptr && !matrix_ok(M, ldx)) || off(grad_w, 2)))
+    if ((grad_x != nullptr && (ldgx < K || !matrix_ok(M, ldgx) || off(grad_x, 2))) || off(grad_w, 2))
         return SPINGTP_ERR_INVALID_ARG;
     if (M > 0) {
         if (bad(grad_h, 2) || bad(g, 16) || bad(u, 16)) return SPINGTP_ERR_INVALID_ARG;

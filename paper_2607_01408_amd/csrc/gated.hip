@@ -626,16 +626,17 @@ hipError_t launch_gated_backward(const GatedBwdArgs& a, hipStream_t stream) {
     }
     if (e == hipSuccess && a.dw != nullptr) {
         GemmArgs g{};
-        g.w = static_cast<const uint8_t*>(a.x);
-        g.ldw = 2 * a.ldx;
+        if (a.x_scales == nullptr && rows_fit(a.K, a.ldx)) {
+            g.w = static_cast<const uint8_t*>(a.x);
+            g.ldw = 2 * a.ldx;
+        } else {
+            g.w = reinterpret_cast<const uint8_t*>(free_at);
+            g.ldw = 2 * kp;
+        }
         if (a.x_scales != nullptr) {
             e = launch_unpack8(SPINGTP_BF16, static_cast<const uint8_t*>(a.x), a.x_scales, free_at, kp, a.M, a.K, stream);
         } else if (!rows_fit(a.K, a.ldx)) {
             e = stage(a.x, a.ldx, free_at, a.M, a.K, stream);
-        }
-        if (a.x_scales != nullptr || !rows_fit(a.K, a.ldx)) {
-            g.w = reinterpret_cast<const uint8_t*>(free_at);
-            g.ldw = 2 * kp;
         }
         g.w2 = g.w;
         g.x = reinterpret_cast<const uint8_t*>(both);

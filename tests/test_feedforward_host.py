@@ -120,3 +120,19 @@ def test_workspace_grows_with_the_operands():
 ])
 def test_more_tiles_than_a_launch_holds_are_refused(name, good, change):
     assert call(name, {**good, **change}) == INVALID
+
+
+@pytest.mark.parametrize("ld", [(1 << 46) + 1, 1 << 62, (1 << 63) - 1])
+def test_strides_out_of_range_have_no_workspace_size(ld):
+    n = ctypes.c_size_t(0)
+    forward, backward = (getattr(_lib.lib(), f"spingtp_gated_{d}_workspace_size") for d in ("forward", "backward"))
+    for M in (1, 100):
+        assert forward(M, 64, 32, ld, 64, 0, ctypes.byref(n)) == INVALID
+        assert forward(M, 64, 32, 64, ld, 0, ctypes.byref(n)) == INVALID
+        assert backward(M, 64, 32, ld, 64, 0, ctypes.byref(n)) == INVALID
+        assert backward(M, 64, 32, 64, ld, 0, ctypes.byref(n)) == INVALID
+        assert backward(M, 64, 32, ld, 64, 1, ctypes.byref(n)) == OK  # x in 8 bits: its stride is not used
+    for name, good, change in (("spingtp_gated_forward", GATED, dict(ldx=ld)), ("spingtp_gated_forward", GATED, dict(ldw=ld)),
+                               ("spingtp_gated_backward", GATED_BWD, dict(ldx=ld)),
+                               ("spingtp_gated_backward", GATED_BWD, dict(ldw=ld))):
+        assert call(name, {**good, **change}) == INVALID
