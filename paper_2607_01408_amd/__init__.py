@@ -21,4 +21,9 @@ def __getattr__(name):  # torch is imported with the first operator that needs i
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
-__all__ = ["Plan", "plan_tables_host", "dense_tensor_host", "mfma_operands_host", "pre_table_host", "conj_map_host", "direct_table_host", "paths_host", "uvw_table_host", "SpinGTPError", "LIB_PATH", "BASIS_PAPER", "BASIS_M0_PAIRED", "BASIS_PARITY", *_FEEDFORWARD]
+def __dir__():
+    return sorted({*globals(), *_FEEDFORWARD})
+
+
+# without the operators: what an import of all names asks of a machine is what the plans need
+__all__ = ["Plan", "plan_tables_host", "dense_tensor_host", "mfma_operands_host", "pre_table_host", "conj_map_host", "direct_table_host", "paths_host", "uvw_table_host", "SpinGTPError", "LIB_PATH", "BASIS_PAPER", "BASIS_M0_PAIRED", "BASIS_PARITY"]
