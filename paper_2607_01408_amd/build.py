@@ -48,8 +48,8 @@ def binding_command(out: str) -> list:
     from torch.utils import cpp_extension
 
     cxx = shutil.which("g++") or shutil.which("c++")
-    if cxx is None:
-        raise RuntimeError("no host C++ compiler found")
+    if cxx is None:  # hipcc's own compiler
+        cxx = os.path.join(os.path.dirname(os.path.realpath(hipcc())), "amdclang++")
     cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
            "-I", sysconfig.get_paths()["include"]]
@@ -61,8 +61,28 @@ def binding_command(out: str) -> list:
     return cmd + ["-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
 
 
+def _wait(procs, verbose: bool) -> str:
+    """What the failed ones of all (source, compiler process) said."""
+    failed = []
+    for src, p in procs:
+        out, _ = p.communicate()
+        text = out.decode(errors="replace")
+        if p.returncode != 0:
+            failed.append(f"--- {src} ---\n{text}")
+        elif verbose and text.strip():
+            print(text)
+    return "\n".join(failed)
+
+
+def _start(src: str, cmd: list, verbose: bool) -> tuple:
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    return src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)
+
+
 def build(verbose: bool = False, jobs: int = 8) -> str:
-    """Compile every source to an object (in parallel), then link the shared library; and the binding."""
+    """Compile every source to an object (in parallel), then link the shared library; and the binding, which the
+    library does not need: without torch it is left out, and its failure is raised once the library is linked."""
     objdir = os.path.join(ROOT, "_build")
     os.makedirs(objdir, exist_ok=True)
     procs, objs = [], []
@@ -74,31 +94,25 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
         if src.endswith(".cpp"):
             cmd.insert(1, "-x")
             cmd.insert(2, "hip")
-        if verbose:
-            print(" ".join(cmd), flush=True)
-        procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
-    cmd = binding_command(BINDING + ".tmp")
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    procs.append(("binding.cpp", subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT)))
-    failed = []
-    for src, p in procs:
-        out, _ = p.communicate()
-        text = out.decode(errors="replace")
-        if p.returncode != 0:
-            failed.append((src, text))
-        elif verbose and text.strip():
-            print(text)
+        procs.append(_start(src, cmd, verbose))
+    try:
+        binding = [_start("binding.cpp", binding_command(BINDING + ".tmp"), verbose)]
+    except ImportError:
+        print(f"no torch: {os.path.basename(BINDING)} (the feed-forward operators on tensors) is not built", flush=True)
+        binding = []
+    failed, failed_binding = _wait(procs, verbose), _wait(binding, verbose)
     if failed:
-        msg = "\n".join(f"--- {s} ---\n{t}" for s, t in failed)
-        raise RuntimeError("compilation failed:\n" + msg)
-    os.replace(BINDING + ".tmp", BINDING)
+        raise RuntimeError("compilation failed:\n" + failed)
     tmp = LIB + ".tmp"
     cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
+    if failed_binding:
+        raise RuntimeError(f"{LIB} is built; compilation failed:\n" + failed_binding)
+    if binding:
+        os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 
