@@ -6,6 +6,8 @@ import subprocess
 
 import pytest
 
+from tests import feedforward_shapes as shapes
+
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_01408_amd", "csrc")
 MAIN = """
 #include <cstdio>
@@ -52,3 +54,26 @@ def test_a_tile_that_one_launch_holds(rule):
             fitting += 1
             assert -(-m // tile) * -(-n // columns) <= MOST, (kind, m, n, tile)
     assert fitting > 100
+
+
+def test_the_shapes_that_run_every_tile(rule):
+    """feedforward_shapes.py: each size takes the tile it stands for, with enough steps and ends inside them."""
+    gated = list(shapes.GATED)
+    assert [t for t, _ in rule([("gated", M, F) for M, K, F in gated])] == list(shapes.GATED.values())
+    assert all(-(-K // 128) >= 9 and K % 64 and M % 64 and F % 128 for M, K, F in gated)  # 17 steps in bf16
+    up = lambda n: -(-n // 64) * 64  # noqa: E731
+    for table in (shapes.BACKWARD, shapes.BACKWARD_LONG):
+        assert [t for t, _ in rule([("16", M, K) for M, K, F in table])] == [x for x, _ in table.values()]
+        assert [t for t, _ in rule([("16", up(F) + F, K) for M, K, F in table])] == [w for _, w in table.values()]
+    assert all(2 * up(F) * M > 1 << 31 for M, K, F in shapes.BACKWARD_LONG)
+    back = list(shapes.BACKWARD)
+    assert all(2 * up(F) // 64 >= 6 and -(-M // 64) >= 6 and M % 64 and K % 64 and F % 64 for M, K, F in back)
+    product = list(shapes.PRODUCT8)
+    assert [t for t, _ in rule([("8", M, N) for M, N, K in product])] == list(shapes.PRODUCT8.values())
+    assert all(-(-K // 128) >= 9 and K % 128 and M % 64 and N % 64 for M, N, K in product)
+    for tiles in (shapes.GATED.values(), [x for x, _ in shapes.BACKWARD.values()], [w for _, w in shapes.BACKWARD.values()],
+                  shapes.PRODUCT8.values()):
+        assert set(tiles) == {64, 128, 256}
+    for sizes in (gated, back):  # K a multiple of 8, and not, with each
+        tile = shapes.GATED if sizes is gated else shapes.BACKWARD
+        assert {(tile[s], s[1] % 8 == 0) for s in sizes} == {(tile[s], fits) for s in sizes for fits in (True, False)}

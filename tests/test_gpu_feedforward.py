@@ -18,6 +18,7 @@ pytestmark = pytest.mark.gpu
 if not torch.cuda.is_available():
     pytest.skip("no GPU visible", allow_module_level=True)
 
+from tests import feedforward_shapes as shapes  # noqa: E402
 import paper_2607_01408_amd as sg  # noqa: E402
 
 F32, BF16 = torch.float32, torch.bfloat16
@@ -681,6 +682,54 @@ def test_gated_copies_more_rows_than_one_launch_has_threads():
         within(h[at], ref, 2.0**-8 * ref.abs() + bound + 1e-38)
     del x, h
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------ every tile, with its whole loop
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("M,K,F", list(shapes.GATED))
+def test_gated_in_every_tile(M, K, F, act):
+    test_gated(M, K, F, act)
+    test_gated_8bit(M, K, F, act)
+
+
+@pytest.mark.parametrize("save", ["same", "8bit"])
+@pytest.mark.parametrize("M,K,F", list(shapes.BACKWARD))
+def test_gated_backward_in_every_tile(M, K, F, save):
+    test_gated_backward(M, K, F, save, "silu")
+
+
+@pytest.mark.parametrize("M,K,F", list(shapes.BACKWARD_LONG))
+def test_gated_backward_past_two_to_the_31_elements_in_the_large_tile(M, K, F):
+    n = 200  # the last rows alone have a gradient
+    x, wg, wu = rand((M, K), BF16, 1), rand((F, K), BF16, 2, K**-0.5), rand((F, K), BF16, 3, K**-0.5)
+    g, u = torch.ones((M, F), dtype=BF16, device="cuda"), torch.ones((M, F), dtype=BF16, device="cuda")
+    dh = torch.zeros((M, F), dtype=BF16, device="cuda")
+    g[-n:], u[-n:], dh[-n:] = rand((n, F), BF16, 4), rand((n, F), BF16, 5), rand((n, F), BF16, 6)
+    dx, dwg, dwu = sg.gated_backward(dh, sg.GatedSaved(x, g, u, "silu", "same"), wg, wu)
+    assert not bool(dx[:-n].any())
+    a, da = act64(g[-n:].double(), "silu")
+    d, u64, xs, wgd, wud = dh[-n:].double(), u[-n:].double(), x[-n:].double(), wg.double(), wu.double()
+    dg, du = d * u64 * da, d * a
+    # as in test_gated_backward: dg and du rounded to bf16, sums in fp32, the result rounded
+    eg = dg.abs() * 2.0**-8 + (d * u64).abs() * 2.0**-20 * (1 + g[-n:].double().abs())
+    eu = du.abs() * 2.0**-8 + d.abs() * 2.0**-20 * g[-n:].double().abs()
+    for y, ref, size, err, terms in (
+            (dx[-n:], dg @ wgd + du @ wud, dg.abs() @ wgd.abs() + du.abs() @ wud.abs(), eg @ wgd.abs() + eu @ wud.abs(), 2 * F),
+            (dwg, dg.t() @ xs, dg.abs().t() @ xs.abs(), eg.t() @ xs.abs(), M),
+            (dwu, du.t() @ xs, du.abs().t() @ xs.abs(), eu.t() @ xs.abs(), M)):
+        within(y, ref, 2.0**-8 * ref.abs() + (terms + 128) * 2.0**-24 * size + err + 1e-38)
+
+
+@pytest.mark.parametrize("M,K,F", [*shapes.GATED, *shapes.BACKWARD])
+def test_every_tile_reads_nothing_beside_its_rows(M, K, F):
+    test_gated_backward_reads_nothing_beside_its_rows(M, K, F)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,N,K", list(shapes.PRODUCT8))
+def test_matmul8_in_every_tile(M, N, K, dtype):
+    test_matmul8(M, N, K, dtype)
 
 
 # ------------------------------------------------------------------ as programs call them
