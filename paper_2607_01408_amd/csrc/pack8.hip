@@ -70,9 +70,9 @@ __device__ __forceinline__ void keep8(uint16_t* p, const float (&v)[8]) {
     for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(p + 2 * i) = bf16_pair(v[2 * i], v[2 * i + 1]);
 }
 
-// Tile first + blockIdx.x (rows; `last` is the matrix's last) x blockIdx.y (columns) of 128 x 128.  It lies in LDS in its own type.  Along the
-// columns a lane takes two neighbouring ones and a wave a quarter of their rows, so its reads of LDS run
-// along the rows, without conflicts, and 32 bytes of each column leave in two stores.
+// Tile first + blockIdx.x (rows; `last` is the matrix's last) x blockIdx.y (columns) of 128 x 128.  It lies in LDS in
+// its own type.  Along the columns a lane takes two neighbouring ones and a wave a quarter of their rows, so its
+// reads of LDS run along the rows, without conflicts, and 32 bytes of each column leave in two stores.
 template <typename T, bool ROWS>
 __global__ __launch_bounds__(256) void pack8_both_kernel(const T* __restrict__ x, int64_t ldx,
                                                          uint8_t* __restrict__ values, uint8_t* __restrict__ scales,

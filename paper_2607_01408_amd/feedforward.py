@@ -2,7 +2,11 @@
 
 Argument checks, outputs and the calls are in ``csrc/binding.cpp``, every step of the computation in the HIP
 kernels of ``libspingtp.so``.  Matrices are 2-D device tensors whose rows are contiguous (``stride(1) == 1``),
-at any row stride.  Every operator runs on the current stream of its tensors' device, or on ``stream=``.
+at any row stride; the gated block's bf16 x and weights start on 16 bytes (a tensor of its own does, a slice may
+not: SpinGTPError).  Every operator runs on the current stream of its tensors' device, or on ``stream=``.
+
+The operators are no part of autograd's graph: what they make requires no gradient, whatever the operands do, and
+gradients are the ``*_backward`` functions' to give (from a ``torch.autograd.Function``, for instance).
 """
 
 import functools
