@@ -678,9 +678,10 @@ spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
  *
  * A matrix [R][D] given as (pointer, ld) has rows of D neighbouring elements, `ld` elements apart
  * (ld >= D).  Sizes are at most 2^31 - 1, matrices 2^46 elements; the products' summed axes are
- * shorter: K <= 8388480 (spingtp_matmul8), K <= 4194240 and F <= 2097120 (gated block), and a product of
+ * shorter: K <= 8388480 (spingtp_matmul8, spingtp_linear_forward8), K <= 4194240 and F <= 2097120 (gated block),
+ * K and N <= 4194240 (linear layer), and a product of
  * [M][N] has ceil(M / 256) ceil(N / 256) <= 2^22 (gated block: [M][F] ceil(M / 256) ceil(F / 128) <= 2^22,
- * and for the gradients [M][K] and [2F + 63][K] as a product).
+ * and for the gradients [M][K] and [2F + 63][K] as a product; the linear layer's gradients: [M][K] and [N][K]).
  * Outputs must not overlap inputs or one another.  R = 0 (M = 0) is valid: gradients of weights are
  * then zero, everything else is empty.  Sums and statistics are fp32, outputs are rounded to nearest
  * even.
@@ -692,7 +693,7 @@ spingtp_status spingtp_plan_kernel_info_v1(spingtp_plan plan, int* info);
  * the smallest power of two that brings the block's largest finite magnitude to 448 or below (at least
  * 2^-126; 1 for a block of zeros); a non-finite element becomes NaN in its own place.
  */
-typedef enum { SPINGTP_SILU = 0, SPINGTP_GELU = 1 } spingtp_activation; /* gelu: x Phi(x), not its tanh form */
+typedef enum { SPINGTP_SILU = 0, SPINGTP_GELU = 1, SPINGTP_IDENTITY = 2 } spingtp_activation; /* gelu: x Phi(x), not its tanh form */
 typedef enum { SPINGTP_SAVE_NONE = 0, SPINGTP_SAVE_BF16 = 1, SPINGTP_SAVE_BLOCK8 = 2 } spingtp_save;
 /* These and spingtp_dtype are passed as int below, so that a value that is none of theirs can be refused. */
 
@@ -779,6 +780,46 @@ spingtp_status spingtp_gated_backward(int act, const void* grad_h, int64_t ldgh,
                                       void* stream);
 spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw,
                                                      int x8, size_t* size);
+
+/*
+ * Linear layer with everything that follows the product: y = act(x w^T + bias) + residual, for bf16 x [M][K] and
+ * w [N][K] (2-byte aligned; read as they are where K and the row strides are multiples of 8 and the rows start on 16
+ * bytes, copied to the workspace elsewhere), bias [N] fp32 or NULL, residual [M][N] of dtype or NULL, y [M][N] of dtype.
+ * act: any spingtp_activation.  z: NULL, or what the backward pass needs of an activation, x w^T + bias rounded to bf16,
+ * dense [M][N].  Sums, bias, activation and residual are fp32, y is rounded once.
+ * workspace (16-byte aligned): the size below, for the same x and w (of whose addresses only the alignment counts).
+ */
+spingtp_status spingtp_linear_forward(int act, const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias,
+                                      int dtype, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                                      void* workspace, size_t workspace_bytes, int64_t M, int64_t K, int64_t N,
+                                      void* stream);
+spingtp_status spingtp_linear_forward_workspace_size(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M,
+                                                     int64_t K, int64_t N, size_t* size);
+
+/* The same from 8-bit blocks, for inference: x and w packed along K. */
+spingtp_status spingtp_linear_forward8(int act, const void* x, const void* x_scales, const void* w, const void* w_scales,
+                                       const float* bias, int dtype, const void* residual, int64_t ldr, void* y,
+                                       int64_t ldy, void* workspace, size_t workspace_bytes, int64_t M, int64_t K,
+                                       int64_t N, void* stream);
+spingtp_status spingtp_linear_forward8_workspace_size(int64_t M, int64_t K, int64_t N, size_t* size);
+
+/*
+ * Gradients of the linear layer, from grad_y [M][N] of dtype, z (the forward's; NULL with SPINGTP_IDENTITY) and the
+ * bf16 operands:
+ *   dz = grad_y act'(z) (rounded to bf16, an operand of the matrix units),
+ *   grad_x [M][K] = dz w (bf16),  grad_w [N][K] = dz^T x (w_dtype, dense),
+ *   grad_bias [N] = sum over the rows of dz before its rounding (fp32; the same order in every call).
+ * The residual's gradient is grad_y.  grad_x, grad_w and grad_bias may be NULL; w is read for grad_x alone, x for
+ * grad_w alone.  workspace (16-byte aligned): the size below, for the same arguments.
+ */
+spingtp_status spingtp_linear_backward(int act, int dtype, const void* grad_y, int64_t ldg, const void* z, const void* x,
+                                       int64_t ldx, const void* w, int64_t ldw, void* grad_x, int64_t ldgx, int w_dtype,
+                                       void* grad_w, float* grad_bias, void* workspace, size_t workspace_bytes,
+                                       int64_t M, int64_t K, int64_t N, void* stream);
+spingtp_status spingtp_linear_backward_workspace_size(int act, int dtype, const void* grad_y, int64_t ldg, const void* x,
+                                                      int64_t ldx, const void* w, int64_t ldw, const void* grad_x,
+                                                      const void* grad_w, const float* grad_bias, int64_t M, int64_t K,
+                                                      int64_t N, size_t* size);
 
 #ifdef __cplusplus
 }

@@ -1,7 +1,7 @@
 """SpinGTP on AMD MI355X: the spin-weighted Gaunt tensor product as a C-ABI HIP library.
 
 ``Plan`` wraps ``spingtp_plan_create`` / ``spingtp_forward`` (``include/spingtp.h``).
-``rms_norm``, ``matmul8``, ``gated``, ``pack8`` and their kin are the feed-forward operators on
+``rms_norm``, ``matmul8``, ``gated``, ``linear``, ``pack8`` and their kin are the feed-forward operators on
 invariant channels (``feedforward``), ``Block8`` their 8-bit block format.
 ``workloads`` holds the seeded synthetic input generators.
 """
@@ -10,7 +10,7 @@ from ._lib import SpinGTPError, LIB_PATH
 from .spingtp import Plan, plan_tables_host, dense_tensor_host, mfma_operands_host, pre_table_host, conj_map_host, direct_table_host, paths_host, uvw_table_host, BASIS_PAPER, BASIS_M0_PAIRED, BASIS_PARITY
 
 _FEEDFORWARD = ("Block8", "GatedSaved", "pack8", "unpack8", "rms_norm", "rms_norm_backward", "matmul8",
-                "matmul8_backward", "gated", "gated_backward")
+                "matmul8_backward", "gated", "gated_backward", "LinearSaved", "linear", "linear_backward")
 
 
 def __getattr__(name):  # torch is imported with the first operator that needs it

@@ -24,7 +24,9 @@ EXPORTED = ("spingtp_plan_create", "spingtp_forward", "spingtp_plan_destroy", "s
             "spingtp_backward_fully_connected", "spingtp_pack8", "spingtp_unpack8", "spingtp_rms_norm",
             "spingtp_rms_norm_backward", "spingtp_rms_norm_backward_workspace_size", "spingtp_matmul8",
             "spingtp_gated_forward", "spingtp_gated_forward_workspace_size", "spingtp_gated_forward8",
-            "spingtp_gated_forward8_workspace_size", "spingtp_gated_backward", "spingtp_gated_backward_workspace_size")
+            "spingtp_gated_forward8_workspace_size", "spingtp_gated_backward", "spingtp_gated_backward_workspace_size", "spingtp_linear_forward",
+            "spingtp_linear_forward_workspace_size", "spingtp_linear_forward8", "spingtp_linear_forward8_workspace_size",
+            "spingtp_linear_backward", "spingtp_linear_backward_workspace_size")
 
 _lib = None
 
@@ -150,7 +152,13 @@ def _feedforward_signatures(L):
                        ("spingtp_gated_forward8", "ipppppppnppznnnp"),
                        ("spingtp_gated_forward8_workspace_size", "nnnis"),
                        ("spingtp_gated_backward", "ipnipppppnpppnpnppznnnp"),
-                       ("spingtp_gated_backward_workspace_size", "nnnnnis")):
+                       ("spingtp_gated_backward_workspace_size", "nnnnnis"),
+                       ("spingtp_linear_forward", "ipnpnpipnpnppznnnp"),
+                       ("spingtp_linear_forward_workspace_size", "pnpnnnns"),
+                       ("spingtp_linear_forward8", "ipppppipnpnpznnnp"),
+                       ("spingtp_linear_forward8_workspace_size", "nnns"),
+                       ("spingtp_linear_backward", "iipnppnpnpnipppznnnp"),
+                       ("spingtp_linear_backward_workspace_size", "iipnpnpnpppnnns")):
         fn = getattr(L, name)
         fn.argtypes = [kinds[a] for a in args]
         fn.restype = ctypes.c_int

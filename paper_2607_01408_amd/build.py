@@ -13,7 +13,7 @@ SOURCES = ["plan.cpp", "api.cpp", "forward.hip", "forward_big_parity.hip", "forw
            "forward_big_parity_padded.hip", "forward_big_parity_padded_minreg.hip", "forward_mfma.hip", "forward_pre.hip",
            "forward_pre_large.hip", "forward_pre_weighted.hip", "forward_direct.hip", "backward.hip", "backward_v1w.hip", "forward_uvw.hip",
            "uvw_blocks.hip", "channel_blocks.hip", "gram_x2.hip", "direct_unrolled_paper.hip", "direct_unrolled_paired.hip", "direct_unrolled_parity.hip",
-           "feedforward.cpp", "norm8.hip", "pack8.hip", "matmul8.hip", "gated.hip"]
+           "feedforward.cpp", "norm8.hip", "pack8.hip", "matmul8.hip", "gated.hip", "linear.hip"]
 # per-source additions
 # the compile-time tensor patterns take more constant-evaluation steps than the default limit
 _CONSTEXPR = ["-fconstexpr-steps=200000000"]

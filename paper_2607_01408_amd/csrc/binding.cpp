@@ -45,6 +45,12 @@ struct Entries {
     decltype(&spingtp_gated_forward8_workspace_size) gated_forward8_workspace_size;
     decltype(&spingtp_gated_backward) gated_backward;
     decltype(&spingtp_gated_backward_workspace_size) gated_backward_workspace_size;
+    decltype(&spingtp_linear_forward) linear_forward;
+    decltype(&spingtp_linear_forward_workspace_size) linear_forward_workspace_size;
+    decltype(&spingtp_linear_forward8) linear_forward8;
+    decltype(&spingtp_linear_forward8_workspace_size) linear_forward8_workspace_size;
+    decltype(&spingtp_linear_backward) linear_backward;
+    decltype(&spingtp_linear_backward_workspace_size) linear_backward_workspace_size;
 } lib;
 
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
@@ -424,6 +430,102 @@ PyObject* gated_backward(Args a) {
     return tuple({wrap(dx), wrap(dw)});
 }
 
+// What follows a linear layer's product: bias [N] | None, residual [M, N] | None and y [M, N], new or given.
+struct LinearTail {
+    const float* bias = nullptr;
+    Matrix r, y;
+    at::Tensor made;
+    LinearTail(PyObject* bias_, PyObject* residual, PyObject* out, at::ScalarType type, const at::Tensor& beside, int64_t M,
+               int64_t N) {
+        Matrix like;
+        like.t = &beside;
+        like.type = type;
+        if (bias_ != Py_None) bias = vector(bias_, "bias", N, beside.device());
+        if (residual != Py_None) r = matrix(residual, "residual", &like, M, N);
+        if (out != Py_None) {
+            y = matrix(out, "out", &like, M, N);
+        } else {
+            made = empty({M, N}, type, beside);
+            y.p = made.data_ptr();
+            y.ld = N;
+        }
+    }
+    PyObject* result(PyObject* out) const { return made.defined() ? wrap(made) : Py_NewRef(out); }
+};
+
+// x, w, bias | None, act, residual | None, save, bf16, out | None, stream -> (y, z | None)
+PyObject* linear(Args a) {
+    const Matrix x = matrix(a[0], "x");
+    need_bf16(x, "x");
+    const int64_t M = x.rows, K = x.columns;
+    const Matrix w = matrix(a[1], "w", &x, -1, K);
+    const int64_t N = w.rows;
+    if (N < 1 || K < 1) throw Refused("the weights are empty");
+    const auto act = integer(a[3]);
+    const at::ScalarType type = truth(a[6]) ? at::kBFloat16 : at::kFloat;
+    const LinearTail t(a[2], a[4], a[7], type, *x.t, M, N);
+    at::Tensor z;
+    if (truth(a[5]) && act != SPINGTP_IDENTITY) z = empty({M, N}, at::kBFloat16, *x.t);
+    size_t bytes = 0;
+    done(lib.linear_forward_workspace_size(x.p, x.ld, w.p, w.ld, M, K, N, &bytes),
+         "spingtp_linear_forward_workspace_size");
+    const at::Tensor ws = workspace(bytes, *x.t);
+    done(lib.linear_forward(act, x.p, x.ld, w.p, w.ld, t.bias, dtype_of(type), t.r.p, t.r.ld, t.y.p, t.y.ld, address(z),
+                            address(ws), bytes, M, K, N, stream_of(a[8])),
+         "spingtp_linear_forward");
+    return tuple({t.result(a[7]), wrap(z)});
+}
+
+// x's and w's values and scales, M, K, N, bias | None, act, residual | None, bf16, out | None, stream -> y
+PyObject* linear8(Args a) {
+    const Block x = block(a[0], a[1]), w = block(a[2], a[3]);
+    if (x.t->device() != w.t->device()) throw Refused("x and w must be on one device");
+    const int64_t M = integer(a[4]), K = integer(a[5]), N = integer(a[6]);
+    if (N < 1 || K < 1) throw Refused("the weights are empty");
+    const at::ScalarType type = truth(a[10]) ? at::kBFloat16 : at::kFloat;
+    const LinearTail t(a[7], a[9], a[11], type, *x.t, M, N);
+    size_t bytes = 0;
+    done(lib.linear_forward8_workspace_size(M, K, N, &bytes), "spingtp_linear_forward8_workspace_size");
+    const at::Tensor ws = workspace(bytes, *x.t);
+    done(lib.linear_forward8(integer(a[8]), x.values, x.scales, w.values, w.scales, t.bias, dtype_of(type), t.r.p, t.r.ld,
+                             t.y.p, t.y.ld, address(ws), bytes, M, K, N, stream_of(a[12])),
+         "spingtp_linear_forward8");
+    return t.result(a[11]);
+}
+
+// grad_y, x, z | None, act, w, need_x, need_w, need_bias, bf16, stream -> (grad_x | None, grad_w | None, grad_bias | None)
+PyObject* linear_backward(Args a) {
+    const Matrix dy = matrix(a[0], "grad_y");
+    const int64_t M = dy.rows, N = dy.columns;
+    Matrix like = dy;
+    like.type = at::kBFloat16;
+    const Matrix x = matrix(a[1], "saved.x", &like, M, -1);
+    const int64_t K = x.columns;
+    const Matrix w = matrix(a[4], "w", &like, N, K);
+    if (N < 1 || K < 1) throw Refused("the weights are empty");
+    const auto act = integer(a[3]);
+    Matrix z;
+    if (act != SPINGTP_IDENTITY) {
+        z = matrix(a[2], "saved.z", &like, M, N);
+        if (M > 1 && z.ld != N) throw Refused("saved.z must be dense");
+    }
+    const at::ScalarType type = truth(a[8]) ? at::kBFloat16 : at::kFloat;
+    at::Tensor dx, dw, db;
+    if (truth(a[5])) dx = empty({M, K}, at::kBFloat16, *dy.t);
+    if (truth(a[6])) dw = empty({N, K}, type, *dy.t);
+    if (truth(a[7])) db = empty({N}, at::kFloat, *dy.t);
+    float* const bias = static_cast<float*>(address(db));
+    size_t bytes = 0;
+    done(lib.linear_backward_workspace_size(act, dtype_of(dy.type), dy.p, dy.ld, x.p, x.ld, w.p, w.ld, address(dx),
+                                            address(dw), bias, M, K, N, &bytes),
+         "spingtp_linear_backward_workspace_size");
+    const at::Tensor ws = workspace(bytes, *dy.t);
+    done(lib.linear_backward(act, dtype_of(dy.type), dy.p, dy.ld, z.p, x.p, x.ld, w.p, w.ld, address(dx), K,
+                             dtype_of(type), address(dw), bias, address(ws), bytes, M, K, N, stream_of(a[9])),
+         "spingtp_linear_backward");
+    return tuple({wrap(dx), wrap(dw), wrap(db)});
+}
+
 // ---------------------------------------------------------------- module
 
 template <PyObject* (*OP)(Args), Py_ssize_t N>
@@ -472,6 +574,9 @@ PyMethodDef methods[] = {OP(bind, 2),
                          OP(gated, 6),
                          OP(gated8, 12),
                          OP(gated_backward, 11),
+                         OP(linear, 9),
+                         OP(linear8, 13),
+                         OP(linear_backward, 10),
                          {nullptr, nullptr, 0, nullptr}};
 #undef OP
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,5 +1,5 @@
 // C entry points of the feed-forward operators: argument checks and launches on the caller's stream.
-// The kernels are in norm8.hip, pack8.hip, matmul8.hip and gated.hip.
+// The kernels are in norm8.hip, pack8.hip, matmul8.hip, gated.hip and linear.hip.
 #include "feedforward.h"
 
 #include <hip/hip_runtime.h>
@@ -265,4 +265,140 @@ extern "C" spingtp_status spingtp_gated_backward(int act, const void* grad_h, in
     a.K = K;
     a.F = F;
     return of(spingtp::launch_gated_backward(a, stream_of(stream)));
+}
+
+namespace {
+
+// K or N is the sum's length in one of the three products, M in the third
+bool linear_sizes_ok(int64_t M, int64_t K, int64_t N) {
+    return size_ok(M, 0) && size_ok(K, 1) && size_ok(N, 1) && K <= int64_t{65535} * 64 && N <= int64_t{65535} * 64 &&
+           matrix_ok(M, K + 511) && matrix_ok(M, N + 511) && matrix_ok(N, K + 511) && spingtp::product_fits(M, N);
+}
+bool act_ok(int a) { return a == spingtp::kSilu || a == spingtp::kGelu || a == spingtp::kIdentity; }
+// what leaves a linear layer's forward
+bool linear_out_ok(int act, const float* bias, int dtype, const void* residual, int64_t ldr, const void* y, int64_t ldy,
+                   int64_t M, int64_t N) {
+    if (!act_ok(act) || !dtype_ok(dtype) || ldy < N || !matrix_ok(M, ldy) || off(bias, 4)) return false;
+    if (residual != nullptr && (ldr < N || !matrix_ok(M, ldr) || off(residual, width(dtype)))) return false;
+    return M == 0 || !bad(y, width(dtype));
+}
+
+}  // namespace
+
+extern "C" spingtp_status spingtp_linear_forward_workspace_size(const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                                                int64_t M, int64_t K, int64_t N, size_t* size) {
+    if (size == nullptr || !linear_sizes_ok(M, K, N) || ldx < K || ldw < K || !matrix_ok(M, ldx) || !matrix_ok(N, ldw))
+        return SPINGTP_ERR_INVALID_ARG;
+    *size = M == 0 ? 0 : spingtp::linear_workspace(x, ldx, w, ldw, M, K, N);
+    return SPINGTP_OK;
+}
+
+extern "C" spingtp_status spingtp_linear_forward(int act, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                                 const float* bias, int dtype, const void* residual, int64_t ldr,
+                                                 void* y, int64_t ldy, void* z, void* workspace, size_t workspace_bytes,
+                                                 int64_t M, int64_t K, int64_t N, void* stream) {
+    size_t need = 0;
+    if (spingtp_linear_forward_workspace_size(x, ldx, w, ldw, M, K, N, &need) != SPINGTP_OK ||
+        !linear_out_ok(act, bias, dtype, residual, ldr, y, ldy, M, N) || off(z, 2))
+        return SPINGTP_ERR_INVALID_ARG;
+    if (M == 0) return SPINGTP_OK;
+    if (bad(x, 2) || bad(w, 2) || (need > 0 && (bad(workspace, 16) || workspace_bytes < need)))
+        return SPINGTP_ERR_INVALID_ARG;
+    const spingtp::LinearArgs a{act, x,   ldx, nullptr, w, ldw,       nullptr, bias, dtype,
+                                residual, ldr, y,       ldy, z, workspace, M,       K,    N};
+    return of(spingtp::launch_linear(a, stream_of(stream)));
+}
+
+extern "C" spingtp_status spingtp_linear_forward8_workspace_size(int64_t M, int64_t K, int64_t N, size_t* size) {
+    if (size == nullptr || !size_ok(M, 0) || !size_ok(K, 1) || !size_ok(N, 1) || K > int64_t{65535} * 128 ||
+        N > int64_t{65535} * 64 || !matrix_ok(M, K + 511) || !matrix_ok(M, N) || !matrix_ok(N, K + 511) ||
+        !spingtp::product_fits(M, N))
+        return SPINGTP_ERR_INVALID_ARG;
+    *size = M == 0 ? 0 : spingtp::linear8_workspace(M, K, N);
+    return SPINGTP_OK;
+}
+
+extern "C" spingtp_status spingtp_linear_forward8(int act, const void* x, const void* x_scales, const void* w,
+                                                  const void* w_scales, const float* bias, int dtype,
+                                                  const void* residual, int64_t ldr, void* y, int64_t ldy,
+                                                  void* workspace, size_t workspace_bytes, int64_t M, int64_t K,
+                                                  int64_t N, void* stream) {
+    size_t need = 0;
+    if (spingtp_linear_forward8_workspace_size(M, K, N, &need) != SPINGTP_OK ||
+        !linear_out_ok(act, bias, dtype, residual, ldr, y, ldy, M, N))
+        return SPINGTP_ERR_INVALID_ARG;
+    if (M == 0) return SPINGTP_OK;
+    if (bad(x, 16) || bad(x_scales, 4) || bad(w, 16) || bad(w_scales, 4) ||
+        (need > 0 && (bad(workspace, 16) || workspace_bytes < need)))
+        return SPINGTP_ERR_INVALID_ARG;
+    const spingtp::LinearArgs a{act,      x,   0, bytes(x_scales), w,       0,         bytes(w_scales), bias, dtype,
+                                residual, ldr, y, ldy,             nullptr, workspace, M,               K,    N};
+    return of(spingtp::launch_linear8(a, stream_of(stream)));
+}
+
+namespace {
+
+bool linear_backward_args(int act, int dtype, const void* grad_y, int64_t ldg, const void* x, int64_t ldx, const void* w,
+                          int64_t ldw, void* grad_x, void* grad_w, float* grad_bias, int64_t M, int64_t K, int64_t N,
+                          spingtp::LinearBwdArgs& a) {
+    if (!act_ok(act) || !dtype_ok(dtype) || !linear_sizes_ok(M, K, N) || ldg < N || !matrix_ok(M, ldg)) return false;
+    if (grad_x != nullptr && (ldw < K || !matrix_ok(N, ldw) || !spingtp::product_fits(M, K))) return false;
+    if (grad_w != nullptr && (ldx < K || !matrix_ok(M, ldx) || !spingtp::product_fits(N, K))) return false;
+    a = spingtp::LinearBwdArgs{};
+    a.act = act;
+    a.dtype = dtype;
+    a.dy = grad_y;
+    a.lddy = ldg;
+    a.x = x;
+    a.ldx = ldx;
+    a.w = w;
+    a.ldw = ldw;
+    a.dx = grad_x;
+    a.dw = grad_w;
+    a.db = grad_bias;
+    a.M = M;
+    a.K = K;
+    a.N = N;
+    return true;
+}
+
+}  // namespace
+
+extern "C" spingtp_status spingtp_linear_backward_workspace_size(int act, int dtype, const void* grad_y, int64_t ldg,
+                                                                 const void* x, int64_t ldx, const void* w, int64_t ldw,
+                                                                 const void* grad_x, const void* grad_w,
+                                                                 const float* grad_bias, int64_t M, int64_t K, int64_t N,
+                                                                 size_t* size) {
+    spingtp::LinearBwdArgs a;
+    if (size == nullptr ||
+        !linear_backward_args(act, dtype, grad_y, ldg, x, ldx, w, ldw, const_cast<void*>(grad_x),
+                              const_cast<void*>(grad_w), const_cast<float*>(grad_bias), M, K, N, a))
+        return SPINGTP_ERR_INVALID_ARG;
+    *size = M == 0 ? 0 : spingtp::linear_backward_workspace(a);
+    return SPINGTP_OK;
+}
+
+extern "C" spingtp_status spingtp_linear_backward(int act, int dtype, const void* grad_y, int64_t ldg, const void* z,
+                                                  const void* x, int64_t ldx, const void* w, int64_t ldw, void* grad_x,
+                                                  int64_t ldgx, int w_dtype, void* grad_w, float* grad_bias,
+                                                  void* workspace, size_t workspace_bytes, int64_t M, int64_t K,
+                                                  int64_t N, void* stream) {
+    spingtp::LinearBwdArgs a;
+    if (!linear_backward_args(act, dtype, grad_y, ldg, x, ldx, w, ldw, grad_x, grad_w, grad_bias, M, K, N, a))
+        return SPINGTP_ERR_INVALID_ARG;
+    if (grad_x != nullptr && (ldgx < K || !matrix_ok(M, ldgx) || off(grad_x, 2))) return SPINGTP_ERR_INVALID_ARG;
+    if (grad_w != nullptr && (!dtype_ok(w_dtype) || off(grad_w, width(w_dtype)))) return SPINGTP_ERR_INVALID_ARG;
+    if (off(grad_bias, 4)) return SPINGTP_ERR_INVALID_ARG;
+    if (grad_x == nullptr && grad_w == nullptr && grad_bias == nullptr) return SPINGTP_OK;
+    a.z = z;
+    a.lddx = ldgx;
+    a.w_dtype = w_dtype;
+    a.workspace = workspace;
+    if (M > 0) {
+        if (bad(grad_y, width(dtype)) || (act != spingtp::kIdentity ? bad(z, 2) : false)) return SPINGTP_ERR_INVALID_ARG;
+        if ((grad_x != nullptr && bad(w, 2)) || (grad_w != nullptr && bad(x, 2))) return SPINGTP_ERR_INVALID_ARG;
+        const size_t need = spingtp::linear_backward_workspace(a);
+        if (need > 0 && (bad(workspace, 16) || workspace_bytes < need)) return SPINGTP_ERR_INVALID_ARG;
+    }
+    return of(spingtp::launch_linear_backward(a, stream_of(stream)));
 }

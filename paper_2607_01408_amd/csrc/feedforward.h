@@ -67,8 +67,8 @@ struct Matmul8Args {
 };
 hipError_t launch_matmul8(int dtype, const Matmul8Args& a, hipStream_t stream);
 
-// The gated block's activation
-enum { kSilu = 0, kGelu = 1 };
+// Activations: of the gated block the first two, of the linear layer any
+enum { kSilu = 0, kGelu = 1, kIdentity = 2 };
 
 // What the forward keeps of the pre-activations g and u: nothing, bf16 or 8-bit blocks
 enum { kSaveNone = 0, kSaveBf16 = 1, kSave8 = 2 };
@@ -124,5 +124,50 @@ struct GatedBwdArgs {
 };
 size_t gated_backward_workspace(int64_t M, int64_t K, int64_t F, int64_t ldx, int64_t ldw, bool x8);
 hipError_t launch_gated_backward(const GatedBwdArgs& a, hipStream_t stream);
+
+// y = act(x w^T + bias) + r
+struct LinearArgs {
+    int act;
+    const void* x;  // bf16, or 8-bit values with scales
+    int64_t ldx;
+    const uint8_t* x_scales;
+    const void* w;
+    int64_t ldw;
+    const uint8_t* w_scales;
+    const float* bias;  // may be null
+    int dtype;          // of r and y
+    const void* r;      // may be null
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+    void* z;  // bf16 [M][N], may be null
+    void* workspace;
+    int64_t M, K, N;
+};
+size_t linear_workspace(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M, int64_t K, int64_t N);
+hipError_t launch_linear(const LinearArgs& a, hipStream_t stream);
+size_t linear8_workspace(int64_t M, int64_t K, int64_t N);
+hipError_t launch_linear8(const LinearArgs& a, hipStream_t stream);
+
+struct LinearBwdArgs {
+    int act;
+    int dtype;  // of dy
+    const void* dy;
+    int64_t lddy;
+    const void* z;  // bf16 [M][N], with an activation
+    const void* x;
+    int64_t ldx;
+    const void* w;
+    int64_t ldw;
+    void* dx;  // may be null
+    int64_t lddx;
+    int w_dtype;  // of dw
+    void* dw;     // [N][K], may be null
+    float* db;    // may be null
+    void* workspace;
+    int64_t M, K, N;
+};
+size_t linear_backward_workspace(const LinearBwdArgs& a);
+hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream);
 
 }  // namespace spingtp

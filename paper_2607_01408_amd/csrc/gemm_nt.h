@@ -263,10 +263,10 @@ struct GemmTile {
         };
         // the last step, where its rows end inside: zeros past their end
         auto load_any = [&](int k, uint8_t* to) {
-            if (!E::kScaled && !KW && a.tail < kStepBytes && k == a.steps - 1) {
+            if (!E::kScaled && !KX && a.tail < kStepBytes && k == a.steps - 1) {
                 const bool cut = chunk >= a.tail;
 #pragma unroll
-                for (int t = 0; t < LW; ++t) ow[t] = cut ? 0x80000000u : ow[t];  // past the buffer
+                for (int t = 0; t < (KW ? 0 : LW); ++t) ow[t] = cut ? 0x80000000u : ow[t];  // past the buffer
 #pragma unroll
                 for (int t = 0; t < LX; ++t) ox[t] = cut ? 0x80000000u : ox[t];
             }

@@ -1,0 +1,601 @@
+// Matrix product with bias, activation and residual in its epilogue, and its gradients:
+//   z = x w^T + b,  y = act(z) + r,
+//   dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = sum over the rows of dz.
+//
+// Forward: the products of gemm_nt.h; a wave's accumulators pass through its own LDS, 16 or 32 rows at a time, so that
+// a lane gets eight neighbouring columns of a row: bias, residual, z and y are whole lines, each touched once.
+// Backward: dz is made once, in bf16, with the columns' partial sums of it before the rounding; where there is no
+// activation and dy is bf16 on 16 bytes it is its own dz.  dx sums over w's rows, dw over those of dz and x: the
+// products read them as they lie.
+//
+// Few tiles and a long sum (the weights' gradients of many rows and few channels; dx of few rows) leave most of the
+// CUs idle: then the sum is cut into slices, a workgroup to each, whose fp32 sums a second kernel adds in order and
+// finishes.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "activation.h"
+#include "feedforward.h"
+#include "gemm_nt.h"
+#include "gemm_skinny.h"
+#include "internal.h"
+#include "lds_common.h"
+
+namespace spingtp {
+namespace {
+
+struct LinearOut {
+    int act;
+    bool wide;          // r and y in fp32
+    const float* bias;  // may be null
+    const void* r;      // may be null
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+    uint16_t* z;     // [M][N], may be null
+    float* partial;  // with slices: [slices][M][N] sums, and nothing else leaves
+    int slice;       // steps of a slice (without: all)
+};
+
+__device__ __forceinline__ void activate(int kind, float (&v)[8]) {
+    if (kind == kSilu) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act<kSilu>(v[i]);
+    } else if (kind == kGelu) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act<kGelu>(v[i]);
+    }
+}
+__device__ __forceinline__ void residual8(const LinearOut& o, int64_t m, int64_t n, int left, float (&v)[8]) {
+    if (o.wide)
+        load8(static_cast<const float*>(o.r) + m * o.ldr + n, left, v);
+    else
+        load8(static_cast<const uint16_t*>(o.r) + m * o.ldr + n, left, v);
+}
+// Eight neighbouring outputs of row m from their sums on (`bias`, `r`: zeros where there is none); the `left`
+// first of them exist.
+__device__ __forceinline__ void finish8(const LinearOut& o, int64_t N, int64_t m, int64_t n, int left, float (&v)[8],
+                                        const float (&bias)[8], const float (&r)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += bias[i];
+    if (o.z != nullptr) store8(o.z + m * N + n, left, v);
+    activate(o.act, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += r[i];
+    if (o.wide)
+        store8(static_cast<float*>(o.y) + m * o.ldy + n, left, v);
+    else
+        store8(static_cast<uint16_t*>(o.y) + m * o.ldy + n, left, v);
+}
+
+// The part of the sum that is this workgroup's slice.
+template <class E, bool KW, bool KX>
+__device__ __forceinline__ void cut_slice(GemmArgs& a, LinearOut& o, int64_t& row_bytes) {
+    if (o.partial == nullptr) return;
+    const int first = blockIdx.y * o.slice, left = a.steps - first;
+    const bool last = left <= o.slice;
+    a.w += KW ? int64_t{64} * first * a.ldw : int64_t{kStepBytes} * first;
+    a.x += KX ? int64_t{64} * first * a.ldx : int64_t{kStepBytes} * first;
+    if constexpr (E::kScaled) a.ws += first, a.xs += first;  // a multiple of 4: whole words
+    a.w_rows -= int64_t{64} * first;
+    a.x_rows -= int64_t{64} * first;
+    row_bytes -= int64_t{kStepBytes} * first;
+    if (!last) {
+        a.tail = kStepBytes;
+        a.w_rows = a.x_rows = int64_t{64} * o.slice;
+        a.steps = o.slice;
+    } else {
+        a.steps = left;
+    }
+    a.w_split = a.steps;
+    o = LinearOut{kIdentity, true, nullptr, nullptr, 0, o.partial + static_cast<int64_t>(blockIdx.y) * a.M * a.N, a.N,
+                  nullptr,   nullptr, 0};
+}
+
+template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX>
+struct LinearTile : GemmTile<E, PN, PM, WN, WM, NS, false, KW, KX> {
+    using Base = GemmTile<E, PN, PM, WN, WM, NS, false, KW, KX>;
+    static constexpr int kPitch = PN + 4;  // floats of a staged row: rows start in different banks
+    static constexpr int kStage = Base::kTile * kPitch * 4;
+    static constexpr int kAllLds = Base::kLds > Base::kWaves * kStage ? Base::kLds : Base::kWaves * kStage;
+    static_assert(kAllLds <= 160 * 1024, "in LDS");
+};
+
+template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX>
+__global__ __launch_bounds__(64 * WN * WM) void linear_kernel(GemmArgs a, LinearOut o) {
+    using Tile = LinearTile<E, PN, PM, WN, WM, NS, KW, KX>;
+    extern __shared__ __align__(16) uint8_t gemm_lds[];
+    int64_t unused = 0;
+    cut_slice<E, KW, KX>(a, o, unused);
+    int tm, tn;
+    tile_of(a.tiles_m, a.tiles_n, tm, tn);
+    const int64_t n0 = static_cast<int64_t>(tn) * Tile::BN, m0 = static_cast<int64_t>(tm) * Tile::BM;
+    Tile t;
+    t.run(a, n0, m0, gemm_lds);  // ends with a barrier behind its reads of LDS
+    constexpr int kLanes = PN / 8, kAtOnce = 64 / kLanes, kTimes = Tile::kTile / kAtOnce;  // lanes of a row
+    uint8_t* const mine = gemm_lds + t.wave * Tile::kStage;
+    const int l = t.lane % kLanes, r0 = t.lane / kLanes, in = t.lane & (Tile::kTile - 1);
+    const int64_t n = n0 + t.wn * PN + 8 * l;
+    const int left = a.N - n >= 8 ? 8 : (a.N > n ? static_cast<int>(a.N - n) : 0);
+    float bias[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bias[i] = 0.f;
+    if (o.bias != nullptr && left > 0) load8(o.bias + n, left, bias);
+#pragma unroll
+    for (int j = 0; j < Tile::TM; ++j) {
+        const int64_t m1 = m0 + t.wm * PM + j * Tile::kTile + r0;
+        float r[kTimes][8];
+#pragma unroll
+        for (int q = 0; q < kTimes; ++q) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) r[q][i] = 0.f;
+            if (o.r != nullptr && left > 0 && m1 + q * kAtOnce < a.M) residual8(o, m1 + q * kAtOnce, n, left, r[q]);
+        }
+#pragma unroll
+        for (int i = 0; i < Tile::TN; ++i)
+#pragma unroll
+            for (int c = 0; c < Tile::kQuads; ++c) {
+                const auto& s = t.acc[i][j];
+                *reinterpret_cast<float4*>(mine + 4 * (in * Tile::kPitch + t.column(i, c) - t.wn * PN)) =
+                    make_float4(s[4 * c], s[4 * c + 1], s[4 * c + 2], s[4 * c + 3]);
+            }
+        wave_lds_order();
+#pragma unroll
+        for (int q = 0; q < kTimes; ++q) {
+            const float4* from = reinterpret_cast<const float4*>(mine + 4 * ((r0 + q * kAtOnce) * Tile::kPitch + 8 * l));
+            const float4 lo = from[0], hi = from[1];
+            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            if (left > 0 && m1 + q * kAtOnce < a.M) finish8(o, a.N, m1 + q * kAtOnce, n, left, v, bias, r[q]);
+        }
+        wave_lds_order();
+    }
+}
+
+// At most kSkinnyRows rows of x.
+template <class E, int TM>
+__global__ __launch_bounds__(64 * kSkinnyWaves) void linear_skinny_kernel(GemmArgs a, int64_t row_bytes, LinearOut o) {
+    cut_slice<E, false, false>(a, o, row_bytes);
+    skinny_tile<E, TM, false>(a, row_bytes, static_cast<int64_t>(blockIdx.x) * 16,
+                              [&](int64_t m, int64_t n, float s, float) {
+                                  if (o.bias != nullptr) s += o.bias[n];
+                                  if (o.z != nullptr) put(o.z + m * a.N + n, s);
+                                  s = o.act == kSilu ? act<kSilu>(s) : (o.act == kGelu ? act<kGelu>(s) : s);
+                                  if (o.r != nullptr)
+                                      s += o.wide ? static_cast<const float*>(o.r)[m * o.ldr + n]
+                                                  : bf16_to_f32(static_cast<const uint16_t*>(o.r)[m * o.ldr + n]);
+                                  if (o.wide)
+                                      put(static_cast<float*>(o.y) + m * o.ldy + n, s);
+                                  else
+                                      put(static_cast<uint16_t*>(o.y) + m * o.ldy + n, s);
+                              });
+}
+
+// The slices' sums added in order, and what follows them: eight neighbouring outputs a thread.
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearOut o, int slices, int64_t M, int64_t N) {
+    const int64_t groups = (N + 7) / 8, stride = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < M * groups; at += stride) {
+        const int64_t m = at / groups, n = (at - m * groups) * 8;
+        const int left = N - n >= 8 ? 8 : static_cast<int>(N - n);
+        float v[8], bias[8], r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = bias[i] = r[i] = 0.f;
+        const float* from = o.partial + m * N + n;
+        if (o.bias != nullptr) load8(o.bias + n, left, bias);
+        if (o.r != nullptr) residual8(o, m, n, left, r);
+#pragma unroll 4
+        for (int s = 0; s < slices; ++s) {
+            float p[8];
+            load8(from + s * M * N, left, p);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += p[i];
+        }
+        finish8(o, N, m, n, left, v, bias, r);
+    }
+}
+
+// Rows of K bf16 elements to rows of a multiple of 64, zeros behind: what the products read where the caller's rows do
+// not start and end on 16 bytes.
+__global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx,
+                                                        uint16_t* __restrict__ out, int64_t R, int64_t K, int64_t pitch) {
+    const int64_t groups = pitch / 8, stride = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < R * groups; i += stride) {
+        const int64_t row = i / groups, c = (i - row * groups) * 8, left = K - c;
+        float v[8];
+        load8(x + row * ldx + (left > 0 ? c : 0), left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0), v);
+        store8(out + row * pitch + c, 8, v);
+    }
+}
+
+// dz [M] rows of `pitch` bf16 elements (zeros behind column N; null: not wanted) and, for each workgroup's rows, the
+// sums of its columns before they are rounded (sums [gridDim.y][N]; null: not wanted).  LANES lanes of eight
+// columns to a row; a lane keeps its columns.
+template <int LANES, typename TD>
+__global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __restrict__ dy, int64_t lddy,
+                                                        const uint16_t* __restrict__ z, uint16_t* __restrict__ dz,
+                                                        int64_t pitch, float* __restrict__ sums, int64_t M, int64_t N,
+                                                        int64_t rows) {
+    constexpr int kAtOnce = 256 / LANES;
+    __shared__ float part[kAtOnce][LANES * 8 + 4];
+    const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
+    const int64_t n = (static_cast<int64_t>(blockIdx.x) * LANES + l) * 8, left = N - n;
+    const int have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
+    const int64_t m1 = static_cast<int64_t>(blockIdx.y) * rows, m2 = m1 + rows < M ? m1 + rows : M;
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    if (n < (dz != nullptr ? pitch : N)) {
+#pragma unroll 4
+        for (int64_t m = m1 + g; m < m2; m += kAtOnce) {
+            float v[8];
+            pass8(dy + m * lddy + (have > 0 ? n : 0), have, v);
+            if (kind != kIdentity) {
+                float p[8];
+                pass8(z + m * N + (have > 0 ? n : 0), have, p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    float y, d;
+                    if (kind == kSilu)
+                        act_grad<kSilu>(p[i], y, d);
+                    else
+                        act_grad<kGelu>(p[i], y, d);
+                    v[i] = i < have ? v[i] * d : 0.f;
+                }
+            }
+            if (dz != nullptr) store8(dz + m * pitch + n, 8, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        }
+    }
+    if (sums == nullptr) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[g][8 * l + i] = sum[i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < 8 * LANES; c += 256) {
+        const int64_t column = static_cast<int64_t>(blockIdx.x) * LANES * 8 + c;
+        if (column >= N) break;
+        float s = 0.f;
+#pragma unroll 8
+        for (int k = 0; k < kAtOnce; ++k) s += part[k][c];
+        sums[static_cast<int64_t>(blockIdx.y) * N + column] = s;
+    }
+}
+
+// The workgroups' sums of a column added in a fixed order: 64 columns a workgroup, its waves every fourth row.
+__global__ __launch_bounds__(256) void linear_db_kernel(const float* __restrict__ sums, int64_t rows, int64_t N,
+                                                        float* __restrict__ db) {
+    __shared__ float part[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+    float s = 0.f;
+    if (n < N) {
+#pragma unroll 8
+        for (int64_t r = wave; r < rows; r += 4) s += sums[r * N + n];
+    }
+    part[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && n < N) db[n] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void linear_zero_kernel(T* p, int64_t n) {
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * 256;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += stride) p[i] = 0;
+}
+
+// of 256 threads, for kernels that walk what is left
+dim3 walking(int64_t threads) {
+    const int64_t blocks = (threads + 255) / 256;
+    return dim3(static_cast<unsigned>(blocks < kMostBlocks ? blocks : kMostBlocks));
+}
+int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+// whether the products can read these rows as they are
+bool rows_fit(const void* p, int64_t K, int64_t ld) {
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && K % 8 == 0 && ld % 8 == 0 && 2 * ld <= kMostRowBytes;
+}
+hipError_t copy_rows(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K, hipStream_t stream) {
+    const int64_t pitch = up(K, 64);
+    hipLaunchKernelGGL(copy_rows_kernel, walking(R * (pitch / 8)), dim3(256), 0, stream, static_cast<const uint16_t*>(x),
+                       ldx, out, R, K, pitch);
+    return hipGetLastError();
+}
+
+// What a product of [M][N] outputs over `steps` steps takes: the tile (0: the few-rows kernel) and the slices of its sum.
+struct Shape {
+    int tile;
+    int64_t slices, per;  // `per` steps each
+    size_t bytes(int64_t M, int64_t N) const { return slices > 1 ? static_cast<size_t>(slices * M * N) * sizeof(float) : 0; }
+};
+// Slices where the tiles leave CUs idle: so many that all have work, of at least 8 steps (a slice's start and end take
+// about as long as four).  `grain`: a slice's steps are a multiple of it.
+Shape shape_of(bool few, const TileCosts& costs, int64_t M, int64_t N, int64_t steps, int64_t grain) {
+    Shape s{0, 1, steps};
+    int64_t tiles = (N + 15) / 16;
+    if (!few) {
+        s.tile = product_tile(costs, M, N);
+        tiles = tiles_of(M, N, s.tile, s.tile);
+    }
+    int64_t slices = 512 / (tiles > 0 ? tiles : 1);
+    if (slices > steps / 8) slices = steps / 8;
+    if (slices > 1) {
+        s.per = up((steps + slices - 1) / slices, grain);
+        s.slices = (steps + s.per - 1) / s.per;
+    }
+    return s;
+}
+
+template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX>
+hipError_t launch_tile(GemmArgs g, const LinearOut& o, int64_t slices, hipStream_t stream) {
+    using Tile = LinearTile<E, PN, PM, WN, WM, NS, KW, KX>;
+    const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
+    if (tm * tn > kMostTiles) return hipErrorInvalidValue;
+    g.tiles_m = static_cast<int>(tm);
+    g.tiles_n = static_cast<int>(tn);
+    constexpr auto kernel = linear_kernel<E, PN, PM, WN, WM, NS, KW, KX>;
+    const hipError_t e = raise_lds_limit<kernel>();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn), static_cast<unsigned>(slices)), dim3(Tile::kThreads),
+                       Tile::kAllLds, stream, g, o);
+    return hipGetLastError();
+}
+
+template <class E, bool KW, bool KX>
+hipError_t launch_tiles(int tile, const GemmArgs& g, const LinearOut& o, int64_t slices, hipStream_t stream) {
+    if constexpr (E::kScaled) {
+        switch (tile) {
+            case 256: return launch_tile<E, 128, 64, 2, 4, 2, KW, KX>(g, o, slices, stream);
+            case 128: return launch_tile<E, 64, 64, 2, 2, 2, KW, KX>(g, o, slices, stream);
+            default: return launch_tile<E, 32, 32, 2, 2, 4, KW, KX>(g, o, slices, stream);
+        }
+    } else {
+        switch (tile) {
+            case 256: return launch_tile<E, 128, 64, 2, 4, 2, KW, KX>(g, o, slices, stream);
+            case 128: return launch_tile<E, 64, 32, 2, 4, 2, KW, KX>(g, o, slices, stream);
+            default: return launch_tile<E, 32, 32, 2, 2, 4, KW, KX>(g, o, slices, stream);
+        }
+    }
+}
+
+template <class E>
+hipError_t launch_few(const GemmArgs& g, int64_t row_bytes, const LinearOut& o, int64_t slices, hipStream_t stream) {
+    const int64_t blocks = (g.N + 15) / 16;
+    if (blocks > kMostTiles) return hipErrorInvalidValue;
+    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(slices)), threads(64 * kSkinnyWaves);
+    if (g.M <= 16)
+        hipLaunchKernelGGL((linear_skinny_kernel<E, 1>), grid, threads, 0, stream, g, row_bytes, o);
+    else if (g.M <= 32)
+        hipLaunchKernelGGL((linear_skinny_kernel<E, 2>), grid, threads, 0, stream, g, row_bytes, o);
+    else
+        hipLaunchKernelGGL((linear_skinny_kernel<E, 4>), grid, threads, 0, stream, g, row_bytes, o);
+    return hipGetLastError();
+}
+
+// The product, its slices in `partial`, and what follows.
+template <class E, bool KW, bool KX>
+hipError_t product(const Shape& s, GemmArgs g, int64_t row_bytes, LinearOut o, float* partial, hipStream_t stream) {
+    o.partial = s.slices > 1 ? partial : nullptr;
+    o.slice = static_cast<int>(s.per);
+    hipError_t e;
+    if (s.tile > 0) {
+        e = launch_tiles<E, KW, KX>(s.tile, g, o, s.slices, stream);
+    } else {
+        if constexpr (KW)
+            e = hipErrorInvalidValue;
+        else
+            e = launch_few<E>(g, row_bytes, o, s.slices, stream);
+    }
+    if (e != hipSuccess || s.slices == 1) return e;
+    hipLaunchKernelGGL(linear_join_kernel, walking(g.M * ((g.N + 7) / 8)), dim3(256), 0, stream, o,
+                       static_cast<int>(s.slices), g.M, g.N);
+    return hipGetLastError();
+}
+
+// As the 8-bit product's rule, measured there.
+bool few_rows(int64_t M, int64_t N, int64_t K) { return M <= 32 || (M <= kSkinnyRows && N <= 2 * K); }
+
+Shape forward_shape(int64_t M, int64_t K, int64_t N) {
+    return shape_of(few_rows(M, N, K), kPlain16, M, N, (K + 63) / 64, 1);
+}
+Shape forward8_shape(int64_t M, int64_t K, int64_t N) {
+    return shape_of(few_rows(M, N, K), kPlain8, M, N, (K + 127) / 128, 4);
+}
+// of dx, and of dw
+Shape dx_shape(int64_t M, int64_t K, int64_t N) { return shape_of(false, kPlain16, M, K, (N + 63) / 64, 1); }
+Shape dw_shape(int64_t M, int64_t K, int64_t N) { return shape_of(false, kPlain16, N, K, (M + 63) / 64, 1); }
+
+LinearOut out_of(const LinearArgs& a) {
+    return LinearOut{a.act, a.dtype == SPINGTP_FP32, a.bias, a.r, a.ldr, a.y, a.ldy, static_cast<uint16_t*>(a.z),
+                     nullptr, 0};
+}
+
+// lanes of a row of dz, and how many rows a workgroup takes
+int dz_lanes(int64_t N) { return N > 256 ? 64 : (N > 64 ? 32 : 8); }
+int64_t dz_rows(int64_t M, int64_t N) {
+    const int lanes = dz_lanes(N), at_once = 256 / lanes;
+    const int64_t across = (up(N, 64) / 8 + lanes - 1) / lanes;
+    int64_t blocks = 1024 / across;
+    if (blocks < 1) blocks = 1;
+    const int64_t rows = up((M + blocks - 1) / blocks, 4 * at_once);
+    return rows < int64_t{1} << 31 ? rows : int64_t{1} << 31;
+}
+int64_t dz_blocks(int64_t M, int64_t N) {
+    const int64_t rows = dz_rows(M, N);
+    return (M + rows - 1) / rows;
+}
+bool own_dz(const LinearBwdArgs& a) {
+    return a.act == kIdentity && a.dtype == SPINGTP_BF16 && rows_fit(a.dy, a.N, a.lddy);
+}
+
+template <int LANES, typename TD>
+hipError_t launch_dz(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+    const int64_t pitch = up(a.N, 64), across = (pitch / 8 + LANES - 1) / LANES;
+    hipLaunchKernelGGL((linear_dz_kernel<LANES, TD>),
+                       dim3(static_cast<unsigned>(across), static_cast<unsigned>(dz_blocks(a.M, a.N))), dim3(256), 0, stream,
+                       a.act, static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z), dz, pitch, sums, a.M,
+                       a.N, dz_rows(a.M, a.N));
+    return hipGetLastError();
+}
+template <typename TD>
+hipError_t make_dz(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+    switch (dz_lanes(a.N)) {
+        case 64: return launch_dz<64, TD>(a, dz, sums, stream);
+        case 32: return launch_dz<32, TD>(a, dz, sums, stream);
+        default: return launch_dz<8, TD>(a, dz, sums, stream);
+    }
+}
+template <typename T>
+hipError_t zero(void* p, int64_t n, hipStream_t stream) {
+    hipLaunchKernelGGL(linear_zero_kernel<T>, walking(n), dim3(256), 0, stream, static_cast<T*>(p), n);
+    return hipGetLastError();
+}
+size_t larger(size_t a, size_t b) { return a > b ? a : b; }
+size_t up16(size_t n) { return (n + 15) / 16 * 16; }
+
+}  // namespace
+
+size_t linear_workspace(const void* x, int64_t ldx, const void* w, int64_t ldw, int64_t M, int64_t K, int64_t N) {
+    const Shape s = forward_shape(M, K, N);
+    const size_t row = static_cast<size_t>(up(K, 64)) * 2;
+    size_t n = s.bytes(M, N);
+    if (s.tile > 0) n = up16(n) + (rows_fit(x, K, ldx) ? 0 : M * row) + (rows_fit(w, K, ldw) ? 0 : N * row);
+    return n;
+}
+
+hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
+    const Shape s = forward_shape(a.M, a.K, a.N);
+    GemmArgs g{};
+    g.M = a.M;
+    g.N = a.N;
+    g.x = static_cast<const uint8_t*>(a.x);
+    g.w = static_cast<const uint8_t*>(a.w);
+    g.ldx = 2 * a.ldx;
+    g.ldw = 2 * a.ldw;
+    g.steps = static_cast<int>((a.K + 63) / 64);
+    g.tail = static_cast<int>(up(a.K, 8) * 2 - (g.steps - 1) * static_cast<int64_t>(kStepBytes));
+    if (s.tile > 0) {
+        const int64_t pitch = up(a.K, 64);
+        uint16_t* free_at = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(a.workspace) + up16(s.bytes(a.M, a.N)));
+        if (!rows_fit(a.x, a.K, a.ldx)) {
+            const hipError_t e = copy_rows(a.x, a.ldx, free_at, a.M, a.K, stream);
+            if (e != hipSuccess) return e;
+            g.x = reinterpret_cast<const uint8_t*>(free_at);
+            g.ldx = 2 * pitch;
+            free_at += a.M * pitch;
+        }
+        if (!rows_fit(a.w, a.K, a.ldw)) {
+            const hipError_t e = copy_rows(a.w, a.ldw, free_at, a.N, a.K, stream);
+            if (e != hipSuccess) return e;
+            g.w = reinterpret_cast<const uint8_t*>(free_at);
+            g.ldw = 2 * pitch;
+        }
+    }
+    return product<Bf16, false, false>(s, g, 2 * a.K, out_of(a), static_cast<float*>(a.workspace), stream);
+}
+
+size_t linear8_workspace(int64_t M, int64_t K, int64_t N) { return forward8_shape(M, K, N).bytes(M, N); }
+
+hipError_t launch_linear8(const LinearArgs& a, hipStream_t stream) {
+    GemmArgs g{};
+    g.M = a.M;
+    g.N = a.N;
+    g.x = static_cast<const uint8_t*>(a.x);
+    g.w = static_cast<const uint8_t*>(a.w);
+    g.ldx = g.ldw = block8_pitch(a.K);
+    g.xs = a.x_scales;
+    g.ws = a.w_scales;
+    g.lds = block8_scale_pitch(a.K);
+    g.steps = static_cast<int>(g.ldx / kStepBytes);
+    g.tail = kStepBytes;
+    return product<Fp8, false, false>(forward8_shape(a.M, a.K, a.N), g, 0, out_of(a), static_cast<float*>(a.workspace),
+                                      stream);
+}
+
+// dz, then the sums of its columns, then what a product needs: the slices' sums and a copy of w or x
+size_t linear_backward_workspace(const LinearBwdArgs& a) {
+    const size_t row = static_cast<size_t>(up(a.K, 64)) * 2;
+    const size_t dx = a.dx == nullptr ? 0
+                                      : up16(dx_shape(a.M, a.K, a.N).bytes(a.M, a.K)) +
+                                            (rows_fit(a.w, a.K, a.ldw) ? 0 : static_cast<size_t>(a.N) * row);
+    const size_t dw = a.dw == nullptr ? 0
+                                      : up16(dw_shape(a.M, a.K, a.N).bytes(a.N, a.K)) +
+                                            (rows_fit(a.x, a.K, a.ldx) ? 0 : static_cast<size_t>(a.M) * row);
+    const size_t dz = own_dz(a) ? 0 : static_cast<size_t>(a.M * up(a.N, 64)) * 2;
+    const size_t sums = a.db == nullptr ? 0 : static_cast<size_t>(dz_blocks(a.M, a.N) * a.N) * sizeof(float);
+    return dz + up16(sums) + larger(dx, dw);
+}
+
+hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
+    if (a.M == 0) {
+        hipError_t e = hipSuccess;
+        if (a.dw != nullptr)
+            e = a.w_dtype == SPINGTP_FP32 ? zero<float>(a.dw, a.N * a.K, stream) : zero<uint16_t>(a.dw, a.N * a.K, stream);
+        if (e == hipSuccess && a.db != nullptr) e = zero<float>(a.db, a.N, stream);
+        return e;
+    }
+    const int64_t np = up(a.N, 64), kp = up(a.K, 64);
+    const bool own = own_dz(a);
+    uint8_t* at = static_cast<uint8_t*>(a.workspace);
+    uint16_t* dz = own ? nullptr : reinterpret_cast<uint16_t*>(at);
+    if (!own) at += 2 * a.M * np;
+    float* sums = a.db != nullptr ? reinterpret_cast<float*>(at) : nullptr;
+    if (a.db != nullptr) at += up16(static_cast<size_t>(dz_blocks(a.M, a.N) * a.N) * sizeof(float));
+    hipError_t e = hipSuccess;
+    if (!own || sums != nullptr)
+        e = a.dtype == SPINGTP_FP32 ? make_dz<float>(a, dz, sums, stream) : make_dz<uint16_t>(a, dz, sums, stream);
+    if (e == hipSuccess && sums != nullptr) {
+        hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>((a.N + 63) / 64)), dim3(256), 0, stream, sums,
+                           dz_blocks(a.M, a.N), a.N, a.db);
+        e = hipGetLastError();
+    }
+    const uint8_t* from = own ? static_cast<const uint8_t*>(a.dy) : reinterpret_cast<const uint8_t*>(dz);
+    const int64_t ldz = 2 * (own ? a.lddy : np);
+    if (e == hipSuccess && a.dx != nullptr) {
+        const Shape s = dx_shape(a.M, a.K, a.N);
+        GemmArgs g{};
+        g.x = from;
+        g.ldx = ldz;
+        g.w = static_cast<const uint8_t*>(a.w);
+        g.ldw = 2 * a.ldw;
+        if (!rows_fit(a.w, a.K, a.ldw)) {
+            uint16_t* copy = reinterpret_cast<uint16_t*>(at + up16(s.bytes(a.M, a.K)));
+            e = copy_rows(a.w, a.ldw, copy, a.N, a.K, stream);
+            g.w = reinterpret_cast<const uint8_t*>(copy);
+            g.ldw = 2 * kp;
+        }
+        g.w2 = g.w;
+        g.M = a.M;
+        g.N = a.K;
+        g.steps = static_cast<int>(np / 64);
+        g.tail = own ? static_cast<int>(2 * a.N - (g.steps - 1) * static_cast<int64_t>(kStepBytes)) : kStepBytes;
+        g.w_rows = a.N;
+        g.w_split = g.steps;
+        const LinearOut o{kIdentity, false, nullptr, nullptr, 0, a.dx, a.lddx, nullptr, nullptr, 0};
+        if (e == hipSuccess) e = product<Bf16, true, false>(s, g, 0, o, reinterpret_cast<float*>(at), stream);
+    }
+    if (e == hipSuccess && a.dw != nullptr) {
+        const Shape s = dw_shape(a.M, a.K, a.N);
+        GemmArgs g{};
+        g.w = static_cast<const uint8_t*>(a.x);
+        g.ldw = 2 * a.ldx;
+        if (!rows_fit(a.x, a.K, a.ldx)) {
+            uint16_t* copy = reinterpret_cast<uint16_t*>(at + up16(s.bytes(a.N, a.K)));
+            e = copy_rows(a.x, a.ldx, copy, a.M, a.K, stream);
+            g.w = reinterpret_cast<const uint8_t*>(copy);
+            g.ldw = 2 * kp;
+        }
+        g.w2 = g.w;
+        g.x = from;
+        g.ldx = ldz;
+        g.M = a.N;
+        g.N = a.K;
+        g.steps = static_cast<int>((a.M + 63) / 64);
+        g.tail = kStepBytes;
+        g.w_rows = g.x_rows = a.M;
+        g.w_split = g.steps;
+        const LinearOut o{kIdentity, a.w_dtype == SPINGTP_FP32, nullptr, nullptr, 0, a.dw, a.K, nullptr, nullptr, 0};
+        if (e == hipSuccess) e = product<Bf16, true, true>(s, g, 0, o, reinterpret_cast<float*>(at), stream);
+    }
+    return e;
+}
+
+}  // namespace spingtp

@@ -1,4 +1,4 @@
-"""The feed-forward operators of ``include/spingtp.h``: norm, 8-bit blocks, 8-bit product, gated block.
+"""The feed-forward operators of ``include/spingtp.h``: norm, 8-bit blocks, 8-bit product, gated block, linear layer.
 
 Argument checks, outputs and the calls are in ``csrc/binding.cpp``, every step of the computation in the HIP
 kernels of ``libspingtp.so``.  Matrices are 2-D device tensors whose rows are contiguous (``stride(1) == 1``),
@@ -19,6 +19,8 @@ from . import _lib
 
 _ACTS = {"silu": 0, "gelu": 1}
 _SAVES = {None: 0, "same": 1, "8bit": 2}
+_LINEAR_ACTS = {**_ACTS, None: 2}
+_LINEAR_SAVES = {None: False, "same": True}
 _TRANSPOSE = {False: 0, True: 1, "both": 2}
 _DTYPES = {torch.float32: False, torch.bfloat16: True}
 
@@ -27,7 +29,9 @@ _BINDING_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_bindi
 _ENTRIES = ("spingtp_pack8", "spingtp_unpack8", "spingtp_rms_norm", "spingtp_rms_norm_backward",
             "spingtp_rms_norm_backward_workspace_size", "spingtp_matmul8", "spingtp_gated_forward",
             "spingtp_gated_forward_workspace_size", "spingtp_gated_forward8", "spingtp_gated_forward8_workspace_size",
-            "spingtp_gated_backward", "spingtp_gated_backward_workspace_size")
+            "spingtp_gated_backward", "spingtp_gated_backward_workspace_size", "spingtp_linear_forward",
+            "spingtp_linear_forward_workspace_size", "spingtp_linear_forward8", "spingtp_linear_forward8_workspace_size",
+            "spingtp_linear_backward", "spingtp_linear_backward_workspace_size")
 
 
 def _load():
@@ -241,3 +245,42 @@ def gated_backward(grad_h, saved, w_gate, w_up, need_x=True, need_w=True):
     if grad_w is None:
         return grad_x, None, None
     return (grad_x, *grad_w.chunk(2))
+
+
+class LinearSaved:
+    """What ``linear`` keeps for ``linear_backward``: ``x`` [M, K] as it is and, where there is an activation ``act``,
+    ``z`` [M, N], x w^T + bias in bf16."""
+
+    __slots__ = ("x", "z", "act")
+
+    def __init__(self, x, z=None, act=None):
+        self.x, self.z, self.act = x, z, act
+
+
+@_on_stream
+def linear(x, w, bias=None, act=None, residual=None, save=None, dtype=torch.bfloat16, out=None):
+    """spingtp_linear_forward / spingtp_linear_forward8: (y [M, N], saved) with y = act(x w^T + bias) + residual.
+
+    x [M, K] and w [N, K] in bf16 (any alignment; rows that do not start and end on 16 bytes are copied) or, for
+    inference, both Block8; bias [N] fp32; act None, ``"silu"`` or ``"gelu"``; residual and y of ``dtype``, bf16 or fp32.
+    ``save="same"`` (bf16) keeps what the backward pass needs; saved is None without it."""
+    code, keep = _choice(_LINEAR_ACTS, act, "act"), _choice(_LINEAR_SAVES, save, "save")
+    bf16 = _choice(_DTYPES, dtype, "dtype")
+    if isinstance(x, Block8):
+        if keep:
+            raise ValueError("save needs bf16 operands")
+        M, K = x.shape
+        pw = _block(w, "w", None, K)
+        return _run(_ops.linear8, x, x.values, x.scales, *pw, M, K, w.shape[0], bias, code, residual, bf16, out), None
+    y, z = _run(_ops.linear, x, x, w, bias, code, residual, keep, bf16, out)
+    return y, LinearSaved(x, z, act) if keep else None
+
+
+@_on_stream
+def linear_backward(grad_y, saved, w, need_x=True, need_w=True, need_bias=True, dtype=torch.bfloat16):
+    """spingtp_linear_backward: (grad_x [M, K] bf16, grad_w [N, K] of ``dtype``, grad_bias [N] fp32), None where not
+    needed.  grad_y is bf16 or fp32; it is also the residual's gradient."""
+    if not isinstance(saved, LinearSaved):
+        raise ValueError("saved must be what linear returned with save, or a LinearSaved")
+    return _run(_ops.linear_backward, grad_y, grad_y, saved.x, saved.z, _choice(_LINEAR_ACTS, saved.act, "saved.act"), w,
+                need_x, need_w, need_bias, _choice(_DTYPES, dtype, "dtype"))
