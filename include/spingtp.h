@@ -821,6 +821,77 @@ spingtp_status spingtp_linear_backward_workspace_size(int act, int dtype, const 
                                                       const void* grad_w, const float* grad_bias, int64_t M, int64_t K,
                                                       int64_t N, size_t* size);
 
+/*
+ * ---------------------------------------------------------------------------------------------
+ * Operators of a training step around the layers.  As the feed-forward operators: no plan, the current device and
+ * the given stream, nothing allocated and nothing waited for.  Matrices have at most 2^46 elements and 33553920
+ * columns, an index n <= 2^31 - 1 entries (index_bytes 8: int64, 4: int32), a table 1 <= V <= 2^31 - 2 rows.
+ * An entry of an index outside [0, V) names no row: the lookup gives zeros, the gradient adds it to nothing.
+ */
+
+/* out [n][D], out[i] = scale table[index[i]], table [V][D] and out of dtype. */
+spingtp_status spingtp_embedding(int dtype, const void* table, int64_t ldt, const void* index, int index_bytes, float scale,
+                                 void* out, int64_t ldo, int64_t n, int64_t V, int64_t D, void* stream);
+
+/* An index in the order of its rows: order [n] its places, equal rows in their own order, and rows [n] what they
+ * name (V: none, at the end).  For the gradients of as many lookups as take the index.  workspace (16-byte
+ * aligned): the size below, 0 up to 8192 entries. */
+spingtp_status spingtp_sort_index(const void* index, int index_bytes, int32_t* order, int32_t* rows, void* workspace,
+                                  size_t workspace_bytes, int64_t n, int64_t V, void* stream);
+spingtp_status spingtp_sort_index_workspace_size(int64_t n, int64_t V, size_t* size);
+
+/* grad_table [V][D] of table_dtype, grad_table[v] = scale sum over {i: index[i] = v} of grad[i] (zeros where there is no
+ * such i), from grad [n][D] of dtype and what spingtp_sort_index made of the index.  Sums are fp32, in the same
+ * order in every call.  workspace (16-byte aligned): the size below. */
+spingtp_status spingtp_embedding_backward(int dtype, const void* grad, int64_t ldg, const int32_t* order,
+                                          const int32_t* rows, float scale, int table_dtype, void* grad_table,
+                                          int64_t ldt, void* workspace, size_t workspace_bytes, int64_t n, int64_t V,
+                                          int64_t D, void* stream);
+spingtp_status spingtp_embedding_backward_workspace_size(int64_t n, int64_t D, size_t* size);
+
+/*
+ * AdamW (decay apart from the gradient) over many tensors, in place:
+ *   g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   param = (1 - lr weight_decay) param - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps),
+ * in fp32, param rounded once (bf16: to nearest, so that a step below half of a weight's last place is lost; an fp32
+ * param with a bf16 copy keeps it).
+ * m and v are fp32 [n], or with m_scales and v_scales 8-bit blocks of a matrix [1][n] (16-byte aligned values) which
+ * hold m and sqrt(v); zeros to begin with.  A new m (v) goes to the lower or upper neighbour in its block's format by
+ * 16 random bits, such that the mean of m (of v) is kept, and there v is raised to (m / c)^2 where it is less,
+ * c = (1 - beta1) / sqrt((1 - beta2) (1 - beta1^2 / beta2)) (unless beta1^2 >= beta2): exact sums are never less.
+ * The bits of element i of tensor k of the list are the low half (m) and the high half (v) of
+ *   f(lo(i) A + hi(i) B + f(f(lo(seed) + k A) + step B + hi(seed))),  A = 0x9E3779B9, B = 0x3C6EF373, modulo 2^32,
+ * lo and hi the 32-bit halves, f: x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16.
+ * Not finite: NaN in its own place.
+ *
+ * step (1 for the first) and lr may be device memory instead, read when the step runs (a captured one): device_step (a
+ * value below 1 counts as 1), device_lr.  grad_scale: NULL or one fp32 number in device memory.
+ * Tensors that are written (param, m, v, scales, copy) must not overlap one another or a gradient.
+ * The two structures are read before the call returns.
+ */
+typedef struct {
+    void* param;      /* [n] of param_dtype */
+    const void* grad; /* [n] of grad_dtype */
+    void* m;
+    void* v;
+    void* m_scales; /* NULL: m and v are fp32 */
+    void* v_scales;
+    void* copy; /* NULL or bf16 [n]: the new param rounded; with an fp32 param only */
+    int64_t n;
+    int param_dtype;
+    int grad_dtype;
+} spingtp_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay; /* 0 <= beta < 1, eps >= 0, all finite */
+    int64_t step;
+    const int64_t* device_step;
+    const float* device_lr;
+    const float* grad_scale;
+    uint64_t seed;
+} spingtp_adamw_options;
+spingtp_status spingtp_adamw(const spingtp_adamw_tensor* tensors, int64_t count, const spingtp_adamw_options* options,
+                             void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -2,7 +2,8 @@
 
 ``Plan`` wraps ``spingtp_plan_create`` / ``spingtp_forward`` (``include/spingtp.h``).
 ``rms_norm``, ``matmul8``, ``gated``, ``linear``, ``pack8`` and their kin are the feed-forward operators on
-invariant channels (``feedforward``), ``Block8`` their 8-bit block format.
+invariant channels (``feedforward``), ``Block8`` their 8-bit block format; ``embedding``, ``sort_index``, ``adamw`` and
+theirs the operators of a training step around the layers (``training``).
 ``workloads`` holds the seeded synthetic input generators.
 """
 
@@ -11,6 +12,7 @@ from .spingtp import Plan, plan_tables_host, dense_tensor_host, mfma_operands_ho
 
 _FEEDFORWARD = ("Block8", "GatedSaved", "pack8", "unpack8", "rms_norm", "rms_norm_backward", "matmul8",
                 "matmul8_backward", "gated", "gated_backward", "LinearSaved", "linear", "linear_backward")
+_TRAINING = ("SortedIndex", "sort_index", "embedding", "embedding_backward", "adamw", "adamw_state")
 
 
 def __getattr__(name):  # torch is imported with the first operator that needs it
@@ -18,11 +20,15 @@ def __getattr__(name):  # torch is imported with the first operator that needs i
         from . import feedforward
         globals().update({n: getattr(feedforward, n) for n in _FEEDFORWARD})
         return globals()[name]
+    if name in _TRAINING:
+        from . import training
+        globals().update({n: getattr(training, n) for n in _TRAINING})
+        return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted({*globals(), *_FEEDFORWARD})
+    return sorted({*globals(), *_FEEDFORWARD, *_TRAINING})
 
 
 # without the operators: what an import of all names asks of a machine is what the plans need

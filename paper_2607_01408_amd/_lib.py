@@ -26,7 +26,9 @@ EXPORTED = ("spingtp_plan_create", "spingtp_forward", "spingtp_plan_destroy", "s
             "spingtp_gated_forward", "spingtp_gated_forward_workspace_size", "spingtp_gated_forward8",
             "spingtp_gated_forward8_workspace_size", "spingtp_gated_backward", "spingtp_gated_backward_workspace_size", "spingtp_linear_forward",
             "spingtp_linear_forward_workspace_size", "spingtp_linear_forward8", "spingtp_linear_forward8_workspace_size",
-            "spingtp_linear_backward", "spingtp_linear_backward_workspace_size")
+            "spingtp_linear_backward", "spingtp_linear_backward_workspace_size", "spingtp_embedding", "spingtp_sort_index",
+            "spingtp_sort_index_workspace_size", "spingtp_embedding_backward",
+            "spingtp_embedding_backward_workspace_size", "spingtp_adamw")
 
 _lib = None
 
@@ -158,7 +160,11 @@ def _feedforward_signatures(L):
                        ("spingtp_linear_forward8", "ipppppipnpnpznnnp"),
                        ("spingtp_linear_forward8_workspace_size", "nnns"),
                        ("spingtp_linear_backward", "iipnppnpnpnipppznnnp"),
-                       ("spingtp_linear_backward_workspace_size", "iipnpnpnpppnnns")):
+                       ("spingtp_linear_backward_workspace_size", "iipnpnpnpppnnns"),
+                       ("spingtp_embedding", "ipnpifpnnnnp"), ("spingtp_sort_index", "pipppznnp"),
+                       ("spingtp_sort_index_workspace_size", "nns"),
+                       ("spingtp_embedding_backward", "ipnppfipnpznnnp"),
+                       ("spingtp_embedding_backward_workspace_size", "nns"), ("spingtp_adamw", "pnpp")):
         fn = getattr(L, name)
         fn.argtypes = [kinds[a] for a in args]
         fn.restype = ctypes.c_int

@@ -1,4 +1,4 @@
-// The feed-forward operators as Python functions on torch tensors: argument checks, outputs and workspaces
+// The feed-forward and the training step's operators as Python functions on torch tensors: argument checks, outputs and workspaces
 // from torch's allocator, and the call of the C entry point, in one C function each.  (Through ctypes and
 // torch's Python functions the same steps took 9 to 16 us a call, several times the kernels' own time for a
 // single token.)  Every step of the computation is in libspingtp.so, whose entry points bind() is given.
@@ -10,12 +10,15 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <exception>
 #include <initializer_list>
 #include <stdexcept>
 #include <string>
+#include <tuple>
 #include <utility>
+#include <vector>
 
 #include "spingtp.h"
 
@@ -51,6 +54,12 @@ struct Entries {
     decltype(&spingtp_linear_forward8_workspace_size) linear_forward8_workspace_size;
     decltype(&spingtp_linear_backward) linear_backward;
     decltype(&spingtp_linear_backward_workspace_size) linear_backward_workspace_size;
+    decltype(&spingtp_embedding) embedding;
+    decltype(&spingtp_sort_index) sort_index;
+    decltype(&spingtp_sort_index_workspace_size) sort_index_workspace_size;
+    decltype(&spingtp_embedding_backward) embedding_backward;
+    decltype(&spingtp_embedding_backward_workspace_size) embedding_backward_workspace_size;
+    decltype(&spingtp_adamw) adamw;
 } lib;
 
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
@@ -526,6 +535,222 @@ PyObject* linear_backward(Args a) {
     return tuple({wrap(dx), wrap(dw), wrap(db)});
 }
 
+double number(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PythonError{};
+    return v;
+}
+
+// A contiguous [n] tensor of int64 or int32 on a device (`beside`: on its device).
+struct Index {
+    const at::Tensor* t;
+    const void* p;
+    int64_t n;
+    int bytes;
+    Index(PyObject* o, const char* name, const at::Tensor* beside) : t(&tensor(o, name)) {
+        const std::string text = name;
+        const at::ScalarType type = t->scalar_type();
+        if (type != at::kLong && type != at::kInt) throw Refused(text + " must be int64 or int32");
+        if (t->dim() != 1) throw Refused(text + " must be a 1-D tensor");
+        if (!t->is_cuda()) throw Refused(text + " must be on a GPU");
+        if (beside != nullptr && t->device() != beside->device())
+            throw Refused(text + " must be on the device of the other operands");
+        n = t->size(0);
+        if (n > 1 && t->stride(0) != 1) throw Refused(text + " must be contiguous");
+        bytes = type == at::kLong ? 8 : 4;
+        p = t->data_ptr();
+    }
+};
+
+// table, index, scale, stream -> out
+PyObject* embedding(Args a) {
+    const Matrix table = matrix(a[0], "table");
+    const Index index(a[1], "index", table.t);
+    const double scale = number(a[2]);
+    if (table.rows < 1 || table.columns < 1) throw Refused("the table is empty");
+    const at::Tensor out = empty({index.n, table.columns}, table.type, *table.t);
+    done(lib.embedding(dtype_of(table.type), table.p, table.ld, index.p, index.bytes, static_cast<float>(scale),
+                       out.data_ptr(), table.columns, index.n, table.rows, table.columns, stream_of(a[3])),
+         "spingtp_embedding");
+    return wrap(out);
+}
+
+// index sorted for a table of V rows: (order, rows)
+std::pair<at::Tensor, at::Tensor> sorted(const Index& index, int64_t V, void* stream) {
+    if (V < 1) throw Refused("V must be positive");
+    size_t bytes = 0;
+    done(lib.sort_index_workspace_size(index.n, V, &bytes), "spingtp_sort_index_workspace_size");
+    const at::Tensor order = empty({index.n}, at::kInt, *index.t), rows = empty({index.n}, at::kInt, *index.t);
+    const at::Tensor ws = workspace(bytes, *index.t);
+    done(lib.sort_index(index.p, index.bytes, order.data_ptr<int32_t>(), rows.data_ptr<int32_t>(), address(ws), bytes,
+                        index.n, V, stream),
+         "spingtp_sort_index");
+    return {order, rows};
+}
+
+// index, V, stream -> (order, rows)
+PyObject* sort_index(Args a) {
+    const Index index(a[0], "index", nullptr);
+    const auto pair = sorted(index, integer(a[1]), stream_of(a[2]));
+    return tuple({wrap(pair.first), wrap(pair.second)});
+}
+
+// grad, index | order, None | rows, V, scale, bf16 | None, stream -> [V, D]
+PyObject* embedding_backward(Args a) {
+    const Matrix grad = matrix(a[0], "grad");
+    const int64_t D = grad.columns, V = integer(a[3]);
+    if (D < 1) throw Refused("grad has no columns");
+    if (V < 1) throw Refused("V must be positive");
+    const Index index(a[1], "index", grad.t);
+    if (index.n != grad.rows)
+        throw Refused("index must have " + std::to_string(grad.rows) + " entries, not " + std::to_string(index.n));
+    const double scale = number(a[4]);
+    const at::ScalarType type = a[5] == Py_None ? grad.type : (truth(a[5]) ? at::kBFloat16 : at::kFloat);
+    void* stream = stream_of(a[6]);
+    at::Tensor order, rows;
+    if (a[2] == Py_None) {
+        std::tie(order, rows) = sorted(index, V, stream);
+    } else {
+        order = *index.t;
+        const Index second(a[2], "index.rows", grad.t);
+        rows = *second.t;
+        if (second.n != index.n || index.bytes != 4 || second.bytes != 4)
+            throw Refused("index.order and index.rows must be int32 [" + std::to_string(grad.rows) + "]");
+    }
+    size_t bytes = 0;
+    done(lib.embedding_backward_workspace_size(index.n, D, &bytes), "spingtp_embedding_backward_workspace_size");
+    const at::Tensor ws = workspace(bytes, *grad.t), out = empty({V, D}, type, *grad.t);
+    done(lib.embedding_backward(dtype_of(grad.type), grad.p, grad.ld, order.data_ptr<int32_t>(), rows.data_ptr<int32_t>(),
+                                static_cast<float>(scale), dtype_of(type), out.data_ptr(), D, address(ws), bytes, index.n,
+                                V, D, stream),
+         "spingtp_embedding_backward");
+    return wrap(out);
+}
+
+// The tensors of an AdamW step: of one device, contiguous, of `n` elements; and what memory they take.
+struct Places {
+    struct Range {
+        uintptr_t first, last;
+        bool written;
+    };
+    std::vector<Range> all;
+    const at::Tensor* beside = nullptr;
+
+    const at::Tensor& take(PyObject* o, const char* name, int64_t n, bool written) {
+        const at::Tensor& t = tensor(o, name);
+        if (!t.is_cuda()) throw Refused(std::string(name) + " must be on a GPU");
+        if (beside == nullptr) beside = &t;
+        if (t.device() != beside->device()) throw Refused("all tensors must be on one device");
+        if (!t.is_contiguous()) throw Refused(std::string(name) + " must be contiguous");
+        if (n >= 0 && t.numel() != n)
+            throw Refused(std::string(name) + " must have the param's " + std::to_string(n) + " elements, not " +
+                          std::to_string(t.numel()));
+        const auto p = reinterpret_cast<uintptr_t>(t.data_ptr());
+        if (t.numel() > 0) all.push_back({p, p + t.nbytes(), written});
+        return t;
+    }
+    // Refuses memory that is written and held by another as well.
+    void apart() {
+        std::sort(all.begin(), all.end(), [](const Range& x, const Range& y) { return x.first < y.first; });
+        uintptr_t any = 0, written = 0;  // the ends so far
+        for (const Range& r : all) {
+            if (r.first < (r.written ? any : written)) throw Refused("tensors that are written overlap others");
+            any = std::max(any, r.last);
+            if (r.written) written = std::max(written, r.last);
+        }
+    }
+};
+bool floating(at::ScalarType t) { return t == at::kFloat || t == at::kBFloat16; }
+
+// a list's items
+struct Items {
+    PyObject* const* at;
+    Py_ssize_t n;
+    Items(PyObject* o, const char* name, Py_ssize_t want) {
+        if (!PyList_Check(o)) throw Refused(std::string(name) + " must be a list");
+        n = PyList_GET_SIZE(o);
+        if (want >= 0 && n != want)
+            throw Refused(std::string(name) + " must have " + std::to_string(want) + " items, not " + std::to_string(n));
+        at = PySequence_Fast_ITEMS(o);
+    }
+};
+
+// A number of device memory, [1] or a scalar; null for None.
+template <typename T>
+const T* device_number(PyObject* o, const char* name, at::ScalarType type, const at::Tensor& beside) {
+    const at::Tensor& t = tensor(o, name);
+    if (t.scalar_type() != type || t.numel() != 1 || t.device() != beside.device())
+        throw Refused(std::string(name) + " must be one " + (type == at::kLong ? "int64" : "fp32") +
+                      " number beside the params");
+    return t.data_ptr<T>();
+}
+
+// params, grads, m, v (tensors or (values, scales, rows, columns)), copies | None, step, lr, beta1, beta2, eps, weight_decay,
+// grad_scale | None, seed, stream
+PyObject* adamw(Args a) {
+    const Items params(a[0], "params", -1), grads(a[1], "grads", params.n), m(a[2], "m", params.n), v(a[3], "v", params.n);
+    const bool some = a[4] != Py_None;
+    const Items copies(some ? a[4] : a[0], "copies", params.n);
+    std::vector<spingtp_adamw_tensor> list(static_cast<size_t>(params.n));
+    Places places;
+    places.all.reserve(7 * list.size());
+    for (Py_ssize_t i = 0; i < params.n; ++i) {
+        spingtp_adamw_tensor& to = list[static_cast<size_t>(i)];
+        const at::Tensor& p = places.take(params.at[i], "params", -1, true);
+        const int64_t n = p.numel();
+        const at::Tensor& g = places.take(grads.at[i], "grads", n, false);
+        if (!floating(p.scalar_type()) || !floating(g.scalar_type())) throw Refused("params and grads must be fp32 or bf16");
+        to = {p.data_ptr(), g.data_ptr(), nullptr, nullptr, nullptr, nullptr, nullptr, n, dtype_of(p.scalar_type()),
+              dtype_of(g.scalar_type())};
+        PyObject* const states[2] = {m.at[i], v.at[i]};
+        const char* const names[2] = {"m", "v"};
+        if (PyTuple_Check(states[0]) != PyTuple_Check(states[1])) throw Refused("m and v of a tensor must be of one kind");
+        for (int k = 0; k < 2; ++k) {
+            void*& values = k == 0 ? to.m : to.v;
+            if (PyTuple_Check(states[k])) {
+                if (PyTuple_GET_SIZE(states[k]) != 4 || integer(PyTuple_GET_ITEM(states[k], 2)) != 1 ||
+                    integer(PyTuple_GET_ITEM(states[k], 3)) != n)
+                    throw Refused(std::string(names[k]) + " must be a Block8 of shape (1, " + std::to_string(n) + ")");
+                values = places.take(PyTuple_GET_ITEM(states[k], 0), names[k], -1, true).data_ptr();
+                (k == 0 ? to.m_scales : to.v_scales) =
+                    places.take(PyTuple_GET_ITEM(states[k], 1), names[k], -1, true).data_ptr();
+            } else {
+                const at::Tensor& s = places.take(states[k], names[k], n, true);
+                if (s.scalar_type() != at::kFloat) throw Refused(std::string(names[k]) + " must be fp32 or a Block8");
+                values = s.data_ptr();
+            }
+        }
+        if (some && copies.at[i] != Py_None) {
+            const at::Tensor& c = places.take(copies.at[i], "copies", n, true);
+            if (c.scalar_type() != at::kBFloat16 || p.scalar_type() != at::kFloat)
+                throw Refused("copies must be bf16, of fp32 params");
+            to.copy = c.data_ptr();
+        }
+    }
+    places.apart();
+    spingtp_adamw_options o{};
+    if (THPVariable_Check(a[5]))
+        o.device_step = device_number<int64_t>(a[5], "step", at::kLong, *places.beside);
+    else if ((o.step = integer(a[5])) < 1)
+        throw Refused("step must be 1 or more");
+    if (THPVariable_Check(a[6]))
+        o.device_lr = device_number<float>(a[6], "lr", at::kFloat, *places.beside);
+    else
+        o.lr = number(a[6]);
+    o.beta1 = number(a[7]);
+    o.beta2 = number(a[8]);
+    o.eps = number(a[9]);
+    o.weight_decay = number(a[10]);
+    if (!(o.beta1 >= 0 && o.beta1 < 1 && o.beta2 >= 0 && o.beta2 < 1)) throw Refused("betas must be in [0, 1)");
+    if (!(o.eps >= 0)) throw Refused("eps must not be negative");
+    if (a[11] != Py_None) o.grad_scale = device_number<float>(a[11], "grad_scale", at::kFloat, *places.beside);
+    o.seed = PyLong_AsUnsignedLongLongMask(a[12]);
+    if (PyErr_Occurred()) throw PythonError{};
+    done(lib.adamw(list.data(), params.n, &o, stream_of(a[13])), "spingtp_adamw");
+    for (Py_ssize_t i = 0; i < params.n; ++i) tensor(params.at[i], "params").unsafeGetTensorImpl()->bump_version();
+    Py_RETURN_NONE;
+}
+
 // ---------------------------------------------------------------- module
 
 template <PyObject* (*OP)(Args), Py_ssize_t N>
@@ -577,6 +802,10 @@ PyMethodDef methods[] = {OP(bind, 2),
                          OP(linear, 9),
                          OP(linear8, 13),
                          OP(linear_backward, 10),
+                         OP(embedding, 4),
+                         OP(sort_index, 3),
+                         OP(embedding_backward, 7),
+                         OP(adamw, 14),
                          {nullptr, nullptr, 0, nullptr}};
 #undef OP
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,298 @@
+// Lookup of a table's rows and its gradient:
+//   out[i] = scale table[index[i]],   dtable[v] = scale sum over {i: index[i] = v} of dout[i].
+//
+// Forward: a row's columns over the lanes of a group, 16 or 32 bytes each; bound by memory, and for few rows by latency.
+//
+// Backward: over the index in sorted order (sort_index.hip), cut into chunks of equal length whatever the rows' numbers
+// of entries: a group of lanes walks its chunk and keeps the running sum of a row in fp32.  A row whose entries lie in
+// one chunk leaves at once; a row that crosses chunks leaves a part in each, and a second kernel adds the parts in
+// order.  So one row with all entries costs no more than many with a few, every row of the result is written once, and
+// no step depends on the order of arrival.  The rows without entries are zeroed by workgroups of the same launch: a lane
+// looks for its row by bisection.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "block8.h"
+#include "internal.h"
+#include "training.h"
+
+namespace spingtp {
+namespace {
+
+// -1: no row of the table
+__device__ __forceinline__ int64_t row_of(const void* index, bool wide, int64_t i, int64_t V) {
+    const int64_t k = wide ? static_cast<const int64_t*>(index)[i] : static_cast<const int32_t*>(index)[i];
+    return k >= 0 && k < V ? k : -1;
+}
+
+// LANES lanes of eight columns to a row, ROWS rows to a group.
+template <int LANES, int ROWS, typename T>
+__global__ __launch_bounds__(256) void embedding_kernel(const T* __restrict__ table, int64_t ldt, const void* index,
+                                                        bool wide, float scale, T* __restrict__ out, int64_t ldo, int64_t n,
+                                                        int64_t V, int64_t D) {
+    constexpr int kGroups = 256 / LANES;
+    const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
+    const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8;
+    if (c >= D) return;
+    const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
+    for (int64_t first = (static_cast<int64_t>(blockIdx.x) * kGroups + g) * ROWS; first < n;
+         first += static_cast<int64_t>(gridDim.x) * kGroups * ROWS) {
+        int64_t row[ROWS];
+        float v[ROWS][8];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) row[r] = first + r < n ? row_of(index, wide, first + r, V) : -1;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) load8(table + (row[r] < 0 ? 0 : row[r] * ldt + c), row[r] < 0 ? 0 : have, v[r]);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[r][i] *= scale;
+            if (first + r < n) store8(out + (first + r) * ldo + c, have, v[r]);
+        }
+    }
+}
+
+// the first place in the sorted rows whose row is `row` or more
+__device__ __forceinline__ int64_t place_from(const int32_t* rows, int64_t n, int32_t row) {
+    int64_t lo = 0, hi = n;
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (rows[mid] < row)
+            lo = mid + 1;
+        else
+            hi = mid;
+    }
+    return lo;
+}
+
+constexpr int kAhead = 4;  // rows in flight
+
+// Workgroups 0 to sum_blocks - 1: chunks of `chunk` entries, one to a group.  partial [chunks][2][D]: the part of a row that
+// began in an earlier chunk, and of one that begins here and goes on.  The others: 256 rows of the table each.
+template <int LANES, typename TG, typename TO>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict__ grad, int64_t ldg,
+                                                            const int32_t* __restrict__ order,
+                                                            const int32_t* __restrict__ rows, float scale,
+                                                            TO* __restrict__ out, int64_t ldo, float* __restrict__ partial,
+                                                            int64_t n, int64_t V, int64_t D, int64_t chunk,
+                                                            unsigned sum_blocks) {
+    constexpr int kGroups = 256 / LANES;
+    if (blockIdx.x >= sum_blocks) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int64_t first = static_cast<int64_t>(blockIdx.x - sum_blocks) * 256 + 64 * wave, mine = first + lane;
+        bool empty = false;
+        if (mine < V) {
+            const int64_t at = place_from(rows, n, static_cast<int32_t>(mine));
+            empty = at >= n || rows[at] != mine;
+        }
+        const int64_t c0 = static_cast<int64_t>(blockIdx.y) * LANES * 8, c1 = c0 + LANES * 8 < D ? c0 + LANES * 8 : D;
+        const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        constexpr int kAtOnce = 64 / LANES;
+        uint64_t left = __ballot(empty);
+        // kAtOnce empty rows at a time, LANES lanes to each
+        while (left != 0) {
+            int64_t row = -1;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                if (left == 0) break;
+                const int b = __builtin_ctzll(left);
+                left &= left - 1;
+                if (lane / LANES == k) row = first + b;
+            }
+            const int64_t c = c0 + (lane % LANES) * 8;
+            if (row >= 0 && c < c1) store8(out + row * ldo + c, c1 - c >= 8 ? 8 : static_cast<int>(c1 - c), zeros);
+        }
+        return;
+    }
+    const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
+    const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8;
+    const int64_t k = static_cast<int64_t>(blockIdx.x) * kGroups + g, p0 = k * chunk;
+    if (c >= D || p0 >= n) return;
+    const int64_t p1 = p0 + chunk < n ? p0 + chunk : n;
+    const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
+    float sum[8];
+    const uint32_t most = static_cast<uint32_t>(n - 1);
+    int32_t row = rows[p0];
+    bool before = p0 > 0 && rows[p0 - 1] == row;
+    const bool after = p1 < n && rows[p1] == rows[p1 - 1];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    const auto leave = [&](bool goes_on) {
+        if (static_cast<uint32_t>(row) < V) {
+            if (before || goes_on) {
+                store8(partial + (2 * k + (before ? 0 : 1)) * D + c, have, sum);
+            } else {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = sum[i] * scale;
+                store8(out + row * ldo + c, have, v);
+            }
+        }
+    };
+    for (int64_t p = p0; p < p1; p += kAhead) {
+        float v[kAhead][8];
+        int32_t r[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int64_t q = p + j < p1 ? p + j : p1 - 1;
+            r[j] = rows[q];
+            const uint32_t at = static_cast<uint32_t>(order[q]);
+            load8(grad + (at < most ? at : most) * ldg + c, have, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (p + j >= p1) break;
+            if (r[j] != row) {
+                leave(false);
+                row = r[j];
+                before = false;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[j][i];
+        }
+    }
+    leave(after);
+}
+
+constexpr int kJoinThreads = 512;
+
+// A workgroup to a chunk; those in which a row begins that goes on add its parts, the groups each every so many, then
+// the groups' sums in order.
+template <int LANES, typename TO>
+__global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const float* __restrict__ partial,
+                                                                      const int32_t* __restrict__ rows, float scale,
+                                                                      TO* __restrict__ out, int64_t ldo, int64_t n,
+                                                                      int64_t V, int64_t D, int64_t chunk) {
+    constexpr int kGroups = kJoinThreads / LANES;
+    __shared__ float part[kGroups][LANES * 8 + 4];
+    const int64_t k = blockIdx.x, p0 = k * chunk, p1 = p0 + chunk;
+    if (p1 >= n) return;
+    const int32_t row = rows[p1 - 1];
+    if (static_cast<uint32_t>(row) >= V || rows[p1] != row || (p0 > 0 && rows[p0 - 1] == row)) return;
+    const int64_t last = (place_from(rows, n, row + 1) - 1) / chunk;
+    const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
+    const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8, left = D - c;
+    const int have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    if (have > 0) {
+#pragma unroll 4
+        for (int64_t j = k + g; j <= last; j += kGroups) {
+            float v[8];
+            load8(partial + (2 * j + (j == k ? 1 : 0)) * D + c, have, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[g][8 * l + i] = sum[i];
+    __syncthreads();
+    if (g == 0 && have > 0) {
+        const int64_t parts = last - k + 1 < kGroups ? last - k + 1 : kGroups;
+        for (int64_t q = 1; q < parts; ++q) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += part[q][8 * l + i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] *= scale;
+        store8(out + row * ldo + c, have, sum);
+    }
+}
+
+int lanes_of(int64_t D) { return D > 256 ? 64 : (D > 128 ? 32 : (D > 64 ? 16 : (D > 32 ? 8 : 4))); }
+int64_t across_of(int64_t D, int lanes) { return (D + 8 * lanes - 1) / (8 * lanes); }
+
+// Entries of a chunk: 16 or so many that some 4,096 waves have one chunk for each of their groups.
+int64_t chunk_of(int64_t n, int64_t D) {
+    const int lanes = lanes_of(D);
+    int64_t groups = 4096 * (64 / lanes) / across_of(D, lanes);
+    if (groups < 64) groups = 64;
+    const int64_t c = (n + groups - 1) / groups;
+    return c < 16 ? 16 : c;
+}
+int64_t chunks_of(int64_t n, int64_t D) { return (n + chunk_of(n, D) - 1) / chunk_of(n, D); }
+
+template <int LANES, typename T>
+hipError_t lookup(const void* table, int64_t ldt, const void* index, bool wide, float scale, void* out, int64_t ldo,
+                  int64_t n, int64_t V, int64_t D, hipStream_t stream) {
+    constexpr int kGroups = 256 / LANES;
+    const int64_t across = across_of(D, LANES);
+    const bool few = n * across <= 4096 * kGroups;  // one row to a group still leaves CUs without work
+    const int64_t at_once = kGroups * (few ? 1 : 4);
+    int64_t blocks = (n + at_once - 1) / at_once;
+    if (blocks > kMostBlocks / across) blocks = kMostBlocks / across;
+    const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(across));
+    const T* t = static_cast<const T*>(table);
+    if (few)
+        hipLaunchKernelGGL((embedding_kernel<LANES, 1, T>), grid, dim3(256), 0, stream, t, ldt, index, wide, scale,
+                           static_cast<T*>(out), ldo, n, V, D);
+    else
+        hipLaunchKernelGGL((embedding_kernel<LANES, 4, T>), grid, dim3(256), 0, stream, t, ldt, index, wide, scale,
+                           static_cast<T*>(out), ldo, n, V, D);
+    return hipGetLastError();
+}
+
+template <int LANES, typename TG, typename TO>
+hipError_t gradient(const EmbeddingBwdArgs& a, hipStream_t stream) {
+    const int64_t across = across_of(a.D, LANES), chunks = chunks_of(a.n, a.D), chunk = chunk_of(a.n, a.D);
+    const int64_t sums = (chunks + 256 / LANES - 1) / (256 / LANES), empty = (a.V + 255) / 256;
+    hipLaunchKernelGGL((embedding_sum_kernel<LANES, TG, TO>),
+                       dim3(static_cast<unsigned>(sums + empty), static_cast<unsigned>(across)), dim3(256), 0, stream,
+                       static_cast<const TG*>(a.grad), a.ldg, a.order, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo,
+                       a.partial, a.n, a.V, a.D, chunk, static_cast<unsigned>(sums));
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || chunks <= 1) return e;
+    hipLaunchKernelGGL((embedding_join_kernel<LANES, TO>), dim3(static_cast<unsigned>(chunks), static_cast<unsigned>(across)),
+                       dim3(kJoinThreads), 0, stream, a.partial, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo, a.n, a.V,
+                       a.D, chunk);
+    return hipGetLastError();
+}
+
+template <int LANES>
+hipError_t gradient_types(const EmbeddingBwdArgs& a, hipStream_t stream) {
+    if (a.dtype == SPINGTP_FP32)
+        return a.out_dtype == SPINGTP_FP32 ? gradient<LANES, float, float>(a, stream)
+                                           : gradient<LANES, float, uint16_t>(a, stream);
+    return a.out_dtype == SPINGTP_FP32 ? gradient<LANES, uint16_t, float>(a, stream)
+                                       : gradient<LANES, uint16_t, uint16_t>(a, stream);
+}
+
+template <typename T>
+hipError_t lookup_lanes(const void* table, int64_t ldt, const void* index, bool wide, float scale, void* out, int64_t ldo,
+                        int64_t n, int64_t V, int64_t D, hipStream_t stream) {
+    switch (lanes_of(D)) {
+        case 64: return lookup<64, T>(table, ldt, index, wide, scale, out, ldo, n, V, D, stream);
+        case 32: return lookup<32, T>(table, ldt, index, wide, scale, out, ldo, n, V, D, stream);
+        case 16: return lookup<16, T>(table, ldt, index, wide, scale, out, ldo, n, V, D, stream);
+        case 8: return lookup<8, T>(table, ldt, index, wide, scale, out, ldo, n, V, D, stream);
+        default: return lookup<4, T>(table, ldt, index, wide, scale, out, ldo, n, V, D, stream);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_embedding(int dtype, const void* table, int64_t ldt, const void* index, bool wide, float scale, void* out,
+                            int64_t ldo, int64_t n, int64_t V, int64_t D, hipStream_t stream) {
+    return dtype == SPINGTP_FP32 ? lookup_lanes<float>(table, ldt, index, wide, scale, out, ldo, n, V, D, stream)
+                                 : lookup_lanes<uint16_t>(table, ldt, index, wide, scale, out, ldo, n, V, D, stream);
+}
+
+size_t embedding_backward_workspace(int64_t n, int64_t D) {
+    return static_cast<size_t>(2 * chunks_of(n, D) * D) * sizeof(float);
+}
+
+hipError_t launch_embedding_backward(const EmbeddingBwdArgs& a, hipStream_t stream) {
+    switch (lanes_of(a.D)) {
+        case 64: return gradient_types<64>(a, stream);
+        case 32: return gradient_types<32>(a, stream);
+        case 16: return gradient_types<16>(a, stream);
+        case 8: return gradient_types<8>(a, stream);
+        default: return gradient_types<4>(a, stream);
+    }
+}
+
+}  // namespace spingtp

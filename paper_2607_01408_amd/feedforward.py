@@ -31,7 +31,9 @@ _ENTRIES = ("spingtp_pack8", "spingtp_unpack8", "spingtp_rms_norm", "spingtp_rms
             "spingtp_gated_forward_workspace_size", "spingtp_gated_forward8", "spingtp_gated_forward8_workspace_size",
             "spingtp_gated_backward", "spingtp_gated_backward_workspace_size", "spingtp_linear_forward",
             "spingtp_linear_forward_workspace_size", "spingtp_linear_forward8", "spingtp_linear_forward8_workspace_size",
-            "spingtp_linear_backward", "spingtp_linear_backward_workspace_size")
+            "spingtp_linear_backward", "spingtp_linear_backward_workspace_size", "spingtp_embedding", "spingtp_sort_index",
+            "spingtp_sort_index_workspace_size", "spingtp_embedding_backward",
+            "spingtp_embedding_backward_workspace_size", "spingtp_adamw")
 
 
 def _load():
@@ -63,6 +65,8 @@ def _on_stream(op):
         if stream is None:
             return op(*args, **kwargs)
         first = args[0] if args else kwargs.get(name)
+        if isinstance(first, (list, tuple)) and first:
+            first = first[0]
         if stream.device != getattr(first, "device", stream.device):
             raise ValueError(f"the stream is of {stream.device}, the tensors are on {first.device}")
         with torch.cuda.stream(stream):

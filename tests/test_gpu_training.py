@@ -1,0 +1,616 @@
+"""Lookup of embeddings, its gradient and AdamW against float64 (GPU).
+
+Bounds, from the number formats alone: a rounding is off by at most half a step (bf16 2^-8, fp32 2^-24 of the value), a
+sum of n numbers in fp32 by at most n 2^-24 of the sum of their magnitudes.
+"""
+
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():
+    pytest.skip("no GPU visible", allow_module_level=True)
+
+import paper_2607_01408_amd as sg  # noqa: E402
+
+F32, BF16 = torch.float32, torch.bfloat16
+HALF = {F32: 2.0**-24, BF16: 2.0**-8}
+NAN, INF = float("nan"), float("inf")
+
+
+def rand(shape, dtype, seed, scale=1.0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * scale).to(dtype)
+
+
+def whole(shape, most, seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.randint(most, shape, generator=g, device="cuda")
+
+
+def within(got, ref, bound, what=""):
+    got = got.double()
+    fine = torch.isfinite(ref)
+    assert torch.equal(torch.isfinite(got), fine), what
+    over = ((got - ref).abs() - bound)[fine]
+    assert over.numel() == 0 or float(over.max()) <= 0, (what, float(over.max()))
+
+
+def amid(t, fill=NAN):
+    """The same numbers one element off 16 bytes, with others before and behind every row and below the last."""
+    wide = torch.full((t.shape[0] + 5, t.shape[1] + 8), fill, dtype=t.dtype, device="cuda")
+    wide[: t.shape[0], 1 : 1 + t.shape[1]] = t
+    return wide[: t.shape[0], 1 : 1 + t.shape[1]]
+
+
+# ------------------------------------------------------------------ sorting
+
+def index_of(kind, n, V, seed):
+    if kind == "even":
+        return whole((n,), V, seed)
+    if kind == "one":
+        return torch.full((n,), V - 1, dtype=torch.int64, device="cuda")
+    if kind == "skewed":  # half of it a single row, the rest near the first ones
+        i = (whole((n,), 1 << 20, seed).double() / (1 << 20)).pow(6).mul(V).long().clamp(max=V - 1)
+        return torch.where(whole((n,), 2, seed + 1) == 0, V // 2, i)
+    i = whole((n,), 2 * V + 2, seed) - 1  # outside on both sides
+    if n > 2:
+        i[0], i[n // 2] = -(1 << 40), (1 << 32) + 1
+    return i
+
+
+KINDS = ["even", "one", "skewed", "outside"]
+SORTED = [(1, 1), (2, 3), (63, 1000), (64, 2), (65, 511), (1000, 512), (1025, 513), (8191, 100_000), (8192, 262_143),
+          (8193, 262_144), (20_001, 7), (100_000, 4_000), (300_007, 50_000), (1_200_001, 600_000), (70_001, 0x7FFFFFFE)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,V", SORTED)
+def test_sort(n, V, kind):
+    index = index_of(kind, n, V, n + V)
+    rows = torch.where((index >= 0) & (index < V), index, V)
+    want, order = torch.sort(rows, stable=True)
+    for given in (index, index.clamp(-2, min(V, 0x7FFFFFFF)).int()):
+        s = sg.sort_index(given, V)
+        assert s.V == V and s.order.dtype == s.rows.dtype == torch.int32
+        assert torch.equal(s.rows.long(), want) and torch.equal(s.order.long(), order)
+
+
+def test_sort_of_nothing():
+    s = sg.sort_index(torch.empty(0, dtype=torch.int64, device="cuda"), 5)
+    assert s.order.numel() == s.rows.numel() == 0
+
+
+def test_sort_of_many():
+    n, V = 20_000_003, 1_000_000
+    index = whole((n,), V, 1)
+    s = sg.sort_index(index, V)
+    want, order = torch.sort(index, stable=True)
+    assert torch.equal(s.rows.long(), want) and torch.equal(s.order.long(), order)
+
+
+# ------------------------------------------------------------------ lookup and its gradient
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,V,D", [(1, 1, 1), (1, 9, 4096), (3, 2, 7), (33, 100, 31), (700, 5, 64), (65, 77, 65), (301, 50, 129),
+                                   (64, 1000, 256), (5000, 400, 257), (2000, 3000, 2048), (9, 30, 20_001), (60_000, 100, 40)])
+def test_lookup(n, V, D, dtype):
+    for kind in ("even", "outside"):
+        table, index = rand((V, D), dtype, 1), index_of(kind, n, V, 2)
+        inside = (index >= 0) & (index < V)
+        for scale in (1.0, math.sqrt(D)):
+            ref = table[torch.where(inside, index, 0)].double() * torch.tensor(scale, dtype=F32).double()
+            ref = torch.where(inside[:, None], ref, 0.0)
+            want = ref.float().to(dtype) if dtype == BF16 else ref.to(dtype)  # one rounding: bf16 times fp32 fits 32 bits
+            if dtype == F32 or scale == 1:
+                assert torch.equal(sg.embedding(table, index, scale=scale), want)
+            else:
+                within(sg.embedding(table, index, scale=scale), ref, (2.0**-8 + 2.0**-24) * ref.abs())
+            assert torch.equal(sg.embedding(amid(table), index.clamp(-1, 0x7FFFFFFF).int(), scale),
+                               sg.embedding(table, index, scale))
+
+
+def gradient64(grad, index, V, scale):
+    """(sum, sum of magnitudes, entries) of each row."""
+    to, order = torch.sort(torch.where((index >= 0) & (index < V), index, V), stable=True)
+    ends = torch.searchsorted(to, torch.arange(-1, V, device="cuda"), right=True)
+    sums = []  # differences of running sums, off by 2^-53 of the whole one: nothing beside 2^-24 of a row's
+    for t in (grad.double(), grad.double().abs()):
+        run = torch.nn.functional.pad(t[order].cumsum(0), (0, 0, 1, 0))
+        sums.append(run[ends[1:]] - run[ends[:-1]])
+    s = float(torch.tensor(scale, dtype=F32))
+    return sums[0] * s, sums[1] * abs(s), (ends[1:] - ends[:-1]).double()[:, None]
+
+
+GRADIENTS = [(1, 1, 1), (1, 700, 40), (2, 3, 300), (17, 5, 8), (100, 9, 33), (1000, 100, 64), (777, 3000, 65), (5000, 40, 128),
+             (3000, 7, 130), (20_000, 2_000, 100), (40_000, 90, 257), (4_000, 9_000, 1_000), (16_384, 3_000, 2_048),
+             (300, 70, 5_000), (150_000, 1_000, 16)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n,V,D", GRADIENTS)
+def test_gradient(n, V, D, kind):
+    index = index_of(kind, n, V, n)
+    s = sg.sort_index(index, V)
+    for dtype in (F32, BF16):
+        grad = rand((n, D), dtype, 3)
+        for out, scale in ((F32, 1.0), (BF16, 0.3)):
+            ref, size, entries = gradient64(grad, index, V, scale)
+            bound = (entries + 2) * 2.0**-24 * size
+            got = sg.embedding_backward(grad, index, V, scale=scale, dtype=out)
+            assert got.dtype == out and got.shape == (V, D)
+            within(got, ref, bound + HALF[out] * (ref.abs() + bound))
+            assert bool((got[entries[:, 0] == 0] == 0).all())
+            assert torch.equal(got, sg.embedding_backward(amid(grad), s, V, scale, out))
+            assert torch.equal(got, sg.embedding_backward(grad, index.clamp(-1, 0x7FFFFFFF).int(), V, scale, out))
+        assert sg.embedding_backward(grad, s, V).dtype == dtype
+
+
+def test_gradient_of_no_entries():
+    index = torch.empty(0, dtype=torch.int64, device="cuda")
+    assert bool((sg.embedding_backward(torch.empty((0, 70), device="cuda"), index, 300) == 0).all())
+    assert sg.embedding(rand((5, 70), F32, 1), index).shape == (0, 70)
+
+
+def test_gradient_against_differences():
+    n, V, D = 500, 40, 30
+    table, index, grad = rand((V, D), F32, 1), index_of("skewed", n, V, 2), rand((n, D), F32, 3)
+    g = sg.embedding_backward(grad, index, V, scale=0.7)
+    v = rand((V, D), F32, 4)
+    # linear in the table: no error of the difference itself
+    along = (sg.embedding(table + v, index, 0.7).double() * grad).sum() - (sg.embedding(table, index, 0.7).double() * grad).sum()
+    terms = g.double() * v
+    scale = float((sg.embedding(table.abs() + v.abs(), index, 0.7).double() * grad.abs()).sum())
+    assert abs(float(terms.sum() - along)) <= (n + 8) * 2.0**-24 * scale
+
+
+def test_a_number_that_is_not_finite_stays_in_its_row():
+    n, V, D = 5000, 300, 70
+    grad, index = rand((n, D), F32, 1), index_of("even", n, V, 2)
+    grad[7, 3], grad[9, 60] = NAN, INF
+    g = sg.embedding_backward(grad, index, V)
+    bad = torch.zeros((V, D), dtype=torch.bool, device="cuda")
+    bad[index[7], 3] = bad[index[9], 60] = True
+    assert torch.equal(~torch.isfinite(g), bad)
+
+
+def test_lookup_and_gradient_past_two_to_the_31_elements():
+    V, D, n = 1_100_003, 2_000, 700
+    table = torch.empty((V, D), dtype=BF16, device="cuda")
+    table.fill_(0.5)
+    index = torch.cat([whole((n - 3,), V, 1), torch.tensor([V - 1, 0, V - 1], device="cuda")])
+    table[-1] = rand((D,), BF16, 2)
+    assert torch.equal(sg.embedding(table, index), table[index])
+    grad = rand((n, D), BF16, 3)
+    g = sg.embedding_backward(grad, index, V)
+    ref, size, entries = gradient64(grad, torch.unique(index, return_inverse=True)[1], n, 1.0)
+    rows = torch.unique(index)
+    bound = ((entries + 2) * 2.0**-24 * size)[: len(rows)]
+    within(g[rows], ref[: len(rows)], bound + 2.0**-8 * (ref[: len(rows)].abs() + bound))
+    g[rows] = 0
+    assert bool((g == 0).all())
+
+
+# ------------------------------------------------------------------ AdamW
+
+M32 = 0xFFFFFFFF
+
+
+def mix(x):
+    x = x ^ (x >> 16)
+    x = (x * 0x6A09E667) & M32
+    x = x ^ (x >> 15)
+    x = (x * 0xBB67AE85) & M32
+    return x ^ (x >> 16)
+
+
+def words(i, place, step, seed):
+    """The random bits of elements i (an int64 tensor) of a tensor, by their definition."""
+    key = mix((mix(((seed & M32) + place * 0x9E3779B9) & M32) + step * 0x3C6EF373 + (seed >> 32)) & M32)
+    return mix(((i & M32) * 0x9E3779B9 + (i >> 32) * 0x3C6EF373 + key) & M32)
+
+
+def held(b):
+    s = torch.exp2(b.scales.view(torch.uint8).double() - 127).repeat_interleave(128, 1)
+    return (b.values.double() * s[:, : b.values.shape[1]])[0, : b.shape[1]]
+
+
+OPTIONS = dict(lr=1e-2, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.1)
+
+
+def step64(p, g, m, v, step, lr, betas, eps, weight_decay):
+    """(p, its bound, m, its bound, v, its bound) in float64 and for fp32."""
+    b1, b2 = betas
+    m1, size = b1 * m + (1 - b1) * g, b1 * m.abs() + (1 - b1) * g.abs()
+    v1 = b2 * v + (1 - b2) * g * g
+    root = (v1 / (1 - b2**step)).sqrt() + eps
+    p1 = p * (1 - lr * weight_decay) - lr / (1 - b1**step) * m1 / root
+    # each product, sum and constant rounds once: 4 of them in m (of the terms, which may cancel) and 6 in v, 3 from
+    # half of v's to the root, 3 there, 3 in the quotient's factors, and 4 in p
+    em, ev = 4 * 2.0**-24 * size, 6 * 2.0**-24 * v1
+    ep = lr / (1 - b1**step) * (em + 13 * 2.0**-24 * m1.abs()) / root + 4 * 2.0**-24 * (p.abs() + p1.abs())
+    return p1, ep, m1, em + 1e-38, v1, ev + 1e-38
+
+
+SIZES = [1, 7, 8, 127, 128, 129, 300, 2047, 2048, 2049, 70_001]
+
+
+@pytest.mark.parametrize("gtype", [F32, BF16])
+@pytest.mark.parametrize("ptype", [F32, BF16])
+def test_adamw(ptype, gtype):
+    p, g = ([rand((n,), t, 10 * i + k, s) for i, n in enumerate(SIZES)] for k, t, s in ((1, ptype, 1.0), (2, gtype, 0.1)))
+    m, v = ([rand((n,), F32, 10 * i + k, 0.05) for i, n in enumerate(SIZES)] for k in (3, 4))
+    v = [t * t for t in v]
+    factor = torch.tensor([0.37], device="cuda")
+    for step in (1, 1000):
+        for scale in (None, factor):
+            ref = [step64(a.double(), (b.float() * (1 if scale is None else scale)).double(), c.double(), d.double(), step,
+                          **OPTIONS) for a, b, c, d in zip(p, g, m, v)]
+            copies = [torch.empty(n, dtype=BF16, device="cuda") if i % 2 else None for i, n in enumerate(SIZES)]
+            sg.adamw(p, g, m, v, step=step, grad_scale=scale, copies=copies if ptype == F32 else None, **OPTIONS)
+            for a, c, d, copy, (rp, ep, rm, em, rv, ev) in zip(p, m, v, copies, ref):
+                within(a, rp, ep + (HALF[BF16] * (rp.abs() + ep) if ptype == BF16 else 0))
+                within(c, rm, em)
+                within(d, rv, ev)
+                if ptype == F32 and copy is not None:
+                    assert torch.equal(copy, a.to(BF16))
+
+
+def same_rounding(got, ref, share, power, met, error):
+    """`got` [n] are neighbours, in blocks of 128, of the magnitudes `ref` (float64) in the block's format, the upper ones
+    where share is below the chance at which the mean of their `power`-th power is kept.  `met`: the share of the
+    magnitudes that may lie on a number of the format, or as good as; `error`: of that power in fp32."""
+    n = ref.numel()
+    blocks = torch.nn.functional.pad(ref, (0, -n % 128)).view(-1, 128)
+    e = torch.zeros_like(blocks[:, 0])
+    top = blocks.amax(-1)
+    e[top > 0] = torch.ceil(torch.log2(top[top > 0] / 448))
+    unit = torch.exp2(e).repeat_interleave(128)[:n]
+    t, q = ref / unit, got / unit
+    grid = torch.exp2(torch.floor(torch.log2(t.clamp(min=2.0**-6))) - 3)
+    lo = torch.floor(t / grid) * grid
+    hi = lo + grid
+    chance = (t**power - lo**power) / (hi**power - lo**power)
+    want = torch.where(share < chance, hi, lo)
+    # the chance is off by the magnitude's error in steps, and by its own few roundings of numbers that are at most 16
+    # steps from zero; next to the format's numbers either side of the number is right
+    margin = 2.0**-18 + error / unit**power / (hi**power - lo**power)
+    near = ((share - chance).abs() < margin) | (chance < margin) | (chance > 1 - margin)
+    assert bool((q == want)[~near].all())
+    assert bool(((q - t).abs() <= grid * (1 + margin))[near].all()) and float(near.double().mean()) < met + 4 / n
+    return e
+
+
+def blocks_of(x):
+    return sg.pack8(x[None].contiguous())
+
+
+@pytest.mark.parametrize("gtype", [F32, BF16])
+@pytest.mark.parametrize("ptype", [F32, BF16])
+def test_adamw_in_8_bits(ptype, gtype):
+    b1, b2 = OPTIONS["betas"]
+    c = (1 - b1) / math.sqrt((1 - b2) * (1 - b1 * b1 / b2))
+    p, g = ([rand((n,), t, 10 * i + k, s) for i, n in enumerate(SIZES)] for k, t, s in ((1, ptype, 1.0), (2, gtype, 0.1)))
+    spread = [torch.exp(rand((n,), F32, 7 + i)) for i, n in enumerate(SIZES)]
+    m = [blocks_of(rand((n,), F32, 10 * i + 3, 0.02) * s) for (i, n), s in zip(enumerate(SIZES), spread)]
+    v = [blocks_of((rand((n,), F32, 10 * i + 4, 0.05) * s).abs()) for (i, n), s in zip(enumerate(SIZES), spread)]
+    for t, b in ((m, 0), (v, 1)):  # what lies behind the elements does not matter and is zero afterwards
+        for x in t:
+            x.scales.view(torch.uint8)[:, -(-x.shape[1] // 128) :] = 99 + b
+    for step, seed in ((1, 0), (1000, 0x123456789ABCDEF)):
+        old = [(a.double(), b.double(), held(x), held(y) ** 2) for a, b, x, y in zip(p, g, m, v)]
+        copies = [torch.empty(n, dtype=BF16, device="cuda") for n in SIZES] if ptype == F32 else None
+        sg.adamw(p, g, m, v, step=step, seed=seed, copies=copies, **OPTIONS)
+        for k, (a, x, y, (op, og, om, ov)) in enumerate(zip(p, m, v, old)):
+            m1, v1 = b1 * om + (1 - b1) * og, b2 * ov + (1 - b2) * og**2
+            v1 = torch.maximum(v1, (m1 / c) ** 2)
+            root = (v1 / (1 - b2**step)).sqrt() + OPTIONS["eps"]
+            rp = op * (1 - OPTIONS["lr"] * OPTIONS["weight_decay"]) - OPTIONS["lr"] / (1 - b1**step) * m1 / root
+            size = b1 * om.abs() + (1 - b1) * og.abs()
+            # as in step64; where m sets v its error is the quotient's once more
+            ep = OPTIONS["lr"] / (1 - b1**step) * (8 * 2.0**-24 * size + 16 * 2.0**-24 * m1.abs()) / root
+            ep = ep + 4 * 2.0**-24 * (op.abs() + rp.abs())
+            within(a, rp, ep + (HALF[BF16] * (rp.abs() + ep) if ptype == BF16 else 0))
+            if copies is not None:
+                assert torch.equal(copies[k], a.to(BF16))
+            n = m1.numel()
+            w = words(torch.arange(n, device="cuda"), k, step, seed)
+            share = [((w & 0xFFFF).double() + 0.5) / 65536, ((w >> 16).double() + 0.5) / 65536]
+            # an m of 4 bits and a g of 8: 0.9 m + 0.1 g is a number of the format wherever 9 m + g is a multiple of 10 of
+            # its steps, a tenth of the values at most; a g of 24 bits hardly ever meets one
+            met = 0.1 if gtype == BF16 else 0.01
+            # m off by 4 roundings of its terms, which may cancel; v by 6 of its own or, where m sets it, by twice m's
+            off_m = 4 * 2.0**-24 * size
+            off_v = 8 * 2.0**-24 * v1 + 2 * off_m * m1.abs() / c**2
+            em = same_rounding(held(x).abs(), m1.abs(), share[0], 1, met, off_m)
+            ev = same_rounding(held(y), v1.sqrt(), share[1], 2, met, off_v)
+            sign = held(x) * m1 >= 0
+            assert bool(sign.all())
+            for b, e in ((x, em), (y, ev)):
+                assert torch.equal(b.scales.view(torch.uint8)[0, : len(e)].double(), e + 127)
+                assert bool((b.values.view(torch.uint8)[:, n:] & 0x7F == 0).all())
+
+
+def test_rounding_keeps_the_mean():
+    n = 1 << 20
+    for c in (0.1, 0.0137, 3.3e-7):
+        g = torch.full((n,), c, device="cuda")
+        p = torch.zeros(n, device="cuda")
+        m, v = sg.adamw_state(p, bits=8)
+        sg.adamw([p], [g], [m], [v], step=1, seed=3, **OPTIONS)
+        for got, want in ((held(m), 0.1 * float(g[0])), (held(v) ** 2, 0.001 * float(g[0]) ** 2)):
+            span = float(got.max() - got.min())
+            assert span <= want / 3.5  # neighbours: an eighth apart, squares a quarter and a bit
+            # the mean of n independent choices between two: 5 standard deviations of at most half the span
+            assert abs(float(got.mean()) - want) <= 5 * span / 2 / math.sqrt(n) + 2.0**-16 * span + 2.0**-22 * want
+
+
+def test_states_in_8_bits_follow_those_in_32():
+    n, steps = 1 << 16, 300
+    runs = []
+    for bits in (32, 8):
+        p = torch.zeros(n, device="cuda")
+        m, v = sg.adamw_state(p, bits=bits)
+        for step in range(1, steps + 1):
+            sg.adamw([p], [rand((n,), F32, step)], [m], [v], step=step, lr=1e-3, weight_decay=0.0)
+        runs.append((m.double(), v.double(), p) if bits == 32 else (held(m), held(v) ** 2, p))
+    (m, v, p), (m8, v8, p8) = runs
+    # each rounding keeps the mean, so the mean over the elements does; an element's v is off by a third (a rounding every
+    # 200 steps or so by an eighth to a quarter, forgotten over 1,000), the mean of n of them by 5 / 3 / sqrt(n) at most
+    assert abs(float(v8.mean() / v.mean()) - 1) <= 0.01
+    assert abs(float((m8 - m).mean())) <= 5 * float((m8 - m).std()) / math.sqrt(n)
+    assert float((m8 * m).mean() / (m * m).mean()) == pytest.approx(1, abs=0.02)
+    # steps are as long as in 32 bits
+    assert float(p8.double().pow(2).mean() / p.double().pow(2).mean()) == pytest.approx(1, abs=0.2)
+
+
+def test_a_v_that_was_rounded_to_zero_makes_no_long_step():
+    n = 256
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    mm = torch.full((n,), 1e-3, device="cuda")
+    m, v = blocks_of(mm), blocks_of(torch.zeros(n, device="cuda"))
+    sg.adamw([p], [g], [m], [v], step=100_000, lr=1e-3, weight_decay=0.0)
+    b1, b2 = 0.9, 0.999
+    c = (1 - b1) / math.sqrt((1 - b2) * (1 - b1 * b1 / b2))
+    assert bool((p.abs() <= 1e-3 * c * 1.001).all()) and bool((p.abs() > 1e-3).all())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_what_is_not_finite_stays_in_its_place(bits):
+    n = 1000
+    p, g = rand((n,), F32, 1), rand((n,), F32, 2)
+    m, v = sg.adamw_state(p, bits=bits)
+    bad = torch.zeros(n, dtype=torch.bool, device="cuda")
+    bad[5] = bad[130] = bad[999] = True
+    g[5], g[130], g[999] = NAN, INF, -INF
+    sg.adamw([p], [g], [m], [v], step=1, **OPTIONS)
+    assert torch.equal(~torch.isfinite(p), bad)
+    for t in ((held(m), held(v)) if bits == 8 else (m, v)):
+        assert torch.equal(~torch.isfinite(t), bad) and bool((t[~bad].abs() > 0).any())
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_every_option_at_its_ends(bits):
+    p0, g = rand((300,), F32, 1), rand((300,), F32, 2)
+    for betas in ((0.0, 0.0), (0.0, 0.999), (0.9, 0.0), (0.95, 0.9), (0.9, 0.81)):
+        p = p0.clone()
+        m, v = sg.adamw_state(p, bits=bits)
+        sg.adamw([p], [g], [m], [v], step=1, lr=0.01, betas=betas, eps=0.0, weight_decay=0.0)
+        # the first step is lr in every element, by m / sqrt(v) of what was just set
+        within(p, p0.double() - 0.01 * g.double().sign(), 2.0**-24 * p0.double().abs() + 0.01 * 20 * 2.0**-24)
+    p = p0.clone()
+    m, v = sg.adamw_state(p, bits=bits)
+    sg.adamw([p], [torch.zeros_like(g)], [m], [v], step=1, lr=0.5, weight_decay=0.2)
+    within(p, p0.double() * 0.9, 2 * 2.0**-24 * p0.double().abs())
+
+
+def test_a_tensor_alone_as_among_others():
+    """What a tensor becomes depends on its place in the list alone, not on how many share a launch."""
+    sizes = [int(n) for n in whole((130,), 5000, 1)]
+    make = lambda: [[rand((n,), F32, 7 * i + k, 0.1) for i, n in enumerate(sizes)] for k in (1, 2)]  # noqa: E731
+    p, g = make()
+    m, v = zip(*(sg.adamw_state(t, bits=8 if i % 2 else 32) for i, t in enumerate(p)))
+    sg.adamw(p, g, m, v, step=3, **OPTIONS)
+    q, _ = make()
+    zero = torch.zeros(0, device="cuda")
+    for i in (0, 1, 64, 77, 129):
+        a, b = sg.adamw_state(q[i], bits=8 if i % 2 else 32)
+        none = [zero] * i
+        sg.adamw(none + [q[i]], none + [g[i]], none + [a], none + [b], step=3, **OPTIONS)
+        assert torch.equal(p[i], q[i])
+        same = (lambda x, y: torch.equal(x.values.view(torch.uint8), y.values.view(torch.uint8))) if i % 2 else torch.equal
+        assert same(a, m[i]) and same(b, v[i])
+
+
+def test_views_of_one_buffer_and_its_neighbours():
+    sizes = [5, 1, 130, 77, 2050]
+    total = sum(sizes)
+    flat = [rand((total + 2,), F32, k, 0.1).abs() for k in range(4)]
+    keep = [t.clone() for t in flat]
+    views = [list(torch.split(t[1:-1], sizes)) for t in flat]
+    sg.adamw(*views, step=2, **OPTIONS)
+    one = [t[1:-1].clone() for t in keep]
+    sg.adamw(*([t] for t in one), step=2, **OPTIONS)
+    for t, k, w in zip(flat, keep, one):
+        assert torch.equal(t[1:-1], w) and t[0] == k[0] and t[-1] == k[-1]
+
+
+def test_past_two_to_the_31_elements():
+    n = (1 << 31) + 12_345
+    p, g = torch.zeros(n, dtype=BF16, device="cuda"), torch.full((n,), 0.25, dtype=BF16, device="cuda")
+    m, v = sg.adamw_state(p, bits=8)
+    sg.adamw([p], [g], [m], [v], step=1, lr=0.125, weight_decay=0.0)
+    assert bool((p == -0.125).all())
+    last = torch.arange(n - 5_000, n, device="cuda")
+    w = words(last, 0, 1, 0)
+    share = ((w & 0xFFFF).double() + 0.5) / 65536
+    q = m.values[0, n - 5_000 : n].double()
+    t = torch.tensor(0.1, dtype=F32).double() * 0.25
+    t = t * 2.0 ** (127 - int(m.scales.view(torch.uint8)[0, n // 128]))
+    chance = (t - 16 * torch.floor(t / 16)) / 16 if float(t) < 256 else (t - 32 * torch.floor(t / 32)) / 32
+    step = 16 if float(t) < 256 else 32
+    lo = step * torch.floor(t / step)
+    near = (share - chance).abs() < 2.0**-16
+    assert torch.equal(q[~near], torch.where(share < chance, lo + step, lo)[~near])
+
+
+# ------------------------------------------------------------------ as they are used
+
+def network(V, D, F, seed=1):
+    """fp32 weights of a small network and the bf16 copies that its layers read."""
+    master = [rand(s, F32, seed + i, k) for i, (s, k) in enumerate([((V, D), 1.0), ((F, D), D**-0.5), ((F,), 0.1),
+                                                                    ((D, F), F**-0.5)])]
+    return master, [t.to(BF16) if t.dim() == 2 else None for t in master]
+
+
+def training_step(master, copies, states, index, target, step, lr, **on):
+    """Embedding, two layers and the update for half the squared distance to `target`."""
+    table, up, _, down = copies
+    x = sg.embedding(table, index, scale=0.5, **on)
+    h, kept = sg.linear(x, up, bias=master[2], act="silu", save="same", **on)
+    y, last = sg.linear(h, down, residual=x.float(), save="same", dtype=F32, **on)
+    gy = y - target
+    gh, g_down, _ = sg.linear_backward(gy, last, down, need_bias=False, dtype=F32, **on)
+    gx, g_up, g_bias = sg.linear_backward(gh, kept, up, dtype=F32, **on)
+    g_table = sg.embedding_backward(gx.float() + gy, index, len(table), scale=0.5, **on)
+    grads = [g_table, g_up, g_bias, g_down]
+    sg.adamw(master, grads, *zip(*states), step=step, lr=lr, weight_decay=0.0, copies=copies, **on)
+    return y, grads
+
+
+def test_a_training_step_against_autograd():
+    V, D, F, n = 40, 96, 130, 300
+    master, copies = network(V, D, F)
+    index, target = index_of("skewed", n, V, 5), rand((n, D), F32, 6)
+    p = [(c if c is not None else m).double().requires_grad_() for m, c in zip(master, copies)]
+    x = 0.5 * p[0][index]
+    z = x @ p[1].t() + p[2]
+    y = x + (z * torch.sigmoid(z)) @ p[3].t()
+    (0.5 * (y - target.double()).pow(2).sum()).backward()
+    states = [sg.adamw_state(t) for t in master]
+    old = [t.clone() for t in master]
+    got, grads = training_step(master, copies, states, index, target, 1, 1e-2)
+    assert float((got.double() - y).norm() / y.norm()) <= 4 * 2.0**-8
+    for g, t in zip(grads, p):
+        assert float((g.double() - t.grad).norm() / t.grad.norm()) <= 8 * 2.0**-8
+    for a, b, g, copy in zip(master, old, grads, copies):
+        within(a, step64(b.double(), g.double(), torch.zeros_like(g, dtype=torch.float64),
+                         torch.zeros_like(g, dtype=torch.float64), 1, 1e-2, (0.9, 0.999), 1e-8, 0.0)[0], 1e-6)
+        assert copy is None or torch.equal(copy, a.to(BF16))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("n", [3, 700, 9000])
+def test_a_captured_training_step_replays(n, bits):
+    V, D, F = 50, 64, 200
+    index, target = index_of("skewed", n, V, 5), rand((n, D), F32, 6)
+    step, lr = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.tensor(1e-3, device="cuda")
+
+    def start():
+        master, copies = network(V, D, F)
+        return master, copies, [sg.adamw_state(t, bits=bits) for t in master]
+
+    net = start()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        training_step(*start(), index, target, 1, 1e-3)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.add_(1)
+        y, grads = training_step(*net, index, target, step, lr)
+    eager = start()
+    for k in range(1, 4):
+        index.copy_(index_of("even", n, V, 50 + k))
+        lr.fill_(1e-3 * k)
+        graph.replay()
+        wy, wg = training_step(*eager, index, target, k, float(lr))
+        torch.cuda.synchronize()
+        assert torch.equal(y, wy) and all(torch.equal(a, b) for a, b in zip(grads, wg))
+        for a, b in zip(net[0], eager[0]):
+            assert float((a - b).abs().max()) <= 1e-6 * float(b.abs().max())  # lr in fp32, or as a double
+            a.copy_(b)
+        for a, b in zip(net[1], eager[1]):
+            if a is not None:
+                a.copy_(b)
+
+
+def test_another_stream_and_arguments_by_their_names():
+    V, D, F, n = 40, 64, 70, 300
+    index, target = index_of("even", n, V, 5), rand((n, D), F32, 6)
+    side = torch.cuda.Stream()
+    runs = []
+    for on in ({}, {"stream": side}):
+        master, copies = network(V, D, F)
+        states = [sg.adamw_state(t, bits=8) for t in master]
+        torch.cuda.synchronize()
+        s = sg.sort_index(index=index, V=V, **on)
+        g = sg.embedding_backward(grad=target, index=s, V=V, scale=2.0, dtype=BF16, **on)
+        x = sg.embedding(table=copies[0], index=index, scale=2.0, **on)
+        m, v = zip(*states)
+        sg.adamw(params=master, grads=[t.clone() for t in master], m=m, v=v, step=1, lr=1e-3, betas=(0.9, 0.99), eps=1e-6,
+                 weight_decay=0.1, grad_scale=None, copies=copies, seed=1, **on)
+        torch.cuda.synchronize()
+        runs.append([g, x, s.order, *master, *(b.values.view(torch.uint8) for b in m + v)])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_a_step_is_seen_by_autograd():
+    p = torch.nn.Parameter(rand((300,), F32, 1))
+    before = p._version
+    sg.adamw([p], [torch.ones_like(p)], *([s] for s in sg.adamw_state(p)), step=1, lr=1e-3)
+    assert p._version > before and p.requires_grad and p.is_leaf
+
+
+def test_refusals():
+    table, index, grad = rand((9, 64), F32, 1), whole((20,), 9, 2), rand((20, 64), F32, 3)
+    s = sg.sort_index(index, 9)
+    p, g = rand((300,), F32, 1), rand((300,), F32, 2)
+    m, v = sg.adamw_state(p)
+    m8, v8 = sg.adamw_state(p, bits=8)
+    short = sg.adamw_state(p[:256], bits=8)
+    on = dict(step=1, lr=1e-3)
+    two = torch.ones(2, device="cuda")
+    bad = [
+        lambda: sg.embedding(table.half(), index), lambda: sg.embedding(table.t(), index), lambda: sg.embedding(table, index.float()),
+        lambda: sg.embedding(table, index.cpu()), lambda: sg.embedding(table, index[None]), lambda: sg.embedding(table, index[::2]),
+        lambda: sg.embedding(table[:0], index), lambda: sg.embedding(table[:, :0], index), lambda: sg.embedding(table.cpu(), index),
+        lambda: sg.sort_index(index, 0), lambda: sg.sort_index(index.short(), 9), lambda: sg.sort_index(index.cpu(), 9),
+        lambda: sg.embedding_backward(grad, index[:19], 9), lambda: sg.embedding_backward(grad, s, 8),
+        lambda: sg.embedding_backward(grad, index, 0), lambda: sg.embedding_backward(grad, index, 9, dtype=torch.float16),
+        lambda: sg.embedding_backward(grad[:, :0], index, 9), lambda: sg.embedding_backward(grad.half(), index, 9),
+        lambda: sg.embedding_backward(grad, sg.SortedIndex(s.order, s.rows[:19], 9), 9),
+        lambda: sg.embedding_backward(grad, sg.SortedIndex(s.order.long(), s.rows, 9), 9),
+        lambda: sg.adamw([p], [g, g], [m], [v], **on), lambda: sg.adamw([p], [g], [], [v], **on),
+        lambda: sg.adamw([p], [g[:299]], [m], [v], **on), lambda: sg.adamw([p], [g], [m[:299]], [v], **on),
+        lambda: sg.adamw([p.half()], [g], [m], [v], **on), lambda: sg.adamw([p], [g.half()], [m], [v], **on),
+        lambda: sg.adamw([p], [g], [m.bfloat16()], [v], **on), lambda: sg.adamw([p], [g], [m], [v8], **on),
+        lambda: sg.adamw([p], [g], [short[0]], [short[1]], **on), lambda: sg.adamw([p], [g], [m], [m], **on),
+        lambda: sg.adamw([p, p], [g, g], [m, m.clone()], [v, v.clone()], **on), lambda: sg.adamw([p], [p], [m], [v], **on),
+        lambda: sg.adamw([p[:200], p[100:]], [g[:200], g[100:]], [m[:200], m[:200].clone()], [v[:200], v[:200].clone()], **on),
+        lambda: sg.adamw([p], [g], [m8], [m8], **on), lambda: sg.adamw([p[::2]], [g[::2]], [m[:150]], [v[:150]], **on),
+        lambda: sg.adamw([p], [g], [m], [v], step=0, lr=1e-3), lambda: sg.adamw([p], [g], [m], [v], betas=(1.0, 0.9), **on),
+        lambda: sg.adamw([p], [g], [m], [v], betas=(0.9, float("nan")), **on), lambda: sg.adamw([p], [g], [m], [v], eps=-1.0, **on),
+        lambda: sg.adamw([p], [g], [m], [v], grad_scale=two, **on), lambda: sg.adamw([p], [g], [m], [v], step=two, lr=1e-3),
+        lambda: sg.adamw([p], [g], [m], [v], step=1, lr=two), lambda: sg.adamw([p], [g], [m], [v], copies=[p.clone()], **on),
+        lambda: sg.adamw([p.bfloat16()], [g], [m], [v], copies=[g.bfloat16()], **on), lambda: sg.adamw([p.cpu()], [g], [m], [v], **on),
+        lambda: sg.adamw([p], [g.cpu()], [m], [v], **on), lambda: sg.adamw_state(p, bits=16),
+    ]
+    keep = [t.clone() for t in (p, m, v)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i} was not refused")
+    with pytest.raises(TypeError):
+        sg.adamw([p], [g], [m], [v], step=1.5, lr=1e-3)
+    with pytest.raises(sg.SpinGTPError):
+        sg.adamw([p], [g], [m], [v], step=1, lr=INF)
+    sg.adamw([], [], [], [], step=1, lr=1e-3)
+    assert all(torch.equal(a, b) for a, b in zip((p, m, v), keep))
