@@ -37,10 +37,9 @@ struct AdamwEntry {
     int64_t first;  // of the piece in its tensor
     uint32_t place;
     uint32_t kinds;  // kParam16, ...
-    uint32_t block;  // the launch's first workgroup for it
 };
 enum : uint32_t { kParam16 = 1, kGrad16 = 2 };
-constexpr int kMostEntries = 40;  // with them the arguments stay below 4 KB
+constexpr int kMostEntries = 46;  // with them the arguments stay below 4 KB; at most a wave's lanes
 constexpr int kAdamwChunk = 2048;
 
 struct AdamwArgs {
@@ -56,6 +55,7 @@ struct AdamwArgs {
     const float* grad_scale;
     double lr;
     int entries;
+    uint32_t block[kMostEntries];  // an entry's first workgroup
     AdamwEntry entry[kMostEntries];
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
@@ -110,15 +110,12 @@ __device__ __forceinline__ void put_block(const float (&x)[8], const float (&siz
 }
 
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
-    int at = 0;
-    for (int hi = a.entries; hi - at > 1;) {
-        const int mid = (at + hi) / 2;
-        if (a.entry[mid].block <= blockIdx.x)
-            at = mid;
-        else
-            hi = mid;
-    }
+    // the last entry that begins here or before, a lane to each: one read of the arguments
+    const int lane = threadIdx.x & 63;
+    const uint32_t begins = a.block[lane < kMostEntries ? lane : 0];
+    const int at = __popcll(__ballot(lane < a.entries && begins <= blockIdx.x)) - 1;
     const AdamwEntry& t = a.entry[at];
+    const uint32_t block = blockIdx.x - a.block[at];
     float decay = a.decay, rate = a.rate, root = a.root;
     int64_t step = a.step;
     if (a.device_step != nullptr || a.device_lr != nullptr) {
@@ -128,7 +125,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
         rate = static_cast<float>(lr / -expm1(static_cast<double>(step) * a.log_b1));
         root = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(step) * a.log_b2)));
     }
-    const int64_t i0 = static_cast<int64_t>(blockIdx.x - t.block) * kAdamwChunk + threadIdx.x * 8;
+    const int64_t i0 = static_cast<int64_t>(block) * kAdamwChunk + threadIdx.x * 8;
     const int64_t left = t.n - i0;
     const int have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
     const bool blocks = t.ms != nullptr;
@@ -251,6 +248,7 @@ hipError_t launch_adamw(const spingtp_adamw_tensor* tensors, int64_t count, cons
                 const hipError_t e = flush();
                 if (e != hipSuccess) return e;
             }
+            a.block[a.entries] = static_cast<uint32_t>(blocks);
             AdamwEntry& to = a.entry[a.entries++];
             const int64_t pw = x.param_dtype == SPINGTP_FP32 ? 4 : 2, gw = x.grad_dtype == SPINGTP_FP32 ? 4 : 2;
             const bool eight = x.m_scales != nullptr;
@@ -265,7 +263,6 @@ hipError_t launch_adamw(const spingtp_adamw_tensor* tensors, int64_t count, cons
             to.first = first;
             to.place = static_cast<uint32_t>(k);
             to.kinds = (pw == 2 ? kParam16 : 0) | (gw == 2 ? kGrad16 : 0);
-            to.block = static_cast<uint32_t>(blocks);
             blocks += mine;
         }
     }

@@ -36,19 +36,19 @@ __global__ __launch_bounds__(256) void embedding_kernel(const T* __restrict__ ta
     const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8;
     if (c >= D) return;
     const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
-    for (int64_t first = (static_cast<int64_t>(blockIdx.x) * kGroups + g) * ROWS; first < n;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * ROWS + g; first < n;
          first += static_cast<int64_t>(gridDim.x) * kGroups * ROWS) {
         int64_t row[ROWS];
         float v[ROWS][8];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) row[r] = first + r < n ? row_of(index, wide, first + r, V) : -1;
+        for (int r = 0; r < ROWS; ++r) row[r] = first + r * kGroups < n ? row_of(index, wide, first + r * kGroups, V) : -1;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) load8(table + (row[r] < 0 ? 0 : row[r] * ldt + c), row[r] < 0 ? 0 : have, v[r]);
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[r][i] *= scale;
-            if (first + r < n) store8(out + (first + r) * ldo + c, have, v[r]);
+            if (first + r * kGroups < n) store8(out + (first + r * kGroups) * ldo + c, have, v[r]);
         }
     }
 }
@@ -68,25 +68,27 @@ __device__ __forceinline__ int64_t place_from(const int32_t* rows, int64_t n, in
 
 constexpr int kAhead = 4;  // rows in flight
 
-// Workgroups 0 to sum_blocks - 1: chunks of `chunk` entries, one to a group.  partial [chunks][2][D]: the part of a row that
-// began in an earlier chunk, and of one that begins here and goes on.  The others: 256 rows of the table each.
+constexpr int kEmptyRows = 16;  // of the table, that a wave looks after
+
+// Workgroups 0 to sum_blocks - 1: chunks of `chunk` entries, one to a group, `across` workgroups to the columns.  partial
+// [chunks][2][D]: the part of a row that began in an earlier chunk, and of one that begins here and goes on.  The
+// others: rows of the table without entries.
 template <int LANES, typename TG, typename TO>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict__ grad, int64_t ldg,
                                                             const int32_t* __restrict__ order,
                                                             const int32_t* __restrict__ rows, float scale,
                                                             TO* __restrict__ out, int64_t ldo, float* __restrict__ partial,
-                                                            int64_t n, int64_t V, int64_t D, int64_t chunk,
+                                                            int64_t n, int64_t V, int64_t D, int64_t chunk, unsigned across,
                                                             unsigned sum_blocks) {
     constexpr int kGroups = 256 / LANES;
     if (blockIdx.x >= sum_blocks) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int64_t first = static_cast<int64_t>(blockIdx.x - sum_blocks) * 256 + 64 * wave, mine = first + lane;
+        const int64_t first = (static_cast<int64_t>(blockIdx.x - sum_blocks) * 4 + wave) * kEmptyRows, mine = first + lane;
         bool empty = false;
-        if (mine < V) {
+        if (lane < kEmptyRows && mine < V) {
             const int64_t at = place_from(rows, n, static_cast<int32_t>(mine));
             empty = at >= n || rows[at] != mine;
         }
-        const int64_t c0 = static_cast<int64_t>(blockIdx.y) * LANES * 8, c1 = c0 + LANES * 8 < D ? c0 + LANES * 8 : D;
         const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         constexpr int kAtOnce = 64 / LANES;
         uint64_t left = __ballot(empty);
@@ -100,14 +102,15 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
                 left &= left - 1;
                 if (lane / LANES == k) row = first + b;
             }
-            const int64_t c = c0 + (lane % LANES) * 8;
-            if (row >= 0 && c < c1) store8(out + row * ldo + c, c1 - c >= 8 ? 8 : static_cast<int>(c1 - c), zeros);
+            if (row >= 0)
+                for (int64_t c = (lane % LANES) * 8; c < D; c += LANES * 8)
+                    store8(out + row * ldo + c, D - c >= 8 ? 8 : static_cast<int>(D - c), zeros);
         }
         return;
     }
     const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
-    const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8;
-    const int64_t k = static_cast<int64_t>(blockIdx.x) * kGroups + g, p0 = k * chunk;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x % across) * LANES + l) * 8;
+    const int64_t k = static_cast<int64_t>(blockIdx.x / across) * kGroups + g, p0 = k * chunk;
     if (c >= D || p0 >= n) return;
     const int64_t p1 = p0 + chunk < n ? p0 + chunk : n;
     const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
@@ -158,48 +161,87 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
 }
 
 constexpr int kJoinThreads = 512;
+constexpr int kShort = 16;  // chunks beyond the first that a group adds up by itself
 
-// A workgroup to a chunk; those in which a row begins that goes on add its parts, the groups each every so many, then
-// the groups' sums in order.
+// A group to a chunk; those in which a row begins that goes on add its parts: chunk after chunk as long as one starts
+// with the row.  A row of more than kShort chunks is added by the whole workgroup, a group every so many chunks,
+// and the groups' sums in order.
 template <int LANES, typename TO>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const float* __restrict__ partial,
                                                                       const int32_t* __restrict__ rows, float scale,
                                                                       TO* __restrict__ out, int64_t ldo, int64_t n,
-                                                                      int64_t V, int64_t D, int64_t chunk) {
+                                                                      int64_t V, int64_t D, int64_t chunk, int64_t chunks,
+                                                                      unsigned across) {
     constexpr int kGroups = kJoinThreads / LANES;
     __shared__ float part[kGroups][LANES * 8 + 4];
-    const int64_t k = blockIdx.x, p0 = k * chunk, p1 = p0 + chunk;
-    if (p1 >= n) return;
-    const int32_t row = rows[p1 - 1];
-    if (static_cast<uint32_t>(row) >= V || rows[p1] != row || (p0 > 0 && rows[p0 - 1] == row)) return;
-    const int64_t last = (place_from(rows, n, row + 1) - 1) / chunk;
+    __shared__ int32_t long_row[kGroups];  // -1: none begins in the group's chunk
     const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
-    const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8, left = D - c;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x % across) * LANES + l) * 8, left = D - c;
     const int have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
+    const int64_t first = static_cast<int64_t>(blockIdx.x / across) * kGroups;
+    // adds the parts of `row` in chunks j, j + step, ... below `end`; whether all of them were its
+    const auto add = [&](float (&sum)[8], int32_t row, int64_t j, int64_t step, int64_t end) {
+        for (; j < end; j += kAhead * step) {
+            int32_t r[kAhead];
+            float v[kAhead][8];
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const int64_t at = j + q * step < end ? j + q * step : j;
+                r[q] = rows[at * chunk];
+                load8(partial + 2 * at * D + (have > 0 ? c : 0), have, v[q]);
+            }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                if (j + q * step >= end) return true;
+                if (r[q] != row) return false;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] += v[q][i];
+            }
+        }
+        return true;
+    };
+    const auto finish = [&](float (&sum)[8], int32_t row, int64_t k) {
+        float v[8];
+        load8(partial + (2 * k + 1) * D + c, have, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (v[i] + sum[i]) * scale;
+        store8(out + row * ldo + c, have, v);
+    };
+    const int64_t k = first + g, p0 = k * chunk, p1 = p0 + chunk;
+    int32_t row = -1;
+    if (k < chunks && p1 < n) {
+        const int32_t last = rows[p1 - 1], next = rows[p1], before = p0 > 0 ? rows[p0 - 1] : -1;
+        if (static_cast<uint32_t>(last) < V && next == last && before != last) row = last;
+    }
+    const int64_t end = k + 1 + kShort < chunks ? k + 1 + kShort : chunks;
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    if (have > 0) {
-#pragma unroll 4
-        for (int64_t j = k + g; j <= last; j += kGroups) {
-            float v[8];
-            load8(partial + (2 * j + (j == k ? 1 : 0)) * D + c, have, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += v[i];
-        }
+    bool more = false;
+    if (row >= 0) {
+        more = add(sum, row, k + 1, 1, end) && end < chunks && rows[end * chunk] == row;
+        if (!more && have > 0) finish(sum, row, k);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) part[g][8 * l + i] = sum[i];
+    if (l == 0) long_row[g] = more ? row : -1;
     __syncthreads();
-    if (g == 0 && have > 0) {
-        const int64_t parts = last - k + 1 < kGroups ? last - k + 1 : kGroups;
-        for (int64_t q = 1; q < parts; ++q) {
+    for (int at = 0; at < kGroups; ++at) {
+        const int32_t which = long_row[at];
+        if (which < 0) continue;
+        float mine[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += part[q][8 * l + i];
+        for (int i = 0; i < 8; ++i) mine[i] = 0.f;
+        add(mine, which, first + at + 1 + g, kGroups, chunks);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[g][8 * l + i] = mine[i];
+        __syncthreads();
+        if (g == 0 && have > 0) {
+#pragma unroll 4
+            for (int q = 1; q < kGroups; ++q)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mine[i] += part[q][8 * l + i];
+            finish(mine, which, first + at);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] *= scale;
-        store8(out + row * ldo + c, have, sum);
+        __syncthreads();
     }
 }
 
@@ -239,16 +281,17 @@ hipError_t lookup(const void* table, int64_t ldt, const void* index, bool wide, 
 template <int LANES, typename TG, typename TO>
 hipError_t gradient(const EmbeddingBwdArgs& a, hipStream_t stream) {
     const int64_t across = across_of(a.D, LANES), chunks = chunks_of(a.n, a.D), chunk = chunk_of(a.n, a.D);
-    const int64_t sums = (chunks + 256 / LANES - 1) / (256 / LANES), empty = (a.V + 255) / 256;
-    hipLaunchKernelGGL((embedding_sum_kernel<LANES, TG, TO>),
-                       dim3(static_cast<unsigned>(sums + empty), static_cast<unsigned>(across)), dim3(256), 0, stream,
-                       static_cast<const TG*>(a.grad), a.ldg, a.order, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo,
-                       a.partial, a.n, a.V, a.D, chunk, static_cast<unsigned>(sums));
+    const int64_t sums = (chunks + 256 / LANES - 1) / (256 / LANES) * across, looked = 4 * kEmptyRows;
+    const int64_t empty = (a.V + looked - 1) / looked;
+    hipLaunchKernelGGL((embedding_sum_kernel<LANES, TG, TO>), dim3(static_cast<unsigned>(sums + empty)), dim3(256), 0,
+                       stream, static_cast<const TG*>(a.grad), a.ldg, a.order, a.rows, a.scale, static_cast<TO*>(a.out),
+                       a.ldo, a.partial, a.n, a.V, a.D, chunk, static_cast<unsigned>(across), static_cast<unsigned>(sums));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks <= 1) return e;
-    hipLaunchKernelGGL((embedding_join_kernel<LANES, TO>), dim3(static_cast<unsigned>(chunks), static_cast<unsigned>(across)),
+    constexpr int kGroups = kJoinThreads / LANES;
+    hipLaunchKernelGGL((embedding_join_kernel<LANES, TO>), dim3(static_cast<unsigned>((chunks + kGroups - 1) / kGroups * across)),
                        dim3(kJoinThreads), 0, stream, a.partial, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo, a.n, a.V,
-                       a.D, chunk);
+                       a.D, chunk, chunks, static_cast<unsigned>(across));
     return hipGetLastError();
 }
 

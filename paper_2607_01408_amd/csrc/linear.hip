@@ -152,7 +152,7 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_kernel(GemmArgs a, Linear
     }
 }
 
-// At most kSkinnyRows rows of x.
+// At most 16 TM rows of x.
 template <class E, int TM>
 __global__ __launch_bounds__(64 * kSkinnyWaves) void linear_skinny_kernel(GemmArgs a, int64_t row_bytes, LinearOut o) {
     cut_slice<E, false, false>(a, o, row_bytes);
@@ -171,39 +171,76 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void linear_skinny_kernel(GemmAr
                               });
 }
 
-// The slices' sums added in order, and what follows them: eight neighbouring outputs a thread.
+// The slices' sums added in a fixed order, and what follows them: eight neighbouring outputs to PARTS threads, each of
+// which adds every PARTS-th slice (few outputs of many slices would keep few threads busy).
+template <int PARTS>
 __global__ __launch_bounds__(256) void linear_join_kernel(LinearOut o, int slices, int64_t M, int64_t N) {
-    const int64_t groups = (N + 7) / 8, stride = static_cast<int64_t>(gridDim.x) * 256;
-    for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < M * groups; at += stride) {
-        const int64_t m = at / groups, n = (at - m * groups) * 8;
-        const int left = N - n >= 8 ? 8 : static_cast<int>(N - n);
-        float v[8], bias[8], r[8];
+    constexpr int kOutputs = 256 / PARTS;
+    __shared__ float part[PARTS > 1 ? PARTS : 1][PARTS > 1 ? kOutputs : 1][9];
+    const int i0 = threadIdx.x % kOutputs, part_of = threadIdx.x / kOutputs;
+    const int64_t groups = (N + 7) / 8, stride = static_cast<int64_t>(gridDim.x) * kOutputs;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * kOutputs; first < M * groups; first += stride) {
+        const int64_t at = first + i0, m = at / groups, n = (at - m * groups) * 8;
+        const bool mine = at < M * groups;
+        const int left = !mine ? 0 : (N - n >= 8 ? 8 : static_cast<int>(N - n));
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = bias[i] = r[i] = 0.f;
-        const float* from = o.partial + m * N + n;
-        if (o.bias != nullptr) load8(o.bias + n, left, bias);
-        if (o.r != nullptr) residual8(o, m, n, left, r);
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+        const float* from = o.partial + (mine ? m * N + n : 0);
 #pragma unroll 4
-        for (int s = 0; s < slices; ++s) {
+        for (int s = part_of; s < slices; s += PARTS) {
             float p[8];
             load8(from + s * M * N, left, p);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += p[i];
         }
+        if constexpr (PARTS > 1) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[part_of][i0][i] = v[i];
+            __syncthreads();
+            if (part_of == 0) {
+#pragma unroll
+                for (int q = 1; q < PARTS; ++q)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += part[q][i0][i];
+            }
+            __syncthreads();
+            if (part_of != 0) continue;
+        }
+        if (!mine) continue;
+        float bias[8], r[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bias[i] = r[i] = 0.f;
+        if (o.bias != nullptr) load8(o.bias + n, left, bias);
+        if (o.r != nullptr) residual8(o, m, n, left, r);
         finish8(o, N, m, n, left, v, bias, r);
     }
 }
 
 // Rows of K bf16 elements to rows of a multiple of 64, zeros behind: what the products read where the caller's rows do
-// not start and end on 16 bytes.
-__global__ __launch_bounds__(256) void copy_rows_kernel(const uint16_t* __restrict__ x, int64_t ldx,
-                                                        uint16_t* __restrict__ out, int64_t R, int64_t K, int64_t pitch) {
-    const int64_t groups = pitch / 8, stride = static_cast<int64_t>(gridDim.x) * 256;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < R * groups; i += stride) {
-        const int64_t row = i / groups, c = (i - row * groups) * 8, left = K - c;
-        float v[8];
-        load8(x + row * ldx + (left > 0 ? c : 0), left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0), v);
-        store8(out + row * pitch + c, 8, v);
+// not start and end on 16 bytes.  x and w in one launch, LANES lanes of eight elements to a row at a time.
+struct RowCopy {
+    const uint16_t* from;
+    int64_t ld, R;
+    uint16_t* to;
+};
+template <int LANES>
+__global__ __launch_bounds__(256) void copy_rows_kernel(RowCopy a, RowCopy b, int64_t K, int64_t pitch) {
+    constexpr int kAtOnce = 256 / LANES;
+    const int l = threadIdx.x % LANES;
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * kAtOnce + threadIdx.x / LANES; row < a.R + b.R;
+         row += static_cast<int64_t>(gridDim.x) * kAtOnce) {
+        const bool second = row >= a.R;
+        const int64_t r = second ? row - a.R : row;
+        const uint16_t* from = second ? b.from + r * b.ld : a.from + r * a.ld;
+        uint16_t* to = (second ? b.to : a.to) + r * pitch;
+#pragma unroll 4
+        for (int64_t c = 8 * l; c < pitch; c += 8 * LANES) {
+            const int64_t left = K - c;
+            float v[8];
+            load8(from + (left > 0 ? c : 0), left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0), v);
+            store8(to + c, 8, v);
+        }
     }
 }
 
@@ -261,20 +298,25 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __re
     }
 }
 
-// The workgroups' sums of a column added in a fixed order: 64 columns a workgroup, its waves every fourth row.
-__global__ __launch_bounds__(256) void linear_db_kernel(const float* __restrict__ sums, int64_t rows, int64_t N,
-                                                        float* __restrict__ db) {
-    __shared__ float part[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * 64 + lane;
+// The workgroups' sums of a column added in a fixed order: 16 columns a workgroup, 64 parts of the rows.
+__global__ __launch_bounds__(1024) void linear_db_kernel(const float* __restrict__ sums, int64_t rows, int64_t N,
+                                                         float* __restrict__ db) {
+    __shared__ float part[64][17];
+    const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 16 + c;
     float s = 0.f;
     if (n < N) {
 #pragma unroll 8
-        for (int64_t r = wave; r < rows; r += 4) s += sums[r * N + n];
+        for (int64_t r = g; r < rows; r += 64) s += sums[r * N + n];
     }
-    part[wave][lane] = s;
+    part[g][c] = s;
     __syncthreads();
-    if (wave == 0 && n < N) db[n] = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    if (threadIdx.x < 16 && n < N) {
+        float total = 0.f;
+#pragma unroll 16
+        for (int k = 0; k < 64; ++k) total += part[k][c];
+        db[n] = total;
+    }
 }
 
 template <typename T>
@@ -293,35 +335,34 @@ int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 bool rows_fit(const void* p, int64_t K, int64_t ld) {
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && K % 8 == 0 && ld % 8 == 0 && 2 * ld <= kMostRowBytes;
 }
-hipError_t copy_rows(const void* x, int64_t ldx, uint16_t* out, int64_t R, int64_t K, hipStream_t stream) {
-    const int64_t pitch = up(K, 64);
-    hipLaunchKernelGGL(copy_rows_kernel, walking(R * (pitch / 8)), dim3(256), 0, stream, static_cast<const uint16_t*>(x),
-                       ldx, out, R, K, pitch);
+hipError_t copy_rows(const RowCopy& a, const RowCopy& b, int64_t K, hipStream_t stream) {
+    const int64_t pitch = up(K, 64), rows = a.R + b.R;
+    if (pitch <= 256)
+        hipLaunchKernelGGL(copy_rows_kernel<8>, walking(rows * 8), dim3(256), 0, stream, a, b, K, pitch);
+    else
+        hipLaunchKernelGGL(copy_rows_kernel<64>, walking(rows * 64), dim3(256), 0, stream, a, b, K, pitch);
     return hipGetLastError();
 }
 
 // What a product of [M][N] outputs over `steps` steps takes: the tile (0: the few-rows kernel) and the slices of its sum.
-struct Shape {
-    int tile;
-    int64_t slices, per;  // `per` steps each
+struct Shape : SumShape {
     size_t bytes(int64_t M, int64_t N) const { return slices > 1 ? static_cast<size_t>(slices * M * N) * sizeof(float) : 0; }
 };
-// Slices where the tiles leave CUs idle: so many that all have work, of at least 8 steps (a slice's start and end take
-// about as long as four).  `grain`: a slice's steps are a multiple of it.
-Shape shape_of(bool few, const TileCosts& costs, int64_t M, int64_t N, int64_t steps, int64_t grain) {
-    Shape s{0, 1, steps};
-    int64_t tiles = (N + 15) / 16;
-    if (!few) {
-        s.tile = product_tile(costs, M, N);
-        tiles = tiles_of(M, N, s.tile, s.tile);
-    }
-    int64_t slices = 512 / (tiles > 0 ? tiles : 1);
-    if (slices > steps / 8) slices = steps / 8;
-    if (slices > 1) {
-        s.per = up((steps + slices - 1) / slices, grain);
-        s.slices = (steps + s.per - 1) / s.per;
-    }
-    return s;
+Shape shape_of(const SliceCosts& costs, int64_t M, int64_t N, int64_t steps, int64_t grain) {
+    return Shape{sum_shape(costs, M, N, steps, grain)};
+}
+// Up to 16 rows of x the weights' bytes are all that counts, and the few-rows kernel reads them with the least
+// latency: us against the best tile, one row bf16 4,096 x 8,192 (sum x columns) 12.7 / 14.7, 1,024^2 4.1 / 5.9; 24 rows
+// 23 / 16 and 6.7 / 6.2.  Its eight waves have four steps each in flight: a longer sum over few columns is cut, one row of
+// 8,192 x 128 10.6 -> 6.7.
+constexpr int64_t kFewRows = 16;
+Shape few_shape(int64_t N, int64_t steps, int64_t grain) {
+    const int64_t groups = (N + 15) / 16, at_once = 4 * kSkinnyWaves;
+    int64_t slices = 256 / groups;
+    if (slices > steps / at_once) slices = steps / at_once;
+    if (slices < 2) return Shape{{0, 1, steps}};
+    const int64_t per = up((steps + slices - 1) / slices, grain);
+    return Shape{{0, (steps + per - 1) / per, per}};
 }
 
 template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX>
@@ -361,12 +402,7 @@ hipError_t launch_few(const GemmArgs& g, int64_t row_bytes, const LinearOut& o, 
     const int64_t blocks = (g.N + 15) / 16;
     if (blocks > kMostTiles) return hipErrorInvalidValue;
     const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>(slices)), threads(64 * kSkinnyWaves);
-    if (g.M <= 16)
-        hipLaunchKernelGGL((linear_skinny_kernel<E, 1>), grid, threads, 0, stream, g, row_bytes, o);
-    else if (g.M <= 32)
-        hipLaunchKernelGGL((linear_skinny_kernel<E, 2>), grid, threads, 0, stream, g, row_bytes, o);
-    else
-        hipLaunchKernelGGL((linear_skinny_kernel<E, 4>), grid, threads, 0, stream, g, row_bytes, o);
+    hipLaunchKernelGGL((linear_skinny_kernel<E, 1>), grid, threads, 0, stream, g, row_bytes, o);
     return hipGetLastError();
 }
 
@@ -385,23 +421,27 @@ hipError_t product(const Shape& s, GemmArgs g, int64_t row_bytes, LinearOut o, f
             e = launch_few<E>(g, row_bytes, o, s.slices, stream);
     }
     if (e != hipSuccess || s.slices == 1) return e;
-    hipLaunchKernelGGL(linear_join_kernel, walking(g.M * ((g.N + 7) / 8)), dim3(256), 0, stream, o,
-                       static_cast<int>(s.slices), g.M, g.N);
+    const int64_t outputs = g.M * ((g.N + 7) / 8);
+    if (outputs < 32768 && s.slices >= 8)
+        hipLaunchKernelGGL(linear_join_kernel<8>, walking(outputs * 8), dim3(256), 0, stream, o, static_cast<int>(s.slices),
+                           g.M, g.N);
+    else
+        hipLaunchKernelGGL(linear_join_kernel<1>, walking(outputs), dim3(256), 0, stream, o, static_cast<int>(s.slices), g.M,
+                           g.N);
     return hipGetLastError();
 }
 
-// As the 8-bit product's rule, measured there.
-bool few_rows(int64_t M, int64_t N, int64_t K) { return M <= 32 || (M <= kSkinnyRows && N <= 2 * K); }
-
 Shape forward_shape(int64_t M, int64_t K, int64_t N) {
-    return shape_of(few_rows(M, N, K), kPlain16, M, N, (K + 63) / 64, 1);
+    const int64_t steps = (K + 63) / 64;
+    return M <= kFewRows ? few_shape(N, steps, 1) : shape_of(kSlices16, M, N, steps, 1);
 }
 Shape forward8_shape(int64_t M, int64_t K, int64_t N) {
-    return shape_of(few_rows(M, N, K), kPlain8, M, N, (K + 127) / 128, 4);
+    const int64_t steps = (K + 127) / 128;
+    return M <= kFewRows ? few_shape(N, steps, 4) : shape_of(kSlices8, M, N, steps, 4);
 }
 // of dx, and of dw
-Shape dx_shape(int64_t M, int64_t K, int64_t N) { return shape_of(false, kPlain16, M, K, (N + 63) / 64, 1); }
-Shape dw_shape(int64_t M, int64_t K, int64_t N) { return shape_of(false, kPlain16, N, K, (M + 63) / 64, 1); }
+Shape dx_shape(int64_t M, int64_t K, int64_t N) { return shape_of(kSlices16, M, K, (N + 63) / 64, 1); }
+Shape dw_shape(int64_t M, int64_t K, int64_t N) { return shape_of(kSlices16, N, K, (M + 63) / 64, 1); }
 
 LinearOut out_of(const LinearArgs& a) {
     return LinearOut{a.act, a.dtype == SPINGTP_FP32, a.bias, a.r, a.ldr, a.y, a.ldy, static_cast<uint16_t*>(a.z),
@@ -475,18 +515,23 @@ hipError_t launch_linear(const LinearArgs& a, hipStream_t stream) {
     if (s.tile > 0) {
         const int64_t pitch = up(a.K, 64);
         uint16_t* free_at = reinterpret_cast<uint16_t*>(static_cast<uint8_t*>(a.workspace) + up16(s.bytes(a.M, a.N)));
+        RowCopy x{static_cast<const uint16_t*>(a.x), a.ldx, 0, nullptr}, w{static_cast<const uint16_t*>(a.w), a.ldw, 0, nullptr};
         if (!rows_fit(a.x, a.K, a.ldx)) {
-            const hipError_t e = copy_rows(a.x, a.ldx, free_at, a.M, a.K, stream);
-            if (e != hipSuccess) return e;
-            g.x = reinterpret_cast<const uint8_t*>(free_at);
-            g.ldx = 2 * pitch;
+            x.R = a.M;
+            x.to = free_at;
             free_at += a.M * pitch;
+            g.x = reinterpret_cast<const uint8_t*>(x.to);
+            g.ldx = 2 * pitch;
         }
         if (!rows_fit(a.w, a.K, a.ldw)) {
-            const hipError_t e = copy_rows(a.w, a.ldw, free_at, a.N, a.K, stream);
-            if (e != hipSuccess) return e;
-            g.w = reinterpret_cast<const uint8_t*>(free_at);
+            w.R = a.N;
+            w.to = free_at;
+            g.w = reinterpret_cast<const uint8_t*>(w.to);
             g.ldw = 2 * pitch;
+        }
+        if (x.R + w.R > 0) {
+            const hipError_t e = copy_rows(x, w, a.K, stream);
+            if (e != hipSuccess) return e;
         }
     }
     return product<Bf16, false, false>(s, g, 2 * a.K, out_of(a), static_cast<float*>(a.workspace), stream);
@@ -543,7 +588,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
     if (!own || sums != nullptr)
         e = a.dtype == SPINGTP_FP32 ? make_dz<float>(a, dz, sums, stream) : make_dz<uint16_t>(a, dz, sums, stream);
     if (e == hipSuccess && sums != nullptr) {
-        hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>((a.N + 63) / 64)), dim3(256), 0, stream, sums,
+        hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>((a.N + 15) / 16)), dim3(1024), 0, stream, sums,
                            dz_blocks(a.M, a.N), a.N, a.db);
         e = hipGetLastError();
     }
@@ -558,7 +603,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
         g.ldw = 2 * a.ldw;
         if (!rows_fit(a.w, a.K, a.ldw)) {
             uint16_t* copy = reinterpret_cast<uint16_t*>(at + up16(s.bytes(a.M, a.K)));
-            e = copy_rows(a.w, a.ldw, copy, a.N, a.K, stream);
+            e = copy_rows(RowCopy{static_cast<const uint16_t*>(a.w), a.ldw, a.N, copy}, RowCopy{}, a.K, stream);
             g.w = reinterpret_cast<const uint8_t*>(copy);
             g.ldw = 2 * kp;
         }
@@ -579,7 +624,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
         g.ldw = 2 * a.ldx;
         if (!rows_fit(a.x, a.K, a.ldx)) {
             uint16_t* copy = reinterpret_cast<uint16_t*>(at + up16(s.bytes(a.N, a.K)));
-            e = copy_rows(a.x, a.ldx, copy, a.M, a.K, stream);
+            e = copy_rows(RowCopy{static_cast<const uint16_t*>(a.x), a.ldx, a.M, copy}, RowCopy{}, a.K, stream);
             g.w = reinterpret_cast<const uint8_t*>(copy);
             g.ldw = 2 * kp;
         }

@@ -2,8 +2,8 @@
 //
 // Digits of at most 9 bits from the lowest on, each pass stable: a key goes behind all keys of smaller digits, and of
 // its own digit behind those before it.  Within a wave the lanes of the same digit are found by ballots of its bits,
-// so no step depends on the order of arrival.  Up to 8,192 keys one workgroup sorts in LDS; beyond, a pass is two launches, counts
-// per workgroup and the moves, at most 512 workgroups, each of which adds the others' counts up for itself.
+// so no step depends on the order of arrival.  Up to 16,384 keys one workgroup sorts in LDS; beyond, a pass is two launches,
+// counts per workgroup and the moves, at most 512 workgroups, each of which adds the others' counts up for itself.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -16,7 +16,7 @@ namespace spingtp {
 namespace {
 
 constexpr int kMostBits = 9, kBins = 1 << kMostBits;
-constexpr int kSmall = 8192;     // keys that one workgroup sorts
+constexpr int kSmall = 16384;    // keys that one workgroup sorts
 constexpr int kSmallWaves = 16;
 constexpr int kSortWaves = 8;
 constexpr int kMostSortBlocks = 512;
@@ -52,23 +52,10 @@ __device__ __forceinline__ uint32_t place_of(uint32_t digit, int bits, bool have
     return before + __popcll(below);
 }
 
-// counts [waves][kBins] to each wave's first place of each digit; `first`: of thread t's digit, what precedes it outside
-// this workgroup's keys.  Threads 0 to kBins - 1 have a digit each; `scratch`: kBins / 64 words.
-template <int WAVES>
-__device__ __forceinline__ void places(uint32_t* counts, uint32_t* scratch, uint32_t smaller_elsewhere, bool total_given,
-                                       uint32_t total) {
+// Thread t (of kBins and more) with digit t's number of keys: those of smaller digits.  `scratch`: kBins / 64 words.
+__device__ __forceinline__ uint32_t smaller_digits(uint32_t mine, uint32_t* scratch) {
     const int t = threadIdx.x, lane = t & 63;
-    uint32_t mine = 0;
-    if (t < kBins) {
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const uint32_t c = counts[w * kBins + t];
-            counts[w * kBins + t] = mine;
-            mine += c;
-        }
-    }
-    const uint32_t whole = total_given ? total : mine;
-    uint32_t sum = whole;  // of the digits up to this one
+    uint32_t sum = mine;  // of the digits up to this one
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t o = __shfl_up(sum, d, 64);
@@ -76,61 +63,80 @@ __device__ __forceinline__ void places(uint32_t* counts, uint32_t* scratch, uint
     }
     if (t < kBins && lane == 63) scratch[t >> 6] = sum;
     __syncthreads();
-    if (t < kBins) {
-        uint32_t base = smaller_elsewhere + sum - whole;
-        for (int w = 0; w < (t >> 6); ++w) base += scratch[w];
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) counts[w * kBins + t] += base;
-    }
-    __syncthreads();
+    uint32_t base = sum - mine;
+    for (int w = 0; w < (t >> 6) && w < kBins / 64; ++w) base += scratch[w];
+    return base;
 }
 
+// Every wave has its keys, 64 at a time in their order, in registers; LDS takes them once a pass.
 __global__ __launch_bounds__(64 * kSmallWaves) void sort_small_kernel(const void* index, bool wide, int32_t* order,
                                                                       int32_t* rows, int n, uint32_t V, int passes,
                                                                       int bits) {
     extern __shared__ __align__(16) uint32_t sort_lds[];
-    uint32_t* counts = sort_lds;                                // [kSmallWaves][kBins]
-    uint32_t* scratch = counts + kSmallWaves * kBins;           // [16]
-    uint32_t* keys[2] = {scratch + 16, scratch + 16 + kSmall};  // [kSmall] each
-    uint16_t* at[2] = {reinterpret_cast<uint16_t*>(keys[1] + kSmall), reinterpret_cast<uint16_t*>(keys[1] + kSmall) + kSmall};
+    uint32_t* counts = sort_lds;                       // [kSmallWaves][kBins]
+    uint32_t* scratch = counts + kSmallWaves * kBins;  // [16]
+    uint32_t* keys = scratch + 16;                     // [kSmall]
+    uint16_t* at = reinterpret_cast<uint16_t*>(keys + kSmall);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int per = (n + 64 * kSmallWaves - 1) / (64 * kSmallWaves) * 64;  // keys of a wave, in a row
-    for (int i = threadIdx.x; i < n; i += 64 * kSmallWaves) {
-        keys[0][i] = key_of(index, wide, i, V);
-        at[0][i] = static_cast<uint16_t>(i);
+    const uint32_t mask = (1u << bits) - 1;
+    uint32_t* mine = counts + wave * kBins;
+    constexpr int kGroups = kSmall / (64 * kSmallWaves);
+    uint32_t key[kGroups], from[kGroups], place[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        const int i = wave * per + 64 * g + lane;
+        const bool have = 64 * g < per && i < n;
+        key[g] = have ? key_of(index, wide, i, V) : 0;
+        from[g] = i;
     }
     for (int pass = 0; pass < passes; ++pass) {
-        const uint32_t* from = keys[pass & 1];
-        const uint16_t* from_at = at[pass & 1];
-        uint32_t* to = keys[(pass & 1) ^ 1];
-        uint16_t* to_at = at[(pass & 1) ^ 1];
+        const int shift = pass * bits;
         for (int i = threadIdx.x; i < kSmallWaves * kBins; i += 64 * kSmallWaves) counts[i] = 0;
         __syncthreads();
-        constexpr int kGroups = kSmall / (64 * kSmallWaves);
-        uint32_t key[kGroups], place[kGroups];
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            const int i = wave * per + 64 * g + lane;
-            const bool have = 64 * g < per && i < n;
-            key[g] = have ? from[i] : 0;
-            place[g] = place_of((key[g] >> (pass * bits)) & ((1u << bits) - 1), bits, have, counts + wave * kBins, lane);
+            if (64 * g >= per) break;
+            place[g] = place_of((key[g] >> shift) & mask, bits, wave * per + 64 * g + lane < n, mine, lane);
         }
         __syncthreads();
-        places<kSmallWaves>(counts, scratch, 0, false, 0);
+        uint32_t whole = 0;
+        if (threadIdx.x < kBins) {
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            const int i = wave * per + 64 * g + lane;
-            if (64 * g < per && i < n) {
-                const uint32_t p = counts[wave * kBins + ((key[g] >> (pass * bits)) & ((1u << bits) - 1))] + place[g];
-                to[p] = key[g];
-                to_at[p] = from_at[i];
+            for (int w = 0; w < kSmallWaves; ++w) whole += counts[w * kBins + threadIdx.x];
+        }
+        uint32_t base = smaller_digits(whole, scratch);
+        if (threadIdx.x < kBins) {
+#pragma unroll
+            for (int w = 0; w < kSmallWaves; ++w) {
+                const uint32_t c = counts[w * kBins + threadIdx.x];
+                counts[w * kBins + threadIdx.x] = base;
+                base += c;
             }
         }
         __syncthreads();
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            if (64 * g >= per) break;
+            if (wave * per + 64 * g + lane < n) {
+                const uint32_t p = mine[(key[g] >> shift) & mask] + place[g];
+                keys[p] = key[g];
+                at[p] = static_cast<uint16_t>(from[g]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            if (64 * g >= per) break;
+            const int i = wave * per + 64 * g + lane;
+            if (i < n) key[g] = keys[i], from[g] = at[i];
+        }
     }
-    for (int i = threadIdx.x; i < n; i += 64 * kSmallWaves) {
-        rows[i] = static_cast<int32_t>(keys[passes & 1][i]);
-        order[i] = at[passes & 1][i];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        if (64 * g >= per) break;
+        const int i = wave * per + 64 * g + lane;
+        if (i < n) rows[i] = static_cast<int32_t>(key[g]), order[i] = static_cast<int32_t>(from[g]);
     }
 }
 
@@ -142,7 +148,7 @@ struct SortFrom {
     const uint32_t* at;
     uint32_t V;
     int shift, bits;
-    int64_t n, per;  // keys of a workgroup, a multiple of 64 * kSortWaves
+    int64_t n, per;  // keys of a workgroup
 };
 __device__ __forceinline__ uint32_t sort_key(const SortFrom& f, int64_t i) {
     return f.index != nullptr ? key_of(f.index, f.wide, i, f.V) : f.keys[i];
@@ -159,37 +165,60 @@ __global__ __launch_bounds__(64 * kSortWaves) void sort_count_kernel(SortFrom f,
     counts[static_cast<int64_t>(blockIdx.x) * kBins + threadIdx.x] = bins[threadIdx.x];
 }
 
+// A workgroup moves its keys in rounds of kRound, in their order.
+constexpr int kMoveGroups = 2, kRound = 64 * kSortWaves * kMoveGroups;
 __global__ __launch_bounds__(64 * kSortWaves) void sort_move_kernel(SortFrom f, const uint32_t* counts, uint32_t* keys,
                                                                     uint32_t* at) {
     __shared__ uint32_t bins[kSortWaves * kBins];
     __shared__ uint32_t scratch[kBins / 64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t mask = (1u << f.bits) - 1;
-    uint32_t before = 0, total = 0;
+    uint32_t* mine = bins + wave * kBins;
+    const int64_t first = blockIdx.x * f.per, end = first + f.per < f.n ? first + f.per : f.n;
+    uint32_t key[kMoveGroups], from[kMoveGroups], place[kMoveGroups];
+    const auto take = [&](int64_t round) {
+#pragma unroll
+        for (int g = 0; g < kMoveGroups; ++g) {
+            const int64_t i = round + (wave * kMoveGroups + g) * 64 + lane;
+            key[g] = i < end ? sort_key(f, i) : 0;
+            from[g] = f.index != nullptr || i >= end ? static_cast<uint32_t>(i) : f.at[i];
+        }
+    };
+    take(first);
+    uint32_t base = 0, total = 0;
 #pragma unroll 8
     for (unsigned b = 0; b < gridDim.x; ++b) {
         const uint32_t c = counts[static_cast<int64_t>(b) * kBins + threadIdx.x];
-        before += b < blockIdx.x ? c : 0;
+        base += b < blockIdx.x ? c : 0;
         total += c;
     }
+    base += smaller_digits(total, scratch);
+    for (int64_t round = first; round < end; round += kRound) {
+        if (round > first) take(round);
 #pragma unroll
-    for (int w = 0; w < kSortWaves; ++w) bins[w * kBins + threadIdx.x] = 0;
-    __syncthreads();
-    uint32_t* mine = bins + wave * kBins;
-    const int64_t per = f.per / kSortWaves, first = blockIdx.x * f.per + wave * per;
-    const int64_t end = first + per < f.n ? first + per : f.n;
-    for (int64_t i = first + lane; i < end; i += 64) atomicAdd(&mine[(sort_key(f, i) >> f.shift) & mask], 1u);
-    __syncthreads();
-    places<kSortWaves>(bins, scratch, before, true, total);
-    for (int64_t g = first; g < end; g += 64) {
-        const int64_t i = g + lane;
-        const bool have = i < end;
-        const uint32_t key = have ? sort_key(f, i) : 0;
-        const uint32_t p = place_of((key >> f.shift) & mask, f.bits, have, mine, lane);
-        if (have) {
-            keys[p] = key;
-            at[p] = f.index != nullptr ? static_cast<uint32_t>(i) : f.at[i];
+        for (int w = 0; w < kSortWaves; ++w) bins[w * kBins + threadIdx.x] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < kMoveGroups; ++g)
+            place[g] = place_of((key[g] >> f.shift) & mask, f.bits, round + (wave * kMoveGroups + g) * 64 + lane < end, mine,
+                                lane);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = bins[w * kBins + threadIdx.x];
+            bins[w * kBins + threadIdx.x] = base;
+            base += c;
         }
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < kMoveGroups; ++g) {
+            if (round + (wave * kMoveGroups + g) * 64 + lane < end) {
+                const uint32_t p = mine[(key[g] >> f.shift) & mask] + place[g];
+                keys[p] = key[g];
+                at[p] = from[g];
+            }
+        }
+        __syncthreads();
     }
 }
 
@@ -217,15 +246,14 @@ hipError_t launch_sort_index(const void* index, bool wide, int32_t* order, int32
     if (n <= kSmall) {
         const hipError_t e = raise_lds_limit<sort_small_kernel>();
         if (e != hipSuccess) return e;
-        constexpr int lds = (kSmallWaves * kBins + 16 + 2 * kSmall) * 4 + 2 * kSmall * 2;
+        constexpr int lds = (kSmallWaves * kBins + 16 + kSmall) * 4 + kSmall * 2;
         static_assert(lds <= 160 * 1024, "in LDS");
         hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(64 * kSmallWaves), lds, stream, index, wide, order, rows,
                            static_cast<int>(n), static_cast<uint32_t>(V), passes, bits);
         return hipGetLastError();
     }
-    constexpr int64_t grain = 2 * 64 * kSortWaves;
     int64_t per = (n + kMostSortBlocks - 1) / kMostSortBlocks;
-    per = (per + grain - 1) / grain * grain;
+    per = (per + kRound - 1) / kRound * kRound;
     const unsigned blocks = static_cast<unsigned>((n + per - 1) / per);
     uint32_t* counts = static_cast<uint32_t*>(workspace);
     uint32_t* tmp = counts + kMostSortBlocks * kBins;

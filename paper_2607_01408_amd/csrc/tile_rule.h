@@ -49,6 +49,56 @@ inline int product_tile(const TileCosts& c, int64_t M, int64_t N) {
 inline int gated_tile(int64_t M, int64_t F) {
     return pick_tile(kGated, tiles_of(M, F, 64, 128), tiles_of(M, F, 128, 128), tiles_of(M, F, 256, 128));
 }
+// The linear layer's products have sums of any length, which may be cut into slices, a workgroup to each.  A tile takes
+// `fixed` for its start and end, and each step of its sum (128 bytes a row) `step`, up to `more` longer with the part of
+// the CUs that is busy; slices are written in fp32 and joined by a second launch.  us, fitted to (64 / 128 / 256):
+//   bf16 (rows x columns of w x sum), 8,192 x 2,048 x 8,192 409 / 240 / 211, 8,192 x 8,192 x 2,048 412 / 255 / 250,
+//     100,000 x 512 x 128 60 / 33 / 63, 5,001 x 4,096 x 1,024 76 / 49 / 70, 3,000^3 114 / 97 / 80, 2,048^3 29 / 24 / 51,
+//     999 x 1,000 x 2,736 14 / 35 / 69, and in 8 slices 30 / 25 / 29; 300 x 300 x 8,192 30 / 75 / 155, in 8 13 / 18 / 40;
+//   8 bits, 64 x 2,048 x 8,192 30 / 58 / -, in 8 slices 12 / 18 / -.
+struct SliceCost {
+    int at_once;
+    double fixed, step, more;
+};
+struct SliceCosts {
+    SliceCost of64, of128, of256;
+};
+constexpr SliceCosts kSlices16 = {{512, 1.7, 0.22, 0.17}, {512, 3.6, 0.57, 0.35}, {256, 12, 1.19, 0.42}};
+constexpr SliceCosts kSlices8 = {{512, 1.7, 0.43, 0.34}, {512, 3.6, 0.87, 0.85}, {256, 12, 2.0, 1.2}};
+inline double slice_time(const SliceCost& c, int64_t workgroups, int64_t steps) {
+    const int64_t full = workgroups / c.at_once, rest = workgroups - full * c.at_once;
+    const double n = static_cast<double>(steps);
+    double t = static_cast<double>(full) * (c.fixed + n * (c.step + c.more));
+    if (rest > 0) t += c.fixed + n * (c.step + c.more * static_cast<double>(rest) / c.at_once);
+    return t;
+}
+// The tile of a product of [M][N] outputs, and how many steps of `steps` a slice of its sum takes (all: one slice; a
+// multiple of `grain`, and 4 or more).
+struct SumShape {
+    int tile;
+    int64_t slices, per;
+};
+inline SumShape sum_shape(const SliceCosts& c, int64_t M, int64_t N, int64_t steps, int64_t grain) {
+    SumShape best{256, 1, steps};
+    double least = 1e300;
+    for (int tile = 64; tile <= 256; tile *= 2) {
+        const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
+        if (tiles > kMostTiles) continue;
+        const SliceCost& cost = tile == 64 ? c.of64 : (tile == 128 ? c.of128 : c.of256);
+        for (int64_t want = 1; want <= 256; want = want < 4 ? want + 1 : want + want / 2) {
+            if (want > 1 && (steps < 4 * want || tiles * want > 1024)) break;
+            const int64_t per = ((steps + want - 1) / want + grain - 1) / grain * grain, slices = (steps + per - 1) / per;
+            double t = slice_time(cost, tiles * slices, want > 1 ? per : steps);
+            if (slices > 1)  // both ways through memory, and a launch
+                t += 4.5 + 8.0 * static_cast<double>(slices) * static_cast<double>(M) * static_cast<double>(N) / 3.8e6;
+            if (t < least) {
+                least = t;
+                best = SumShape{tile, slices, slices > 1 ? per : steps};
+            }
+        }
+    }
+    return best;
+}
 // whether a launch can hold them in the largest tiles
 inline bool product_fits(int64_t M, int64_t N) { return tiles_of(M, N, 256, 256) <= kMostTiles; }
 inline bool gated_fits(int64_t M, int64_t F) { return tiles_of(M, F, 256, 128) <= kMostTiles; }

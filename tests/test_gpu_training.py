@@ -67,7 +67,7 @@ def index_of(kind, n, V, seed):
 
 KINDS = ["even", "one", "skewed", "outside"]
 SORTED = [(1, 1), (2, 3), (63, 1000), (64, 2), (65, 511), (1000, 512), (1025, 513), (8191, 100_000), (8192, 262_143),
-          (8193, 262_144), (20_001, 7), (100_000, 4_000), (300_007, 50_000), (1_200_001, 600_000), (70_001, 0x7FFFFFFE)]
+          (8193, 262_144), (16_384, 70_000), (16_385, 100), (20_001, 7), (100_000, 4_000), (300_007, 50_000), (1_200_001, 600_000), (70_001, 0x7FFFFFFE)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
