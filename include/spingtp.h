@@ -835,7 +835,7 @@ spingtp_status spingtp_embedding(int dtype, const void* table, int64_t ldt, cons
 
 /* An index in the order of its rows: order [n] its places, equal rows in their own order, and rows [n] what they
  * name (V: none, at the end).  For the gradients of as many lookups as take the index.  workspace (16-byte
- * aligned): the size below, 0 up to 16384 entries. */
+ * aligned): the size below, 0 up to 8192 entries. */
 spingtp_status spingtp_sort_index(const void* index, int index_bytes, int32_t* order, int32_t* rows, void* workspace,
                                   size_t workspace_bytes, int64_t n, int64_t V, void* stream);
 spingtp_status spingtp_sort_index_workspace_size(int64_t n, int64_t V, size_t* size);

@@ -2,8 +2,8 @@
 //   g' = grad_scale g,  m = b1 m + (1 - b1) g',  v = b2 v + (1 - b2) g'^2,
 //   p = (1 - lr wd) p - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
 //
-// One launch for as many tensors as its arguments hold; a workgroup finds its tensor there and takes 2,048 neighbouring
-// elements of it, eight to a lane.  Nothing is uploaded, so a captured launch keeps its own table.
+// One launch for as many tensors of a kind (types, states) as its arguments hold; a workgroup finds its tensor there and
+// takes 2,048 neighbouring elements of it, eight to a lane.  Nothing is uploaded, so a captured launch keeps its own table.
 //
 // States in 8 bits: m and sqrt(v) (half of v's range of exponents) in blocks of 128 elements, 16 lanes.  A step of v moves
 // it by a thousandth, a step of the format is a sixteenth to an eighth: rounded to nearest, v would stay where it is.  So
@@ -17,6 +17,7 @@
 
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "block8.h"
 #include "internal.h"
@@ -25,40 +26,53 @@
 namespace spingtp {
 namespace {
 
-struct AdamwEntry {
+constexpr int kAdamwChunk = 2048;
+constexpr int kArgumentBytes = 4096;
+
+// A tensor, or a piece of one.
+struct Entry32 {
     void* p;
     const void* g;
-    void* m;
-    void* v;
+    float* m;
+    float* v;
+    uint16_t* copy;
+    uint32_t n;  // elements
+};
+struct Entry8 {
+    void* p;
+    const void* g;
+    uint8_t* m;
+    uint8_t* v;
     uint8_t* ms;
     uint8_t* vs;
     uint16_t* copy;
-    int64_t n;      // elements, of this piece
-    int64_t first;  // of the piece in its tensor
-    uint32_t place;
-    uint32_t kinds;  // kParam16, ...
+    uint32_t n;
+    uint32_t place;  // in the list
+    int64_t first;   // element of the tensor
 };
-enum : uint32_t { kParam16 = 1, kGrad16 = 2 };
-constexpr int kMostEntries = 46;  // with them the arguments stay below 4 KB; at most a wave's lanes
-constexpr int kAdamwChunk = 2048;
-
-struct AdamwArgs {
+struct AdamwNumbers {
     float b1, c1, b2, c2;  // c: 1 - b
-    float eps, least;      // 1 / c above, 0 where there is no bound
+    float eps, least;      // least: 1 / c above, 0 where there is no bound
     float decay, rate;     // 1 - lr wd, lr / (1 - b1^t)
     float root;            // (1 - b2^t)^(-1/2)
-    double wd, log_b1, log_b2;
+    int entries;
+    bool around;  // the tensors are too large for the caches
+    double wd, lr, log_b1, log_b2;
     int64_t step;
     uint64_t seed;
     const int64_t* device_step;  // may be null: the step, lr and the factor of the gradients
     const float* device_lr;
     const float* grad_scale;
-    double lr;
-    int entries;
-    uint32_t block[kMostEntries];  // an entry's first workgroup
-    AdamwEntry entry[kMostEntries];
 };
-static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
+template <bool BITS8>
+struct AdamwArgs {
+    using Entry = std::conditional_t<BITS8, Entry8, Entry32>;
+    static constexpr int kMost = (kArgumentBytes - sizeof(AdamwNumbers)) / (sizeof(Entry) + 4);
+    AdamwNumbers o;
+    uint32_t block[kMost];  // an entry's first workgroup
+    Entry entry[kMost];
+};
+static_assert(sizeof(AdamwArgs<false>) <= kArgumentBytes && sizeof(AdamwArgs<true>) <= kArgumentBytes);
 
 __host__ __device__ inline uint32_t mix(uint32_t x) {
     x ^= x >> 16;
@@ -109,41 +123,29 @@ __device__ __forceinline__ void put_block(const float (&x)[8], const float (&siz
     if (leader) *scale = static_cast<uint8_t>(e);
 }
 
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
+template <bool BITS8, typename TP, typename TG>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8> a) {
     // the last entry that begins here or before, a lane to each: one read of the arguments
+    const AdamwNumbers& o = a.o;
     const int lane = threadIdx.x & 63;
-    const uint32_t begins = a.block[lane < kMostEntries ? lane : 0];
-    const int at = __popcll(__ballot(lane < a.entries && begins <= blockIdx.x)) - 1;
-    const AdamwEntry& t = a.entry[at];
-    const uint32_t block = blockIdx.x - a.block[at];
-    float decay = a.decay, rate = a.rate, root = a.root;
-    int64_t step = a.step;
-    if (a.device_step != nullptr || a.device_lr != nullptr) {
-        if (a.device_step != nullptr) step = *a.device_step > 1 ? *a.device_step : 1;
-        const double lr = a.device_lr != nullptr ? static_cast<double>(*a.device_lr) : a.lr;
-        decay = static_cast<float>(1.0 - lr * a.wd);
-        rate = static_cast<float>(lr / -expm1(static_cast<double>(step) * a.log_b1));
-        root = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(step) * a.log_b2)));
+    int at = -1;
+#pragma unroll
+    for (int first = 0; first < AdamwArgs<BITS8>::kMost; first += 64) {
+        const int e = first + lane < o.entries ? first + lane : 0;
+        at += __popcll(__ballot(first + lane < o.entries && a.block[e] <= blockIdx.x));
     }
-    const int64_t i0 = static_cast<int64_t>(block) * kAdamwChunk + threadIdx.x * 8;
-    const int64_t left = t.n - i0;
+    const auto& t = a.entry[at];
+    const int64_t n = t.n, i0 = static_cast<int64_t>(blockIdx.x - a.block[at]) * kAdamwChunk + threadIdx.x * 8;
+    const int64_t left = n - i0;
     const int have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
-    const bool blocks = t.ms != nullptr;
     // a block's sixteen lanes stay together: their places reach past n
-    if (i0 >= (blocks ? (t.n + kBlock8 - 1) / kBlock8 * kBlock8 : t.n)) return;
+    if (i0 >= (BITS8 ? (n + kBlock8 - 1) / kBlock8 * kBlock8 : n)) return;
     const int64_t from = have > 0 ? i0 : 0;
     float p[8], g[8], m[8], v[8];
-    if (t.kinds & kParam16)
-        pass8(static_cast<const uint16_t*>(t.p) + from, have, p);
-    else
-        pass8(static_cast<const float*>(t.p) + from, have, p);
-    if (t.kinds & kGrad16)
-        pass8(static_cast<const uint16_t*>(t.g) + from, have, g);
-    else
-        pass8(static_cast<const float*>(t.g) + from, have, g);
-    if (blocks) {
-        const uint2 wm = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.m) + i0);
-        const uint2 wv = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + i0);
+    pass8(static_cast<const TP*>(t.p) + from, have, p);
+    pass8(static_cast<const TG*>(t.g) + from, have, g);
+    if constexpr (BITS8) {
+        const uint2 wm = *reinterpret_cast<const uint2*>(t.m + i0), wv = *reinterpret_cast<const uint2*>(t.v + i0);
         const float sm = block8_power(t.ms[i0 / kBlock8]), sv = block8_power(t.vs[i0 / kBlock8]);
         float lo[4], hi[4];
         block8_values(wm.x, lo);
@@ -158,115 +160,150 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs a) {
             v[i] = x * x, v[4 + i] = y * y;
         }
     } else {
-        pass8(static_cast<const float*>(t.m) + from, have, m);
-        pass8(static_cast<const float*>(t.v) + from, have, v);
+        pass8(t.m + from, have, m);
+        pass8(t.v + from, have, v);
     }
-    const float factor = a.grad_scale != nullptr ? *a.grad_scale : 1.f;
+    float decay = o.decay, rate = o.rate, root = o.root;
+    int64_t step = o.step;
+    if (o.device_step != nullptr || o.device_lr != nullptr) {
+        if (o.device_step != nullptr) step = *o.device_step > 1 ? *o.device_step : 1;
+        const double lr = o.device_lr != nullptr ? static_cast<double>(*o.device_lr) : o.lr;
+        decay = static_cast<float>(1.0 - lr * o.wd);
+        rate = static_cast<float>(lr / -expm1(static_cast<double>(step) * o.log_b1));
+        root = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(step) * o.log_b2)));
+    }
+    const float factor = o.grad_scale != nullptr ? *o.grad_scale : 1.f;
     float size[8], s[8];
     {
 #pragma clang fp contract(off)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float x = g[i] * factor;
-            m[i] = a.b1 * m[i] + a.c1 * x;
-            v[i] = a.b2 * v[i] + a.c2 * (x * x);
-            if (blocks) {
-                const float y = m[i] * a.least, least = y * y;
+            m[i] = o.b1 * m[i] + o.c1 * x;
+            v[i] = o.b2 * v[i] + o.c2 * (x * x);
+            if constexpr (BITS8) {
+                const float y = m[i] * o.least, least = y * y;
                 v[i] = least > v[i] ? least : v[i];
                 if (i >= have) m[i] = v[i] = 0.f;  // zeros behind the tensor whatever lies there
             }
             s[i] = sqrtf(v[i]);
             size[i] = fabsf(m[i]);
-            p[i] = p[i] * decay - rate * (m[i] / (s[i] * root + a.eps));
+            p[i] = p[i] * decay - rate * (m[i] / (s[i] * root + o.eps));
         }
     }
-    if (t.kinds & kParam16) {
-        store8(static_cast<uint16_t*>(t.p) + from, have, p);
-    } else {
-        store8(static_cast<float*>(t.p) + from, have, p);
-        if (t.copy != nullptr) store8(t.copy + from, have, p);
-    }
-    if (!blocks) {
-        store8(static_cast<float*>(t.m) + from, have, m);
-        store8(static_cast<float*>(t.v) + from, have, v);
-        return;
-    }
-    const uint32_t key =
-        mix(mix(static_cast<uint32_t>(a.seed) + t.place * 0x9E3779B9u) + static_cast<uint32_t>(step) * 0x3C6EF373u +
-            static_cast<uint32_t>(a.seed >> 32));
-    const int64_t e = t.first + i0;
-    const uint32_t high = static_cast<uint32_t>(e >> 32) * 0x3C6EF373u + key;  // of all eight: a multiple of 8
-    uint32_t word[8];
+    pass_store8(static_cast<TP*>(t.p) + from, have, p, o.around);
+    if (sizeof(TP) == 4 && t.copy != nullptr) pass_store8(t.copy + from, have, p, o.around);
+    if constexpr (BITS8) {
+        const uint32_t key =
+            mix(mix(static_cast<uint32_t>(o.seed) + t.place * 0x9E3779B9u) + static_cast<uint32_t>(step) * 0x3C6EF373u +
+                static_cast<uint32_t>(o.seed >> 32));
+        const int64_t e = t.first + i0;
+        const uint32_t high = static_cast<uint32_t>(e >> 32) * 0x3C6EF373u + key;  // of all eight: a multiple of 8
+        uint32_t word[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) word[i] = mix((static_cast<uint32_t>(e) + i) * 0x9E3779B9u + high);
-    const bool leader = (threadIdx.x & 15) == 0;
-    put_block<false>(m, size, word, static_cast<uint8_t*>(t.m) + i0, t.ms + i0 / kBlock8, leader);
-    put_block<true>(v, s, word, static_cast<uint8_t*>(t.v) + i0, t.vs + i0 / kBlock8, leader);
+        for (int i = 0; i < 8; ++i) word[i] = mix((static_cast<uint32_t>(e) + i) * 0x9E3779B9u + high);
+        const bool leader = (threadIdx.x & 15) == 0;
+        put_block<false>(m, size, word, t.m + i0, t.ms + i0 / kBlock8, leader);
+        put_block<true>(v, s, word, t.v + i0, t.vs + i0 / kBlock8, leader);
+    } else {
+        pass_store8(t.m + from, have, m, o.around);
+        pass_store8(t.v + from, have, v, o.around);
+    }
 }
 
 constexpr int64_t kMostPiece = int64_t{1} << 30;  // elements of an entry
 
-}  // namespace
-
-hipError_t launch_adamw(const spingtp_adamw_tensor* tensors, int64_t count, const spingtp_adamw_options& o,
-                        hipStream_t stream) {
-    AdamwArgs a{};
-    a.b1 = static_cast<float>(o.beta1);
-    a.c1 = static_cast<float>(1.0 - o.beta1);
-    a.b2 = static_cast<float>(o.beta2);
-    a.c2 = static_cast<float>(1.0 - o.beta2);
-    a.eps = static_cast<float>(o.eps);
-    const double bound = o.beta2 > 0 ? 1.0 - o.beta1 * o.beta1 / o.beta2 : 0.0;
-    a.least = bound > 0 ? static_cast<float>(std::sqrt((1.0 - o.beta2) * bound) / (1.0 - o.beta1)) : 0.f;
-    a.wd = o.weight_decay;
-    a.lr = o.lr;
-    a.log_b1 = std::log(o.beta1);
-    a.log_b2 = std::log(o.beta2);
-    a.step = o.step;
-    a.seed = o.seed;
-    a.device_step = o.device_step;
-    a.device_lr = o.device_lr;
-    a.grad_scale = o.grad_scale;
-    const double t = static_cast<double>(o.step > 1 ? o.step : 1);
-    a.decay = static_cast<float>(1.0 - o.lr * o.weight_decay);
-    a.rate = static_cast<float>(o.lr / -std::expm1(t * a.log_b1));
-    a.root = static_cast<float>(1.0 / std::sqrt(-std::expm1(t * a.log_b2)));
+// The list's tensors of one kind, in as few launches as hold them.
+template <bool BITS8, typename TP, typename TG>
+hipError_t launch_kind(const spingtp_adamw_tensor* tensors, int64_t count, const AdamwNumbers& o, hipStream_t stream) {
+    AdamwArgs<BITS8> a;
+    a.o = o;
+    a.o.entries = 0;
     int64_t blocks = 0;
     const auto flush = [&]() {
-        if (a.entries == 0) return hipSuccess;
-        hipLaunchKernelGGL(adamw_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
-        a.entries = 0;
+        if (a.o.entries == 0) return hipSuccess;
+        hipLaunchKernelGGL((adamw_kernel<BITS8, TP, TG>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        a.o.entries = 0;
         blocks = 0;
         return hipGetLastError();
     };
+    constexpr int pd = sizeof(TP) == 4 ? SPINGTP_FP32 : SPINGTP_BF16, gd = sizeof(TG) == 4 ? SPINGTP_FP32 : SPINGTP_BF16;
     for (int64_t k = 0; k < count; ++k) {
         const spingtp_adamw_tensor& x = tensors[k];
+        if (x.param_dtype != pd || x.grad_dtype != gd || (x.m_scales != nullptr) != BITS8) continue;
         for (int64_t first = 0; first < x.n; first += kMostPiece) {
             const int64_t n = x.n - first < kMostPiece ? x.n - first : kMostPiece;
             const int64_t mine = (n + kAdamwChunk - 1) / kAdamwChunk;
-            if (a.entries == kMostEntries || blocks + mine > kMostBlocks) {
+            if (a.o.entries == AdamwArgs<BITS8>::kMost || blocks + mine > kMostBlocks) {
                 const hipError_t e = flush();
                 if (e != hipSuccess) return e;
             }
-            a.block[a.entries] = static_cast<uint32_t>(blocks);
-            AdamwEntry& to = a.entry[a.entries++];
-            const int64_t pw = x.param_dtype == SPINGTP_FP32 ? 4 : 2, gw = x.grad_dtype == SPINGTP_FP32 ? 4 : 2;
-            const bool eight = x.m_scales != nullptr;
-            to.p = static_cast<uint8_t*>(x.param) + first * pw;
-            to.g = static_cast<const uint8_t*>(x.grad) + first * gw;
-            to.m = static_cast<uint8_t*>(x.m) + first * (eight ? 1 : 4);
-            to.v = static_cast<uint8_t*>(x.v) + first * (eight ? 1 : 4);
-            to.ms = eight ? static_cast<uint8_t*>(x.m_scales) + first / kBlock8 : nullptr;
-            to.vs = eight ? static_cast<uint8_t*>(x.v_scales) + first / kBlock8 : nullptr;
+            a.block[a.o.entries] = static_cast<uint32_t>(blocks);
+            auto& to = a.entry[a.o.entries++];
+            to.p = static_cast<TP*>(x.param) + first;
+            to.g = static_cast<const TG*>(x.grad) + first;
             to.copy = x.copy != nullptr ? static_cast<uint16_t*>(x.copy) + first : nullptr;
-            to.n = n;
-            to.first = first;
-            to.place = static_cast<uint32_t>(k);
-            to.kinds = (pw == 2 ? kParam16 : 0) | (gw == 2 ? kGrad16 : 0);
+            to.n = static_cast<uint32_t>(n);
+            if constexpr (BITS8) {
+                to.m = static_cast<uint8_t*>(x.m) + first;
+                to.v = static_cast<uint8_t*>(x.v) + first;
+                to.ms = static_cast<uint8_t*>(x.m_scales) + first / kBlock8;
+                to.vs = static_cast<uint8_t*>(x.v_scales) + first / kBlock8;
+                to.place = static_cast<uint32_t>(k);
+                to.first = first;
+            } else {
+                to.m = static_cast<float*>(x.m) + first;
+                to.v = static_cast<float*>(x.v) + first;
+            }
             blocks += mine;
         }
     }
     return flush();
+}
+
+}  // namespace
+
+hipError_t launch_adamw(const spingtp_adamw_tensor* tensors, int64_t count, const spingtp_adamw_options& given,
+                        hipStream_t stream) {
+    AdamwNumbers o{};
+    o.b1 = static_cast<float>(given.beta1);
+    o.c1 = static_cast<float>(1.0 - given.beta1);
+    o.b2 = static_cast<float>(given.beta2);
+    o.c2 = static_cast<float>(1.0 - given.beta2);
+    o.eps = static_cast<float>(given.eps);
+    const double bound = given.beta2 > 0 ? 1.0 - given.beta1 * given.beta1 / given.beta2 : 0.0;
+    o.least = bound > 0 ? static_cast<float>(std::sqrt((1.0 - given.beta2) * bound) / (1.0 - given.beta1)) : 0.f;
+    o.wd = given.weight_decay;
+    o.lr = given.lr;
+    o.log_b1 = std::log(given.beta1);
+    o.log_b2 = std::log(given.beta2);
+    o.step = given.step;
+    o.seed = given.seed;
+    o.device_step = given.device_step;
+    o.device_lr = given.device_lr;
+    o.grad_scale = given.grad_scale;
+    const double t = static_cast<double>(given.step > 1 ? given.step : 1);
+    o.decay = static_cast<float>(1.0 - given.lr * given.weight_decay);
+    o.rate = static_cast<float>(given.lr / -std::expm1(t * o.log_b1));
+    o.root = static_cast<float>(1.0 / std::sqrt(-std::expm1(t * o.log_b2)));
+    int64_t elements = 0;
+    for (int64_t k = 0; k < count; ++k) elements += tensors[k].n;
+    o.around = elements > int64_t{1} << 22;
+    bool kinds[8] = {};
+    for (int64_t k = 0; k < count; ++k)
+        kinds[(tensors[k].m_scales != nullptr) * 4 + (tensors[k].param_dtype == SPINGTP_BF16) * 2 +
+              (tensors[k].grad_dtype == SPINGTP_BF16)] = true;
+    using Launch = hipError_t (*)(const spingtp_adamw_tensor*, int64_t, const AdamwNumbers&, hipStream_t);
+    constexpr Launch launch[8] = {launch_kind<false, float, float>,    launch_kind<false, float, uint16_t>,
+                                  launch_kind<false, uint16_t, float>, launch_kind<false, uint16_t, uint16_t>,
+                                  launch_kind<true, float, float>,     launch_kind<true, float, uint16_t>,
+                                  launch_kind<true, uint16_t, float>,  launch_kind<true, uint16_t, uint16_t>};
+    for (int i = 0; i < 8; ++i)
+        if (kinds[i]) {
+            const hipError_t e = launch[i](tensors, count, o, stream);
+            if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
 }
 
 }  // namespace spingtp

@@ -151,10 +151,9 @@ Block block(PyObject* values, PyObject* scales) {
 }
 
 // values, scales, R, D: refuses what is no Block8 of that shape
-PyObject* check_block(Args a) {
-    const at::Tensor& v = tensor(a[0], "values");
-    const at::Tensor& s = tensor(a[1], "scales");
-    const int64_t R = integer(a[2]), D = integer(a[3]);
+void check_block(PyObject* values, PyObject* scales, int64_t R, int64_t D) {
+    const at::Tensor& v = tensor(values, "values");
+    const at::Tensor& s = tensor(scales, "scales");
     if (R < 0 || D < 0) throw Refused("no matrix has the shape " + shape_text(R, D));
     const int64_t pitch = up(D, 128), spitch = up(D, 512) / 128;
     if (v.scalar_type() != at::kFloat8_e4m3fn || v.dim() != 2 || v.size(0) != R || v.size(1) != pitch ||
@@ -163,6 +162,9 @@ PyObject* check_block(Args a) {
     if (s.scalar_type() != at::kFloat8_e8m0fnu || s.dim() != 2 || s.size(0) != R || s.size(1) != spitch ||
         !s.is_contiguous() || s.device() != v.device())
         throw Refused("scales must be a contiguous float8_e8m0fnu " + shape_text(R, spitch) + " tensor beside the values");
+}
+PyObject* check_block(Args a) {
+    check_block(a[0], a[1], integer(a[2]), integer(a[3]));
     Py_RETURN_NONE;
 }
 
@@ -627,36 +629,50 @@ PyObject* embedding_backward(Args a) {
     return wrap(out);
 }
 
-// The tensors of an AdamW step: of one device, contiguous, of `n` elements; and what memory they take.
+// The tensors of an AdamW step: of one device, contiguous, of `n` elements; and what memory they take, a list of each
+// kind (mostly in the order of its addresses already).
 struct Places {
     struct Range {
         uintptr_t first, last;
-        bool written;
     };
-    std::vector<Range> all;
+    enum Kind { kParam, kGrad, kM, kV, kScaleM, kScaleV, kCopy, kKinds };
+    std::vector<Range> all[kKinds];
     const at::Tensor* beside = nullptr;
 
-    const at::Tensor& take(PyObject* o, const char* name, int64_t n, bool written) {
+    const at::Tensor& take(PyObject* o, const char* name, int64_t n, Kind kind) {
         const at::Tensor& t = tensor(o, name);
         if (!t.is_cuda()) throw Refused(std::string(name) + " must be on a GPU");
         if (beside == nullptr) beside = &t;
         if (t.device() != beside->device()) throw Refused("all tensors must be on one device");
         if (!t.is_contiguous()) throw Refused(std::string(name) + " must be contiguous");
-        if (n >= 0 && t.numel() != n)
+        const int64_t have = t.numel();
+        if (n >= 0 && have != n)
             throw Refused(std::string(name) + " must have the param's " + std::to_string(n) + " elements, not " +
-                          std::to_string(t.numel()));
+                          std::to_string(have));
         const auto p = reinterpret_cast<uintptr_t>(t.data_ptr());
-        if (t.numel() > 0) all.push_back({p, p + t.nbytes(), written});
+        if (have > 0) all[kind].push_back({p, p + static_cast<uintptr_t>(have) * t.element_size()});
         return t;
     }
     // Refuses memory that is written and held by another as well.
     void apart() {
-        std::sort(all.begin(), all.end(), [](const Range& x, const Range& y) { return x.first < y.first; });
+        const auto less = [](const Range& x, const Range& y) { return x.first < y.first; };
+        const Range* at[kKinds];
+        const Range* end[kKinds];
+        for (int k = 0; k < kKinds; ++k) {
+            if (!std::is_sorted(all[k].begin(), all[k].end(), less)) std::sort(all[k].begin(), all[k].end(), less);
+            at[k] = all[k].data();
+            end[k] = at[k] + all[k].size();
+        }
         uintptr_t any = 0, written = 0;  // the ends so far
-        for (const Range& r : all) {
-            if (r.first < (r.written ? any : written)) throw Refused("tensors that are written overlap others");
+        for (;;) {
+            int next = -1;
+            for (int k = 0; k < kKinds; ++k)
+                if (at[k] != end[k] && (next < 0 || at[k]->first < at[next]->first)) next = k;
+            if (next < 0) return;
+            const Range& r = *at[next]++;
+            if (r.first < (next != kGrad ? any : written)) throw Refused("tensors that are written overlap others");
             any = std::max(any, r.last);
-            if (r.written) written = std::max(written, r.last);
+            if (next != kGrad) written = std::max(written, r.last);
         }
     }
 };
@@ -685,7 +701,15 @@ const T* device_number(PyObject* o, const char* name, at::ScalarType type, const
     return t.data_ptr<T>();
 }
 
-// params, grads, m, v (tensors or (values, scales, rows, columns)), copies | None, step, lr, beta1, beta2, eps, weight_decay,
+// A new reference that goes with its place.
+struct Held {
+    PyObject* o;
+    explicit Held(PyObject* o_) : o(o_) {}
+    Held(const Held&) = delete;
+    ~Held() { Py_XDECREF(o); }
+};
+
+// params, grads, m, v (tensors or Block8), copies | None, step, lr, beta1, beta2, eps, weight_decay,
 // grad_scale | None, seed, stream
 PyObject* adamw(Args a) {
     const Items params(a[0], "params", -1), grads(a[1], "grads", params.n), m(a[2], "m", params.n), v(a[3], "v", params.n);
@@ -693,35 +717,41 @@ PyObject* adamw(Args a) {
     const Items copies(some ? a[4] : a[0], "copies", params.n);
     std::vector<spingtp_adamw_tensor> list(static_cast<size_t>(params.n));
     Places places;
-    places.all.reserve(7 * list.size());
+    for (auto& ranges : places.all) ranges.reserve(list.size());
     for (Py_ssize_t i = 0; i < params.n; ++i) {
         spingtp_adamw_tensor& to = list[static_cast<size_t>(i)];
-        const at::Tensor& p = places.take(params.at[i], "params", -1, true);
+        const at::Tensor& p = places.take(params.at[i], "params", -1, Places::kParam);
         const int64_t n = p.numel();
-        const at::Tensor& g = places.take(grads.at[i], "grads", n, false);
+        const at::Tensor& g = places.take(grads.at[i], "grads", n, Places::kGrad);
         if (!floating(p.scalar_type()) || !floating(g.scalar_type())) throw Refused("params and grads must be fp32 or bf16");
         to = {p.data_ptr(), g.data_ptr(), nullptr, nullptr, nullptr, nullptr, nullptr, n, dtype_of(p.scalar_type()),
               dtype_of(g.scalar_type())};
         PyObject* const states[2] = {m.at[i], v.at[i]};
         const char* const names[2] = {"m", "v"};
-        if (PyTuple_Check(states[0]) != PyTuple_Check(states[1])) throw Refused("m and v of a tensor must be of one kind");
+        const bool eight = !THPVariable_Check(states[0]);
+        if (eight == static_cast<bool>(THPVariable_Check(states[1])))
+            throw Refused("m and v of a tensor must be of one kind");
         for (int k = 0; k < 2; ++k) {
-            void*& values = k == 0 ? to.m : to.v;
-            if (PyTuple_Check(states[k])) {
-                if (PyTuple_GET_SIZE(states[k]) != 4 || integer(PyTuple_GET_ITEM(states[k], 2)) != 1 ||
-                    integer(PyTuple_GET_ITEM(states[k], 3)) != n)
-                    throw Refused(std::string(names[k]) + " must be a Block8 of shape (1, " + std::to_string(n) + ")");
-                values = places.take(PyTuple_GET_ITEM(states[k], 0), names[k], -1, true).data_ptr();
+            if (eight) {
+                const Held values(PyObject_GetAttrString(states[k], "values")),
+                    scales(PyObject_GetAttrString(states[k], "scales"));
+                if (values.o == nullptr || scales.o == nullptr) {
+                    PyErr_Clear();
+                    throw Refused(std::string(names[k]) + " must be tensors or Block8");
+                }
+                check_block(values.o, scales.o, 1, n);
+                (k == 0 ? to.m : to.v) =
+                    places.take(values.o, names[k], -1, k == 0 ? Places::kM : Places::kV).data_ptr();
                 (k == 0 ? to.m_scales : to.v_scales) =
-                    places.take(PyTuple_GET_ITEM(states[k], 1), names[k], -1, true).data_ptr();
+                    places.take(scales.o, names[k], -1, k == 0 ? Places::kScaleM : Places::kScaleV).data_ptr();
             } else {
-                const at::Tensor& s = places.take(states[k], names[k], n, true);
+                const at::Tensor& s = places.take(states[k], names[k], n, k == 0 ? Places::kM : Places::kV);
                 if (s.scalar_type() != at::kFloat) throw Refused(std::string(names[k]) + " must be fp32 or a Block8");
-                values = s.data_ptr();
+                (k == 0 ? to.m : to.v) = s.data_ptr();
             }
         }
         if (some && copies.at[i] != Py_None) {
-            const at::Tensor& c = places.take(copies.at[i], "copies", n, true);
+            const at::Tensor& c = places.take(copies.at[i], "copies", n, Places::kCopy);
             if (c.scalar_type() != at::kBFloat16 || p.scalar_type() != at::kFloat)
                 throw Refused("copies must be bf16, of fp32 params");
             to.copy = c.data_ptr();
@@ -788,7 +818,7 @@ PyObject* bind(Args a) {
 }
 
 #define OP(NAME, N) \
-    { #NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<&NAME, N>)), METH_FASTCALL, nullptr }
+    { #NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&entry<static_cast<PyObject* (*)(Args)>(&NAME), N>)), METH_FASTCALL, nullptr }
 PyMethodDef methods[] = {OP(bind, 2),
                          OP(check_block, 4),
                          OP(pack8, 3),

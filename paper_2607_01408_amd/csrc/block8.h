@@ -151,6 +151,23 @@ __device__ __forceinline__ void store8(uint16_t* p, int n, const float (&v)[8]) 
             if (i < n) p[i] = f32_to_bf16(v[i]);
     }
 }
+// store8 of a matrix that is too large for the caches: past them (`around`), lines that are not to stay.
+__device__ __forceinline__ void pass_store8(float* p, int n, const float (&v)[8], bool around) {
+    if (n >= 8 && around) {
+        __builtin_nontemporal_store(u4f{v[0], v[1], v[2], v[3]}, reinterpret_cast<u4f*>(p));
+        __builtin_nontemporal_store(u4f{v[4], v[5], v[6], v[7]}, reinterpret_cast<u4f*>(p + 4));
+    } else {
+        store8(p, n, v);
+    }
+}
+__device__ __forceinline__ void pass_store8(uint16_t* p, int n, const float (&v)[8], bool around) {
+    if (n >= 8 && around)
+        __builtin_nontemporal_store(
+            u4u{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])},
+            reinterpret_cast<u4u*>(p));
+    else
+        store8(p, n, v);
+}
 // v rounded to the element type
 __device__ __forceinline__ float as_type(float v, const float*) { return v; }
 __device__ __forceinline__ float as_type(float v, const uint16_t*) { return bf16_to_f32(f32_to_bf16(v)); }

@@ -30,7 +30,7 @@ __device__ __forceinline__ int64_t row_of(const void* index, bool wide, int64_t 
 template <int LANES, int ROWS, typename T>
 __global__ __launch_bounds__(256) void embedding_kernel(const T* __restrict__ table, int64_t ldt, const void* index,
                                                         bool wide, float scale, T* __restrict__ out, int64_t ldo, int64_t n,
-                                                        int64_t V, int64_t D) {
+                                                        int64_t V, int64_t D, bool around) {
     constexpr int kGroups = 256 / LANES;
     const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
     const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8;
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(256) void embedding_kernel(const T* __restrict__ ta
         for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[r][i] *= scale;
-            if (first + r * kGroups < n) store8(out + (first + r * kGroups) * ldo + c, have, v[r]);
+            if (first + r * kGroups < n) pass_store8(out + (first + r * kGroups) * ldo + c, have, v[r], around);
         }
     }
 }
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
                                                             const int32_t* __restrict__ rows, float scale,
                                                             TO* __restrict__ out, int64_t ldo, float* __restrict__ partial,
                                                             int64_t n, int64_t V, int64_t D, int64_t chunk, unsigned across,
-                                                            unsigned sum_blocks) {
+                                                            unsigned sum_blocks, bool around) {
     constexpr int kGroups = 256 / LANES;
     if (blockIdx.x >= sum_blocks) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
             }
             if (row >= 0)
                 for (int64_t c = (lane % LANES) * 8; c < D; c += LANES * 8)
-                    store8(out + row * ldo + c, D - c >= 8 ? 8 : static_cast<int>(D - c), zeros);
+                    pass_store8(out + row * ldo + c, D - c >= 8 ? 8 : static_cast<int>(D - c), zeros, around);
         }
         return;
     }
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = sum[i] * scale;
-                store8(out + row * ldo + c, have, v);
+                pass_store8(out + row * ldo + c, have, v, around);
             }
         }
     };
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
 }
 
 constexpr int kJoinThreads = 512;
-constexpr int kShort = 16;  // chunks beyond the first that a group adds up by itself
+constexpr int kShort = 8;  // chunks beyond the first that a group adds up by itself
 
 // A group to a chunk; those in which a row begins that goes on add its parts: chunk after chunk as long as one starts
 // with the row.  A row of more than kShort chunks is added by the whole workgroup, a group every so many chunks,
@@ -245,6 +245,8 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const floa
     }
 }
 
+// matrices of more elements than this leave past the caches
+bool large(int64_t elements) { return elements > int64_t{1} << 22; }
 int lanes_of(int64_t D) { return D > 256 ? 64 : (D > 128 ? 32 : (D > 64 ? 16 : (D > 32 ? 8 : 4))); }
 int64_t across_of(int64_t D, int lanes) { return (D + 8 * lanes - 1) / (8 * lanes); }
 
@@ -271,10 +273,10 @@ hipError_t lookup(const void* table, int64_t ldt, const void* index, bool wide, 
     const T* t = static_cast<const T*>(table);
     if (few)
         hipLaunchKernelGGL((embedding_kernel<LANES, 1, T>), grid, dim3(256), 0, stream, t, ldt, index, wide, scale,
-                           static_cast<T*>(out), ldo, n, V, D);
+                           static_cast<T*>(out), ldo, n, V, D, large(n * D));
     else
         hipLaunchKernelGGL((embedding_kernel<LANES, 4, T>), grid, dim3(256), 0, stream, t, ldt, index, wide, scale,
-                           static_cast<T*>(out), ldo, n, V, D);
+                           static_cast<T*>(out), ldo, n, V, D, large(n * D));
     return hipGetLastError();
 }
 
@@ -285,7 +287,8 @@ hipError_t gradient(const EmbeddingBwdArgs& a, hipStream_t stream) {
     const int64_t empty = (a.V + looked - 1) / looked;
     hipLaunchKernelGGL((embedding_sum_kernel<LANES, TG, TO>), dim3(static_cast<unsigned>(sums + empty)), dim3(256), 0,
                        stream, static_cast<const TG*>(a.grad), a.ldg, a.order, a.rows, a.scale, static_cast<TO*>(a.out),
-                       a.ldo, a.partial, a.n, a.V, a.D, chunk, static_cast<unsigned>(across), static_cast<unsigned>(sums));
+                       a.ldo, a.partial, a.n, a.V, a.D, chunk, static_cast<unsigned>(across), static_cast<unsigned>(sums),
+                       large(a.V * a.D));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks <= 1) return e;
     constexpr int kGroups = kJoinThreads / LANES;

@@ -55,8 +55,8 @@ def embedding_backward(grad, index, V, scale=1.0, dtype=None):
                 None if dtype is None else _choice(_DTYPES, dtype, "dtype"))
 
 
-def _state(t):
-    return (t.values, t.scales, *t.shape) if isinstance(t, Block8) else t
+def _list(x):
+    return x if type(x) is list else list(x)
 
 
 @_on_stream
@@ -70,11 +70,10 @@ def adamw(params, grads, m, v, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_de
     (zeros to begin with: ``adamw_state``).  ``copies``: bf16 tensors (or None) that receive fp32 params rounded, the weights
     that layers read.  ``grad_scale``: a device fp32 tensor of one element, a factor of all gradients.  ``step`` (1 for the
     first) and ``lr`` are numbers or, for captured steps, device tensors of one element, int64 and fp32."""
-    params = list(params)
-    if not params:
-        return
-    _run(_ops.adamw, params[0], params, list(grads), [_state(t) for t in m], [_state(t) for t in v],
-         None if copies is None else list(copies), step, lr, *betas, eps, weight_decay, grad_scale, seed)
+    params = _list(params)
+    if params:
+        _run(_ops.adamw, params[0], params, _list(grads), _list(m), _list(v), None if copies is None else _list(copies), step,
+             lr, *betas, eps, weight_decay, grad_scale, seed)
 
 
 def adamw_state(param, bits=32):

@@ -59,9 +59,9 @@ def test_nothing_to_do(name, good, none):
 def test_workspace_sizes():
     n = ctypes.c_size_t(0)
     sort, gradient = _lib.lib().spingtp_sort_index_workspace_size, _lib.lib().spingtp_embedding_backward_workspace_size
-    assert sort(16_384, 1 << 30, ctypes.byref(n)) == OK and n.value == 0  # one workgroup's LDS
-    assert sort(16_385, 511, ctypes.byref(n)) == OK and n.value == 4 * 512 * 512  # one digit: counts alone
-    assert sort(16_385, 512, ctypes.byref(n)) == OK and n.value == 4 * (512 * 512 + 2 * 16_388)
+    assert sort(8192, 1 << 30, ctypes.byref(n)) == OK and n.value == 0  # one workgroup's LDS
+    assert sort(8193, 511, ctypes.byref(n)) == OK and n.value == 4 * 512 * 512  # one digit: counts alone
+    assert sort(8193, 512, ctypes.byref(n)) == OK and n.value == 4 * (512 * 512 + 2 * 8196)
     assert gradient(0, 8, ctypes.byref(n)) == OK and n.value == 0
     assert gradient(100, 8, ctypes.byref(n)) == OK and n.value > 0
     for bad in ((-1, 4), (BIG, 4), (4, 0), (4, BIG)):
