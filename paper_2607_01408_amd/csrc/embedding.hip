@@ -26,16 +26,59 @@ __device__ __forceinline__ int64_t row_of(const void* index, bool wide, int64_t 
     return k >= 0 && k < V ? k : -1;
 }
 
+// A lane's eight columns of its group's 8 LANES: neighbours (16 bytes in bf16) or, of fp32 rows that leave as fp32, two
+// fours 4 LANES apart, so that a group's loads and stores are lines without gaps.  `c`: the first; `end`: the row's.
+template <int LANES, bool FOURS, typename T>
+__device__ __forceinline__ void load_columns(const T* row, int64_t c, int64_t end, float (&v)[8]) {
+    if constexpr (FOURS) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = c + 4 * LANES * h;
+            if (at + 4 <= end) {
+                const u4f x = *reinterpret_cast<const u4f*>(row + at);
+                v[4 * h] = x.x, v[4 * h + 1] = x.y, v[4 * h + 2] = x.z, v[4 * h + 3] = x.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[4 * h + i] = at + i < end ? row[at + i] : 0.f;
+            }
+        }
+    } else {
+        load8(row + c, end - c >= 8 ? 8 : static_cast<int>(end - c), v);
+    }
+}
+template <int LANES, bool FOURS, typename T>
+__device__ __forceinline__ void store_columns(T* row, int64_t c, int64_t end, const float (&v)[8], bool around) {
+    if constexpr (FOURS) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t at = c + 4 * LANES * h;
+            if (at + 4 <= end) {
+                const u4f x{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+                if (around)
+                    __builtin_nontemporal_store(x, reinterpret_cast<u4f*>(row + at));
+                else
+                    *reinterpret_cast<u4f*>(row + at) = x;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (at + i < end) row[at + i] = v[4 * h + i];
+            }
+        }
+    } else {
+        pass_store8(row + c, end - c >= 8 ? 8 : static_cast<int>(end - c), v, around);
+    }
+}
+
 // LANES lanes of eight columns to a row, ROWS rows to a group.
 template <int LANES, int ROWS, typename T>
 __global__ __launch_bounds__(256) void embedding_kernel(const T* __restrict__ table, int64_t ldt, const void* index,
                                                         bool wide, float scale, T* __restrict__ out, int64_t ldo, int64_t n,
                                                         int64_t V, int64_t D, bool around) {
     constexpr int kGroups = 256 / LANES;
+    constexpr bool kFours = sizeof(T) == 4;
     const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
-    const int64_t c = (static_cast<int64_t>(blockIdx.y) * LANES + l) * 8;
+    const int64_t c = static_cast<int64_t>(blockIdx.y) * LANES * 8 + l * (kFours ? 4 : 8);
     if (c >= D) return;
-    const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kGroups * ROWS + g; first < n;
          first += static_cast<int64_t>(gridDim.x) * kGroups * ROWS) {
         int64_t row[ROWS];
@@ -43,12 +86,19 @@ __global__ __launch_bounds__(256) void embedding_kernel(const T* __restrict__ ta
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) row[r] = first + r * kGroups < n ? row_of(index, wide, first + r * kGroups, V) : -1;
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) load8(table + (row[r] < 0 ? 0 : row[r] * ldt + c), row[r] < 0 ? 0 : have, v[r]);
+        for (int r = 0; r < ROWS; ++r) {
+            if (row[r] >= 0) {
+                load_columns<LANES, kFours>(table + row[r] * ldt, c, D, v[r]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[r][i] = 0.f;
+            }
+        }
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[r][i] *= scale;
-            if (first + r * kGroups < n) pass_store8(out + (first + r * kGroups) * ldo + c, have, v[r], around);
+            for (int i = 0; i < 8; ++i) v[r][i] = row[r] >= 0 ? v[r][i] * scale : 0.f;
+            if (first + r * kGroups < n) store_columns<LANES, kFours>(out + (first + r * kGroups) * ldo, c, D, v[r], around);
         }
     }
 }
@@ -81,6 +131,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
                                                             int64_t n, int64_t V, int64_t D, int64_t chunk, unsigned across,
                                                             unsigned sum_blocks, bool around) {
     constexpr int kGroups = 256 / LANES;
+    constexpr bool kFours = sizeof(TG) == 4 && sizeof(TO) == 4;
     if (blockIdx.x >= sum_blocks) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         const int64_t first = (static_cast<int64_t>(blockIdx.x - sum_blocks) * 4 + wave) * kEmptyRows, mine = first + lane;
@@ -103,17 +154,16 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
                 if (lane / LANES == k) row = first + b;
             }
             if (row >= 0)
-                for (int64_t c = (lane % LANES) * 8; c < D; c += LANES * 8)
-                    pass_store8(out + row * ldo + c, D - c >= 8 ? 8 : static_cast<int>(D - c), zeros, around);
+                for (int64_t c = (lane % LANES) * (kFours ? 4 : 8); c < D; c += LANES * 8)
+                    store_columns<LANES, kFours>(out + row * ldo, c, D, zeros, around);
         }
         return;
     }
     const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
-    const int64_t c = (static_cast<int64_t>(blockIdx.x % across) * LANES + l) * 8;
+    const int64_t c = static_cast<int64_t>(blockIdx.x % across) * LANES * 8 + l * (kFours ? 4 : 8);
     const int64_t k = static_cast<int64_t>(blockIdx.x / across) * kGroups + g, p0 = k * chunk;
     if (c >= D || p0 >= n) return;
     const int64_t p1 = p0 + chunk < n ? p0 + chunk : n;
-    const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
     float sum[8];
     const uint32_t most = static_cast<uint32_t>(n - 1);
     int32_t row = rows[p0];
@@ -124,12 +174,12 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
     const auto leave = [&](bool goes_on) {
         if (static_cast<uint32_t>(row) < V) {
             if (before || goes_on) {
-                store8(partial + (2 * k + (before ? 0 : 1)) * D + c, have, sum);
+                store_columns<LANES, kFours>(partial + (2 * k + (before ? 0 : 1)) * D, c, D, sum, false);
             } else {
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) v[i] = sum[i] * scale;
-                pass_store8(out + row * ldo + c, have, v, around);
+                store_columns<LANES, kFours>(out + row * ldo, c, D, v, around);
             }
         }
     };
@@ -141,7 +191,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
             const int64_t q = p + j < p1 ? p + j : p1 - 1;
             r[j] = rows[q];
             const uint32_t at = static_cast<uint32_t>(order[q]);
-            load8(grad + (at < most ? at : most) * ldg + c, have, v[j]);
+            load_columns<LANES, kFours>(grad + (at < most ? at : most) * ldg, c, D, v[j]);
         }
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {

@@ -44,7 +44,7 @@ struct GemmArgs {
     int64_t lds;        // bytes of a row of scales (both operands: the same K)
     int64_t M, N;
     int steps;          // of 128 bytes
-    int tail;           // bf16: bytes of the last step that exist, a multiple of 16 (128: all)
+    int tail;           // bf16: bytes of the last step that exist, a multiple of 16 (128: all, 0: none)
     int tiles_m, tiles_n;
     // columns along k: rows of w (of each matrix) and x, the step from which on w2 is read, and output rows left
     // out: [gap_at, gap_at + gap), those behind move up
@@ -180,9 +180,10 @@ struct GemmTile {
         return v4i{lo.x, lo.y, hi.x, hi.y};
     }
 
-    __device__ __forceinline__ void run(const GemmArgs& a, int64_t n0, int64_t m0, uint8_t* lds) {
+    // first_wave: of the workgroup's, where several tiles' waves share one (they take as many steps each)
+    __device__ __forceinline__ void run(const GemmArgs& a, int64_t n0, int64_t m0, uint8_t* lds, int first_wave = 0) {
         lane = threadIdx.x & 63;
-        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - first_wave;
         wn = wave % WN;
         wm = wave / WN;
 #pragma unroll
@@ -208,8 +209,10 @@ struct GemmTile {
         const uint8_t* aw = a.w + 2 * n0;
         const uint8_t* ax = a.x + 2 * m0;
         const uint32_t all_w = 64 * ldw - 2 * n0, all_x = 64 * ldx - 2 * m0;
-        const uint32_t last_w = KW ? (a.w_rows - 64 * (a.w_split - 1)) * ldw - 2 * n0 : 0;
-        const uint32_t last_x = KX ? (a.x_rows - 64 * (a.steps - 1)) * ldx - 2 * m0 : 0;
+        // (none of them: a step past the last row)
+        const int64_t end_w = a.w_rows - 64 * (a.w_split - 1), end_x = a.x_rows - 64 * (a.steps - 1);
+        const uint32_t last_w = KW && end_w > 0 ? end_w * ldw - 2 * n0 : 0;
+        const uint32_t last_x = KX && end_x > 0 ? end_x * ldx - 2 * m0 : 0;
         const auto size_w = [&](int k) { return k + 1 == a.w_split || k + 1 == a.steps ? last_w : all_w; };
         const auto size_x = [&](int k) { return k + 1 == a.steps ? last_x : all_x; };
         uint32_t sw = size_w(0), sx = size_x(0);

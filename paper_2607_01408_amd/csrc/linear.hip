@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "activation.h"
 #include "feedforward.h"
@@ -92,20 +93,44 @@ __device__ __forceinline__ void cut_slice(GemmArgs& a, LinearOut& o, int64_t& ro
                   nullptr,   false, nullptr, 0};
 }
 
-template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX>
+// One of PARTS equal parts of the sum, a step more or less: that step is of zeros.
+template <class E, bool KW, bool KX, int PARTS>
+__device__ __forceinline__ void cut_part(GemmArgs& a, int part) {
+    const int first = static_cast<int>(static_cast<int64_t>(a.steps) * part / PARTS);
+    const int count = static_cast<int>(static_cast<int64_t>(a.steps) * (part + 1) / PARTS) - first;
+    const int most = (a.steps + PARTS - 1) / PARTS;
+    a.w += KW ? int64_t{64} * first * a.ldw : int64_t{kStepBytes} * first;
+    a.x += KX ? int64_t{64} * first * a.ldx : int64_t{kStepBytes} * first;
+    if constexpr (E::kScaled) a.ws += first, a.xs += first;
+    const int64_t rows = int64_t{64} * count;
+    a.w_rows -= int64_t{64} * first;
+    a.x_rows -= int64_t{64} * first;
+    if (a.w_rows > rows) a.w_rows = rows;
+    if (a.x_rows > rows) a.x_rows = rows;
+    if (part < PARTS - 1) a.tail = kStepBytes;
+    if (count < most) {
+        // (where the part ends inside a step, its last step is one that exists: only the last part does, and it is whole)
+        a.tail = 0;
+    }
+    a.steps = a.w_split = most;
+}
+
+// PARTS times the waves of a tile share its sum, each tile's worth in LDS of its own.
+template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX, int PARTS>
 struct LinearTile : GemmTile<E, PN, PM, WN, WM, NS, false, KW, KX> {
     using Base = GemmTile<E, PN, PM, WN, WM, NS, false, KW, KX>;
     static constexpr int kPitch = PN + 4;  // floats of a staged row: rows start in different banks
     static constexpr int kStage = Base::kTile * kPitch * 4;
-    static constexpr int kAllLds = Base::kLds > Base::kWaves * kStage ? Base::kLds : Base::kWaves * kStage;
+    static constexpr int kStages = PARTS * Base::kWaves * (PARTS > 1 ? Base::TM : 1) * kStage;
+    static constexpr int kAllLds = PARTS * Base::kLds > kStages ? PARTS * Base::kLds : kStages;
     static_assert(kAllLds <= 160 * 1024, "in LDS");
 };
 
 // ACT: a parameter, for the epilogue's size (with all of them in it the loop over the accumulators is not unrolled,
 // and they lie in memory).
-template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX, int ACT>
-__global__ __launch_bounds__(64 * WN * WM) void linear_kernel(GemmArgs a, LinearOut o) {
-    using Tile = LinearTile<E, PN, PM, WN, WM, NS, KW, KX>;
+template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX, int PARTS, int ACT>
+__global__ __launch_bounds__(64 * WN * WM * PARTS) void linear_kernel(GemmArgs a, LinearOut o) {
+    using Tile = LinearTile<E, PN, PM, WN, WM, NS, KW, KX, PARTS>;
     extern __shared__ __align__(16) uint8_t gemm_lds[];
     int tm, tn;
     if (o.partial == nullptr) {
@@ -121,10 +146,12 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_kernel(GemmArgs a, Linear
         cut_slice<E, KW, KX>(a, o, unused, slice);
     }
     const int64_t n0 = static_cast<int64_t>(tn) * Tile::BN, m0 = static_cast<int64_t>(tm) * Tile::BM;
+    const int part = PARTS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / Tile::kWaves : 0;
+    if constexpr (PARTS > 1) cut_part<E, KW, KX, PARTS>(a, part);
     Tile t;
-    t.run(a, n0, m0, gemm_lds);  // ends with a barrier behind its reads of LDS
+    t.run(a, n0, m0, gemm_lds + part * Tile::kLds, part * Tile::kWaves);  // ends with a barrier behind its reads of LDS
     constexpr int kLanes = PN / 8, kAtOnce = 64 / kLanes, kTimes = Tile::kTile / kAtOnce;  // lanes of a row
-    uint8_t* const mine = gemm_lds + t.wave * Tile::kStage;
+    uint8_t* const mine = gemm_lds + (part * Tile::kWaves + t.wave) * (PARTS > 1 ? Tile::TM : 1) * Tile::kStage;
     const int l = t.lane % kLanes, r0 = t.lane / kLanes, in = t.lane & (Tile::kTile - 1);
     const int64_t n = n0 + t.wn * PN + 8 * l;
     const int left = a.N - n >= 8 ? 8 : (a.N > n ? static_cast<int>(a.N - n) : 0);
@@ -135,9 +162,7 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_kernel(GemmArgs a, Linear
         for (int i = 0; i < 8; ++i) bias[i] = 0.f;
         if (o.bias != nullptr && left > 0) load8(o.bias + n, left, bias);
     }
-#pragma unroll
-    for (int j = 0; j < Tile::TM; ++j) {
-        const int64_t m1 = m0 + t.wm * PM + j * Tile::kTile + r0;
+    const auto residuals = [&](int64_t m1) {
         if constexpr (!KW) {
 #pragma unroll
             for (int q = 0; q < kTimes; ++q) {
@@ -146,20 +171,31 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_kernel(GemmArgs a, Linear
                 if (o.r != nullptr && left > 0 && m1 + q * kAtOnce < a.M) residual8(o, m1 + q * kAtOnce, n, left, r[q]);
             }
         }
+    };
+    const auto stage = [&](int j, uint8_t* to) {
 #pragma unroll
         for (int i = 0; i < Tile::TN; ++i)
 #pragma unroll
             for (int c = 0; c < Tile::kQuads; ++c) {
                 const auto& s = t.acc[i][j];
-                *reinterpret_cast<float4*>(mine + 4 * (in * Tile::kPitch + t.column(i, c) - t.wn * PN)) =
+                *reinterpret_cast<float4*>(to + 4 * (in * Tile::kPitch + t.column(i, c) - t.wn * PN)) =
                     make_float4(s[4 * c], s[4 * c + 1], s[4 * c + 2], s[4 * c + 3]);
             }
-        wave_lds_order();
+    };
+    // rows m1 + q kAtOnce from their sums, `parts` of them kPart bytes apart
+    constexpr int kPart = Tile::kWaves * Tile::TM * Tile::kStage;
+    const auto finish = [&](int64_t m1, const uint8_t* at) {
 #pragma unroll
         for (int q = 0; q < kTimes; ++q) {
-            const float4* from = reinterpret_cast<const float4*>(mine + 4 * ((r0 + q * kAtOnce) * Tile::kPitch + 8 * l));
-            const float4 lo = from[0], hi = from[1];
+            const float4* from = reinterpret_cast<const float4*>(at + 4 * ((r0 + q * kAtOnce) * Tile::kPitch + 8 * l));
+            float4 lo = from[0], hi = from[1];
             float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+            for (int p = 1; p < PARTS; ++p) {
+                lo = from[p * (kPart / 16)], hi = from[p * (kPart / 16) + 1];
+                v[0] += lo.x, v[1] += lo.y, v[2] += lo.z, v[3] += lo.w;
+                v[4] += hi.x, v[5] += hi.y, v[6] += hi.z, v[7] += hi.w;
+            }
             const int64_t m = m1 + q * kAtOnce;
             if (left <= 0 || m >= a.M) continue;
             if constexpr (!KW) {
@@ -170,7 +206,25 @@ __global__ __launch_bounds__(64 * WN * WM) void linear_kernel(GemmArgs a, Linear
                 pass_store8(static_cast<uint16_t*>(o.y) + m * o.ldy + n, left, v, o.around);
             }
         }
-        wave_lds_order();
+    };
+    const int64_t first = m0 + t.wm * PM + r0;
+    if constexpr (PARTS == 1) {
+#pragma unroll
+        for (int j = 0; j < Tile::TM; ++j) {
+            residuals(first + j * Tile::kTile);
+            stage(j, mine);
+            wave_lds_order();
+            finish(first + j * Tile::kTile, mine);
+            wave_lds_order();
+        }
+    } else {
+        residuals(first + part * Tile::kTile);  // of the rows below
+#pragma unroll
+        for (int j = 0; j < Tile::TM; ++j) stage(j, mine + j * Tile::kStage);
+        __syncthreads();
+        static_assert(Tile::TM <= PARTS);
+        if (part < Tile::TM)
+            finish(first + part * Tile::kTile, gemm_lds + (t.wave * Tile::TM + part) * Tile::kStage);
     }
 }
 
@@ -251,18 +305,34 @@ struct RowCopy {
     int64_t ld, R;
     uint16_t* to;
 };
+// Loads and stores of W elements, neighbouring lanes' side by side: rows on 4 bytes go by twos, others one by one.
+template <int W>
 __global__ __launch_bounds__(256) void copy_rows_kernel(RowCopy a, RowCopy b, int64_t K, int64_t pitch, int lanes) {
-    const int64_t c = (static_cast<int64_t>(blockIdx.y) * lanes + (threadIdx.x & (lanes - 1))) * 8, left = K - c;
-    if (c >= pitch) return;
-    const int at_once = 256 / lanes, have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
+    using T = std::conditional_t<W == 2, uint32_t, uint16_t>;
+    constexpr int kTimes = 8 / W;
+    const int64_t c0 = (static_cast<int64_t>(blockIdx.y) * lanes) * 8 + (threadIdx.x & (lanes - 1)) * W;
+    const int at_once = 256 / lanes;
     for (int64_t row = static_cast<int64_t>(blockIdx.x) * at_once + threadIdx.x / lanes; row < a.R + b.R;
          row += static_cast<int64_t>(gridDim.x) * at_once) {
         const bool second = row >= a.R;
         const int64_t r = second ? row - a.R : row;
         const uint16_t* from = second ? b.from + r * b.ld : a.from + r * a.ld;
-        float v[8];
-        load8(from + (have > 0 ? c : 0), have, v);
-        store8((second ? b.to : a.to) + r * pitch + c, 8, v);
+        uint16_t* to = (second ? b.to : a.to) + r * pitch;
+        T v[kTimes];
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const int64_t c = c0 + static_cast<int64_t>(i) * lanes * W;
+            v[i] = 0;
+            if (c + W <= K)
+                v[i] = *reinterpret_cast<const T*>(from + c);
+            else if (c < K)
+                v[i] = from[c];  // the row's last one
+        }
+#pragma unroll
+        for (int i = 0; i < kTimes; ++i) {
+            const int64_t c = c0 + static_cast<int64_t>(i) * lanes * W;
+            if (c < pitch) *reinterpret_cast<T*>(to + c) = v[i];
+        }
     }
 }
 
@@ -284,7 +354,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __re
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
     if (n < (dz != nullptr ? pitch : N)) {
-#pragma unroll 4
+#pragma unroll 2
         for (int64_t m = m1 + g; m < m2; m += kAtOnce) {
             float v[8];
             pass8(dy + m * lddy + (have > 0 ? n : 0), have, v);
@@ -363,9 +433,14 @@ hipError_t copy_rows(const RowCopy& a, const RowCopy& b, int64_t K, hipStream_t 
     while (lanes < 64 && lanes < groups) lanes *= 2;
     const int64_t across = (groups + lanes - 1) / lanes, most = kMostBlocks / across;
     const int64_t down = (rows + 256 / lanes - 1) / (256 / lanes);
-    hipLaunchKernelGGL(copy_rows_kernel,
-                       dim3(static_cast<unsigned>(down < most ? down : most), static_cast<unsigned>(across)), dim3(256), 0,
-                       stream, a, b, K, pitch, lanes);
+    const dim3 grid(static_cast<unsigned>(down < most ? down : most), static_cast<unsigned>(across));
+    const auto twos = [](const RowCopy& c) {
+        return c.R == 0 || ((reinterpret_cast<uintptr_t>(c.from) & 3) == 0 && c.ld % 2 == 0);
+    };
+    if (twos(a) && twos(b))
+        hipLaunchKernelGGL(copy_rows_kernel<2>, grid, dim3(256), 0, stream, a, b, K, pitch, lanes);
+    else
+        hipLaunchKernelGGL(copy_rows_kernel<1>, grid, dim3(256), 0, stream, a, b, K, pitch, lanes);
     return hipGetLastError();
 }
 
@@ -385,34 +460,38 @@ Shape few_shape(int64_t N, int64_t steps, int64_t grain) {
     const int64_t groups = (N + 15) / 16, at_once = 4 * kSkinnyWaves;
     int64_t slices = 256 / groups;
     if (slices > steps / at_once) slices = steps / at_once;
-    if (slices < 2) return Shape{{0, 1, steps}};
+    if (slices < 2) return Shape{{0, 1, 1, steps}};
     const int64_t per = up((steps + slices - 1) / slices, grain);
-    return Shape{{0, (steps + per - 1) / per, per}};
+    return Shape{{0, 1, (steps + per - 1) / per, per}};
 }
 
-template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX, int ACT>
+template <class E, int PN, int PM, int WN, int WM, int NS, bool KW, bool KX, int PARTS, int ACT>
 hipError_t launch_tile(GemmArgs g, const LinearOut& o, int64_t slices, hipStream_t stream) {
-    using Tile = LinearTile<E, PN, PM, WN, WM, NS, KW, KX>;
+    using Tile = LinearTile<E, PN, PM, WN, WM, NS, KW, KX, PARTS>;
     const int64_t tm = (g.M + Tile::BM - 1) / Tile::BM, tn = (g.N + Tile::BN - 1) / Tile::BN;
     if (tm * tn > kMostTiles) return hipErrorInvalidValue;
     g.tiles_m = static_cast<int>(tm);
     g.tiles_n = static_cast<int>(tn);
-    constexpr auto kernel = linear_kernel<E, PN, PM, WN, WM, NS, KW, KX, ACT>;
+    constexpr auto kernel = linear_kernel<E, PN, PM, WN, WM, NS, KW, KX, PARTS, ACT>;
     const hipError_t e = raise_lds_limit<kernel>();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn * slices)), dim3(Tile::kThreads), Tile::kAllLds, stream, g,
-                       o);
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(tm * tn * slices)), dim3(Tile::kThreads * PARTS), Tile::kAllLds,
+                       stream, g, o);
     return hipGetLastError();
 }
 
 template <class E, bool KW, bool KX, int ACT>
-hipError_t launch_tiles(int tile, const GemmArgs& g, const LinearOut& o, int64_t slices, hipStream_t stream) {
+hipError_t launch_tiles(const Shape& s, const GemmArgs& g, const LinearOut& o, hipStream_t stream) {
     // 128: 8 bits in four waves, for registers
     constexpr int PM = E::kScaled ? 64 : 32, WM = E::kScaled ? 2 : 4;
-    switch (tile) {
-        case 256: return launch_tile<E, 128, 64, 2, 4, 2, KW, KX, ACT>(g, o, slices, stream);
-        case 128: return launch_tile<E, 64, PM, 2, WM, 2, KW, KX, ACT>(g, o, slices, stream);
-        default: return launch_tile<E, 32, 32, 2, 2, 4, KW, KX, ACT>(g, o, slices, stream);
+    switch (s.tile) {
+        case 256: return launch_tile<E, 128, 64, 2, 4, 2, KW, KX, 1, ACT>(g, o, s.slices, stream);
+        case 128:
+            if (s.parts == 2) return launch_tile<E, 64, PM, 2, WM, 2, KW, KX, 2, ACT>(g, o, s.slices, stream);
+            return launch_tile<E, 64, PM, 2, WM, 2, KW, KX, 1, ACT>(g, o, s.slices, stream);
+        default:
+            if (s.parts == 2) return launch_tile<E, 32, 32, 2, 2, 4, KW, KX, 2, ACT>(g, o, s.slices, stream);
+            return launch_tile<E, 32, 32, 2, 2, 4, KW, KX, 1, ACT>(g, o, s.slices, stream);
     }
 }
 
@@ -435,10 +514,10 @@ hipError_t product(const Shape& s, GemmArgs g, int64_t row_bytes, LinearOut o, f
         // slices leave as sums
         const int act = KW || s.slices > 1 ? static_cast<int>(kIdentity) : o.act;
         if constexpr (!KW) {
-            if (act == kSilu) return launch_tiles<E, KW, KX, kSilu>(s.tile, g, o, 1, stream);
-            if (act == kGelu) return launch_tiles<E, KW, KX, kGelu>(s.tile, g, o, 1, stream);
+            if (act == kSilu) return launch_tiles<E, KW, KX, kSilu>(s, g, o, stream);
+            if (act == kGelu) return launch_tiles<E, KW, KX, kGelu>(s, g, o, stream);
         }
-        e = launch_tiles<E, KW, KX, kIdentity>(s.tile, g, o, s.slices, stream);
+        e = launch_tiles<E, KW, KX, kIdentity>(s, g, o, stream);
     } else {
         if constexpr (KW)
             e = hipErrorInvalidValue;
@@ -491,7 +570,7 @@ int dz_lanes(int64_t N) { return N > 256 ? 64 : (N > 64 ? 32 : 8); }
 int64_t dz_rows(int64_t M, int64_t N) {
     const int lanes = dz_lanes(N), at_once = 256 / lanes;
     const int64_t across = (up(N, 64) / 8 + lanes - 1) / lanes;
-    int64_t blocks = 1024 / across;
+    int64_t blocks = 2048 / across;
     if (blocks < 1) blocks = 1;
     const int64_t rows = up((M + blocks - 1) / blocks, 4 * at_once);
     return rows < int64_t{1} << 31 ? rows : int64_t{1} << 31;

@@ -49,51 +49,64 @@ inline int product_tile(const TileCosts& c, int64_t M, int64_t N) {
 inline int gated_tile(int64_t M, int64_t F) {
     return pick_tile(kGated, tiles_of(M, F, 64, 128), tiles_of(M, F, 128, 128), tiles_of(M, F, 256, 128));
 }
-// The linear layer's products have sums of any length, which may be cut into slices, a workgroup to each.  A tile takes
-// `fixed` for its start and end, and each step of its sum (128 bytes a row) `step`, up to `more` longer with the part of
-// the CUs that is busy; slices are written in fp32 and joined by a second launch.  us, fitted to (64 / 128 / 256):
-//   bf16 (rows x columns of w x sum), 8,192 x 2,048 x 8,192 409 / 240 / 211, 8,192 x 8,192 x 2,048 412 / 255 / 250,
-//     100,000 x 512 x 128 60 / 33 / 63, 5,001 x 4,096 x 1,024 76 / 49 / 70, 3,000^3 114 / 97 / 80, 2,048^3 29 / 24 / 51,
-//     999 x 1,000 x 2,736 14 / 35 / 69, and in 8 slices 30 / 25 / 29; 300 x 300 x 8,192 30 / 75 / 155, in 8 13 / 18 / 40;
-//   8 bits, 64 x 2,048 x 8,192 30 / 58 / -, in 8 slices 12 / 18 / -.
+// The linear layer's products have sums of any length.  A sum may be cut into slices, a workgroup to each, or a tile's
+// workgroup may have twice the waves, each half of them half of the sum (64 and 128 alone: two tiles' worth of LDS).  A tile
+// takes `fixed` for its start and end, and each step of its sum (128 bytes a row; two of them where two halves go) `step`, up
+// to `more` longer with the part of the CUs that is busy; slices are written in fp32 and joined by a second launch.
+// us, fitted to (64 / 64 by halves / 128 / 128 by halves / 256):
+//   bf16 (rows x columns of w x sum), 8,192 x 2,048 x 8,192 409 / - / 240 / - / 211, 8,192 x 8,192 x 2,048 412 / - / 255 / - /
+//     250, 100,000 x 512 x 128 60 / - / 33 / - / 63, 5,001 x 4,096 x 1,024 76 / - / 49 / - / 70, 3,000^3 114 / - / 97 / - / 80,
+//     2,048^3 29 / 33 / 24 / 22 / 43, 3,000 x 1,500 x 1,024 21 / 26 / 16 / 22 / 30, 999 x 1,000 x 2,736 14 / 15 / 35 / 33 / 63,
+//     700 x 700 x 2,048 11 / 8 / 16 / 14 / 45, 24 x 8,192 x 4,096 16 / 13 / 39 / 30 / 73; 300 x 300 x 8,192 30 / 22 / 74 / 59 /
+//     144, in 8 slices 12 / 11 / 15 / 15 / 31;
+//   8 bits, 24 x 2,048 x 8,192 29 / 20 / 57 / 44 / 141, in 8 slices 10 / 10 / 15 / 14 / 27, 2,048^3 26 / 32 / 21 / 18 / 44.
 struct SliceCost {
-    int at_once;
+    int tile, parts, at_once;
     double fixed, step, more;
 };
 struct SliceCosts {
-    SliceCost of64, of128, of256;
+    SliceCost of[5];
 };
-constexpr SliceCosts kSlices16 = {{512, 1.7, 0.22, 0.17}, {512, 3.6, 0.57, 0.35}, {256, 12, 1.19, 0.42}};
-constexpr SliceCosts kSlices8 = {{512, 1.7, 0.43, 0.34}, {512, 3.6, 0.87, 0.85}, {256, 12, 2.0, 1.2}};
+constexpr SliceCosts kSlices16 = {{{64, 1, 512, 1.7, 0.22, 0.17},
+                                   {64, 2, 256, 1.8, 0.25, 0.27},
+                                   {128, 1, 512, 3.6, 0.57, 0.35},
+                                   {128, 2, 256, 3.6, 0.82, 0.18},
+                                   {256, 1, 256, 12, 1.19, 0.42}}};
+constexpr SliceCosts kSlices8 = {{{64, 1, 512, 1.7, 0.42, 0.34},
+                                  {64, 2, 256, 1.8, 0.5, 0.15},
+                                  {128, 1, 512, 3.6, 0.83, 0.85},
+                                  {128, 2, 256, 3.6, 1.25, 0.35},
+                                  {256, 1, 256, 12, 2.0, 1.2}}};
 inline double slice_time(const SliceCost& c, int64_t workgroups, int64_t steps) {
     const int64_t full = workgroups / c.at_once, rest = workgroups - full * c.at_once;
-    const double n = static_cast<double>(steps);
+    const double n = static_cast<double>((steps + c.parts - 1) / c.parts);
     double t = static_cast<double>(full) * (c.fixed + n * (c.step + c.more));
     if (rest > 0) t += c.fixed + n * (c.step + c.more * static_cast<double>(rest) / c.at_once);
     return t;
 }
-// The tile of a product of [M][N] outputs, and how many steps of `steps` a slice of its sum takes (all: one slice; a
-// multiple of `grain`, and 4 or more).
+// The tile of a product of [M][N] outputs, the parts that its waves go by, and how many steps of `steps` a slice of its sum
+// takes (all: one slice; 4 or more).  Slices and halves start at multiples of `grain` steps.
 struct SumShape {
-    int tile;
+    int tile, parts;
     int64_t slices, per;
 };
-inline SumShape sum_shape(const SliceCosts& c, int64_t M, int64_t N, int64_t steps, int64_t grain) {
-    SumShape best{256, 1, steps};
+inline SumShape sum_shape(const SliceCosts& costs, int64_t M, int64_t N, int64_t steps, int64_t grain) {
+    SumShape best{256, 1, 1, steps};
     double least = 1e300;
-    for (int tile = 64; tile <= 256; tile *= 2) {
-        const int64_t tiles = ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
+    for (const SliceCost& c : costs.of) {
+        const int64_t tiles = ((M + c.tile - 1) / c.tile) * ((N + c.tile - 1) / c.tile);
         if (tiles > kMostTiles) continue;
-        const SliceCost& cost = tile == 64 ? c.of64 : (tile == 128 ? c.of128 : c.of256);
+        if (c.parts > 1 && (steps < 8 || (grain > 1 && steps % (c.parts * grain) != 0))) continue;
+        const int64_t g = grain > 1 ? c.parts * grain : 1;
         for (int64_t want = 1; want <= 256; want = want < 4 ? want + 1 : want + want / 2) {
-            if (want > 1 && (steps < 4 * want || tiles * want > 1024)) break;
-            const int64_t per = ((steps + want - 1) / want + grain - 1) / grain * grain, slices = (steps + per - 1) / per;
-            double t = slice_time(cost, tiles * slices, want > 1 ? per : steps);
+            if (want > 1 && (steps < 4 * c.parts * want || tiles * want > 1024)) break;
+            const int64_t per = ((steps + want - 1) / want + g - 1) / g * g, slices = (steps + per - 1) / per;
+            double t = slice_time(c, tiles * slices, slices > 1 ? per : steps);
             if (slices > 1)  // both ways through memory, and a launch
                 t += 4.5 + 8.0 * static_cast<double>(slices) * static_cast<double>(M) * static_cast<double>(N) / 3.8e6;
             if (t < least) {
                 least = t;
-                best = SumShape{tile, slices, slices > 1 ? per : steps};
+                best = SumShape{c.tile, c.parts, slices, slices > 1 ? per : steps};
             }
         }
     }
