@@ -299,40 +299,42 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearOut o, int slice
 }
 
 // Rows of K bf16 elements to rows of a multiple of 64, zeros behind: what the products read where the caller's rows do
-// not start and end on 16 bytes.  x and w in one launch, eight elements a thread, `lanes` (a power of two) threads to a row.
+// not start and end on 16 bytes.  x and w in one launch, eight elements a thread (at any address), `lanes` (a power of two)
+// threads to a row, four rows in flight.
 struct RowCopy {
     const uint16_t* from;
     int64_t ld, R;
     uint16_t* to;
 };
-// Loads and stores of W elements, neighbouring lanes' side by side: rows on 4 bytes go by twos, others one by one.
-template <int W>
 __global__ __launch_bounds__(256) void copy_rows_kernel(RowCopy a, RowCopy b, int64_t K, int64_t pitch, int lanes) {
-    using T = std::conditional_t<W == 2, uint32_t, uint16_t>;
-    constexpr int kTimes = 8 / W;
-    const int64_t c0 = (static_cast<int64_t>(blockIdx.y) * lanes) * 8 + (threadIdx.x & (lanes - 1)) * W;
+    constexpr int kRows = 4;
+    const int64_t c = (static_cast<int64_t>(blockIdx.y) * lanes + (threadIdx.x & (lanes - 1))) * 8, left = K - c;
+    if (c >= pitch) return;
     const int at_once = 256 / lanes;
-    for (int64_t row = static_cast<int64_t>(blockIdx.x) * at_once + threadIdx.x / lanes; row < a.R + b.R;
-         row += static_cast<int64_t>(gridDim.x) * at_once) {
-        const bool second = row >= a.R;
-        const int64_t r = second ? row - a.R : row;
-        const uint16_t* from = second ? b.from + r * b.ld : a.from + r * a.ld;
-        uint16_t* to = (second ? b.to : a.to) + r * pitch;
-        T v[kTimes];
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * at_once * kRows + threadIdx.x / lanes; first < a.R + b.R;
+         first += static_cast<int64_t>(gridDim.x) * at_once * kRows) {
+        u4u v[kRows];
+        uint16_t* to[kRows];
 #pragma unroll
-        for (int i = 0; i < kTimes; ++i) {
-            const int64_t c = c0 + static_cast<int64_t>(i) * lanes * W;
-            v[i] = 0;
-            if (c + W <= K)
-                v[i] = *reinterpret_cast<const T*>(from + c);
-            else if (c < K)
-                v[i] = from[c];  // the row's last one
+        for (int i = 0; i < kRows; ++i) {
+            const int64_t row = first + i * at_once, r = row < a.R ? row : row - a.R;
+            const uint16_t* from = (row < a.R ? a.from + r * a.ld : b.from + r * b.ld) + c;
+            to[i] = (row < a.R ? a.to : b.to) + r * pitch + c;
+            v[i] = u4u{0, 0, 0, 0};
+            if (row >= a.R + b.R) continue;
+            if (left >= 8) {
+                v[i] = *reinterpret_cast<const u4u*>(from);
+            } else {
+                uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 7; ++j)
+                    if (j < left) w[j / 2] |= static_cast<uint32_t>(from[j]) << (16 * (j & 1));
+                v[i] = u4u{w[0], w[1], w[2], w[3]};
+            }
         }
 #pragma unroll
-        for (int i = 0; i < kTimes; ++i) {
-            const int64_t c = c0 + static_cast<int64_t>(i) * lanes * W;
-            if (c < pitch) *reinterpret_cast<T*>(to + c) = v[i];
-        }
+        for (int i = 0; i < kRows; ++i)
+            if (first + i * at_once < a.R + b.R) *reinterpret_cast<u4u*>(to[i]) = v[i];
     }
 }
 
@@ -432,15 +434,10 @@ hipError_t copy_rows(const RowCopy& a, const RowCopy& b, int64_t K, hipStream_t 
     int lanes = 8;
     while (lanes < 64 && lanes < groups) lanes *= 2;
     const int64_t across = (groups + lanes - 1) / lanes, most = kMostBlocks / across;
-    const int64_t down = (rows + 256 / lanes - 1) / (256 / lanes);
-    const dim3 grid(static_cast<unsigned>(down < most ? down : most), static_cast<unsigned>(across));
-    const auto twos = [](const RowCopy& c) {
-        return c.R == 0 || ((reinterpret_cast<uintptr_t>(c.from) & 3) == 0 && c.ld % 2 == 0);
-    };
-    if (twos(a) && twos(b))
-        hipLaunchKernelGGL(copy_rows_kernel<2>, grid, dim3(256), 0, stream, a, b, K, pitch, lanes);
-    else
-        hipLaunchKernelGGL(copy_rows_kernel<1>, grid, dim3(256), 0, stream, a, b, K, pitch, lanes);
+    const int64_t at_once = 4 * (256 / lanes), down = (rows + at_once - 1) / at_once;
+    hipLaunchKernelGGL(copy_rows_kernel,
+                       dim3(static_cast<unsigned>(down < most ? down : most), static_cast<unsigned>(across)), dim3(256), 0,
+                       stream, a, b, K, pitch, lanes);
     return hipGetLastError();
 }
 
@@ -672,18 +669,18 @@ hipError_t launch_linear8(const LinearArgs& a, hipStream_t stream) {
                                       stream);
 }
 
-// dz, then the sums of its columns, then what a product needs: the slices' sums and a copy of w or x
+// dz, the sums of its columns, copies of w and x, and the slices' sums of a product
+bool makes_dz(const LinearBwdArgs& a) { return (a.dx != nullptr || a.dw != nullptr) && !own_dz(a); }
+bool copies_w(const LinearBwdArgs& a) { return a.dx != nullptr && !rows_fit(a.w, a.K, a.ldw); }
+bool copies_x(const LinearBwdArgs& a) { return a.dw != nullptr && !rows_fit(a.x, a.K, a.ldx); }
 size_t linear_backward_workspace(const LinearBwdArgs& a) {
     const size_t row = static_cast<size_t>(up(a.K, 64)) * 2;
-    const size_t dx = a.dx == nullptr ? 0
-                                      : up16(dx_shape(a.M, a.K, a.N).bytes(a.M, a.K)) +
-                                            (rows_fit(a.w, a.K, a.ldw) ? 0 : static_cast<size_t>(a.N) * row);
-    const size_t dw = a.dw == nullptr ? 0
-                                      : up16(dw_shape(a.M, a.K, a.N).bytes(a.N, a.K)) +
-                                            (rows_fit(a.x, a.K, a.ldx) ? 0 : static_cast<size_t>(a.M) * row);
-    const size_t dz = own_dz(a) ? 0 : static_cast<size_t>(a.M * up(a.N, 64)) * 2;
+    const size_t dx = a.dx == nullptr ? 0 : dx_shape(a.M, a.K, a.N).bytes(a.M, a.K);
+    const size_t dw = a.dw == nullptr ? 0 : dw_shape(a.M, a.K, a.N).bytes(a.N, a.K);
+    const size_t copies = ((copies_w(a) ? a.N : 0) + (copies_x(a) ? a.M : 0)) * row;
+    const size_t dz = makes_dz(a) ? static_cast<size_t>(a.M * up(a.N, 64)) * 2 : 0;
     const size_t sums = a.db == nullptr ? 0 : static_cast<size_t>(dz_blocks(a.M, a.N) * a.N) * sizeof(float);
-    return dz + up16(sums) + larger(dx, dw);
+    return dz + up16(sums) + copies + larger(dx, dw);
 }
 
 hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
@@ -697,18 +694,30 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
     const int64_t np = up(a.N, 64), kp = up(a.K, 64);
     const bool own = own_dz(a);
     uint8_t* at = static_cast<uint8_t*>(a.workspace);
-    uint16_t* dz = own ? nullptr : reinterpret_cast<uint16_t*>(at);
-    if (!own) at += 2 * a.M * np;
+    uint16_t* dz = makes_dz(a) ? reinterpret_cast<uint16_t*>(at) : nullptr;
+    if (dz != nullptr) at += 2 * a.M * np;
     float* sums = a.db != nullptr ? reinterpret_cast<float*>(at) : nullptr;
     if (a.db != nullptr) at += up16(static_cast<size_t>(dz_blocks(a.M, a.N) * a.N) * sizeof(float));
     hipError_t e = hipSuccess;
-    if (!own || sums != nullptr)
+    if (dz != nullptr || sums != nullptr)
         e = a.dtype == SPINGTP_FP32 ? make_dz<float>(a, dz, sums, stream) : make_dz<uint16_t>(a, dz, sums, stream);
     if (e == hipSuccess && sums != nullptr) {
         hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>((a.N + 15) / 16)), dim3(1024), 0, stream, sums,
                            dz_blocks(a.M, a.N), a.N, a.db);
         e = hipGetLastError();
     }
+    RowCopy w{static_cast<const uint16_t*>(a.w), a.ldw, 0, nullptr}, x{static_cast<const uint16_t*>(a.x), a.ldx, 0, nullptr};
+    if (copies_w(a)) {
+        w.R = a.N;
+        w.to = reinterpret_cast<uint16_t*>(at);
+        at += 2 * a.N * kp;
+    }
+    if (copies_x(a)) {
+        x.R = a.M;
+        x.to = reinterpret_cast<uint16_t*>(at);
+        at += 2 * a.M * kp;
+    }
+    if (e == hipSuccess && w.R + x.R > 0) e = copy_rows(w, x, a.K, stream);
     const uint8_t* from = own ? static_cast<const uint8_t*>(a.dy) : reinterpret_cast<const uint8_t*>(dz);
     const int64_t ldz = 2 * (own ? a.lddy : np);
     if (e == hipSuccess && a.dx != nullptr) {
@@ -716,14 +725,8 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
         GemmArgs g{};
         g.x = from;
         g.ldx = ldz;
-        g.w = static_cast<const uint8_t*>(a.w);
-        g.ldw = 2 * a.ldw;
-        if (!rows_fit(a.w, a.K, a.ldw)) {
-            uint16_t* copy = reinterpret_cast<uint16_t*>(at + up16(s.bytes(a.M, a.K)));
-            e = copy_rows(RowCopy{static_cast<const uint16_t*>(a.w), a.ldw, a.N, copy}, RowCopy{}, a.K, stream);
-            g.w = reinterpret_cast<const uint8_t*>(copy);
-            g.ldw = 2 * kp;
-        }
+        g.w = w.R > 0 ? reinterpret_cast<const uint8_t*>(w.to) : static_cast<const uint8_t*>(a.w);
+        g.ldw = 2 * (w.R > 0 ? kp : a.ldw);
         g.w2 = g.w;
         g.M = a.M;
         g.N = a.K;
@@ -737,14 +740,8 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
     if (e == hipSuccess && a.dw != nullptr) {
         const Shape s = dw_shape(a.M, a.K, a.N);
         GemmArgs g{};
-        g.w = static_cast<const uint8_t*>(a.x);
-        g.ldw = 2 * a.ldx;
-        if (!rows_fit(a.x, a.K, a.ldx)) {
-            uint16_t* copy = reinterpret_cast<uint16_t*>(at + up16(s.bytes(a.N, a.K)));
-            e = copy_rows(RowCopy{static_cast<const uint16_t*>(a.x), a.ldx, a.M, copy}, RowCopy{}, a.K, stream);
-            g.w = reinterpret_cast<const uint8_t*>(copy);
-            g.ldw = 2 * kp;
-        }
+        g.w = x.R > 0 ? reinterpret_cast<const uint8_t*>(x.to) : static_cast<const uint8_t*>(a.x);
+        g.ldw = 2 * (x.R > 0 ? kp : a.ldx);
         g.w2 = g.w;
         g.x = from;
         g.ldx = ldz;

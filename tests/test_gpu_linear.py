@@ -18,6 +18,7 @@ pytestmark = pytest.mark.gpu
 if not torch.cuda.is_available():
     pytest.skip("no GPU visible", allow_module_level=True)
 
+from tests import linear_shapes as shapes  # noqa: E402
 import paper_2607_01408_amd as sg  # noqa: E402
 
 F32, BF16 = torch.float32, torch.bfloat16
@@ -110,6 +111,18 @@ def test_forward_from_8_bits(M, K, N, act):
         within(got, y, ey)
 
 
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("M,K,N", list(shapes.FORWARD16))
+def test_forward_in_every_tile(M, K, N, act):
+    test_forward(M, K, N, act)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("M,K,N", list(shapes.FORWARD8))
+def test_forward_from_8_bits_in_every_tile(M, K, N, act):
+    test_forward_from_8_bits(M, K, N, act)
+
+
 def backward64(dy, z, act, x, w):
     """((grad_x, bound), (grad_w, bound before its rounding), (grad_bias, bound)); dz is rounded to bf16."""
     (M, K), N = x.shape, w.shape[0]
@@ -144,6 +157,12 @@ def test_backward(M, K, N, act):
                 assert torch.equal(a, b) if need >> i & 1 else a is None
 
 
+@pytest.mark.parametrize("act", [None, "gelu"])
+@pytest.mark.parametrize("M,K,N", list(shapes.BACKWARD))
+def test_backward_in_every_tile(M, K, N, act):
+    test_backward(M, K, N, act)
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_backward_against_differences(act):
     M, K, N = 70, 96, 130
@@ -173,7 +192,7 @@ def amid(t, fill=NAN, shift=0):
 
 @pytest.mark.parametrize("shift", [0, 1])
 @pytest.mark.parametrize("M,K,N", [(1, 8, 1), (40, 72, 99), (70, 72, 104), (70, 2056, 100), (65, 24, 65), (257, 264, 200),
-                                   (129, 65, 64), (9, 130, 2056)])
+                                   (129, 65, 64), (9, 130, 2056), (300, 1100, 300), (999, 1096, 2730), (1300, 1001, 1500)])
 def test_nothing_beside_the_rows_is_read_or_written(M, K, N, shift):
     x, w, bias = rand((M, K), BF16, 1), rand((N, K), BF16, 2, K**-0.5), rand((N,), F32, 3)
     r, z, dy = rand((M, N), BF16, 4), rand((M, N), BF16, 5), rand((M, N), BF16, 6)

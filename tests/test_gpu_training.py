@@ -614,3 +614,23 @@ def test_refusals():
         sg.adamw([p], [g], [m], [v], step=1, lr=INF)
     sg.adamw([], [], [], [], step=1, lr=1e-3)
     assert all(torch.equal(a, b) for a, b in zip((p, m, v), keep))
+
+
+def test_the_example_updates_its_weights():
+    import importlib.util
+    import os
+
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    spec = importlib.util.spec_from_file_location("interaction_layer", os.path.join(root, "examples", "interaction_layer.py"))
+    layer = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(layer)
+    w = layer.weights(24, 130)
+    old = {k: v.clone() for k, v in w.items()}
+    update = layer.Update(w)
+    grads = {k: rand(v.shape, BF16 if v.dim() == 2 else F32, 3) for k, v in w.items()}
+    update.step(grads, lr=1e-2)
+    for k, v in w.items():
+        zero = torch.zeros(v.shape, dtype=torch.float64, device="cuda")
+        want, bound, *_ = step64(old[k].double(), grads[k].double(), zero, zero, 1, 1e-2, (0.9, 0.999), 1e-8, 0.01)
+        within(update.master[k], want, bound)
+        assert torch.equal(v, update.master[k].to(v.dtype))
