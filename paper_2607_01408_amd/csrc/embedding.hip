@@ -210,14 +210,44 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
     leave(after);
 }
 
+constexpr int kWindow = 32;  // chunks
+
+// Sums of the parts of kWindow chunks (sums [windows][D]) that all start with one row from an earlier chunk: of a row with
+// thousands of chunks a single workgroup would add the parts at the rate of its CU (187,008 entries over 9 rows, the
+// largest with 60 % of them: 53 us).
+template <int LANES>
+__global__ __launch_bounds__(256) void embedding_window_kernel(const float* __restrict__ partial,
+                                                               const int32_t* __restrict__ rows, float* __restrict__ sums,
+                                                               int64_t D, int64_t chunk, int64_t windows, unsigned across) {
+    constexpr int kGroups = 256 / LANES;
+    const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x % across) * LANES + l) * 8;
+    const int64_t w = static_cast<int64_t>(blockIdx.x / across) * kGroups + g, first = w * kWindow;
+    if (c >= D || w >= windows || first == 0) return;
+    if (rows[first * chunk - 1] != rows[(first + kWindow - 1) * chunk]) return;
+    const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+#pragma unroll 8
+    for (int j = 0; j < kWindow; ++j) {
+        float v[8];
+        load8(partial + 2 * (first + j) * D + c, have, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];
+    }
+    store8(sums + w * D + c, have, sum);
+}
+
 constexpr int kJoinThreads = 512;
 constexpr int kShort = 8;  // chunks beyond the first that a group adds up by itself
 
 // A group to a chunk; those in which a row begins that goes on add its parts: chunk after chunk as long as one starts
-// with the row.  A row of more than kShort chunks is added by the whole workgroup, a group every so many chunks,
-// and the groups' sums in order.
+// with the row.  A row of more than kShort chunks is added by the whole workgroup, a group every so many chunks (or
+// windows of them: `sums`, may be null), and the groups' sums in order.
 template <int LANES, typename TO>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const float* __restrict__ partial,
+                                                                      const float* __restrict__ sums,
                                                                       const int32_t* __restrict__ rows, float scale,
                                                                       TO* __restrict__ out, int64_t ldo, int64_t n,
                                                                       int64_t V, int64_t D, int64_t chunk, int64_t chunks,
@@ -225,23 +255,25 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const floa
     constexpr int kGroups = kJoinThreads / LANES;
     __shared__ float part[kGroups][LANES * 8 + 4];
     __shared__ int32_t long_row[kGroups];  // -1: none begins in the group's chunk
+    __shared__ int first_open;             // the first window that the row does not fill
     const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
     const int64_t c = (static_cast<int64_t>(blockIdx.x % across) * LANES + l) * 8, left = D - c;
     const int have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
     const int64_t first = static_cast<int64_t>(blockIdx.x / across) * kGroups;
     // adds the parts of `row` in chunks j, j + step, ... below `end`; whether all of them were its
     const auto add = [&](float (&sum)[8], int32_t row, int64_t j, int64_t step, int64_t end) {
-        for (; j < end; j += kAhead * step) {
-            int32_t r[kAhead];
-            float v[kAhead][8];
+        constexpr int kAtOnce = 4;
+        for (; j < end; j += kAtOnce * step) {
+            int32_t r[kAtOnce];
+            float v[kAtOnce][8];
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
+            for (int q = 0; q < kAtOnce; ++q) {
                 const int64_t at = j + q * step < end ? j + q * step : j;
                 r[q] = rows[at * chunk];
                 load8(partial + 2 * at * D + (have > 0 ? c : 0), have, v[q]);
             }
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
+            for (int q = 0; q < kAtOnce; ++q) {
                 if (j + q * step >= end) return true;
                 if (r[q] != row) return false;
 #pragma unroll
@@ -280,7 +312,26 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const floa
         float mine[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) mine[i] = 0.f;
-        add(mine, which, first + at + 1 + g, kGroups, chunks);
+        const int64_t after = first + at + 1;
+        if (sums == nullptr) {
+            add(mine, which, after + g, kGroups, chunks);
+        } else {
+            const int64_t from = (after + kWindow - 1) / kWindow;
+            if (threadIdx.x == 0) first_open = 0x7fffffff;
+            __syncthreads();
+            add(mine, which, after + g, kGroups, from * kWindow < chunks ? from * kWindow : chunks);
+            int64_t w = from + g;
+#pragma unroll 4
+            for (; w < chunks / kWindow && rows[(w * kWindow + kWindow - 1) * chunk] == which; w += kGroups) {
+                float v[8];
+                load8(sums + w * D + (have > 0 ? c : 0), have, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) mine[i] += v[i];
+            }
+            if (l == 0) atomicMin(&first_open, static_cast<int>(w));
+            __syncthreads();
+            add(mine, which, static_cast<int64_t>(first_open) * kWindow + g, kGroups, chunks);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) part[g][8 * l + i] = mine[i];
         __syncthreads();
@@ -309,6 +360,11 @@ int64_t chunk_of(int64_t n, int64_t D) {
     return c < 16 ? 16 : c;
 }
 int64_t chunks_of(int64_t n, int64_t D) { return (n + chunk_of(n, D) - 1) / chunk_of(n, D); }
+// Windows where a row may well have many of them: 1,000 chunks or more, eight to a row in the mean.
+int64_t windows_of(int64_t n, int64_t V, int64_t D) {
+    const int64_t chunks = chunks_of(n, D);
+    return chunks >= 1000 && V <= chunks / 8 ? chunks / kWindow : 0;
+}
 
 template <int LANES, typename T>
 hipError_t lookup(const void* table, int64_t ldt, const void* index, bool wide, float scale, void* out, int64_t ldo,
@@ -341,9 +397,19 @@ hipError_t gradient(const EmbeddingBwdArgs& a, hipStream_t stream) {
                        large(a.V * a.D));
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks <= 1) return e;
+    const int64_t windows = windows_of(a.n, a.V, a.D);
+    float* const window_sums = windows > 0 ? a.partial + 2 * chunks * a.D : nullptr;
+    if (windows > 0) {
+        constexpr int kAtOnce = 256 / LANES;
+        hipLaunchKernelGGL((embedding_window_kernel<LANES>),
+                           dim3(static_cast<unsigned>((windows + kAtOnce - 1) / kAtOnce * across)), dim3(256), 0, stream,
+                           a.partial, a.rows, window_sums, a.D, chunk, windows, static_cast<unsigned>(across));
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     constexpr int kGroups = kJoinThreads / LANES;
     hipLaunchKernelGGL((embedding_join_kernel<LANES, TO>), dim3(static_cast<unsigned>((chunks + kGroups - 1) / kGroups * across)),
-                       dim3(kJoinThreads), 0, stream, a.partial, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo, a.n, a.V,
+                       dim3(kJoinThreads), 0, stream, a.partial, window_sums, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo, a.n, a.V,
                        a.D, chunk, chunks, static_cast<unsigned>(across));
     return hipGetLastError();
 }
@@ -378,7 +444,8 @@ hipError_t launch_embedding(int dtype, const void* table, int64_t ldt, const voi
 }
 
 size_t embedding_backward_workspace(int64_t n, int64_t D) {
-    return static_cast<size_t>(2 * chunks_of(n, D) * D) * sizeof(float);
+    const int64_t chunks = chunks_of(n, D);
+    return static_cast<size_t>((2 * chunks + chunks / kWindow) * D) * sizeof(float);
 }
 
 hipError_t launch_embedding_backward(const EmbeddingBwdArgs& a, hipStream_t stream) {

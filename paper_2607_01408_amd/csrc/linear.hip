@@ -343,7 +343,7 @@ __global__ __launch_bounds__(256) void copy_rows_kernel(RowCopy a, RowCopy b, in
 // columns to a row; a lane keeps its columns.
 template <int LANES, typename TD>
 __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __restrict__ dy, int64_t lddy,
-                                                        const uint16_t* __restrict__ z, uint16_t* __restrict__ dz,
+                                                        const uint16_t* __restrict__ z, uint16_t* __restrict__ dz, bool past,
                                                         int64_t pitch, float* __restrict__ sums, int64_t M, int64_t N,
                                                         int64_t rows) {
     constexpr int kAtOnce = 256 / LANES;
@@ -359,10 +359,16 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __re
 #pragma unroll 2
         for (int64_t m = m1 + g; m < m2; m += kAtOnce) {
             float v[8];
-            pass8(dy + m * lddy + (have > 0 ? n : 0), have, v);
+            if (past)  // large, and lines that no two rows share
+                pass8(dy + m * lddy + (have > 0 ? n : 0), have, v);
+            else
+                load8(dy + m * lddy + (have > 0 ? n : 0), have, v);
             if (kind != kIdentity) {
                 float p[8];
-                pass8(z + m * N + (have > 0 ? n : 0), have, p);
+                if (past)
+                    pass8(z + m * N + (have > 0 ? n : 0), have, p);
+                else
+                    load8(z + m * N + (have > 0 ? n : 0), have, p);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float y, d;
@@ -585,7 +591,8 @@ hipError_t launch_dz(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStrea
     const int64_t pitch = up(a.N, 64), across = (pitch / 8 + LANES - 1) / LANES;
     hipLaunchKernelGGL((linear_dz_kernel<LANES, TD>),
                        dim3(static_cast<unsigned>(across), static_cast<unsigned>(dz_blocks(a.M, a.N))), dim3(256), 0, stream,
-                       a.act, static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z), dz, pitch, sums, a.M,
+                       a.act, static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z), dz,
+                       large(a.M * a.N) && a.N % 8 == 0, pitch, sums, a.M,
                        a.N, dz_rows(a.M, a.N));
     return hipGetLastError();
 }

@@ -130,7 +130,7 @@ def gradient64(grad, index, V, scale):
 
 GRADIENTS = [(1, 1, 1), (1, 700, 40), (2, 3, 300), (17, 5, 8), (100, 9, 33), (1000, 100, 64), (777, 3000, 65), (5000, 40, 128),
              (3000, 7, 130), (20_000, 2_000, 100), (40_000, 90, 257), (4_000, 9_000, 1_000), (16_384, 3_000, 2_048),
-             (300, 70, 5_000), (150_000, 1_000, 16)]
+             (300, 70, 5_000), (150_000, 1_000, 16), (187_000, 9, 128), (40_000, 100, 40), (33_333, 3, 300), (70_000, 2, 9)]
 
 
 @pytest.mark.parametrize("kind", KINDS)
