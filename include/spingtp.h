@@ -785,7 +785,7 @@ spingtp_status spingtp_gated_backward_workspace_size(int64_t M, int64_t K, int64
  * Linear layer with everything that follows the product: y = act(x w^T + bias) + residual, for bf16 x [M][K] and
  * w [N][K] (2-byte aligned; read as they are where K and the row strides are multiples of 8 and the rows start on 16
  * bytes, copied to the workspace elsewhere), bias [N] fp32 or NULL, residual [M][N] of dtype or NULL, y [M][N] of dtype.
- * act: any spingtp_activation.  z: NULL, or what the backward pass needs of an activation, x w^T + bias rounded to bf16,
+ * act: any spingtp_activation.  y may be the residual itself, at the same stride.  z: NULL, or what the backward pass needs of an activation, x w^T + bias rounded to bf16,
  * dense [M][N].  Sums, bias, activation and residual are fp32, y is rounded once.
  * workspace (16-byte aligned): the size below, for the same x and w (of whose addresses only the alignment counts).
  */

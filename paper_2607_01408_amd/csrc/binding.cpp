@@ -724,6 +724,7 @@ PyObject* adamw(Args a) {
         const int64_t n = p.numel();
         const at::Tensor& g = places.take(grads.at[i], "grads", n, Places::kGrad);
         if (!floating(p.scalar_type()) || !floating(g.scalar_type())) throw Refused("params and grads must be fp32 or bf16");
+        if (g.sizes() != p.sizes()) throw Refused("a gradient must have its param's shape");
         to = {p.data_ptr(), g.data_ptr(), nullptr, nullptr, nullptr, nullptr, nullptr, n, dtype_of(p.scalar_type()),
               dtype_of(g.scalar_type())};
         PyObject* const states[2] = {m.at[i], v.at[i]};
@@ -776,8 +777,11 @@ PyObject* adamw(Args a) {
     if (a[11] != Py_None) o.grad_scale = device_number<float>(a[11], "grad_scale", at::kFloat, *places.beside);
     o.seed = PyLong_AsUnsignedLongLongMask(a[12]);
     if (PyErr_Occurred()) throw PythonError{};
+    for (Py_ssize_t i = 0; i < params.n; ++i) {  // before the launch: it refuses what may not be written
+        tensor(params.at[i], "params").unsafeGetTensorImpl()->bump_version();
+        if (some && copies.at[i] != Py_None) tensor(copies.at[i], "copies").unsafeGetTensorImpl()->bump_version();
+    }
     done(lib.adamw(list.data(), params.n, &o, stream_of(a[13])), "spingtp_adamw");
-    for (Py_ssize_t i = 0; i < params.n; ++i) tensor(params.at[i], "params").unsafeGetTensorImpl()->bump_version();
     Py_RETURN_NONE;
 }
 

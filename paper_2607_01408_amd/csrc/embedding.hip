@@ -134,28 +134,32 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
     constexpr bool kFours = sizeof(TG) == 4 && sizeof(TO) == 4;
     if (blockIdx.x >= sum_blocks) {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        const int64_t first = (static_cast<int64_t>(blockIdx.x - sum_blocks) * 4 + wave) * kEmptyRows, mine = first + lane;
-        bool empty = false;
-        if (lane < kEmptyRows && mine < V) {
-            const int64_t at = place_from(rows, n, static_cast<int32_t>(mine));
-            empty = at >= n || rows[at] != mine;
-        }
         const float zeros[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         constexpr int kAtOnce = 64 / LANES;
-        uint64_t left = __ballot(empty);
-        // kAtOnce empty rows at a time, LANES lanes to each
-        while (left != 0) {
-            int64_t row = -1;
-#pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                if (left == 0) break;
-                const int b = __builtin_ctzll(left);
-                left &= left - 1;
-                if (lane / LANES == k) row = first + b;
+        const int64_t stride = static_cast<int64_t>(gridDim.x - sum_blocks) * 4 * kEmptyRows;
+        for (int64_t first = (static_cast<int64_t>(blockIdx.x - sum_blocks) * 4 + wave) * kEmptyRows; first < V;
+             first += stride) {
+            const int64_t mine = first + lane;
+            bool empty = false;
+            if (lane < kEmptyRows && mine < V) {
+                const int64_t at = place_from(rows, n, static_cast<int32_t>(mine));
+                empty = at >= n || rows[at] != mine;
             }
-            if (row >= 0)
-                for (int64_t c = (lane % LANES) * (kFours ? 4 : 8); c < D; c += LANES * 8)
-                    store_columns<LANES, kFours>(out + row * ldo, c, D, zeros, around);
+            uint64_t left = __ballot(empty);
+            // kAtOnce empty rows at a time, LANES lanes to each
+            while (left != 0) {
+                int64_t row = -1;
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (left == 0) break;
+                    const int b = __builtin_ctzll(left);
+                    left &= left - 1;
+                    if (lane / LANES == k) row = first + b;
+                }
+                if (row >= 0)
+                    for (int64_t c = (lane % LANES) * (kFours ? 4 : 8); c < D; c += LANES * 8)
+                        store_columns<LANES, kFours>(out + row * ldo, c, D, zeros, around);
+            }
         }
         return;
     }
@@ -390,7 +394,8 @@ template <int LANES, typename TG, typename TO>
 hipError_t gradient(const EmbeddingBwdArgs& a, hipStream_t stream) {
     const int64_t across = across_of(a.D, LANES), chunks = chunks_of(a.n, a.D), chunk = chunk_of(a.n, a.D);
     const int64_t sums = (chunks + 256 / LANES - 1) / (256 / LANES) * across, looked = 4 * kEmptyRows;
-    const int64_t empty = (a.V + looked - 1) / looked;
+    int64_t empty = (a.V + looked - 1) / looked;
+    if (empty > kMostBlocks) empty = kMostBlocks;
     hipLaunchKernelGGL((embedding_sum_kernel<LANES, TG, TO>), dim3(static_cast<unsigned>(sums + empty)), dim3(256), 0,
                        stream, static_cast<const TG*>(a.grad), a.ldg, a.order, a.rows, a.scale, static_cast<TO*>(a.out),
                        a.ldo, a.partial, a.n, a.V, a.D, chunk, static_cast<unsigned>(across), static_cast<unsigned>(sums),

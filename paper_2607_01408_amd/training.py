@@ -63,7 +63,8 @@ def _list(x):
 def adamw(params, grads, m, v, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, grad_scale=None, copies=None,
           seed=0):
     """spingtp_adamw: one step over the tensors of ``params`` (fp32 or bf16), in place, from ``grads`` (fp32 or bf16) and
-    the states ``m`` and ``v``, lists of as many.  All tensors are contiguous and on one device.
+    the states ``m`` and ``v``, lists of as many.  All tensors are contiguous and on one device, a gradient in its
+    param's shape.
 
     A state is an fp32 tensor of as many elements or a Block8 of shape (1, elements), both of a tensor alike; in 8
     bits ``v`` holds its root, and values are rounded by random bits from ``seed``, the step and the element's place

@@ -209,6 +209,16 @@ def test_nothing_beside_the_rows_is_read_or_written(M, K, N, shift):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("M,K,N", [(1, 72, 40), (70, 8200, 65), (300, 1100, 301), (2050, 1064, 3000), (3000, 3000, 3001)])
+def test_onto_the_residual_in_place(M, K, N, dtype):
+    x, w, r = rand((M, K), BF16, 1), rand((N, K), BF16, 2, K**-0.5), rand((M, N), dtype, 3)
+    for a, b in ((x, w), (sg.pack8(x), sg.pack8(w))):
+        want, there = sg.linear(a, b, residual=r, act="silu", dtype=dtype)[0], r.clone()
+        got = sg.linear(a, b, residual=there, act="silu", dtype=dtype, out=there)[0]
+        assert got is there and torch.equal(there, want)
+
+
 @pytest.mark.parametrize("M", [1, 100, 700])
 def test_values_that_are_not_numbers_stay_in_their_rows(M):
     K, N = 300, 200

@@ -197,6 +197,19 @@ def test_lookup_and_gradient_past_two_to_the_31_elements():
     assert bool((g == 0).all())
 
 
+def test_gradient_of_more_rows_than_a_launch_has_threads():
+    V, n = 1_100_000_003, 5000
+    index = torch.cat([whole((n - 2,), V, 1), torch.tensor([V - 1, 0], device="cuda")])
+    grad = rand((n, 1), BF16, 2)
+    g = sg.embedding_backward(grad, index, V, dtype=BF16)
+    rows, back = torch.unique(index, return_inverse=True)
+    ref, size, entries = gradient64(grad, back, len(rows), 1.0)
+    bound = (entries + 2) * 2.0**-24 * size
+    within(g[rows], ref, bound + 2.0**-8 * (ref.abs() + bound))
+    g[rows] = 0
+    assert not bool(g.any())
+
+
 # ------------------------------------------------------------------ AdamW
 
 M32 = 0xFFFFFFFF
@@ -589,7 +602,7 @@ def test_refusals():
         lambda: sg.embedding_backward(grad, sg.SortedIndex(s.order, s.rows[:19], 9), 9),
         lambda: sg.embedding_backward(grad, sg.SortedIndex(s.order.long(), s.rows, 9), 9),
         lambda: sg.adamw([p], [g, g], [m], [v], **on), lambda: sg.adamw([p], [g], [], [v], **on),
-        lambda: sg.adamw([p], [g[:299]], [m], [v], **on), lambda: sg.adamw([p], [g], [m[:299]], [v], **on),
+        lambda: sg.adamw([p.view(20, 15)], [g.view(15, 20)], [m], [v], **on), lambda: sg.adamw([p], [g[:299]], [m], [v], **on), lambda: sg.adamw([p], [g], [m[:299]], [v], **on),
         lambda: sg.adamw([p.half()], [g], [m], [v], **on), lambda: sg.adamw([p], [g.half()], [m], [v], **on),
         lambda: sg.adamw([p], [g], [m.bfloat16()], [v], **on), lambda: sg.adamw([p], [g], [m], [v8], **on),
         lambda: sg.adamw([p], [g], [short[0]], [short[1]], **on), lambda: sg.adamw([p], [g], [m], [m], **on),
