@@ -29,27 +29,34 @@ namespace {
 constexpr int kAdamwChunk = 2048;
 constexpr int kArgumentBytes = 4096;
 
-// A tensor, or a piece of one.
-struct Entry32 {
+// A tensor, or a piece of one: what every kind has, its states in fp32 or 8 bits, the bf16 copy where the list has any.
+// The shorter an entry, the more tensors to a launch: 97 in fp32 without copies, where entries with room for them
+// held 76.
+struct EntryBase {
+    uint32_t block;  // first workgroup
+    uint32_t n;      // elements
     void* p;
     const void* g;
+};
+struct Entry32 : EntryBase {
     float* m;
     float* v;
-    uint16_t* copy;
-    uint32_t n;  // elements
 };
-struct Entry8 {
-    void* p;
-    const void* g;
+struct Entry8 : EntryBase {
     uint8_t* m;
     uint8_t* v;
     uint8_t* ms;
     uint8_t* vs;
-    uint16_t* copy;
-    uint32_t n;
     uint32_t place;  // in the list
-    int64_t first;   // element of the tensor
+    uint32_t piece;  // of the tensor, kMostPiece elements each
 };
+template <typename T, bool COPY>
+struct EntryWith : T {};
+template <typename T>
+struct EntryWith<T, true> : T {
+    uint16_t* copy;
+};
+constexpr int64_t kMostPiece = int64_t{1} << 30;  // elements of an entry
 struct AdamwNumbers {
     float b1, c1, b2, c2;  // c: 1 - b
     float eps, least;      // least: 1 / c above, 0 where there is no bound
@@ -64,15 +71,14 @@ struct AdamwNumbers {
     const float* device_lr;
     const float* grad_scale;
 };
-template <bool BITS8>
+template <bool BITS8, bool COPY>
 struct AdamwArgs {
-    using Entry = std::conditional_t<BITS8, Entry8, Entry32>;
-    static constexpr int kMost = (kArgumentBytes - sizeof(AdamwNumbers)) / (sizeof(Entry) + 4);
+    using Entry = EntryWith<std::conditional_t<BITS8, Entry8, Entry32>, COPY>;
+    static constexpr int kMost = (kArgumentBytes - sizeof(AdamwNumbers)) / sizeof(Entry);
     AdamwNumbers o;
-    uint32_t block[kMost];  // an entry's first workgroup
     Entry entry[kMost];
 };
-static_assert(sizeof(AdamwArgs<false>) <= kArgumentBytes && sizeof(AdamwArgs<true>) <= kArgumentBytes);
+static_assert(sizeof(AdamwArgs<false, false>) <= kArgumentBytes && sizeof(AdamwArgs<true, true>) <= kArgumentBytes);
 
 __host__ __device__ inline uint32_t mix(uint32_t x) {
     x ^= x >> 16;
@@ -123,19 +129,19 @@ __device__ __forceinline__ void put_block(const float (&x)[8], const float (&siz
     if (leader) *scale = static_cast<uint8_t>(e);
 }
 
-template <bool BITS8, typename TP, typename TG>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8> a) {
+template <bool BITS8, typename TP, typename TG, bool COPY>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8, COPY> a) {
     // the last entry that begins here or before, a lane to each: one read of the arguments
     const AdamwNumbers& o = a.o;
     const int lane = threadIdx.x & 63;
     int at = -1;
 #pragma unroll
-    for (int first = 0; first < AdamwArgs<BITS8>::kMost; first += 64) {
+    for (int first = 0; first < AdamwArgs<BITS8, COPY>::kMost; first += 64) {
         const int e = first + lane < o.entries ? first + lane : 0;
-        at += __popcll(__ballot(first + lane < o.entries && a.block[e] <= blockIdx.x));
+        at += __popcll(__ballot(first + lane < o.entries && a.entry[e].block <= blockIdx.x));
     }
     const auto& t = a.entry[at];
-    const int64_t n = t.n, i0 = static_cast<int64_t>(blockIdx.x - a.block[at]) * kAdamwChunk + threadIdx.x * 8;
+    const int64_t n = t.n, i0 = static_cast<int64_t>(blockIdx.x - t.block) * kAdamwChunk + threadIdx.x * 8;
     const int64_t left = n - i0;
     const int have = left >= 8 ? 8 : (left > 0 ? static_cast<int>(left) : 0);
     // a block's sixteen lanes stay together: their places reach past n
@@ -192,12 +198,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8> a) {
         }
     }
     pass_store8(static_cast<TP*>(t.p) + from, have, p, o.around);
-    if (sizeof(TP) == 4 && t.copy != nullptr) pass_store8(t.copy + from, have, p, o.around);
+    if constexpr (COPY) {
+        if (t.copy != nullptr) pass_store8(t.copy + from, have, p, o.around);
+    }
     if constexpr (BITS8) {
         const uint32_t key =
             mix(mix(static_cast<uint32_t>(o.seed) + t.place * 0x9E3779B9u) + static_cast<uint32_t>(step) * 0x3C6EF373u +
                 static_cast<uint32_t>(o.seed >> 32));
-        const int64_t e = t.first + i0;
+        const int64_t e = t.piece * kMostPiece + i0;
         const uint32_t high = static_cast<uint32_t>(e >> 32) * 0x3C6EF373u + key;  // of all eight: a multiple of 8
         uint32_t word[8];
 #pragma unroll
@@ -211,18 +219,16 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8> a) {
     }
 }
 
-constexpr int64_t kMostPiece = int64_t{1} << 30;  // elements of an entry
-
 // The list's tensors of one kind, in as few launches as hold them.
-template <bool BITS8, typename TP, typename TG>
+template <bool BITS8, typename TP, typename TG, bool COPY>
 hipError_t launch_kind(const spingtp_adamw_tensor* tensors, int64_t count, const AdamwNumbers& o, hipStream_t stream) {
-    AdamwArgs<BITS8> a;
+    AdamwArgs<BITS8, COPY> a;
     a.o = o;
     a.o.entries = 0;
     int64_t blocks = 0;
     const auto flush = [&]() {
         if (a.o.entries == 0) return hipSuccess;
-        hipLaunchKernelGGL((adamw_kernel<BITS8, TP, TG>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
+        hipLaunchKernelGGL((adamw_kernel<BITS8, TP, TG, COPY>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a);
         a.o.entries = 0;
         blocks = 0;
         return hipGetLastError();
@@ -234,15 +240,15 @@ hipError_t launch_kind(const spingtp_adamw_tensor* tensors, int64_t count, const
         for (int64_t first = 0; first < x.n; first += kMostPiece) {
             const int64_t n = x.n - first < kMostPiece ? x.n - first : kMostPiece;
             const int64_t mine = (n + kAdamwChunk - 1) / kAdamwChunk;
-            if (a.o.entries == AdamwArgs<BITS8>::kMost || blocks + mine > kMostBlocks) {
+            if (a.o.entries == AdamwArgs<BITS8, COPY>::kMost || blocks + mine > kMostBlocks) {
                 const hipError_t e = flush();
                 if (e != hipSuccess) return e;
             }
-            a.block[a.o.entries] = static_cast<uint32_t>(blocks);
             auto& to = a.entry[a.o.entries++];
+            to.block = static_cast<uint32_t>(blocks);
             to.p = static_cast<TP*>(x.param) + first;
             to.g = static_cast<const TG*>(x.grad) + first;
-            to.copy = x.copy != nullptr ? static_cast<uint16_t*>(x.copy) + first : nullptr;
+            if constexpr (COPY) to.copy = x.copy != nullptr ? static_cast<uint16_t*>(x.copy) + first : nullptr;
             to.n = static_cast<uint32_t>(n);
             if constexpr (BITS8) {
                 to.m = static_cast<uint8_t*>(x.m) + first;
@@ -250,7 +256,7 @@ hipError_t launch_kind(const spingtp_adamw_tensor* tensors, int64_t count, const
                 to.ms = static_cast<uint8_t*>(x.m_scales) + first / kBlock8;
                 to.vs = static_cast<uint8_t*>(x.v_scales) + first / kBlock8;
                 to.place = static_cast<uint32_t>(k);
-                to.first = first;
+                to.piece = static_cast<uint32_t>(first / kMostPiece);
             } else {
                 to.m = static_cast<float*>(x.m) + first;
                 to.v = static_cast<float*>(x.v) + first;
@@ -289,18 +295,25 @@ hipError_t launch_adamw(const spingtp_adamw_tensor* tensors, int64_t count, cons
     int64_t elements = 0;
     for (int64_t k = 0; k < count; ++k) elements += tensors[k].n;
     o.around = elements > int64_t{1} << 22;
-    bool kinds[8] = {};
-    for (int64_t k = 0; k < count; ++k)
+    bool kinds[8] = {}, copies = false;
+    for (int64_t k = 0; k < count; ++k) {
         kinds[(tensors[k].m_scales != nullptr) * 4 + (tensors[k].param_dtype == SPINGTP_BF16) * 2 +
               (tensors[k].grad_dtype == SPINGTP_BF16)] = true;
+        copies = copies || tensors[k].copy != nullptr;
+    }
     using Launch = hipError_t (*)(const spingtp_adamw_tensor*, int64_t, const AdamwNumbers&, hipStream_t);
-    constexpr Launch launch[8] = {launch_kind<false, float, float>,    launch_kind<false, float, uint16_t>,
-                                  launch_kind<false, uint16_t, float>, launch_kind<false, uint16_t, uint16_t>,
-                                  launch_kind<true, float, float>,     launch_kind<true, float, uint16_t>,
-                                  launch_kind<true, uint16_t, float>,  launch_kind<true, uint16_t, uint16_t>};
+    constexpr Launch plain[8] = {
+        launch_kind<false, float, float, false>,    launch_kind<false, float, uint16_t, false>,
+        launch_kind<false, uint16_t, float, false>, launch_kind<false, uint16_t, uint16_t, false>,
+        launch_kind<true, float, float, false>,     launch_kind<true, float, uint16_t, false>,
+        launch_kind<true, uint16_t, float, false>,  launch_kind<true, uint16_t, uint16_t, false>};
+    // bf16 parameters have no copy
+    constexpr Launch copying[8] = {
+        launch_kind<false, float, float, true>, launch_kind<false, float, uint16_t, true>, plain[2], plain[3],
+        launch_kind<true, float, float, true>,  launch_kind<true, float, uint16_t, true>,  plain[6], plain[7]};
     for (int i = 0; i < 8; ++i)
         if (kinds[i]) {
-            const hipError_t e = launch[i](tensors, count, o, stream);
+            const hipError_t e = (copies ? copying : plain)[i](tensors, count, o, stream);
             if (e != hipSuccess) return e;
         }
     return hipSuccess;
