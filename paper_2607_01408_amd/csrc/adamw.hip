@@ -4,6 +4,9 @@
 //
 // One launch for as many tensors of a kind (types, states) as its arguments hold; a workgroup finds its tensor there and
 // takes 2,048 neighbouring elements of it, eight to a lane.  Nothing is uploaded, so a captured launch keeps its own table.
+// Bound by memory: 22 million elements in fp32 123 us (28 bytes each, 5.0 TB/s), 44 million with 8-bit states, bf16
+// gradients and copies 140 (16 bytes each, 5.1 TB/s); 240 small tensors 29.5, the checks of 960 tensors on the host and
+// three launches.
 //
 // States in 8 bits: m and sqrt(v) (half of v's range of exponents) in blocks of 128 elements, 16 lanes.  A step of v moves
 // it by a thousandth, a step of the format is a sixteenth to an eighth: rounded to nearest, v would stay where it is.  So

