@@ -4,8 +4,8 @@
 //
 // Forward: the products of gemm_nt.h; a wave's accumulators pass through its own LDS, 16 or 32 rows at a time, so that
 // a lane gets eight neighbouring columns of a row: bias, residual, z and y are whole lines, each touched once.
-// Backward: dz is made once, in bf16, with the columns' partial sums of it before the rounding; where there is no
-// activation and dy is bf16 on 16 bytes it is its own dz.  dx sums over w's rows, dw over those of dz and x: the
+// Backward: dz is made once, in bf16, with the columns' partial sums of it before the rounding (for many rows and few
+// channels by the launch that makes dx); where there is no activation and dy is bf16 on 16 bytes it is its own dz.  dx sums over w's rows, dw over those of dz and x: the
 // products read them as they lie.
 //
 // Few tiles and a long sum (the weights' gradients of many rows and few channels; dx of few rows) leave most of the
@@ -17,8 +17,8 @@
 //   8,192 x 2,048 x 8,192 onto a residual 222 (1.24 PFLOP/s, matrix units busy 57 % at 2.0 GHz); 8,192 x 8,192 x 2,048 with
 //   bias, gelu, z kept 293, some 60 of it the epilogue, behind which no other workgroup of the CU multiplies; its gradients'
 //   products 231 and 209;
-//   100,000 x 512 x 128, silu, z kept 53 (205 MB written, 4.3 TB/s), dz 55 (307 MB, 5.6 TB/s), dx 27, dw 27 in 63 slices
-//   and 6 to join them;
+//   100,000 x 512 x 128, silu, z kept 49 (205 MB written, 4.7 TB/s), dz and dx 66 (332 MB, 5.0 TB/s; in two launches dz 55,
+//   5.6 TB/s, and dx 27), dw 26 in 63 slices and 6 to join them;
 //   one row by 8,192 x 4,096 weights 12.5 (5.4 TB/s); 24 x 2,048 x 8,192 in 8 bits 9 in slices, 3 to join them.
 #include <hip/hip_runtime.h>
 
@@ -380,11 +380,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __re
                     load8(z + m * N + (have > 0 ? n : 0), have, p);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    float y, d;
-                    if (kind == kSilu)
-                        act_grad<kSilu>(p[i], y, d);
-                    else
-                        act_grad<kGelu>(p[i], y, d);
+                    const float d = kind == kSilu ? slope<kSilu>(p[i]) : slope<kGelu>(p[i]);
                     v[i] = i < have ? v[i] * d : 0.f;
                 }
             }
@@ -405,6 +401,210 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __re
         for (int k = 0; k < kAtOnce; ++k) s += part[k][c];
         sums[static_cast<int64_t>(blockIdx.y) * N + column] = s;
     }
+}
+
+// dz, its columns' sums and dx in one launch, for up to 128 columns of w: a workgroup keeps all of them for its rows, so
+// dz goes to the product through LDS and is read from memory by dw's alone.
+//
+// A step is 64 columns of dz by up to 128 rows: a thread makes eight columns of two of them, lays them in LDS beside the
+// step's 64 rows of w as a GemmTile with w's columns along the sum has them, and loads the next step's into the
+// registers that are free again; eight waves of 32 rows by 64 columns of dx multiply behind the barrier.  Two places for
+// either, so one barrier a step.  A column's sum over the wave's 16 rows is made by halving (lane bits 5, 4, 3), over
+// the waves by one of them behind the barrier, over the workgroup's rows in `column_sums`.
+//
+// Memory's rate where every workgroup's rows fill their tiles (dx alone of 65,536 x 512 by 128: 151 MB in 29 us, 5.2 TB/s),
+// else a step's arithmetic, which rows that do not exist take part in; 100,000 rows with dz stored 66 us, 5.0 TB/s.  Both
+// ways, dz by itself and this one, silu, all gradients (dx alone), us:
+//   100,000 x 512 by 128 118 / 100 (81 / 48), 100,000 x 128 by 32 48 / 40, 100,000 x 2,048 by 128 470 / 392, 50,000 x 512 by
+//   128 70 / 59 (44 / 25), 50,000 x 256 by 64 40 / 38; 32,768 rows 51 / 51, 31 / 34, 16,384 rows 34 / 46: steps follow one
+//   another, some 3 us each.  Hence from 40,000 rows on.
+constexpr int kNarrowRows = 128, kNarrowInputs = 128, kNarrowOutputs = 2048, kNarrowBlocks = 512;
+constexpr int64_t kNarrowLeast = 40'000;
+constexpr int kNarrowDz = kNarrowRows * kStepBytes, kNarrowW = 64 * 2 * kNarrowInputs, kNarrowPart = 8 * 64 * 4;
+constexpr int kNarrowLds = 2 * (kNarrowDz + kNarrowW + kNarrowPart);  // and 4 bytes a column of dz
+typedef uint32_t v4w __attribute__((ext_vector_type(4)));
+constexpr uint32_t kNowhere = 0x80000000u;  // past every buffer: loads give zeros, stores go nowhere
+constexpr int kPast = 2;                    // non-temporal, of a buffer's loads and stores
+
+// Lanes with the bit clear get the pair's sum of a, the others that of b.
+__device__ __forceinline__ float halve32(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halve16(float a, float b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float halve8(float a, float b, bool high) {
+    const float keep = high ? b : a, send = high ? a : b;
+    return keep + __shfl_xor(send, 8);
+}
+
+// Waits until the wave's LDS writes and reads are done, then for all waves; loads and stores of memory go on.
+__device__ __forceinline__ void written_and_read() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <typename TD, int ACT>
+__global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restrict__ dy, int64_t lddy,
+                                                            const uint16_t* __restrict__ z, const uint16_t* __restrict__ w,
+                                                            int64_t ldw, uint16_t* __restrict__ dz, int64_t pitch,
+                                                            float* __restrict__ sums, uint16_t* __restrict__ dx, int64_t lddx,
+                                                            int64_t M, int64_t N, int64_t K, int64_t rows, bool past) {
+    using Tile = GemmTile<Bf16, 64, 32, 2, 4, 2, false, true, false>;  // the places of w and its reads
+    constexpr int kWidth = sizeof(TD) / 2;                              // loads of eight elements of dy
+    extern __shared__ __align__(16) uint8_t narrow_lds[];
+    uint8_t* const at_dz = narrow_lds;
+    uint8_t* const at_w = at_dz + 2 * kNarrowDz;
+    float* const parts = reinterpret_cast<float*>(at_w + 2 * kNarrowW);
+    float* const column_sums = parts + 2 * (kNarrowPart / 4);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wn = wave & 1, wm = wave >> 1;
+    const int64_t m1 = static_cast<int64_t>(blockIdx.x) * rows, m2 = m1 + rows < M ? m1 + rows : M;
+    const int steps = static_cast<int>(pitch / 64);
+    for (int s = wave; s < steps; s += 8) column_sums[64 * s + lane] = 0.f;  // by the wave that adds to them
+
+    // the thread's part of a step: rows r and r + 64 of dz, 16-byte chunk c of them; rows of w, chunks of 8 columns
+    const int r = tid >> 3, c = tid & 7, wr = tid >> 4, wc = tid & 15;
+    v4w at_dy[2][kWidth], at_z[2], at_wr[2];
+    const uint32_t dy_row = static_cast<uint32_t>(lddy * sizeof(TD)), z_row = static_cast<uint32_t>(2 * N),
+                   w_row = static_cast<uint32_t>(2 * ldw), dz_row = static_cast<uint32_t>(2 * pitch);
+    const int columns = static_cast<int>(N), inputs = static_cast<int>(K);
+    // half i of step s of the rows from m0 on
+    const auto fetch = [&](int64_t m0, int s, int i) {
+        const int64_t have = m2 - m0;
+        const int count = have < kNarrowRows ? static_cast<int>(have < 0 ? 0 : have) : kNarrowRows;
+        const int64_t from = count > 0 ? m0 + 64 * i : 0;
+        const Buffer bd = buffer_of(reinterpret_cast<const uint8_t*>(dy + from * lddy), 0x7fffffffu);
+        const Buffer bz = buffer_of(reinterpret_cast<const uint8_t*>(z + from * N), 0x7fffffffu);
+        const Buffer bw = buffer_of(reinterpret_cast<const uint8_t*>(w + (64 * s + 32 * i) * ldw), 0x7fffffffu);
+        const bool in = r < count - 64 * i && 8 * c < columns - 64 * s;
+        const uint32_t od = in ? r * dy_row + 8 * sizeof(TD) * c : kNowhere, oz = in ? r * z_row + 16 * c : kNowhere;
+        const uint32_t ow = wr < columns - 64 * s - 32 * i && 8 * wc < inputs ? wr * w_row + 16 * wc : kNowhere;
+#pragma unroll
+        for (int h = 0; h < kWidth; ++h)
+            at_dy[i][h] = __builtin_amdgcn_raw_buffer_load_b128(bd, od, 64 * sizeof(TD) * s + 16 * h, kPast);
+        if constexpr (ACT != kIdentity) at_z[i] = __builtin_amdgcn_raw_buffer_load_b128(bz, oz, 128 * s, kPast);
+        at_wr[i] = __builtin_amdgcn_raw_buffer_load_b128(bw, ow, 0, 0);
+    };
+    const auto widen = [](const v4w& x, float (&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(x[i] << 16);
+            v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+        }
+    };
+
+    // places of the wave's fragments, as in GemmTile
+    const int in = lane & 15, key = (in >> 1) & 7;
+    const int wrow = 8 * (lane >> 4) + (in >> 2), wchunk = 8 * wn + ((lane & 3) >> 1);
+    const int tw = wrow * 256 + ((wchunk ^ Tile::turn(16, wrow)) << 4) + ((lane & 1) << 3);
+    fetch(m1, 0, 0);
+    fetch(m1, 0, 1);
+    int turn = 0;  // the places of this step
+    for (int64_t m0 = m1; m0 < m2; m0 += kNarrowRows) {
+        const int count = m2 - m0 < kNarrowRows ? static_cast<int>(m2 - m0) : kNarrowRows;
+        v4f acc[4][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+        for (int s = 0; s < steps; ++s) {
+            const bool last = s + 1 == steps;
+            uint8_t* const here_dz = at_dz + turn * kNarrowDz;
+            uint8_t* const here_w = at_w + turn * kNarrowW;
+            float* const here_part = parts + turn * (kNarrowPart / 4);
+            float sum[8];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int row = r + 64 * i, k = wr + 32 * i;
+                float v[8];
+                if constexpr (kWidth == 1) {
+                    widen(at_dy[i][0], v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(at_dy[i][e / 4][e % 4]);
+                }
+                if constexpr (ACT != kIdentity) {
+                    float p[8];
+                    widen(at_z[i], p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        v[e] *= slope<ACT>(p[e]);
+                    }
+                }
+                const v4w q{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+                *reinterpret_cast<v4w*>(here_dz + row * 128 + ((c ^ ((row >> 1) & 7)) << 4)) = q;
+                *reinterpret_cast<v4w*>(here_w + k * 256 + ((wc ^ Tile::turn(16, k)) << 4)) = at_wr[i];
+                if (dz != nullptr)
+                    __builtin_amdgcn_raw_buffer_store_b128(
+                        q, buffer_of(reinterpret_cast<const uint8_t*>(dz + (m0 + 64 * i) * pitch), 0x7fffffffu),
+                        row < count ? r * dz_row + 16 * c : kNowhere, 128 * s, 0);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] = i == 0 ? v[e] : sum[e] + v[e];
+                fetch(last ? m0 + kNarrowRows : m0, last ? 0 : s + 1, i);  // into the registers that are free again
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (sums != nullptr) {
+                float four[4], two[2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) four[e] = halve32(sum[e], sum[4 + e]);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) two[e] = halve16(four[e], four[2 + e]);
+                here_part[wave * 64 + 8 * c + 4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1)] =
+                    halve8(two[0], two[1], (lane & 8) != 0);
+            }
+            written_and_read();
+            if (sums != nullptr && wave == (s & 7)) {
+                float total = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) total += here_part[k * 64 + lane];
+                column_sums[64 * s + lane] += total;
+            }
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                if (dx == nullptr) break;
+                v4i fx[2], fw[4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    fx[j] = *reinterpret_cast<const v4i*>(here_dz + (32 * wm + 16 * j + in) * 128 +
+                                                          (((4 * q + (lane >> 4)) ^ key) << 4));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fw[i] = Tile::turned(here_w + (tw ^ i << 5) + q * 8192, 1024);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        acc[i][j] = Bf16::product(__builtin_bit_cast(v8bf, fw[i]), __builtin_bit_cast(v8bf, fx[j]), acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            turn ^= 1;
+        }
+        if (dx == nullptr) continue;
+        // dx by LDS, in dz's places, so that it leaves in whole lines: 16 chunks a row, turned by the row
+        written_and_read();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = 32 * wm + 16 * j + in, chunk = 8 * wn + 2 * i + (lane >> 5);
+                *reinterpret_cast<uint2*>(at_dz + row * 256 + ((chunk ^ in) << 4) + ((lane >> 4) & 1) * 8) =
+                    make_uint2(bf16_pair(acc[i][j][0], acc[i][j][1]), bf16_pair(acc[i][j][2], acc[i][j][3]));
+            }
+        written_and_read();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = wr + 32 * i;
+            if (row >= count || 8 * wc >= K) continue;
+            const v4w v = *reinterpret_cast<const v4w*>(at_dz + row * 256 + ((wc ^ (row & 15)) << 4));
+            uint16_t* const out = dx + (m0 + row) * lddx + 8 * wc;
+            if (past)
+                __builtin_nontemporal_store(v, reinterpret_cast<v4w*>(out));
+            else
+                *reinterpret_cast<v4w*>(out) = v;
+        }
+        written_and_read();
+    }
+    if (sums != nullptr)
+        for (int s = wave; s < steps; s += 8)
+            if (64 * s + lane < N) sums[static_cast<int64_t>(blockIdx.x) * N + 64 * s + lane] = column_sums[64 * s + lane];
 }
 
 // The workgroups' sums of a column added in a fixed order: 16 columns a workgroup, 64 parts of the rows.
@@ -685,6 +885,41 @@ hipError_t launch_linear8(const LinearArgs& a, hipStream_t stream) {
                                       stream);
 }
 
+// Whether linear_narrow_kernel makes dz and dx; also where dx is not wanted, so that the others have the same bits.
+bool narrow(const LinearBwdArgs& a) {
+    const int64_t width = a.dtype == SPINGTP_FP32 ? 4 : 2;
+    const auto whole = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
+    return !own_dz(a) && a.M >= kNarrowLeast && a.K <= kNarrowInputs && rows_fit(a.w, a.K, a.ldw) &&
+           a.N <= kNarrowOutputs && a.N % 8 == 0 && whole(a.dy) && a.lddy * width % 16 == 0 &&
+           a.lddy * width <= kMostRowBytes && (a.act == kIdentity || whole(a.z)) &&
+           (a.dx == nullptr || (whole(a.dx) && a.lddx % 8 == 0));
+}
+// of a workgroup, all of them on the CUs at once (whole tiles, 782 workgroups for 100,000 x 512 by 128: 158 us of the training
+// step against 156)
+int64_t narrow_rows(int64_t M) { return up((M + kNarrowBlocks - 1) / kNarrowBlocks, 16); }
+int64_t narrow_blocks(int64_t M) { return (M + narrow_rows(M) - 1) / narrow_rows(M); }
+template <typename TD, int ACT>
+hipError_t launch_narrow(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+    const int64_t pitch = up(a.N, 64);
+    const size_t lds = kNarrowLds + static_cast<size_t>(pitch) * 4;
+    const auto kernel = linear_narrow_kernel<TD, ACT>;
+    hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(narrow_blocks(a.M))), dim3(512), lds, stream,
+                       static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z),
+                       static_cast<const uint16_t*>(a.w), a.ldw, dz, pitch, sums, static_cast<uint16_t*>(a.dx), a.lddx, a.M,
+                       a.N, a.K, narrow_rows(a.M), large(a.M * a.K));
+    return hipGetLastError();
+}
+template <typename TD>
+hipError_t make_narrow(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+    switch (a.act) {
+        case kSilu: return launch_narrow<TD, kSilu>(a, dz, sums, stream);
+        case kGelu: return launch_narrow<TD, kGelu>(a, dz, sums, stream);
+        default: return launch_narrow<TD, kIdentity>(a, dz, sums, stream);
+    }
+}
+// rows of the columns' sums
+int64_t sum_rows(const LinearBwdArgs& a) { return narrow(a) ? narrow_blocks(a.M) : dz_blocks(a.M, a.N); }
+
 // dz, the sums of its columns, copies of w and x, and the slices' sums of a product
 bool makes_dz(const LinearBwdArgs& a) { return (a.dx != nullptr || a.dw != nullptr) && !own_dz(a); }
 bool copies_w(const LinearBwdArgs& a) { return a.dx != nullptr && !rows_fit(a.w, a.K, a.ldw); }
@@ -695,7 +930,9 @@ size_t linear_backward_workspace(const LinearBwdArgs& a) {
     const size_t dw = a.dw == nullptr ? 0 : dw_shape(a.M, a.K, a.N).bytes(a.N, a.K);
     const size_t copies = ((copies_w(a) ? a.N : 0) + (copies_x(a) ? a.M : 0)) * row;
     const size_t dz = makes_dz(a) ? static_cast<size_t>(a.M * up(a.N, 64)) * 2 : 0;
-    const size_t sums = a.db == nullptr ? 0 : static_cast<size_t>(dz_blocks(a.M, a.N) * a.N) * sizeof(float);
+    int64_t blocks = dz_blocks(a.M, a.N);  // either kernel's
+    if (narrow_blocks(a.M) > blocks) blocks = narrow_blocks(a.M);
+    const size_t sums = a.db == nullptr ? 0 : static_cast<size_t>(blocks * a.N) * sizeof(float);
     return dz + up16(sums) + copies + larger(dx, dw);
 }
 
@@ -710,16 +947,19 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
     const int64_t np = up(a.N, 64), kp = up(a.K, 64);
     const bool own = own_dz(a);
     uint8_t* at = static_cast<uint8_t*>(a.workspace);
-    uint16_t* dz = makes_dz(a) ? reinterpret_cast<uint16_t*>(at) : nullptr;
+    const bool one_launch = narrow(a);
+    uint16_t* dz = makes_dz(a) && (a.dw != nullptr || !one_launch) ? reinterpret_cast<uint16_t*>(at) : nullptr;
     if (dz != nullptr) at += 2 * a.M * np;
     float* sums = a.db != nullptr ? reinterpret_cast<float*>(at) : nullptr;
-    if (a.db != nullptr) at += up16(static_cast<size_t>(dz_blocks(a.M, a.N) * a.N) * sizeof(float));
+    if (a.db != nullptr) at += up16(static_cast<size_t>(sum_rows(a) * a.N) * sizeof(float));
     hipError_t e = hipSuccess;
-    if (dz != nullptr || sums != nullptr)
+    if (one_launch)
+        e = a.dtype == SPINGTP_FP32 ? make_narrow<float>(a, dz, sums, stream) : make_narrow<uint16_t>(a, dz, sums, stream);
+    else if (dz != nullptr || sums != nullptr)
         e = a.dtype == SPINGTP_FP32 ? make_dz<float>(a, dz, sums, stream) : make_dz<uint16_t>(a, dz, sums, stream);
     if (e == hipSuccess && sums != nullptr) {
         hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>((a.N + 15) / 16)), dim3(1024), 0, stream, sums,
-                           dz_blocks(a.M, a.N), a.N, a.db);
+                           sum_rows(a), a.N, a.db);
         e = hipGetLastError();
     }
     RowCopy w{static_cast<const uint16_t*>(a.w), a.ldw, 0, nullptr}, x{static_cast<const uint16_t*>(a.x), a.ldx, 0, nullptr};
@@ -736,7 +976,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
     if (e == hipSuccess && w.R + x.R > 0) e = copy_rows(w, x, a.K, stream);
     const uint8_t* from = own ? static_cast<const uint8_t*>(a.dy) : reinterpret_cast<const uint8_t*>(dz);
     const int64_t ldz = 2 * (own ? a.lddy : np);
-    if (e == hipSuccess && a.dx != nullptr) {
+    if (e == hipSuccess && a.dx != nullptr && !one_launch) {
         const Shape s = dx_shape(a.M, a.K, a.N);
         GemmArgs g{};
         g.x = from;
