@@ -5,8 +5,8 @@
 // Forward: the products of gemm_nt.h; a wave's accumulators pass through its own LDS, 16 or 32 rows at a time, so that
 // a lane gets eight neighbouring columns of a row: bias, residual, z and y are whole lines, each touched once.
 // Backward: dz is made once, in bf16, with the columns' partial sums of it before the rounding (for many rows and few
-// channels by the launch that makes dx); where there is no activation and dy is bf16 on 16 bytes it is its own dz.  dx sums over w's rows, dw over those of dz and x: the
-// products read them as they lie.
+// channels by the launch that makes dx); where there is no activation and dy is bf16 on 16 bytes it is its own dz.  dx sums
+// over w's rows, dw over those of dz and x: the products read them as they lie.
 //
 // Few tiles and a long sum (the weights' gradients of many rows and few channels; dx of few rows) leave most of the
 // CUs idle: then the sum is cut into slices, a workgroup to each, whose fp32 sums a second kernel adds in order and
@@ -18,7 +18,7 @@
 //   bias, gelu, z kept 293, some 60 of it the epilogue, behind which no other workgroup of the CU multiplies; its gradients'
 //   products 231 and 209;
 //   100,000 x 512 x 128, silu, z kept 49 (205 MB written, 4.7 TB/s), dz and dx 66 (332 MB, 5.0 TB/s; in two launches dz 55,
-//   5.6 TB/s, and dx 27), dw 26 in 63 slices and 6 to join them;
+//   5.6 TB/s, and dx 27), dw 26 in 63 slices, 8 to join them and to add db up;
 //   one row by 8,192 x 4,096 weights 12.5 (5.4 TB/s); 24 x 2,048 x 8,192 in 8 bits 9 in slices, 3 to join them.
 #include <hip/hip_runtime.h>
 
@@ -256,14 +256,47 @@ __global__ __launch_bounds__(64 * kSkinnyWaves) void linear_skinny_kernel(GemmAr
                               });
 }
 
+// db: the workgroups' sums of a column added in a fixed order, 16 columns a workgroup of 256, 16 parts of the rows.
+struct ColumnSums {
+    const float* sums;  // [rows][N]
+    int64_t rows, N;
+    float* db;  // null: not wanted
+    int64_t blocks() const { return db != nullptr ? (N + 15) / 16 : 0; }
+};
+__device__ __forceinline__ void add_columns(const ColumnSums& d, int64_t block) {
+    __shared__ float part[16][17];
+    const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+    const int64_t n = block * 16 + c;
+    float s = 0.f;
+    if (n < d.N) {
+#pragma unroll 16
+        for (int64_t r = g; r < d.rows; r += 16) s += d.sums[r * d.N + n];
+    }
+    part[g][c] = s;
+    __syncthreads();
+    if (threadIdx.x < 16 && n < d.N) {
+        float total = 0.f;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) total += part[k][c];
+        d.db[n] = total;
+    }
+}
+__global__ __launch_bounds__(256) void linear_db_kernel(ColumnSums d) { add_columns(d, blockIdx.x); }
+
 // The slices' sums added in a fixed order, and what follows them: eight neighbouring outputs to PARTS threads, each of
-// which adds every PARTS-th slice (few outputs of many slices would keep few threads busy).
+// which adds every PARTS-th slice (few outputs of many slices would keep few threads busy).  The workgroups from `blocks` on
+// make db, which saves its launch: all gradients of 100,000 x 128 by 32 40 -> 36 us.
 template <int PARTS>
-__global__ __launch_bounds__(256) void linear_join_kernel(LinearOut o, int slices, int64_t M, int64_t N) {
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearOut o, int slices, int64_t M, int64_t N, unsigned blocks,
+                                                          ColumnSums d) {
+    if (blockIdx.x >= blocks) {
+        add_columns(d, blockIdx.x - blocks);
+        return;
+    }
     constexpr int kOutputs = 256 / PARTS;
     __shared__ float part[PARTS > 1 ? PARTS : 1][PARTS > 1 ? kOutputs : 1][9];
     const int i0 = threadIdx.x % kOutputs, part_of = threadIdx.x / kOutputs;
-    const int64_t groups = (N + 7) / 8, stride = static_cast<int64_t>(gridDim.x) * kOutputs;
+    const int64_t groups = (N + 7) / 8, stride = static_cast<int64_t>(blocks) * kOutputs;
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * kOutputs; first < M * groups; first += stride) {
         const int64_t at = first + i0, m = at / groups, n = (at - m * groups) * 8;
         const bool mine = at < M * groups;
@@ -607,27 +640,6 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
             if (64 * s + lane < N) sums[static_cast<int64_t>(blockIdx.x) * N + 64 * s + lane] = column_sums[64 * s + lane];
 }
 
-// The workgroups' sums of a column added in a fixed order: 16 columns a workgroup, 64 parts of the rows.
-__global__ __launch_bounds__(1024) void linear_db_kernel(const float* __restrict__ sums, int64_t rows, int64_t N,
-                                                         float* __restrict__ db) {
-    __shared__ float part[64][17];
-    const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
-    const int64_t n = static_cast<int64_t>(blockIdx.x) * 16 + c;
-    float s = 0.f;
-    if (n < N) {
-#pragma unroll 8
-        for (int64_t r = g; r < rows; r += 64) s += sums[r * N + n];
-    }
-    part[g][c] = s;
-    __syncthreads();
-    if (threadIdx.x < 16 && n < N) {
-        float total = 0.f;
-#pragma unroll 16
-        for (int k = 0; k < 64; ++k) total += part[k][c];
-        db[n] = total;
-    }
-}
-
 template <typename T>
 __global__ __launch_bounds__(256) void linear_zero_kernel(T* p, int64_t n) {
     const int64_t stride = static_cast<int64_t>(gridDim.x) * 256;
@@ -716,9 +728,17 @@ hipError_t launch_few(const GemmArgs& g, int64_t row_bytes, const LinearOut& o, 
     return hipGetLastError();
 }
 
-// The product, its slices in `partial`, and what follows.
+template <int PARTS>
+void join(const Shape& s, const GemmArgs& g, const LinearOut& o, const ColumnSums& d, hipStream_t stream) {
+    const unsigned blocks = walking(g.M * ((g.N + 7) / 8) * PARTS).x;
+    hipLaunchKernelGGL(linear_join_kernel<PARTS>, dim3(blocks + static_cast<unsigned>(d.blocks())), dim3(256), 0, stream, o,
+                       static_cast<int>(s.slices), g.M, g.N, blocks, d);
+}
+
+// The product, its slices in `partial`, and what follows; where there are slices, db in the launch that joins them.
 template <class E, bool KW, bool KX>
-hipError_t product(const Shape& s, GemmArgs g, int64_t row_bytes, LinearOut o, float* partial, hipStream_t stream) {
+hipError_t product(const Shape& s, GemmArgs g, int64_t row_bytes, LinearOut o, float* partial, hipStream_t stream,
+                   const ColumnSums& d = ColumnSums{}) {
     o.partial = s.slices > 1 ? partial : nullptr;
     o.slice = static_cast<int>(s.per);
     hipError_t e;
@@ -739,11 +759,9 @@ hipError_t product(const Shape& s, GemmArgs g, int64_t row_bytes, LinearOut o, f
     if (e != hipSuccess || s.slices == 1) return e;
     const int64_t outputs = g.M * ((g.N + 7) / 8);
     if (outputs < 32768 && s.slices >= 8)
-        hipLaunchKernelGGL(linear_join_kernel<8>, walking(outputs * 8), dim3(256), 0, stream, o, static_cast<int>(s.slices),
-                           g.M, g.N);
+        join<8>(s, g, o, d, stream);
     else
-        hipLaunchKernelGGL(linear_join_kernel<1>, walking(outputs), dim3(256), 0, stream, o, static_cast<int>(s.slices), g.M,
-                           g.N);
+        join<1>(s, g, o, d, stream);
     return hipGetLastError();
 }
 
@@ -957,9 +975,10 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
         e = a.dtype == SPINGTP_FP32 ? make_narrow<float>(a, dz, sums, stream) : make_narrow<uint16_t>(a, dz, sums, stream);
     else if (dz != nullptr || sums != nullptr)
         e = a.dtype == SPINGTP_FP32 ? make_dz<float>(a, dz, sums, stream) : make_dz<uint16_t>(a, dz, sums, stream);
-    if (e == hipSuccess && sums != nullptr) {
-        hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>((a.N + 15) / 16)), dim3(1024), 0, stream, sums,
-                           sum_rows(a), a.N, a.db);
+    ColumnSums d{sums, sums != nullptr ? sum_rows(a) : 0, a.N, sums != nullptr ? a.db : nullptr};
+    const bool joined = a.dw != nullptr && dw_shape(a.M, a.K, a.N).slices > 1 && d.blocks() <= kMostBlocks;
+    if (e == hipSuccess && sums != nullptr && !joined) {
+        hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>(d.blocks())), dim3(256), 0, stream, d);
         e = hipGetLastError();
     }
     RowCopy w{static_cast<const uint16_t*>(a.w), a.ldw, 0, nullptr}, x{static_cast<const uint16_t*>(a.x), a.ldx, 0, nullptr};
@@ -1008,7 +1027,7 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
         g.w_rows = g.x_rows = a.M;
         g.w_split = g.steps;
         const LinearOut o{kIdentity, a.w_dtype == SPINGTP_FP32, nullptr, nullptr, 0, a.dw, a.K, nullptr, false, nullptr, 0};
-        if (e == hipSuccess) e = product<Bf16, true, true>(s, g, 0, o, reinterpret_cast<float*>(at), stream);
+        if (e == hipSuccess) e = product<Bf16, true, true>(s, g, 0, o, reinterpret_cast<float*>(at), stream, joined ? d : ColumnSums{});
     }
     return e;
 }
