@@ -476,7 +476,8 @@ __device__ __forceinline__ float halve8(float a, float b, bool high) {
 // Waits until the wave's LDS writes and reads are done, then for all waves; loads and stores of memory go on.
 __device__ __forceinline__ void written_and_read() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-template <typename TD, int ACT>
+// WHOLE: dx's rows start and end on 16 bytes (a parameter, for the registers that the other way takes).
+template <typename TD, int ACT, bool WHOLE>
 __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restrict__ dy, int64_t lddy,
                                                             const uint16_t* __restrict__ z, const uint16_t* __restrict__ w,
                                                             int64_t ldw, uint16_t* __restrict__ dz, int64_t pitch,
@@ -499,6 +500,7 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
     v4w at_dy[2][kWidth], at_z[2], at_wr[2];
     const uint32_t dy_row = static_cast<uint32_t>(lddy * sizeof(TD)), z_row = static_cast<uint32_t>(2 * N),
                    w_row = static_cast<uint32_t>(2 * ldw), dz_row = static_cast<uint32_t>(2 * pitch);
+    const uint32_t w_bytes = dx != nullptr ? 0x7fffffffu : 0;  // without dx there may be no w: no byte of it is read
     const int columns = static_cast<int>(N), inputs = static_cast<int>(K);
     // half i of step s of the rows from m0 on
     const auto fetch = [&](int64_t m0, int s, int i) {
@@ -507,7 +509,7 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
         const int64_t from = count > 0 ? m0 + 64 * i : 0;
         const Buffer bd = buffer_of(reinterpret_cast<const uint8_t*>(dy + from * lddy), 0x7fffffffu);
         const Buffer bz = buffer_of(reinterpret_cast<const uint8_t*>(z + from * N), 0x7fffffffu);
-        const Buffer bw = buffer_of(reinterpret_cast<const uint8_t*>(w + (64 * s + 32 * i) * ldw), 0x7fffffffu);
+        const Buffer bw = buffer_of(reinterpret_cast<const uint8_t*>(w + (64 * s + 32 * i) * ldw), w_bytes);
         const bool in = r < count - 64 * i && 8 * c < columns - 64 * s;
         const uint32_t od = in ? r * dy_row + 8 * sizeof(TD) * c : kNowhere, oz = in ? r * z_row + 16 * c : kNowhere;
         const uint32_t ow = wr < columns - 64 * s - 32 * i && 8 * wc < inputs ? wr * w_row + 16 * wc : kNowhere;
@@ -626,12 +628,18 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
         for (int i = 0; i < 4; ++i) {
             const int row = wr + 32 * i;
             if (row >= count || 8 * wc >= K) continue;
-            const v4w v = *reinterpret_cast<const v4w*>(at_dz + row * 256 + ((wc ^ (row & 15)) << 4));
+            const uint8_t* const staged = at_dz + row * 256 + ((wc ^ (row & 15)) << 4);
             uint16_t* const out = dx + (m0 + row) * lddx + 8 * wc;
-            if (past)
-                __builtin_nontemporal_store(v, reinterpret_cast<v4w*>(out));
-            else
-                *reinterpret_cast<v4w*>(out) = v;
+            if constexpr (WHOLE) {
+                const v4w v = *reinterpret_cast<const v4w*>(staged);
+                if (past)
+                    __builtin_nontemporal_store(v, reinterpret_cast<v4w*>(out));
+                else
+                    *reinterpret_cast<v4w*>(out) = v;
+            } else {
+#pragma unroll 1
+                for (int e = 0; e < 8 && 8 * wc + e < inputs; ++e) out[e] = reinterpret_cast<const uint16_t*>(staged)[e];
+            }
         }
         written_and_read();
     }
@@ -903,37 +911,47 @@ hipError_t launch_linear8(const LinearArgs& a, hipStream_t stream) {
                                       stream);
 }
 
-// Whether linear_narrow_kernel makes dz and dx; also where dx is not wanted, so that the others have the same bits.
+// Whether linear_narrow_kernel makes dz and dx: whatever w, dx and the gradients that are wanted, so that db has the same
+// bits with any of them (w is read for dx alone, and may be null without it).
 bool narrow(const LinearBwdArgs& a) {
     const int64_t width = a.dtype == SPINGTP_FP32 ? 4 : 2;
     const auto whole = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
-    return !own_dz(a) && a.M >= kNarrowLeast && a.K <= kNarrowInputs && rows_fit(a.w, a.K, a.ldw) &&
-           a.N <= kNarrowOutputs && a.N % 8 == 0 && whole(a.dy) && a.lddy * width % 16 == 0 &&
-           a.lddy * width <= kMostRowBytes && (a.act == kIdentity || whole(a.z)) &&
-           (a.dx == nullptr || (whole(a.dx) && a.lddx % 8 == 0));
+    return !own_dz(a) && a.M >= kNarrowLeast && a.K <= kNarrowInputs && a.N <= kNarrowOutputs && a.N % 8 == 0 &&
+           whole(a.dy) && a.lddy * width % 16 == 0 && a.lddy * width <= kMostRowBytes && (a.act == kIdentity || whole(a.z));
 }
 // of a workgroup, all of them on the CUs at once (whole tiles, 782 workgroups for 100,000 x 512 by 128: 158 us of the training
 // step against 156)
 int64_t narrow_rows(int64_t M) { return up((M + kNarrowBlocks - 1) / kNarrowBlocks, 16); }
 int64_t narrow_blocks(int64_t M) { return (M + narrow_rows(M) - 1) / narrow_rows(M); }
-template <typename TD, int ACT>
-hipError_t launch_narrow(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+template <typename TD, int ACT, bool WHOLE>
+hipError_t launch_narrow(const LinearBwdArgs& a, const uint16_t* w, int64_t ldw, uint16_t* dz, float* sums,
+                         hipStream_t stream) {
     const int64_t pitch = up(a.N, 64);
     const size_t lds = kNarrowLds + static_cast<size_t>(pitch) * 4;
-    const auto kernel = linear_narrow_kernel<TD, ACT>;
+    const auto kernel = linear_narrow_kernel<TD, ACT, WHOLE>;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(narrow_blocks(a.M))), dim3(512), lds, stream,
-                       static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z),
-                       static_cast<const uint16_t*>(a.w), a.ldw, dz, pitch, sums, static_cast<uint16_t*>(a.dx), a.lddx, a.M,
-                       a.N, a.K, narrow_rows(a.M), large(a.M * a.K));
+                       static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z), w, ldw, dz, pitch, sums,
+                       static_cast<uint16_t*>(a.dx), a.lddx, a.M, a.N, a.K, narrow_rows(a.M),
+                       large(a.M * a.K));
     return hipGetLastError();
 }
-template <typename TD>
-hipError_t make_narrow(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+template <typename TD, bool WHOLE>
+hipError_t make_narrow(const LinearBwdArgs& a, const uint16_t* w, int64_t ldw, uint16_t* dz, float* sums,
+                       hipStream_t stream) {
     switch (a.act) {
-        case kSilu: return launch_narrow<TD, kSilu>(a, dz, sums, stream);
-        case kGelu: return launch_narrow<TD, kGelu>(a, dz, sums, stream);
-        default: return launch_narrow<TD, kIdentity>(a, dz, sums, stream);
+        case kSilu: return launch_narrow<TD, kSilu, WHOLE>(a, w, ldw, dz, sums, stream);
+        case kGelu: return launch_narrow<TD, kGelu, WHOLE>(a, w, ldw, dz, sums, stream);
+        default: return launch_narrow<TD, kIdentity, WHOLE>(a, w, ldw, dz, sums, stream);
     }
+}
+hipError_t make_narrow(const LinearBwdArgs& a, const uint16_t* w, int64_t ldw, uint16_t* dz, float* sums,
+                       hipStream_t stream) {
+    const bool whole = rows_fit(a.dx, a.K, a.lddx) || a.dx == nullptr;
+    if (a.dtype == SPINGTP_FP32)
+        return whole ? make_narrow<float, true>(a, w, ldw, dz, sums, stream)
+                     : make_narrow<float, false>(a, w, ldw, dz, sums, stream);
+    return whole ? make_narrow<uint16_t, true>(a, w, ldw, dz, sums, stream)
+                 : make_narrow<uint16_t, false>(a, w, ldw, dz, sums, stream);
 }
 // rows of the columns' sums
 int64_t sum_rows(const LinearBwdArgs& a) { return narrow(a) ? narrow_blocks(a.M) : dz_blocks(a.M, a.N); }
@@ -970,17 +988,6 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
     if (dz != nullptr) at += 2 * a.M * np;
     float* sums = a.db != nullptr ? reinterpret_cast<float*>(at) : nullptr;
     if (a.db != nullptr) at += up16(static_cast<size_t>(sum_rows(a) * a.N) * sizeof(float));
-    hipError_t e = hipSuccess;
-    if (one_launch)
-        e = a.dtype == SPINGTP_FP32 ? make_narrow<float>(a, dz, sums, stream) : make_narrow<uint16_t>(a, dz, sums, stream);
-    else if (dz != nullptr || sums != nullptr)
-        e = a.dtype == SPINGTP_FP32 ? make_dz<float>(a, dz, sums, stream) : make_dz<uint16_t>(a, dz, sums, stream);
-    ColumnSums d{sums, sums != nullptr ? sum_rows(a) : 0, a.N, sums != nullptr ? a.db : nullptr};
-    const bool joined = a.dw != nullptr && dw_shape(a.M, a.K, a.N).slices > 1 && d.blocks() <= kMostBlocks;
-    if (e == hipSuccess && sums != nullptr && !joined) {
-        hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>(d.blocks())), dim3(256), 0, stream, d);
-        e = hipGetLastError();
-    }
     RowCopy w{static_cast<const uint16_t*>(a.w), a.ldw, 0, nullptr}, x{static_cast<const uint16_t*>(a.x), a.ldx, 0, nullptr};
     if (copies_w(a)) {
         w.R = a.N;
@@ -992,7 +999,20 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
         x.to = reinterpret_cast<uint16_t*>(at);
         at += 2 * a.M * kp;
     }
-    if (e == hipSuccess && w.R + x.R > 0) e = copy_rows(w, x, a.K, stream);
+    hipError_t e = hipSuccess;
+    if (w.R + x.R > 0) e = copy_rows(w, x, a.K, stream);
+    const uint16_t* const w_rows = w.R > 0 ? w.to : static_cast<const uint16_t*>(a.w);
+    const int64_t ldw = w.R > 0 ? kp : a.ldw;
+    if (e == hipSuccess && one_launch)
+        e = make_narrow(a, w_rows, ldw, dz, sums, stream);
+    else if (e == hipSuccess && (dz != nullptr || sums != nullptr))
+        e = a.dtype == SPINGTP_FP32 ? make_dz<float>(a, dz, sums, stream) : make_dz<uint16_t>(a, dz, sums, stream);
+    ColumnSums d{sums, sums != nullptr ? sum_rows(a) : 0, a.N, sums != nullptr ? a.db : nullptr};
+    const bool joined = a.dw != nullptr && dw_shape(a.M, a.K, a.N).slices > 1 && d.blocks() <= kMostBlocks;
+    if (e == hipSuccess && sums != nullptr && !joined) {
+        hipLaunchKernelGGL(linear_db_kernel, dim3(static_cast<unsigned>(d.blocks())), dim3(256), 0, stream, d);
+        e = hipGetLastError();
+    }
     const uint8_t* from = own ? static_cast<const uint8_t*>(a.dy) : reinterpret_cast<const uint8_t*>(dz);
     const int64_t ldz = 2 * (own ? a.lddy : np);
     if (e == hipSuccess && a.dx != nullptr && !one_launch) {
@@ -1000,8 +1020,8 @@ hipError_t launch_linear_backward(const LinearBwdArgs& a, hipStream_t stream) {
         GemmArgs g{};
         g.x = from;
         g.ldx = ldz;
-        g.w = w.R > 0 ? reinterpret_cast<const uint8_t*>(w.to) : static_cast<const uint8_t*>(a.w);
-        g.ldw = 2 * (w.R > 0 ? kp : a.ldw);
+        g.w = reinterpret_cast<const uint8_t*>(w_rows);
+        g.ldw = 2 * ldw;
         g.w2 = g.w;
         g.M = a.M;
         g.N = a.K;

@@ -17,7 +17,7 @@ from tests.test_gpu_linear import (ACTS, BF16, F32, HALF, INF, NAN, amid, backwa
 # one tile of rows a workgroup and more; sums that end inside a step; channels from a chunk of 8 to all 128; the fewest rows,
 # the most outputs
 SHAPES = [(40_000, 128, 512), (40_001, 8, 8), (66_000, 128, 64), (45_011, 64, 200), (65_537, 120, 72), (70_001, 16, 520),
-          (100_003, 128, 136), (41_001, 72, 2048)]
+          (100_003, 128, 136), (41_001, 72, 2048), (43_007, 100, 264), (50_001, 3, 40)]
 
 
 @pytest.mark.parametrize("act", ACTS)
@@ -60,6 +60,46 @@ def test_values_that_are_not_numbers_stay_in_their_rows():
             others = torch.arange(N, device="cuda") != 7
             assert not bool(torch.isfinite(gw[7]).any()) and bool(torch.isfinite(gw[others]).all())
             assert not bool(torch.isfinite(gb[7])) and bool(torch.isfinite(gb[others]).all())
+
+
+@pytest.mark.parametrize("K,lddx,shift", [(128, 136, 0), (128, 129, 0), (96, 104, 1), (100, 100, 0), (37, 40, 0)])
+def test_from_c_without_weights_and_onto_any_rows(K, lddx, shift):
+    """Without grad_x there need not be weights, and grad_bias and grad_w have the same bits as with it; grad_x onto rows with
+    others beside them."""
+    import ctypes
+
+    from paper_2607_01408_amd import _lib
+
+    C = _lib.lib()
+    M, N = 42_003, 72
+    x, w, z, dy = rand((M, K), BF16, 1), rand((N, K), BF16, 2, K**-0.5), rand((M, N), BF16, 3), rand((M, N), BF16, 4)
+    want = sg.linear_backward(dy, sg.LinearSaved(x, z, "silu"), w)
+    wide = torch.full((M * lddx + 16,), 9.0, dtype=BF16, device="cuda")
+    gx = wide[shift : shift + M * lddx].view(M, lddx)
+    gw, gb = torch.empty((N, K), dtype=BF16, device="cuda"), torch.empty(N, device="cuda")
+
+    def p(t):
+        return None if t is None else ctypes.c_void_p(t.data_ptr())
+
+    def run(w, gx):
+        n = ctypes.c_size_t()
+        head = (ctypes.c_int(0), ctypes.c_int(1), p(dy), ctypes.c_int64(N))
+        tail = tuple(ctypes.c_int64(v) for v in (M, K, N))
+        size = C.spingtp_linear_backward_workspace_size
+        assert size(*head, p(x), ctypes.c_int64(K), p(w), ctypes.c_int64(K), p(gx), p(gw), p(gb), *tail, ctypes.byref(n)) == 0
+        ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+        stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        assert C.spingtp_linear_backward(*head, p(z), p(x), ctypes.c_int64(K), p(w), ctypes.c_int64(K), p(gx),
+                                         ctypes.c_int64(lddx), ctypes.c_int(1), p(gw), p(gb), p(ws),
+                                         ctypes.c_size_t(n.value), *tail, stream) == 0
+        torch.cuda.synchronize()
+
+    run(w, gx)
+    assert all(torch.equal(a, b) for a, b in zip((gx[:, :K], gw, gb), want))
+    assert bool((gx[:, K:] == 9).all()) and bool((wide[:shift] == 9).all()) and bool((wide[shift + M * lddx :] == 9).all())
+    gw.fill_(0), gb.fill_(0)
+    run(None, None)
+    assert torch.equal(gw, want[1]) and torch.equal(gb, want[2])
 
 
 def test_a_captured_backward_replays():
