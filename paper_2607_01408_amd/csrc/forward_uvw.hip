@@ -47,6 +47,7 @@
 #include <cstdint>
 
 #include "internal.h"
+#include "lds_common.h"
 
 namespace spingtp {
 namespace {
@@ -527,6 +528,8 @@ hipError_t launch_uvw_grad_x2(const float* x1, const float* g, const float* w, f
     const int64_t gx = (N + kEdges - 1) / kEdges;
     if (lds == 0 || gx > 0x7fffffff || n_blocks2 > 65535) return hipErrorInvalidValue;
     const unsigned gz = static_cast<unsigned>(V < 65535 ? V : 65535);
+    const hipError_t raised = raise_lds_limit<&spingtp_uvw_grad_x2_kernel>();
+    if (raised != hipSuccess) return raised;
     hipLaunchKernelGGL(spingtp_uvw_grad_x2_kernel,
                        dim3(static_cast<unsigned>(gx), static_cast<unsigned>(n_blocks2), gz), dim3(kThreads), lds,
                        stream, x1, g, w, gx2, N, U, V, W, table, table2, n_paths, nc1, nc2, nco, d1max, d2max);

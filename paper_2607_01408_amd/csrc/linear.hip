@@ -928,7 +928,10 @@ hipError_t launch_narrow(const LinearBwdArgs& a, const uint16_t* w, int64_t ldw,
                          hipStream_t stream) {
     const int64_t pitch = up(a.N, 64);
     const size_t lds = kNarrowLds + static_cast<size_t>(pitch) * 4;
-    const auto kernel = linear_narrow_kernel<TD, ACT, WHOLE>;
+    static_assert(2 * (kNarrowLds + 4 * kNarrowOutputs) <= 160 * 1024, "two workgroups to a CU");
+    constexpr auto kernel = linear_narrow_kernel<TD, ACT, WHOLE>;
+    const hipError_t e = raise_lds_limit<kernel>();
+    if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(narrow_blocks(a.M))), dim3(512), lds, stream,
                        static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z), w, ldw, dz, pitch, sums,
                        static_cast<uint16_t*>(a.dx), a.lddx, a.M, a.N, a.K, narrow_rows(a.M),
