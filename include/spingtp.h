@@ -858,7 +858,9 @@ spingtp_status spingtp_embedding_backward_workspace_size(int64_t n, int64_t D, s
  * m and v are fp32 [n], or with m_scales and v_scales 8-bit blocks of a matrix [1][n] (16-byte aligned values) which
  * hold m and sqrt(v); zeros to begin with.  A new m (v) goes to the lower or upper neighbour in its block's format by
  * 16 random bits, such that the mean of m (of v) is kept, and there v is raised to (m / c)^2 where it is less,
- * c = (1 - beta1) / sqrt((1 - beta2) (1 - beta1^2 / beta2)) (unless beta1^2 >= beta2): exact sums are never less.
+ * c = (1 - beta1) / sqrt((1 - beta2) (1 - r)), r = beta1^2 / beta2: exact sums are never less.  Where r >= 1 - 2^-20, 1 - r
+ * there is (1 - r) / (1 - r^step), the same for the steps so far, and a v above zero that would go to zero goes to the
+ * smallest number of its block's format instead (the mean of such a v is not kept).
  * The bits of element i of tensor k of the list are the low half (m) and the high half (v) of
  *   f(lo(i) A + hi(i) B + f(f(lo(seed) + k A) + step B + hi(seed))),  A = 0x9E3779B9, B = 0x3C6EF373, modulo 2^32,
  * lo and hi the 32-bit halves, f: x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16.

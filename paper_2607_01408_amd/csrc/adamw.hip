@@ -15,7 +15,9 @@
 // and in however many launches it runs; m and v are computed without contraction for the same reason.  A v that was
 // rounded to zero beside an m that was not would make an endless step: v is at least (m / c)^2,
 // c = (1 - b1) / sqrt((1 - b2) (1 - b1^2 / b2)), which exact sums of the same gradients keep by themselves
-// (Cauchy and Schwarz).
+// (Cauchy and Schwarz).  From r = b1^2 / b2 = 1 - 2^-20 on that sum over all steps bounds nothing, and two things take its
+// place: the sum over the t steps so far, 1 + r + ... + r^(t-1) in place of 1 / (1 - r), which is no bound either once r^t
+// is large; and a v above zero is never rounded to zero but to the smallest number of its block's format.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -62,11 +64,12 @@ struct EntryWith<T, true> : T {
 constexpr int64_t kMostPiece = int64_t{1} << 30;  // elements of an entry
 struct AdamwNumbers {
     float b1, c1, b2, c2;  // c: 1 - b
-    float eps, least;      // least: 1 / c above, 0 where there is no bound
+    float eps, least;      // least: 1 / c above, 0 where c is infinite
     float decay, rate;     // 1 - lr wd, lr / (1 - b1^t)
     float root;            // (1 - b2^t)^(-1/2)
     int entries;
     bool around;  // the tensors are too large for the caches
+    bool short_bound;  // c is of the steps so far, and no v above zero is rounded to zero
     double wd, lr, log_b1, log_b2;
     int64_t step;
     uint64_t seed;
@@ -82,6 +85,14 @@ struct AdamwArgs {
     Entry entry[kMost];
 };
 static_assert(sizeof(AdamwArgs<false, false>) <= kArgumentBytes && sizeof(AdamwArgs<true, true>) <= kArgumentBytes);
+
+// 1 / c of the first t steps: c^2 = (1 - b1)^2 / (1 - b2) (r^t - 1) / (r - 1); 0 where that is infinite
+__host__ __device__ inline float least_of_steps(const AdamwNumbers& o, int64_t t) {
+    const double log_r = 2.0 * o.log_b1 - o.log_b2;
+    const double sum = log_r == 0.0 ? static_cast<double>(t) : expm1(static_cast<double>(t) * log_r) / expm1(log_r);
+    const double c1 = -expm1(o.log_b1), c2 = -expm1(o.log_b2);
+    return sum > 0.0 && sum < 1e300 ? static_cast<float>(sqrt(c2 / sum) / c1) : 0.f;
+}
 
 __host__ __device__ inline uint32_t mix(uint32_t x) {
     x ^= x >> 16;
@@ -107,7 +118,7 @@ __device__ __forceinline__ float share_of(uint32_t r) {
 // m, and v by its root, to their blocks: eight elements a lane, 16 lanes a block.
 template <bool ROOT>
 __device__ __forceinline__ void put_block(const float (&x)[8], const float (&size)[8], const uint32_t (&word)[8],
-                                          uint8_t* values, uint8_t* scale, bool leader) {
+                                          uint8_t* values, uint8_t* scale, bool leader, bool none_to_zero) {
 #pragma clang fp contract(off)
     const int e = block8_scale(block8_top(size));
     const float inv = block8_inverse(e);
@@ -120,7 +131,7 @@ __device__ __forceinline__ void put_block(const float (&x)[8], const float (&siz
         const float share = share_of(ROOT ? word[i] >> 16 : word[i] & 0xFFFFu);
         bool more;
         if constexpr (ROOT)
-            more = share * ((hi - lo) * (hi + lo)) < x[i] * inv * inv - lo * lo;
+            more = share * ((hi - lo) * (hi + lo)) < x[i] * inv * inv - lo * lo || (none_to_zero && lo == 0.f && x[i] > 0.f);
         else
             more = share * (hi - lo) < t - lo;
         float y = fminf(more ? hi : lo, 448.f);
@@ -172,7 +183,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8, COPY> a) {
         pass8(t.m + from, have, m);
         pass8(t.v + from, have, v);
     }
-    float decay = o.decay, rate = o.rate, root = o.root;
+    float decay = o.decay, rate = o.rate, root = o.root, bound = o.least;
     int64_t step = o.step;
     if (o.device_step != nullptr || o.device_lr != nullptr) {
         if (o.device_step != nullptr) step = *o.device_step > 1 ? *o.device_step : 1;
@@ -180,6 +191,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8, COPY> a) {
         decay = static_cast<float>(1.0 - lr * o.wd);
         rate = static_cast<float>(lr / -expm1(static_cast<double>(step) * o.log_b1));
         root = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(step) * o.log_b2)));
+        if (BITS8 && o.short_bound) bound = least_of_steps(o, step);
     }
     const float factor = o.grad_scale != nullptr ? *o.grad_scale : 1.f;
     float size[8], s[8];
@@ -191,7 +203,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8, COPY> a) {
             m[i] = o.b1 * m[i] + o.c1 * x;
             v[i] = o.b2 * v[i] + o.c2 * (x * x);
             if constexpr (BITS8) {
-                const float y = m[i] * o.least, least = y * y;
+                const float y = m[i] * bound, least = y * y;
                 v[i] = least > v[i] ? least : v[i];
                 if (i >= have) m[i] = v[i] = 0.f;  // zeros behind the tensor whatever lies there
             }
@@ -214,8 +226,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwArgs<BITS8, COPY> a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) word[i] = mix((static_cast<uint32_t>(e) + i) * 0x9E3779B9u + high);
         const bool leader = (threadIdx.x & 15) == 0;
-        put_block<false>(m, size, word, t.m + i0, t.ms + i0 / kBlock8, leader);
-        put_block<true>(v, s, word, t.v + i0, t.vs + i0 / kBlock8, leader);
+        put_block<false>(m, size, word, t.m + i0, t.ms + i0 / kBlock8, leader, false);
+        put_block<true>(v, s, word, t.v + i0, t.vs + i0 / kBlock8, leader, o.short_bound);
     } else {
         pass_store8(t.m + from, have, m, o.around);
         pass_store8(t.v + from, have, v, o.around);
@@ -281,7 +293,7 @@ hipError_t launch_adamw(const spingtp_adamw_tensor* tensors, int64_t count, cons
     o.c2 = static_cast<float>(1.0 - given.beta2);
     o.eps = static_cast<float>(given.eps);
     const double bound = given.beta2 > 0 ? 1.0 - given.beta1 * given.beta1 / given.beta2 : 0.0;
-    o.least = bound > 0 ? static_cast<float>(std::sqrt((1.0 - given.beta2) * bound) / (1.0 - given.beta1)) : 0.f;
+    o.short_bound = !(bound > 0x1p-20);
     o.wd = given.weight_decay;
     o.lr = given.lr;
     o.log_b1 = std::log(given.beta1);
@@ -292,6 +304,8 @@ hipError_t launch_adamw(const spingtp_adamw_tensor* tensors, int64_t count, cons
     o.device_lr = given.device_lr;
     o.grad_scale = given.grad_scale;
     const double t = static_cast<double>(given.step > 1 ? given.step : 1);
+    o.least = o.short_bound ? least_of_steps(o, given.step > 1 ? given.step : 1)
+                            : static_cast<float>(std::sqrt((1.0 - given.beta2) * bound) / (1.0 - given.beta1));
     o.decay = static_cast<float>(1.0 - given.lr * given.weight_decay);
     o.rate = static_cast<float>(given.lr / -std::expm1(t * o.log_b1));
     o.root = static_cast<float>(1.0 / std::sqrt(-std::expm1(t * o.log_b2)));
