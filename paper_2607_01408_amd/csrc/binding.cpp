@@ -20,6 +20,7 @@
 #include <utility>
 #include <vector>
 
+#include "overlap.h"
 #include "spingtp.h"
 
 namespace {
@@ -441,6 +442,13 @@ PyObject* gated_backward(Args a) {
     return tuple({wrap(dx), wrap(dw)});
 }
 
+Rows rows_of(const Matrix& m) { return Rows(m.p, m.rows, m.columns, m.ld, m.t->element_size()); }
+Rows rows_of(const at::Tensor& dense) { return Rows(dense.data_ptr(), 1, dense.numel(), dense.numel(), dense.element_size()); }
+template <typename T>
+void apart(const Matrix& out, const T& other, const char* name) {
+    if (overlap(rows_of(out), rows_of(other))) throw Refused(std::string("out overlaps ") + name);
+}
+
 // What follows a linear layer's product: bias [N] | None, residual [M, N] | None and y [M, N], new or given.
 struct LinearTail {
     const float* bias = nullptr;
@@ -455,6 +463,9 @@ struct LinearTail {
         if (residual != Py_None) r = matrix(residual, "residual", &like, M, N);
         if (out != Py_None) {
             y = matrix(out, "out", &like, M, N);
+            if (bias != nullptr) apart(y, tensor(bias_, "bias"), "bias");
+            // the residual itself may be written: each of its elements is read where its output is made, before it
+            if (residual != Py_None && (r.p != y.p || r.ld != y.ld)) apart(y, r, "residual");
         } else {
             made = empty({M, N}, type, beside);
             y.p = made.data_ptr();
@@ -475,6 +486,10 @@ PyObject* linear(Args a) {
     const auto act = integer(a[3]);
     const at::ScalarType type = truth(a[6]) ? at::kBFloat16 : at::kFloat;
     const LinearTail t(a[2], a[4], a[7], type, *x.t, M, N);
+    if (a[7] != Py_None) {
+        apart(t.y, x, "x");
+        apart(t.y, w, "w");
+    }
     at::Tensor z;
     if (truth(a[5]) && act != SPINGTP_IDENTITY) z = empty({M, N}, at::kBFloat16, *x.t);
     size_t bytes = 0;
@@ -495,6 +510,9 @@ PyObject* linear8(Args a) {
     if (N < 1 || K < 1) throw Refused("the weights are empty");
     const at::ScalarType type = truth(a[10]) ? at::kBFloat16 : at::kFloat;
     const LinearTail t(a[7], a[9], a[11], type, *x.t, M, N);
+    if (a[11] != Py_None) {
+        for (int i = 0; i < 4; ++i) apart(t.y, tensor(a[i], "a block"), i < 2 ? "x" : "w");
+    }
     size_t bytes = 0;
     done(lib.linear_forward8_workspace_size(M, K, N, &bytes), "spingtp_linear_forward8_workspace_size");
     const at::Tensor ws = workspace(bytes, *x.t);

@@ -267,7 +267,7 @@ def linear(x, w, bias=None, act=None, residual=None, save=None, dtype=torch.bflo
 
     x [M, K] and w [N, K] in bf16 (any alignment; rows that do not start and end on 16 bytes are copied) or, for
     inference, both Block8; bias [N] fp32; act None, ``"silu"`` or ``"gelu"``; residual and y of ``dtype``, bf16 or fp32;
-    ``out`` may be the residual itself.
+    ``out`` may be the residual itself, and overlaps no operand otherwise.
     ``save="same"`` (bf16) keeps what the backward pass needs; saved is None without it."""
     code, keep = _choice(_LINEAR_ACTS, act, "act"), _choice(_LINEAR_SAVES, save, "save")
     bf16 = _choice(_DTYPES, dtype, "dtype")
