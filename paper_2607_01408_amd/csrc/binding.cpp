@@ -211,6 +211,9 @@ PyObject* tuple(std::initializer_list<PyObject*> parts) {
 }
 PyObject* wrap(const NewBlock& b) { return tuple({wrap(b.values), wrap(b.scales)}); }
 
+// Autograd sees that a given output is written (before the launch: it refuses what may not be).
+void writes(const Matrix& out) { out.t->unsafeGetTensorImpl()->bump_version(); }
+
 void done(spingtp_status s, const char* where) {
     if (s != SPINGTP_OK) throw Failed{s, where};
 }
@@ -246,6 +249,7 @@ PyObject* unpack8(Args a) {
     like.type = type;
     if (a[5] != Py_None) {
         out = matrix(a[5], "out", &like, R, D);
+        writes(out);
     } else {
         made = empty({R, D}, type, *b.t);
         out.p = made.data_ptr();
@@ -319,6 +323,7 @@ PyObject* matmul8(Args a) {
     like.type = type;
     if (a[8] != Py_None) {
         out = matrix(a[8], "out", &like, M, N);
+        writes(out);
     } else {
         made = empty({M, N}, type, *x.t);
         out.p = made.data_ptr();
@@ -489,6 +494,7 @@ PyObject* linear(Args a) {
     if (a[7] != Py_None) {
         apart(t.y, x, "x");
         apart(t.y, w, "w");
+        writes(t.y);
     }
     at::Tensor z;
     if (truth(a[5]) && act != SPINGTP_IDENTITY) z = empty({M, N}, at::kBFloat16, *x.t);
@@ -512,6 +518,7 @@ PyObject* linear8(Args a) {
     const LinearTail t(a[7], a[9], a[11], type, *x.t, M, N);
     if (a[11] != Py_None) {
         for (int i = 0; i < 4; ++i) apart(t.y, tensor(a[i], "a block"), i < 2 ? "x" : "w");
+        writes(t.y);
     }
     size_t bytes = 0;
     done(lib.linear_forward8_workspace_size(M, K, N, &bytes), "spingtp_linear_forward8_workspace_size");

@@ -61,3 +61,18 @@ def test_outputs_beside_other_operands_are_written():
     r = rand((M, N), BF16, 5)
     want = sg.linear(x, w, residual=r)[0]
     assert sg.linear(x, w, residual=r, out=r)[0] is r and torch.equal(r, want)
+
+
+def test_a_given_output_is_seen_by_autograd():
+    x, w = rand((M, K), BF16, 1), rand((N, K), BF16, 2)
+    x8, w8 = sg.pack8(x), sg.pack8(w)
+    for call in (lambda out: sg.linear(x, w, residual=out, out=out), lambda out: sg.linear(x8, w8, out=out),
+                 lambda out: sg.matmul8(x8, w8, out=out), lambda out: sg.unpack8(x8, out=out)):
+        out = rand((M, N), BF16, 3)
+        factor = torch.ones((M, N), dtype=BF16, device="cuda", requires_grad=True)
+        kept = (out * factor).sum()
+        before = out._version
+        call(out)
+        assert out._version > before
+        with pytest.raises(RuntimeError, match="inplace"):
+            kept.backward()
