@@ -7,10 +7,12 @@
 // Backward: over the index in sorted order (sort_index.hip), cut into chunks of equal length whatever the rows' numbers
 // of entries: a group of lanes walks its chunk and keeps the running sum of a row in fp32.  A row whose entries lie in
 // one chunk leaves at once; a row that crosses chunks leaves a part in each, and a second kernel adds the parts in
-// order.  So one row with all entries costs no more than many with a few, every row of the result is written once, and
-// no step depends on the order of arrival.  The rows without entries are zeroed by workgroups of the same launch: a lane
+// order; where all parts of a workgroup belong to one row that began earlier, it leaves their sum too, so that a long row
+// has few of them.  So one row with all entries costs little more than many with a few (200,000 rows of 128 in fp32 onto
+// one row of 50,000 40 us, onto all of them 30), every row of the result is written once, and no step depends on the
+// order of arrival.  The rows without entries are zeroed by workgroups of the same launch: a lane
 // looks for its row by bisection.  16,384 entries over 50,000 rows of 2,048 in bf16: 45 us (68 MB in, 205 MB out, 6.0 TB/s)
-// and 9 for the rows that cross chunks; 100,000 over 4,000 of 128 in fp32: 13 and 6.
+// and 9 for the rows that cross chunks; 100,000 over 4,000 of 128 in fp32: 14 and 6.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -123,15 +125,17 @@ constexpr int kAhead = 4;  // rows in flight
 constexpr int kEmptyRows = 16;  // of the table, that a wave looks after
 
 // Workgroups 0 to sum_blocks - 1: chunks of `chunk` entries, one to a group, `across` workgroups to the columns.  partial
-// [chunks][2][D]: the part of a row that began in an earlier chunk, and of one that begins here and goes on.  The
-// others: rows of the table without entries.
+// [chunks][2][D]: the part of a row that began in an earlier chunk, and of one that begins here and goes on.  sums
+// [chunks / kGroups][D]: where all chunks of a workgroup start with one row from an earlier workgroup's, the sum of these
+// parts (a row with thousands of chunks is joined by them).  The other workgroups: rows of the table without entries.
 template <int LANES, typename TG, typename TO>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict__ grad, int64_t ldg,
                                                             const int32_t* __restrict__ order,
                                                             const int32_t* __restrict__ rows, float scale,
                                                             TO* __restrict__ out, int64_t ldo, float* __restrict__ partial,
-                                                            int64_t n, int64_t V, int64_t D, int64_t chunk, unsigned across,
-                                                            unsigned sum_blocks, bool around) {
+                                                            float* __restrict__ sums, int64_t n, int64_t V, int64_t D,
+                                                            int64_t chunk, unsigned across, unsigned sum_blocks,
+                                                            bool around) {
     constexpr int kGroups = 256 / LANES;
     constexpr bool kFours = sizeof(TG) == 4 && sizeof(TO) == 4;
     if (blockIdx.x >= sum_blocks) {
@@ -167,8 +171,10 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
     }
     const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
     const int64_t c = static_cast<int64_t>(blockIdx.x % across) * LANES * 8 + l * (kFours ? 4 : 8);
-    const int64_t k = static_cast<int64_t>(blockIdx.x / across) * kGroups + g, p0 = k * chunk;
-    if (c >= D || p0 >= n) return;
+    const int64_t window = blockIdx.x / across, k = window * kGroups + g, p0 = k * chunk;
+    const int64_t last = ((window + 1) * kGroups - 1) * chunk;  // of the last chunk, its first entry
+    const bool one_row = window > 0 && last < n && rows[window * kGroups * chunk - 1] == rows[last];
+    if (!one_row && (c >= D || p0 >= n)) return;  // (lanes past the columns load and store nothing)
     const int64_t p1 = p0 + chunk < n ? p0 + chunk : n;
     float sum[8];
     const uint32_t most = static_cast<uint32_t>(n - 1);
@@ -214,51 +220,35 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const TG* __restrict
         }
     }
     leave(after);
-}
-
-constexpr int kWindow = 32;  // chunks
-
-// Sums of the parts of kWindow chunks (sums [windows][D]) that all start with one row from an earlier chunk: of a row with
-// thousands of chunks a single workgroup would add the parts at the rate of its CU (187,008 entries over 9 rows, the
-// largest with 60 % of them: 53 us).
-template <int LANES>
-__global__ __launch_bounds__(256) void embedding_window_kernel(const float* __restrict__ partial,
-                                                               const int32_t* __restrict__ rows, float* __restrict__ sums,
-                                                               int64_t D, int64_t chunk, int64_t windows, unsigned across) {
-    constexpr int kGroups = 256 / LANES;
-    const int l = threadIdx.x % LANES, g = threadIdx.x / LANES;
-    const int64_t c = (static_cast<int64_t>(blockIdx.x % across) * LANES + l) * 8;
-    const int64_t w = static_cast<int64_t>(blockIdx.x / across) * kGroups + g, first = w * kWindow;
-    if (c >= D || w >= windows || first == 0) return;
-    if (rows[first * chunk - 1] != rows[(first + kWindow - 1) * chunk]) return;
-    const int have = D - c >= 8 ? 8 : static_cast<int>(D - c);
-    float sum[8];
+    if (!one_row) return;
+    __syncthreads();
+    if (g != 0 || static_cast<uint32_t>(rows[last]) >= V) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-#pragma unroll 8
-    for (int j = 0; j < kWindow; ++j) {
+#pragma unroll 4
+    for (int q = 0; q < kGroups; ++q) {
         float v[8];
-        load8(partial + 2 * (first + j) * D + c, have, v);
+        load_columns<LANES, kFours>(partial + 2 * (k + q) * D, c, D, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += v[i];
     }
-    store8(sums + w * D + c, have, sum);
+    store_columns<LANES, kFours>(sums + window * D, c, D, sum, false);
 }
 
 constexpr int kJoinThreads = 512;
 constexpr int kShort = 8;  // chunks beyond the first that a group adds up by itself
 
 // A group to a chunk; those in which a row begins that goes on add its parts: chunk after chunk as long as one starts
-// with the row.  A row of more than kShort chunks is added by the whole workgroup, a group every so many chunks (or
-// windows of them: `sums`, may be null), and the groups' sums in order.
-template <int LANES, typename TO>
+// with the row.  A row of more than kShort chunks is added by the whole workgroup, a group every so many chunks (or, where
+// there are more than kLong, sums of kWindow of them), and the groups' sums in order.
+template <int LANES, int kWindow, typename TO>
 __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const float* __restrict__ partial,
                                                                       const float* __restrict__ sums,
                                                                       const int32_t* __restrict__ rows, float scale,
                                                                       TO* __restrict__ out, int64_t ldo, int64_t n,
                                                                       int64_t V, int64_t D, int64_t chunk, int64_t chunks,
                                                                       unsigned across) {
-    constexpr int kGroups = kJoinThreads / LANES;
+    constexpr int kGroups = kJoinThreads / LANES, kLong = (1 << 18) / (32 * LANES);  // 256 KB of parts
     __shared__ float part[kGroups][LANES * 8 + 4];
     __shared__ int32_t long_row[kGroups];  // -1: none begins in the group's chunk
     __shared__ int first_open;             // the first window that the row does not fill
@@ -319,23 +309,26 @@ __global__ __launch_bounds__(kJoinThreads) void embedding_join_kernel(const floa
 #pragma unroll
         for (int i = 0; i < 8; ++i) mine[i] = 0.f;
         const int64_t after = first + at + 1;
-        if (sums == nullptr) {
+        if (after + kLong >= chunks || rows[(after + kLong) * chunk] != which) {
             add(mine, which, after + g, kGroups, chunks);
         } else {
-            const int64_t from = (after + kWindow - 1) / kWindow;
-            if (threadIdx.x == 0) first_open = 0x7fffffff;
+            const int64_t from = (after + kWindow - 1) / kWindow, end = chunks / kWindow;
+            if (threadIdx.x == 0) first_open = static_cast<int>(end);
             __syncthreads();
+            for (int64_t w = from + threadIdx.x; w < end; w += kJoinThreads)
+                if (rows[(w * kWindow + kWindow - 1) * chunk] != which) {
+                    atomicMin(&first_open, static_cast<int>(w));
+                    break;
+                }
             add(mine, which, after + g, kGroups, from * kWindow < chunks ? from * kWindow : chunks);
-            int64_t w = from + g;
-#pragma unroll 4
-            for (; w < chunks / kWindow && rows[(w * kWindow + kWindow - 1) * chunk] == which; w += kGroups) {
+            __syncthreads();
+#pragma unroll 8
+            for (int64_t w = from + g; w < first_open; w += kGroups) {
                 float v[8];
                 load8(sums + w * D + (have > 0 ? c : 0), have, v);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) mine[i] += v[i];
             }
-            if (l == 0) atomicMin(&first_open, static_cast<int>(w));
-            __syncthreads();
             add(mine, which, static_cast<int64_t>(first_open) * kWindow + g, kGroups, chunks);
         }
 #pragma unroll
@@ -366,12 +359,6 @@ int64_t chunk_of(int64_t n, int64_t D) {
     return c < 16 ? 16 : c;
 }
 int64_t chunks_of(int64_t n, int64_t D) { return (n + chunk_of(n, D) - 1) / chunk_of(n, D); }
-// Windows where a row may well have many of them: 1,000 chunks or more, eight to a row in the mean.
-int64_t windows_of(int64_t n, int64_t V, int64_t D) {
-    const int64_t chunks = chunks_of(n, D);
-    return chunks >= 1000 && V <= chunks / 8 ? chunks / kWindow : 0;
-}
-
 template <int LANES, typename T>
 hipError_t lookup(const void* table, int64_t ldt, const void* index, bool wide, float scale, void* out, int64_t ldo,
                   int64_t n, int64_t V, int64_t D, hipStream_t stream) {
@@ -396,28 +383,21 @@ template <int LANES, typename TG, typename TO>
 hipError_t gradient(const EmbeddingBwdArgs& a, hipStream_t stream) {
     const int64_t across = across_of(a.D, LANES), chunks = chunks_of(a.n, a.D), chunk = chunk_of(a.n, a.D);
     const int64_t sums = (chunks + 256 / LANES - 1) / (256 / LANES) * across, looked = 4 * kEmptyRows;
+    float* const window_sums = a.partial + 2 * chunks * a.D;
     int64_t empty = (a.V + looked - 1) / looked;
     if (empty > kMostBlocks) empty = kMostBlocks;
     hipLaunchKernelGGL((embedding_sum_kernel<LANES, TG, TO>), dim3(static_cast<unsigned>(sums + empty)), dim3(256), 0,
                        stream, static_cast<const TG*>(a.grad), a.ldg, a.order, a.rows, a.scale, static_cast<TO*>(a.out),
-                       a.ldo, a.partial, a.n, a.V, a.D, chunk, static_cast<unsigned>(across), static_cast<unsigned>(sums),
-                       large(a.V * a.D));
-    hipError_t e = hipGetLastError();
+                       a.ldo, a.partial, window_sums, a.n, a.V, a.D, chunk, static_cast<unsigned>(across),
+                       static_cast<unsigned>(sums), large(a.V * a.D));
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || chunks <= 1) return e;
-    const int64_t windows = windows_of(a.n, a.V, a.D);
-    float* const window_sums = windows > 0 ? a.partial + 2 * chunks * a.D : nullptr;
-    if (windows > 0) {
-        constexpr int kAtOnce = 256 / LANES;
-        hipLaunchKernelGGL((embedding_window_kernel<LANES>),
-                           dim3(static_cast<unsigned>((windows + kAtOnce - 1) / kAtOnce * across)), dim3(256), 0, stream,
-                           a.partial, a.rows, window_sums, a.D, chunk, windows, static_cast<unsigned>(across));
-        e = hipGetLastError();
-        if (e != hipSuccess) return e;
-    }
-    constexpr int kGroups = kJoinThreads / LANES;
-    hipLaunchKernelGGL((embedding_join_kernel<LANES, TO>), dim3(static_cast<unsigned>((chunks + kGroups - 1) / kGroups * across)),
-                       dim3(kJoinThreads), 0, stream, a.partial, window_sums, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo, a.n, a.V,
-                       a.D, chunk, chunks, static_cast<unsigned>(across));
+    constexpr int kJoinLanes = LANES < 32 ? LANES : 32, kGroups = kJoinThreads / kJoinLanes;
+    const int64_t join_across = across_of(a.D, kJoinLanes);
+    hipLaunchKernelGGL((embedding_join_kernel<kJoinLanes, 256 / LANES, TO>),
+                       dim3(static_cast<unsigned>((chunks + kGroups - 1) / kGroups * join_across)), dim3(kJoinThreads), 0, stream,
+                       a.partial, window_sums, a.rows, a.scale, static_cast<TO*>(a.out), a.ldo, a.n, a.V, a.D, chunk, chunks,
+                       static_cast<unsigned>(join_across));
     return hipGetLastError();
 }
 
@@ -452,7 +432,7 @@ hipError_t launch_embedding(int dtype, const void* table, int64_t ldt, const voi
 
 size_t embedding_backward_workspace(int64_t n, int64_t D) {
     const int64_t chunks = chunks_of(n, D);
-    return static_cast<size_t>((2 * chunks + chunks / kWindow) * D) * sizeof(float);
+    return static_cast<size_t>((2 * chunks + chunks / (256 / lanes_of(D))) * D) * sizeof(float);
 }
 
 hipError_t launch_embedding_backward(const EmbeddingBwdArgs& a, hipStream_t stream) {
