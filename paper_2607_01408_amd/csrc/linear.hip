@@ -459,6 +459,13 @@ typedef uint32_t v4w __attribute__((ext_vector_type(4)));
 constexpr uint32_t kNowhere = 0x80000000u;  // past every buffer: loads give zeros, stores go nowhere
 constexpr int kPast = 2;                    // non-temporal, of a buffer's loads and stores
 
+// 16 bytes to `offset` of a buffer.  The offset goes by the lane's register alone: behind a store of more than 8 bytes the
+// first of its data registers may not be written by the next instruction, and the compiler leaves room for that only where
+// the store has no scalar offset (seen: lanes with zeros for their first two elements).
+__device__ __forceinline__ void store16(v4w v, const uint16_t* base, uint32_t offset) {
+    __builtin_amdgcn_raw_buffer_store_b128(v, buffer_of(reinterpret_cast<const uint8_t*>(base), 0x7fffffffu), offset, 0, 0);
+}
+
 // Lanes with the bit clear get the pair's sum of a, the others that of b.
 __device__ __forceinline__ float halve32(float a, float b) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
@@ -569,9 +576,7 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
                 *reinterpret_cast<v4w*>(here_dz + row * 128 + ((c ^ ((row >> 1) & 7)) << 4)) = q;
                 *reinterpret_cast<v4w*>(here_w + k * 256 + ((wc ^ Tile::turn(16, k)) << 4)) = at_wr[i];
                 if (dz != nullptr)
-                    __builtin_amdgcn_raw_buffer_store_b128(
-                        q, buffer_of(reinterpret_cast<const uint8_t*>(dz + (m0 + 64 * i) * pitch), 0x7fffffffu),
-                        row < count ? r * dz_row + 16 * c : kNowhere, 128 * s, 0);
+                    store16(q, dz + (m0 + 64 * i) * pitch + 64 * s, row < count ? r * dz_row + 16 * c : kNowhere);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] = i == 0 ? v[e] : sum[e] + v[e];
                 fetch(last ? m0 + kNarrowRows : m0, last ? 0 : s + 1, i);  // into the registers that are free again
