@@ -42,6 +42,10 @@ __device__ __forceinline__ float normal(float g, float& bell) {
     p = fmaf(p, t, 0.119821183f);
     p = fmaf(p, t, 0.139863536f);
     p = fmaf(p, t, 0.139621302f);
+    if constexpr (BELOW) {  // nothing left to contract: the same bits in every kernel
+        const float part = p * t;
+        return g > 0.f ? fmaf(-part, bell, 1.f) : part * bell;
+    }
     const float below = p * t * bell;
     return g > 0.f ? 1.f - below : below;
 }

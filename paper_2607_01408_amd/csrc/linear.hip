@@ -448,9 +448,9 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __re
 // Memory's rate where every workgroup's rows fill their tiles (dx alone of 65,536 x 512 by 128: 151 MB in 29 us, 5.2 TB/s),
 // else a step's arithmetic, which rows that do not exist take part in; 100,000 rows with dz stored 66 us, 5.0 TB/s.  Both
 // ways, dz by itself and this one, silu, all gradients (dx alone), us:
-//   100,000 x 512 by 128 118 / 100 (81 / 48), 100,000 x 128 by 32 48 / 40, 100,000 x 2,048 by 128 470 / 392, 50,000 x 512 by
-//   128 70 / 59 (44 / 25), 50,000 x 256 by 64 40 / 38; 32,768 rows 51 / 51, 31 / 34, 16,384 rows 34 / 46: steps follow one
-//   another, some 3 us each.  Hence from 40,000 rows on.
+//   100,000 x 512 by 128 118 / 100 (81 / 51), 100,000 x 128 by 32 48 / 36, 100,000 x 2,048 by 128 470 / 395, 50,000 x 512 by
+//   128 70 / 59 (44 / 26), 50,000 x 256 by 64 40 / 35; 32,768 rows 51 / 51, 31 / 34, 16,384 rows 34 / 46: steps follow one
+//   another, some 3 us each.  Hence from 40,000 rows on.  (Without dx: linear_narrow_dz_kernel.)
 constexpr int kNarrowRows = 128, kNarrowInputs = 128, kNarrowOutputs = 2048, kNarrowBlocks = 512;
 constexpr int64_t kNarrowLeast = 40'000;
 constexpr int kNarrowDz = kNarrowRows * kStepBytes, kNarrowW = 64 * 2 * kNarrowInputs, kNarrowPart = 8 * 64 * 4;
@@ -480,6 +480,54 @@ __device__ __forceinline__ float halve8(float a, float b, bool high) {
     return keep + __shfl_xor(send, 8);
 }
 
+// Eight elements of dz from what was loaded of dy and z.
+__device__ __forceinline__ void widen(const v4w& x, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(x[i] << 16);
+        v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+    }
+}
+template <int ACT, int WIDTH>
+__device__ __forceinline__ void dz_of(const v4w (&dy)[WIDTH], const v4w& z, float (&v)[8]) {
+    if constexpr (WIDTH == 1) {
+        widen(dy[0], v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(dy[e / 4][e % 4]);
+    }
+    if constexpr (ACT != kIdentity) {
+        float p[8];
+        widen(z, p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= slope<ACT>(p[e]);
+    }
+}
+// (no product is contracted into the sum: both kernels below round alike)
+__device__ __forceinline__ void add_rows(float (&sum)[8], const float (&v)[8], bool first) {
+#pragma clang fp contract(off)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = first ? v[e] : sum[e] + v[e];
+}
+// A thread's sums of eight columns to `part` [64] as sums over the wave's rows (lane bits 5, 4, 3); lane bits 2 to 0 are the
+// chunk of columns.
+__device__ __forceinline__ void leave_column_sums(const float (&sum)[8], float* part, int lane) {
+    float four[4], two[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) four[e] = halve32(sum[e], sum[4 + e]);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) two[e] = halve16(four[e], four[2 + e]);
+    part[8 * (lane & 7) + 4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1)] =
+        halve8(two[0], two[1], (lane & 8) != 0);
+}
+// the waves' sums of a column, added in order
+__device__ __forceinline__ float add_waves(const float* part, int pitch) {
+    float total = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) total += part[k * pitch];
+    return total;
+}
+
 // Waits until the wave's LDS writes and reads are done, then for all waves; loads and stores of memory go on.
 __device__ __forceinline__ void written_and_read() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
@@ -507,7 +555,6 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
     v4w at_dy[2][kWidth], at_z[2], at_wr[2];
     const uint32_t dy_row = static_cast<uint32_t>(lddy * sizeof(TD)), z_row = static_cast<uint32_t>(2 * N),
                    w_row = static_cast<uint32_t>(2 * ldw), dz_row = static_cast<uint32_t>(2 * pitch);
-    const uint32_t w_bytes = dx != nullptr ? 0x7fffffffu : 0;  // without dx there may be no w: no byte of it is read
     const int columns = static_cast<int>(N), inputs = static_cast<int>(K);
     // half i of step s of the rows from m0 on
     const auto fetch = [&](int64_t m0, int s, int i) {
@@ -516,7 +563,7 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
         const int64_t from = count > 0 ? m0 + 64 * i : 0;
         const Buffer bd = buffer_of(reinterpret_cast<const uint8_t*>(dy + from * lddy), 0x7fffffffu);
         const Buffer bz = buffer_of(reinterpret_cast<const uint8_t*>(z + from * N), 0x7fffffffu);
-        const Buffer bw = buffer_of(reinterpret_cast<const uint8_t*>(w + (64 * s + 32 * i) * ldw), w_bytes);
+        const Buffer bw = buffer_of(reinterpret_cast<const uint8_t*>(w + (64 * s + 32 * i) * ldw), 0x7fffffffu);
         const bool in = r < count - 64 * i && 8 * c < columns - 64 * s;
         const uint32_t od = in ? r * dy_row + 8 * sizeof(TD) * c : kNowhere, oz = in ? r * z_row + 16 * c : kNowhere;
         const uint32_t ow = wr < columns - 64 * s - 32 * i && 8 * wc < inputs ? wr * w_row + 16 * wc : kNowhere;
@@ -526,14 +573,6 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
         if constexpr (ACT != kIdentity) at_z[i] = __builtin_amdgcn_raw_buffer_load_b128(bz, oz, 128 * s, kPast);
         at_wr[i] = __builtin_amdgcn_raw_buffer_load_b128(bw, ow, 0, 0);
     };
-    const auto widen = [](const v4w& x, float (&v)[8]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(x[i] << 16);
-            v[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
-        }
-    };
-
     // places of the wave's fragments, as in GemmTile
     const int in = lane & 15, key = (in >> 1) & 7;
     const int wrow = 8 * (lane >> 4) + (in >> 2), wchunk = 8 * wn + ((lane & 3) >> 1);
@@ -558,49 +597,21 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
             for (int i = 0; i < 2; ++i) {
                 const int row = r + 64 * i, k = wr + 32 * i;
                 float v[8];
-                if constexpr (kWidth == 1) {
-                    widen(at_dy[i][0], v);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(at_dy[i][e / 4][e % 4]);
-                }
-                if constexpr (ACT != kIdentity) {
-                    float p[8];
-                    widen(at_z[i], p);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        v[e] *= slope<ACT>(p[e]);
-                    }
-                }
+                dz_of<ACT>(at_dy[i], at_z[i], v);
                 const v4w q{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
                 *reinterpret_cast<v4w*>(here_dz + row * 128 + ((c ^ ((row >> 1) & 7)) << 4)) = q;
                 *reinterpret_cast<v4w*>(here_w + k * 256 + ((wc ^ Tile::turn(16, k)) << 4)) = at_wr[i];
                 if (dz != nullptr)
                     store16(q, dz + (m0 + 64 * i) * pitch + 64 * s, row < count ? r * dz_row + 16 * c : kNowhere);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = i == 0 ? v[e] : sum[e] + v[e];
+                add_rows(sum, v, i == 0);
                 fetch(last ? m0 + kNarrowRows : m0, last ? 0 : s + 1, i);  // into the registers that are free again
                 __builtin_amdgcn_sched_barrier(0);
             }
-            if (sums != nullptr) {
-                float four[4], two[2];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) four[e] = halve32(sum[e], sum[4 + e]);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) two[e] = halve16(four[e], four[2 + e]);
-                here_part[wave * 64 + 8 * c + 4 * (lane >> 5) + 2 * ((lane >> 4) & 1) + ((lane >> 3) & 1)] =
-                    halve8(two[0], two[1], (lane & 8) != 0);
-            }
+            if (sums != nullptr) leave_column_sums(sum, here_part + wave * 64, lane);
             written_and_read();
-            if (sums != nullptr && wave == (s & 7)) {
-                float total = 0.f;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) total += here_part[k * 64 + lane];
-                column_sums[64 * s + lane] += total;
-            }
+            if (sums != nullptr && wave == (s & 7)) column_sums[64 * s + lane] += add_waves(here_part + lane, 64);
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                if (dx == nullptr) break;
                 v4i fx[2], fw[4];
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
@@ -617,7 +628,6 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
             }
             turn ^= 1;
         }
-        if (dx == nullptr) continue;
         // dx by LDS, in dz's places, so that it leaves in whole lines: 16 chunks a row, turned by the row
         written_and_read();
 #pragma unroll
@@ -651,6 +661,99 @@ __global__ __launch_bounds__(512, 4) void linear_narrow_kernel(const TD* __restr
     if (sums != nullptr)
         for (int s = wave; s < steps; s += 8)
             if (64 * s + lane < N) sums[static_cast<int64_t>(blockIdx.x) * N + 64 * s + lane] = column_sums[64 * s + lane];
+}
+
+// dz and its columns' sums without dx, with the bits that the kernel above gives them: the same rows to a workgroup and to a
+// wave, the same sums in the same order.  LANES lanes of eight columns to a row (1 KB of 512 columns), so that most of
+// the halving is a lane's own: rows 4, 2 and 1 apart, as lane bits 5, 4 and 3 are there.  Columns of a workgroup: 8 LANES;
+// the waves meet once in 128 rows.  Memory's rate: db alone of 200,000 x 2,048 270 us (6.1 TB/s).
+//
+// dw and db, silu, us: the kernel above without its product / linear_dz_kernel, whose sums go in another order / this one
+//   100,000 x 2,048 by 128 372 / 349 / 340, 200,000 788 / 699 / 680, 50,000 168 / 158 / 147; 100,000 x 512 by 128 88 / 92 / 89,
+//   65,536 61 / 67 / 64, 200,000 182 / 178 / 178; 100,000 x 128 by 32 32 / 39 / 32.
+template <int LANES, typename TD, int ACT>
+__global__ __launch_bounds__(512, 4) void linear_narrow_dz_kernel(const TD* __restrict__ dy, int64_t lddy,
+                                                               const uint16_t* __restrict__ z, uint16_t* __restrict__ dz,
+                                                               int64_t pitch, float* __restrict__ sums, int64_t M, int64_t N,
+                                                               int64_t rows, unsigned across, unsigned blocks, bool columns_first) {
+    constexpr int kWidth = sizeof(TD) / 2, kColumns = 8 * LANES;
+    constexpr int kGroups = 64 / LANES, kOwn = 8 / kGroups;  // rows of a wave at a time; of a lane, of the wave's eight
+    __shared__ float parts[2][8][kColumns];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned bn = columns_first ? blockIdx.x % across : blockIdx.x / blocks;
+    const unsigned bm = columns_first ? blockIdx.x / across : blockIdx.x % blocks;
+    const int64_t m1 = static_cast<int64_t>(bm) * rows, m2 = m1 + rows < M ? m1 + rows : M;
+    const int64_t n = static_cast<int64_t>(bn) * kColumns + 8 * (lane % LANES);
+    const uint32_t dy_row = static_cast<uint32_t>(lddy * sizeof(TD)), z_row = static_cast<uint32_t>(2 * N),
+                   dz_row = static_cast<uint32_t>(2 * pitch);
+    // of the lane: its row among those of a time, and its places (past the buffers where it has no column)
+    const int lane_row = lane / LANES;
+    const uint32_t at_od = n < N ? lane_row * dy_row + static_cast<uint32_t>(sizeof(TD) * n) : kNowhere,
+                   at_oz = n < N ? lane_row * z_row + static_cast<uint32_t>(2 * n) : kNowhere,
+                   at_out = n < pitch ? lane_row * dz_row + static_cast<uint32_t>(2 * n) : kNowhere;
+    // row e of time t: rows 64 apart; the times 4, 2 and 1 apart
+    const auto row_of = [&](int t, int e) {
+        const int first = kOwn == 8 ? (t & 1) * 4 + (t & 2) + (t >> 2) : (kOwn == 4 ? (t & 1) * 4 + (t & 2) : 4 * t);
+        return 8 * wave + first + 64 * e;
+    };
+    v4w at_dy[2][kWidth], at_z[2];
+    const auto fetch = [&](int64_t m0, int t, int e) {
+        const int64_t have = m2 - m0, from = have > 0 ? m0 : 0;
+        const int row = row_of(t, e);
+        const Buffer bd = buffer_of(reinterpret_cast<const uint8_t*>(dy + from * lddy), 0x7fffffffu);
+        const Buffer bz = buffer_of(reinterpret_cast<const uint8_t*>(z + from * N), 0x7fffffffu);
+        const bool in = row + lane_row < have;
+        const uint32_t od = in ? at_od : kNowhere, oz = in ? at_oz : kNowhere;
+#pragma unroll
+        for (int h = 0; h < kWidth; ++h)
+            at_dy[e][h] = __builtin_amdgcn_raw_buffer_load_b128(bd, od, row * dy_row + 16 * h, kPast);
+        if constexpr (ACT != kIdentity) at_z[e] = __builtin_amdgcn_raw_buffer_load_b128(bz, oz, row * z_row, kPast);
+    };
+#pragma unroll
+    for (int e = 0; e < 2; ++e) fetch(m1, 0, e);
+    float total = 0.f;  // of the thread's column
+    int turn = 0;
+    for (int64_t m0 = m1; m0 < m2; m0 += kNarrowRows) {
+        float sum[8], half[8], pair[8], one[8];
+        // (not unrolled: the additions would move behind all loads, whose registers do not suffice)
+#pragma unroll 1
+        for (int t = 0; t < kOwn; ++t) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float v[8];
+                dz_of<ACT>(at_dy[e], at_z[e], v);
+                const bool last = t + 1 == kOwn;
+                fetch(last ? m0 + kNarrowRows : m0, last ? 0 : t + 1, e);  // into the registers that are free again
+                const int row = row_of(t, e);
+                if (dz != nullptr)
+                    store16(v4w{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])},
+                            dz + (m0 + row) * pitch, row + lane_row < m2 - m0 ? at_out : kNowhere);
+                add_rows(one, v, e == 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            add_rows(pair, one, (t & 1) == 0);
+            if (kOwn == 1 || (t & 1) == 1) add_rows(half, pair, (t & 2) == 0);
+            if (kOwn < 4 || (t & 3) == 3) add_rows(sum, half, (t & 4) == 0);
+        }
+#pragma unroll
+        for (int d = 32; d >= LANES; d >>= 1) {
+            if (d > 4 * LANES) continue;
+            float other[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[i] = __shfl_xor(sum[i], d);
+            add_rows(sum, other, false);
+        }
+        if (lane < LANES) {
+            float4* const to = reinterpret_cast<float4*>(&parts[turn][wave][8 * lane]);
+            to[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
+            to[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+        }
+        written_and_read();
+        if (tid < kColumns) total += add_waves(&parts[turn][0][tid], kColumns);
+        turn ^= 1;
+    }
+    const int64_t at = static_cast<int64_t>(bn) * kColumns + tid;
+    if (sums != nullptr && tid < kColumns && at < N) sums[static_cast<int64_t>(bm) * N + at] = total;
 }
 
 template <typename T>
@@ -952,9 +1055,38 @@ hipError_t make_narrow(const LinearBwdArgs& a, const uint16_t* w, int64_t ldw, u
         default: return launch_narrow<TD, kIdentity, WHOLE>(a, w, ldw, dz, sums, stream);
     }
 }
+template <int LANES, typename TD, int ACT>
+hipError_t launch_narrow_dz(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+    const int64_t pitch = up(a.N, 64);
+    const unsigned across = static_cast<unsigned>((pitch + 8 * LANES - 1) / (8 * LANES));
+    const unsigned blocks = static_cast<unsigned>(narrow_blocks(a.M));
+    hipLaunchKernelGGL((linear_narrow_dz_kernel<LANES, TD, ACT>), dim3(across * blocks), dim3(512), 0, stream,
+                       static_cast<const TD*>(a.dy), a.lddy, static_cast<const uint16_t*>(a.z), dz, pitch, sums, a.M, a.N,
+                       narrow_rows(a.M), across, blocks, across > 2);  // long rows: all of their columns at once (2,048
+                                                                       // columns of 65,536 rows 221 us, else 239)
+    return hipGetLastError();
+}
+template <typename TD, int ACT>
+hipError_t launch_narrow_dz(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+    if (a.N > 512) return launch_narrow_dz<64, TD, ACT>(a, dz, sums, stream);
+    if (a.N > 256) return launch_narrow_dz<32, TD, ACT>(a, dz, sums, stream);
+    if (a.N > 128) return launch_narrow_dz<16, TD, ACT>(a, dz, sums, stream);
+    return launch_narrow_dz<8, TD, ACT>(a, dz, sums, stream);
+}
+template <typename TD>
+hipError_t make_narrow_dz(const LinearBwdArgs& a, uint16_t* dz, float* sums, hipStream_t stream) {
+    switch (a.act) {
+        case kSilu: return launch_narrow_dz<TD, kSilu>(a, dz, sums, stream);
+        case kGelu: return launch_narrow_dz<TD, kGelu>(a, dz, sums, stream);
+        default: return launch_narrow_dz<TD, kIdentity>(a, dz, sums, stream);
+    }
+}
 hipError_t make_narrow(const LinearBwdArgs& a, const uint16_t* w, int64_t ldw, uint16_t* dz, float* sums,
                        hipStream_t stream) {
-    const bool whole = rows_fit(a.dx, a.K, a.lddx) || a.dx == nullptr;
+    if (a.dx == nullptr)
+        return a.dtype == SPINGTP_FP32 ? make_narrow_dz<float>(a, dz, sums, stream)
+                                       : make_narrow_dz<uint16_t>(a, dz, sums, stream);
+    const bool whole = rows_fit(a.dx, a.K, a.lddx);
     if (a.dtype == SPINGTP_FP32)
         return whole ? make_narrow<float, true>(a, w, ldw, dz, sums, stream)
                      : make_narrow<float, false>(a, w, ldw, dz, sums, stream);
