@@ -35,8 +35,7 @@ constexpr int kAdamwChunk = 2048;
 constexpr int kArgumentBytes = 4096;
 
 // A tensor, or a piece of one: what every kind has, its states in fp32 or 8 bits, the bf16 copy where the list has any.
-// The shorter an entry, the more tensors to a launch: 97 in fp32 without copies, where entries with room for them
-// held 76.
+// The shorter an entry, the more tensors to a launch: 99 in fp32 without copies, 82 where there is room for them.
 struct EntryBase {
     uint32_t block;  // first workgroup
     uint32_t n;      // elements
@@ -85,6 +84,8 @@ struct AdamwArgs {
     Entry entry[kMost];
 };
 static_assert(sizeof(AdamwArgs<false, false>) <= kArgumentBytes && sizeof(AdamwArgs<true, true>) <= kArgumentBytes);
+static_assert(AdamwArgs<false, false>::kMost == 99 && AdamwArgs<false, true>::kMost == 82);
+static_assert(AdamwArgs<true, false>::kMost == 62 && AdamwArgs<true, true>::kMost == 55);
 
 // 1 / c of the first t steps: c^2 = (1 - b1)^2 / (1 - b2) (r^t - 1) / (r - 1); 0 where that is infinite
 __host__ __device__ inline float least_of_steps(const AdamwNumbers& o, int64_t t) {
