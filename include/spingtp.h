@@ -808,7 +808,8 @@ spingtp_status spingtp_linear_forward8_workspace_size(int64_t M, int64_t K, int6
  * bf16 operands:
  *   dz = grad_y act'(z) (rounded to bf16, an operand of the matrix units),
  *   grad_x [M][K] = dz w (bf16),  grad_w [N][K] = dz^T x (w_dtype, dense),
- *   grad_bias [N] = sum over the rows of dz before its rounding (fp32; the same order in every call).
+ *   grad_bias [N] = sum over the rows of dz before its rounding (fp32; in the same order in every call of these sizes,
+ *   types and alignments, whichever gradients are wanted).
  * The residual's gradient is grad_y.  grad_x, grad_w and grad_bias may be NULL; w is read for grad_x alone, x for
  * grad_w alone.  workspace (16-byte aligned): the size below, for the same arguments.
  */

@@ -12,14 +12,17 @@
 // CUs idle: then the sum is cut into slices, a workgroup to each, whose fp32 sums a second kernel adds in order and
 // finishes.
 //
-// Measured (us; a large copy reaches 5.1 TB/s here, the library's bf16 product of 8,192^3 1,631 TFLOP/s, its products of
-// 8,192 x 2,048 x 8,192 and 8,192 x 8,192 x 2,048, no epilogue, 192 and 195):
-//   8,192 x 2,048 x 8,192 onto a residual 222 (1.24 PFLOP/s, matrix units busy 57 % at 2.0 GHz); 8,192 x 8,192 x 2,048 with
-//   bias, gelu, z kept 293, some 60 of it the epilogue, behind which no other workgroup of the CU multiplies; its gradients'
-//   products 231 and 209;
-//   100,000 x 512 x 128, silu, z kept 49 (205 MB written, 4.7 TB/s), dz and dx 66 (332 MB, 5.0 TB/s; in two launches dz 55,
-//   5.6 TB/s, and dx 27), dw 26 in 63 slices, 8 to join them and to add db up;
-//   one row by 8,192 x 4,096 weights 12.5 (5.4 TB/s); 24 x 2,048 x 8,192 in 8 bits 9 in slices, 3 to join them.
+// Measured (us, on one card, where a large copy reaches 5.2 TB/s, the library's bf16 product of 8,192^3 1,631 TFLOP/s, its
+// products of 8,192 x 2,048 x 8,192 and 8,192 x 8,192 x 2,048 177 and 189, of the latter's gradients 205 and 240):
+//   8,192 x 2,048 x 8,192 207, onto a residual 220 (1.25 PFLOP/s, matrix units busy 57 % at 2.0 GHz); 8,192 x 8,192 x 2,048
+//   207, with bias and gelu 243, z kept too 253 and among a training step's other launches 298, behind whose epilogue no
+//   other workgroup of the CU multiplies; its gradients' products 227 and 211;
+//   100,000 x 512 x 128, silu, z kept 49 (205 MB written, 4.7 TB/s), dz and dx 66 (340 MB, 5.1 TB/s; in two launches dz 55,
+//   5.6 TB/s, and dx 27), dw 27 in 63 slices, 8 to join them and to add db up;
+//   one row by 8,192 x 4,096 weights 12.5 (5.4 TB/s); 24 x 2,048 x 8,192 in 8 bits 9 in slices, 3 to join them; 8 bits,
+//   8,192 x 2,048 x 8,192 189, onto a residual 193, 8,192 x 8,192 x 2,048 with bias and gelu 266, 512 x 2,048 x 8,192 25;
+//   all gradients of few rows (rows x outputs x inputs), silu: 1 x 8,192 x 4,096 40 (dx 21, dw 20, db 8), 24 46 (26, 24, 8),
+//   256 x 2,048 x 2,048 27 (16, 14, 8).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(int kind, const TD* __re
 // either, so one barrier a step.  A column's sum over the wave's 16 rows is made by halving (lane bits 5, 4, 3), over
 // the waves by one of them behind the barrier, over the workgroup's rows in `column_sums`.
 //
-// Memory's rate where every workgroup's rows fill their tiles (dx alone of 65,536 x 512 by 128: 151 MB in 29 us, 5.2 TB/s),
+// Memory's rate where every workgroup's rows fill their tiles (dx alone of 65,536 x 512 by 128: 151 MB in 30 us, 5.0 TB/s),
 // else a step's arithmetic, which rows that do not exist take part in; 100,000 rows with dz stored 66 us, 5.0 TB/s.  Both
 // ways, dz by itself and this one, silu, all gradients (dx alone), us:
 //   100,000 x 512 by 128 118 / 100 (81 / 51), 100,000 x 128 by 32 48 / 36, 100,000 x 2,048 by 128 470 / 395, 50,000 x 512 by
@@ -792,9 +795,11 @@ Shape shape_of(const SliceCosts& costs, int64_t M, int64_t N, int64_t steps, int
     return Shape{sum_shape(costs, M, N, steps, grain)};
 }
 // Up to 16 rows of x the weights' bytes are all that counts, and the few-rows kernel reads them with the least
-// latency: us against the best tile, one row bf16 4,096 x 8,192 (sum x columns) 12.7 / 14.7, 1,024^2 4.1 / 5.9; 24 rows
-// 23 / 16 and 6.7 / 6.2.  Its eight waves have four steps each in flight: a longer sum over few columns is cut, one row of
-// 8,192 x 128 10.6 -> 6.7.
+// latency: us against the best tile (sum x columns), one row bf16 4,096 x 8,192 12.7 / 14.7, 1,024^2 4.1 / 5.9; 24 rows
+// 23 / 16 and 6.7 / 6.2.  8 bits, 17 rows 8,192 x 2,048 13.5 / 11.5, 4,096^2 8.1 / 9.5, 2,048 x 8,192 7.3 / 8.2, 8,192^2
+// 26 / 18; 24 rows 15.6 / 11.5, 9.1 / 9.6, 8.1 / 8.1, 30 / 18; 32 rows 17.7 / 11.6, 10.2 / 9.9, 9.0 / 8.1, 34 / 18; 64 rows
+// 28 / 12, 16 / 12, 10 / 8, 55 / 19: sums of up to 4,096 could go on to 24 rows for 1 us.  Its eight waves have four steps
+// each in flight: a longer sum over few columns is cut, one row of 8,192 x 128 10.6 -> 6.7.
 constexpr int64_t kFewRows = 16;
 Shape few_shape(int64_t N, int64_t steps, int64_t grain) {
     const int64_t groups = (N + 15) / 16, at_once = 4 * kSkinnyWaves;
@@ -893,8 +898,9 @@ Shape forward8_shape(int64_t M, int64_t K, int64_t N) {
 Shape dx_shape(int64_t M, int64_t K, int64_t N) { return shape_of(kSlices16, M, K, (N + 63) / 64, 1); }
 Shape dw_shape(int64_t M, int64_t K, int64_t N) { return shape_of(kSlices16, N, K, (M + 63) / 64, 1); }
 
-// Outputs of more elements than this leave past the caches: 100,000 x 512 of 128 terms with silu, z kept, 72 -> 46 us
-// (without either 48 -> 31), 8,192 x 8,192 of 2,048 with gelu 273 -> 264.  Smaller ones stay for who reads them next.
+// Outputs of more elements than this leave past the caches: 100,000 x 512 of 128 terms with silu, z kept, 66 -> 49 us
+// (without either 34 -> 32), 8,192 x 8,192 of 2,048 with gelu 262 -> 243, z kept too 279 -> 253.  Smaller ones stay for
+// who reads them next.
 bool large(int64_t elements) { return elements > int64_t{1} << 24; }
 
 LinearOut out_of(const LinearArgs& a) {
