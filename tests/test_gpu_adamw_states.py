@@ -18,13 +18,10 @@ BETAS = [(0.95, 0.9), (0.9, 0.81), (0.9, 0.8), (0.99, 0.5)]
 
 
 @pytest.mark.parametrize("where", ["host", "device"])
-@pytest.mark.parametrize("step", [1, 2, 10, 300])
-@pytest.mark.parametrize("betas", BETAS)
+@pytest.mark.parametrize("betas,step", [(b, t) for b in BETAS for t in (1, 2, 10, 300) if (b[0] ** 2 / b[1]) ** t < 1e6])
 def test_a_v_of_zero_beside_an_m_makes_no_step_past_the_steps_bound(betas, step, where):
     """|m| <= c sqrt(v) for sums of `step` gradients, c^2 = (1 - b1)^2 / (1 - b2) (1 + r + ... + r^(step - 1))."""
     n, (b1, b2) = 256, betas
-    if b1 * b1 / b2 > 1.5 and step > 10:
-        pytest.skip("c^2 grows past 1e80")
     p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
     m, v = blocks_of(torch.full((n,), 1e-3, device="cuda")), blocks_of(torch.zeros(n, device="cuda"))
     at = step if where == "host" else torch.tensor([step], device="cuda")
@@ -32,7 +29,7 @@ def test_a_v_of_zero_beside_an_m_makes_no_step_past_the_steps_bound(betas, step,
     r = b1 * b1 / b2
     c = (1 - b1) / math.sqrt(1 - b2) * math.sqrt(math.fsum(r**i for i in range(step)))
     want = 1e-3 * c * math.sqrt(1 - b2**step) / (1 - b1**step)
-    # some ten roundings in fp32, and those of 2^step in double
+    # some ten roundings in fp32
     assert bool(((p.abs() / want - 1).abs() <= 2.0**-19).all()), float(p.abs().max() / want)
 
 
