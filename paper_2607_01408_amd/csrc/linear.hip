@@ -1025,8 +1025,8 @@ hipError_t launch_linear8(const LinearArgs& a, hipStream_t stream) {
                                       stream);
 }
 
-// Whether linear_narrow_kernel makes dz and dx: whatever w, dx and the gradients that are wanted, so that db has the same
-// bits with any of them (w is read for dx alone, and may be null without it).
+// Whether linear_narrow_kernel makes dz and dx (without dx linear_narrow_dz_kernel dz): whatever w, dx and the gradients that
+// are wanted, so that db has the same bits with any of them.
 bool narrow(const LinearBwdArgs& a) {
     const int64_t width = a.dtype == SPINGTP_FP32 ? 4 : 2;
     const auto whole = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
